@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define BC_ABI_VERSION 10
+#define BC_ABI_VERSION 11
 
 typedef enum {
     BC_OK = 0,
@@ -569,6 +569,120 @@ bc_status bc_rmsprop_step_many(const bc_param *params, int32_t n, float lr, floa
 bc_status bc_block_rewards(const float *d_ig, const uint8_t *d_mask, const float *d_prob,
                            int32_t n, bc_grid g, float tau, float gamma, float mu, float *d_mavg,
                            float *d_reward, float *d_cost, float *d_loss, void *stream);
+
+/* ------------------------------------------------------------------------------
+ * Trainable normalisation and orthogonalised updates. The online update sees one frame at
+ * a time, too few for batch statistics: a layer normalised over its own channels needs
+ * none, and its gains train with the other weights. Weight matrices can be updated along
+ * the orthogonal factor of their momentum instead of element by element.
+ * ------------------------------------------------------------------------------ */
+
+/*
+ * Block-sparse layer normalisation over the channels of each pixel:
+ *   out[block] = act((in - mean) / sqrt(var + eps) * gamma + beta (+ residual))[block] for
+ *   the active blocks, out[other] untouched (feature transfer); mean and var (the mean of
+ *   the squared differences) over the c channels of the pixel; act is ReLU when relu = 1.
+ * Arithmetic fp32, the mean and then the differences' squares summed; one round to nearest
+ * even to the dtype. A NaN stays within its pixel.
+ *   desc        of in, residual and out: NHWC, any dtype, any c >= 1, any element alignment.
+ *   d_gamma, d_beta   [c] fp32, or NULL (1, 0).
+ *   d_residual  shaped and typed like out, or NULL; read only at active blocks.
+ *   d_out       may be d_in or d_residual itself (each pixel is read before it is written);
+ *               otherwise it overlaps neither (BC_ERR_ALIAS).
+ * Index, capacity and registered-buffer rules as bc_sparse_conv2d. One launch, no workspace.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE (sizes; relu; eps negative or not finite), BC_ERR_DTYPE,
+ * BC_ERR_LAYOUT (NCHW), BC_ERR_NOT_DIVISIBLE, BC_ERR_CAPACITY, BC_ERR_ALIAS,
+ * BC_ERR_UNINITIALIZED, BC_ERR_HIP.
+ */
+bc_status bc_sparse_layer_norm(const void *d_in, bc_tensor desc, const float *d_gamma,
+                               const float *d_beta, const void *d_residual, float eps,
+                               int32_t relu, void *d_out, bc_grid g, const int32_t *d_idx,
+                               const int32_t *d_count, int32_t capacity, void *stream);
+
+/* Bytes of the workspace that bc_layer_norm_grad needs for maps like desc. Host only.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_LAYOUT. */
+bc_status bc_layer_norm_grad_work(bc_tensor desc, int64_t *bytes);
+
+/*
+ * Backward pass of bc_sparse_layer_norm over every pixel. With dy' = grad_out * [y > 0]
+ * (grad_out where d_y is NULL), g = dy' gamma, xhat = (in - mean) / sqrt(var + eps):
+ *   d_grad_in  = (g - mean(g) - xhat mean(g xhat)) / sqrt(var + eps), means over channels;
+ *   d_grad_res = dy', the residual's gradient (NULL: not wanted);
+ *   d_dgamma[c] = sum over pixels of dy' xhat, d_dbeta[c] = sum of dy' (either may be NULL),
+ *   written, or added to what is there with accumulate = 1.
+ * mean and var are computed again from d_in, the forward input. A position masked by d_y
+ * contributes nothing, whatever grad_out holds there. fp32 arithmetic; the sums over pixels
+ * are taken in a fixed order: equal inputs give equal bits.
+ *   desc        of d_in, d_y (the forward output, behind a ReLU), d_grad_out, d_grad_in and
+ *               d_grad_res: NHWC, any dtype, any c >= 1, any element alignment.
+ *   d_grad_in, d_grad_res   either may be d_grad_out itself, d_grad_in also d_in; otherwise
+ *               no output overlaps an input or another output (BC_ERR_ALIAS).
+ *   d_work      device, at least bc_layer_norm_grad_work bytes, aligned to 16 bytes, the
+ *               caller's: calls that may overlap in time need one each. Nothing is kept in it.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_LAYOUT, BC_ERR_CAPACITY (work_bytes
+ * too small), BC_ERR_UNSUPPORTED (d_work not aligned), BC_ERR_ALIAS, BC_ERR_HIP.
+ */
+bc_status bc_layer_norm_grad(const void *d_in, bc_tensor desc, const float *d_gamma,
+                             const void *d_y, const void *d_grad_out, float eps,
+                             void *d_grad_in, void *d_grad_res, float *d_dgamma,
+                             float *d_dbeta, int32_t accumulate, void *d_work,
+                             int64_t work_bytes, void *stream);
+
+/* Newton-Schulz iteration: X_0 = G / (|G|_F + eps) and `steps` (1..64) times
+ * X <- a X + (b A + c A^2) X with A = X X^T (of the shorter side). a = 3.4445, b = -4.7750,
+ * c = 2.0315, steps = 5 bring singular values from 0.01..1 into about 0.7..1.2. */
+typedef struct { int32_t steps; float a, b, c, eps; } bc_newton_schulz;
+
+/* Bytes of the workspace of bc_orthogonalize. Host only. Errors: BC_ERR_NULL, BC_ERR_SHAPE. */
+bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32_t steps,
+                                int64_t *bytes);
+
+/*
+ * Orthogonalises each of `batch` matrices: d_out = X of the iteration *ns on d_g.
+ *   d_g, d_out   [batch][rows][cols] of in_dtype and out_dtype (any dtypes, any sizes >= 1,
+ *                any element alignment); d_out may be d_g itself if the dtypes agree.
+ * fp32 accuracy whatever the dtypes (operands held as two fp16 numbers, three matrix-core
+ * products, fp32 sums; the norm in fp64), one round to out_dtype. A matrix of zeros gives
+ * zeros (eps > 0); a NaN or infinity stays within its matrix. Equal inputs give equal bits.
+ *   ns       a > 0, and coefficients under which no value of the iteration passes 15 for
+ *            singular values in [0, 1] (else BC_ERR_UNSUPPORTED).
+ *   d_work   as for bc_layer_norm_grad, bc_orthogonalize_work bytes.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_CAPACITY, BC_ERR_ALIAS,
+ * BC_ERR_UNSUPPORTED, BC_ERR_HIP.
+ */
+bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int32_t rows,
+                           int32_t cols, const bc_newton_schulz *ns, void *d_out,
+                           int32_t out_dtype, void *d_work, int64_t work_bytes, void *stream);
+
+/* One weight matrix of an orthogonalised step: fp32 weights, momentum and gradient of
+ * rows x cols elements, and an optional 16-bit copy of the weights. A convolution's weights
+ * [cout][kh][kw][cin] are the matrix of cout rows. */
+typedef struct { float *w, *momentum, *grad; void *w16; int32_t rows, cols; } bc_matrix;
+
+/* Hyper-parameters of bc_muon_step_many. */
+typedef struct {
+    float lr, momentum, weight_decay;
+    int32_t nesterov;
+    bc_newton_schulz ns;
+} bc_muon;
+
+/* Bytes of the workspace of bc_muon_step_many (only rows and cols of params are read). Host
+ * only. Errors: BC_ERR_NULL, BC_ERR_SHAPE. */
+bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t steps,
+                                 int64_t *bytes);
+
+/*
+ * One orthogonalised step of n weight matrices (1 <= n <= 64), all in the same launches:
+ *   m = momentum m + grad;  u = nesterov ? grad + momentum m : m;
+ *   w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) X(u);  grad = 0;
+ * X(u) as bc_orthogonalize gives it in fp32, and w16, if not NULL, the weights rounded to
+ * `dtype` (BC_BF16 or BC_F16). `params` is a host array read during the call. No two buffers
+ * may overlap. d_work as for bc_orthogonalize, bc_muon_step_many_work bytes.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_CAPACITY, BC_ERR_ALIAS,
+ * BC_ERR_UNSUPPORTED, BC_ERR_HIP.
+ */
+bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *muon,
+                            int32_t dtype, void *d_work, int64_t work_bytes, void *stream);
 
 #ifdef __cplusplus
 }

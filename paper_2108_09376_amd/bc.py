@@ -44,6 +44,22 @@ class bc_param(ctypes.Structure):
                 ("w16", ctypes.c_void_p), ("count", ctypes.c_int64)]
 
 
+class bc_newton_schulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class bc_matrix(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("momentum", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("w16", ctypes.c_void_p), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32)]
+
+
+class bc_muon(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32),
+                ("ns", bc_newton_schulz)]
+
+
 class bc_conv(ctypes.Structure):
     _fields_ = [("kh", ctypes.c_int32), ("kw", ctypes.c_int32), ("stride", ctypes.c_int32),
                 ("pad", ctypes.c_int32), ("relu", ctypes.c_int32)]
@@ -105,6 +121,17 @@ _sigs = {
     "bc_conv2d_weight_grad": ([ctypes.POINTER(bc_conv), _vp, bc_tensor, _vp, bc_tensor, _vp, _vp, _vp], _i32),
     "bc_rmsprop_step": ([_vp, _vp, _vp, ctypes.c_int64, _f32, _f32, _f32, _f32, _vp, _i32, _vp], _i32),
     "bc_rmsprop_step_many": ([ctypes.POINTER(bc_param), _i32, _f32, _f32, _f32, _f32, _i32, _vp], _i32),
+    "bc_sparse_layer_norm": ([_vp, bc_tensor, _vp, _vp, _vp, _f32, _i32, _vp, bc_grid, _vp, _vp, _i32,
+                              _vp], _i32),
+    "bc_layer_norm_grad_work": ([bc_tensor, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_layer_norm_grad": ([_vp, bc_tensor, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp, _i32, _vp,
+                            ctypes.c_int64, _vp], _i32),
+    "bc_orthogonalize_work": ([_i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_orthogonalize": ([_vp, _i32, _i32, _i32, _i32, ctypes.POINTER(bc_newton_schulz), _vp, _i32, _vp,
+                          ctypes.c_int64, _vp], _i32),
+    "bc_muon_step_many_work": ([ctypes.POINTER(bc_matrix), _i32, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_muon_step_many": ([ctypes.POINTER(bc_matrix), _i32, ctypes.POINTER(bc_muon), _i32, _vp,
+                           ctypes.c_int64, _vp], _i32),
     "bc_block_rewards": ([_vp, _vp, _vp, _i32, bc_grid, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _vp], _i32),
 }
 for _name, (_args, _res) in _sigs.items():
@@ -116,7 +143,7 @@ EXPORTED = tuple(_sigs)
 
 # The ABI these bindings marshal for (BC_ABI_VERSION of include/bc.h); a library built
 # from other sources is refused rather than called with mismatched arguments.
-ABI_VERSION = 10
+ABI_VERSION = 11
 if _lib.bc_abi_version() != ABI_VERSION:
     raise ImportError(f"{LIB_PATH} has ABI {_lib.bc_abi_version()}, the bindings expect "
                       f"{ABI_VERSION}: rebuild with `python -m paper_2108_09376_amd.build`")
@@ -440,6 +467,143 @@ def bc_block_rewards(ig, mask, prob, grid, tau, gamma, mu, mavg, reward, cost=No
                                float(tau), float(gamma), float(mu), _ptr(mavg), _ptr(reward),
                                _ptr(cost), _ptr(loss), _stream(stream))
     _check(st, "bc_block_rewards")
+
+
+def _work(work, need, device):
+    """The caller's workspace, or a new one of need() bytes on the current stream."""
+    if work is None:
+        import torch
+        work = torch.empty(need(), dtype=torch.uint8, device=device)
+    return work
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def _alike(t, like, name):
+    if t is not None and (t.shape != like.shape or t.dtype != like.dtype or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous and shaped and typed like the map")
+
+
+def _is_f32(t) -> bool:
+    return t.is_floating_point() and t.element_size() == 4 and t.is_contiguous()
+
+
+def _per_channel(t, c, name):
+    """An fp32 vector of one value per channel (or None)."""
+    if t is not None and (t.numel() != c or not _is_f32(t)):
+        raise ValueError(f"{name} must be {c} contiguous float32 values")
+
+
+def bc_sparse_layer_norm(x, layout, gamma, beta, residual, eps, relu, out, grid, idx, count, stream=None):
+    """out[active blocks] = relu?(layer norm of x over its channels * gamma + beta + residual);
+    x, residual and out [n, h, w, c] (layout BC_NHWC), gamma and beta float32 [c] or None."""
+    cap = 0 if idx is None else int(idx.numel())
+    d = _desc(x, layout)
+    _alike(out, x, "out")
+    _alike(residual, x, "residual")
+    _per_channel(gamma, d.c, "gamma")
+    _per_channel(beta, d.c, "beta")
+    st = _lib.bc_sparse_layer_norm(_ptr(x), d, _ptr(gamma), _ptr(beta), _ptr(residual), float(eps), int(relu),
+                                   _ptr(out), _grid(grid), _ptr(idx), _ptr(count), cap, _stream(stream))
+    _check(st, "bc_sparse_layer_norm")
+
+
+def bc_layer_norm_grad_work(x, layout) -> int:
+    """Bytes of bc_layer_norm_grad's workspace for maps like x."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_layer_norm_grad_work(_desc(x, layout), ctypes.byref(n)), "bc_layer_norm_grad_work")
+    return n.value
+
+
+def bc_layer_norm_grad(x, layout, gamma, y, grad_out, eps, grad_in, grad_res, dgamma, dbeta,
+                       accumulate=False, work=None, stream=None):
+    """grad_in (and grad_res, the residual's gradient, if not None) from grad_out, with the
+    ReLU's mask from the forward output y (None: no ReLU); dgamma, dbeta float32 [c] (or None)
+    written, or added to with accumulate. work: a uint8 device tensor that the caller keeps
+    (None: allocated here, for work enqueued on torch's current stream)."""
+    d = _desc(x, layout)
+    for t, name in ((y, "y"), (grad_out, "grad_out"), (grad_in, "grad_in"), (grad_res, "grad_res")):
+        _alike(t, x, name)
+    for t, name in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
+        _per_channel(t, d.c, name)
+    work = _work(work, lambda: bc_layer_norm_grad_work(x, layout), x.device)
+    st = _lib.bc_layer_norm_grad(_ptr(x), d, _ptr(gamma), _ptr(y), _ptr(grad_out), float(eps), _ptr(grad_in),
+                                 _ptr(grad_res), _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(work),
+                                 _nbytes(work), _stream(stream))
+    _check(st, "bc_layer_norm_grad")
+
+
+NS_STEPS, NS_COEF, NS_EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
+
+
+@functools.lru_cache(maxsize=64)
+def _newton_schulz(steps, coef, eps) -> bc_newton_schulz:
+    return bc_newton_schulz(int(steps), *[float(v) for v in coef], float(eps))
+
+
+def _matrices(g):
+    if g.dim() not in (2, 3) or not g.is_contiguous():
+        raise ValueError("matrices are contiguous, [rows, cols] or [batch, rows, cols]")
+    return (1, *g.shape) if g.dim() == 2 else tuple(g.shape)
+
+
+def bc_orthogonalize_work(g, steps=NS_STEPS) -> int:
+    """Bytes of bc_orthogonalize's workspace for matrices like g."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_orthogonalize_work(*_matrices(g), int(steps), ctypes.byref(n)), "bc_orthogonalize_work")
+    return n.value
+
+
+def bc_orthogonalize(g, out, steps=NS_STEPS, coef=NS_COEF, eps=NS_EPS, work=None, stream=None):
+    """out = Newton-Schulz iteration of g, [rows, cols] or [batch, rows, cols] (each matrix by
+    itself), any dtypes. work as for bc_layer_norm_grad."""
+    if out.shape != g.shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous and shaped like g")
+    work = _work(work, lambda: bc_orthogonalize_work(g, steps), g.device)
+    st = _lib.bc_orthogonalize(_ptr(g), _dtype_code(g), *_matrices(g),
+                               ctypes.byref(_newton_schulz(steps, tuple(coef), eps)), _ptr(out),
+                               _dtype_code(out), _ptr(work), _nbytes(work), _stream(stream))
+    _check(st, "bc_orthogonalize")
+
+
+def _matrix_array(params):
+    arr = (bc_matrix * len(params))()
+    dt = BC_BF16
+    for a, (w, m, grad, w16) in zip(arr, params):
+        count, rows = w.numel(), w.shape[0]
+        for t in (w, m, grad):
+            if t.numel() != count or not _is_f32(t):
+                raise ValueError("weights, momentum and gradient are contiguous float32 of one size")
+        a.w, a.momentum, a.grad = w.data_ptr(), m.data_ptr(), grad.data_ptr()
+        a.rows, a.cols = rows, count // rows
+        if w16 is not None:
+            if w16.numel() != count or not w16.is_contiguous():
+                raise ValueError("the 16-bit copy must be contiguous and as large as the weights")
+            a.w16, dt = w16.data_ptr(), _dtype_code(w16)
+    return arr, dt
+
+
+def bc_muon_step_many_work(params, steps=NS_STEPS) -> int:
+    """Bytes of bc_muon_step_many's workspace for these params."""
+    n = ctypes.c_int64()
+    arr, _ = _matrix_array(params)
+    _check(_lib.bc_muon_step_many_work(arr, len(params), int(steps), ctypes.byref(n)), "bc_muon_step_many_work")
+    return n.value
+
+
+def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=NS_STEPS, coef=NS_COEF,
+                      eps=NS_EPS, work=None, stream=None):
+    """One orthogonalised step of every (w, momentum, grad, w16 or None) of `params` (w [rows,
+    ...], float32, grad reset to 0; the 16-bit copies share one dtype). work as for
+    bc_layer_norm_grad."""
+    arr, dt = _matrix_array(params)
+    work = _work(work, lambda: bc_muon_step_many_work(params, steps), params[0][0].device)
+    h = bc_muon(float(lr), float(momentum), float(weight_decay), int(nesterov),
+                _newton_schulz(steps, tuple(coef), eps))
+    st = _lib.bc_muon_step_many(arr, len(params), ctypes.byref(h), dt, _ptr(work), _nbytes(work), _stream(stream))
+    _check(st, "bc_muon_step_many")
 
 
 def _np_ptr(a):

@@ -1094,4 +1094,244 @@ bc_status bc_block_rewards(const float *d_ig, const uint8_t *d_mask, const float
     return ok();
 }
 
+// ---------------------------------------------------------------- normalisation
+
+static bc_status norm_geom(const bc_tensor &t, float eps, bc::NormGeom &G)
+{
+    bc_status st = check_tensor(t, "desc");
+    if (st) return st;
+    if (t.layout != BC_NHWC) return fail(BC_ERR_LAYOUT, "layer normalisation takes channels-last maps");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(BC_ERR_SHAPE, "eps must be finite and not negative");
+    G = bc::NormGeom{};
+    G.rows = (uint32_t)((size_t)t.n * t.h * t.w);     // at most 4e9 elements
+    G.c = t.c;
+    G.inv_c = 1.f / (float)t.c;
+    G.eps = eps;
+    return BC_OK;
+}
+
+// The caller's workspace of a call that needs `need` bytes.
+static bc_status check_work(const void *d_work, int64_t work_bytes, size_t need)
+{
+    if (!d_work) return fail(BC_ERR_NULL, "d_work is required");
+    if (work_bytes < 0 || (size_t)work_bytes < need)
+        return fail(BC_ERR_CAPACITY, "the workspace has %lld bytes, %zu are needed", (long long)work_bytes, need);
+    if ((uintptr_t)d_work & 15) return fail(BC_ERR_UNSUPPORTED, "d_work must be aligned to 16 bytes");
+    return BC_OK;
+}
+
+// Every buffer against every other; sorted by start address, any overlap shows between
+// neighbours.
+struct Extent {
+    const void *p;
+    size_t b;
+};
+
+static bool any_overlap(std::vector<Extent> &v)
+{
+    std::sort(v.begin(), v.end(), [](const Extent &x, const Extent &y) { return (uintptr_t)x.p < (uintptr_t)y.p; });
+    for (size_t i = 0; i + 1 < v.size(); ++i)
+        if (overlap(v[i].p, v[i].b, v[i + 1].p, v[i + 1].b)) return true;
+    return false;
+}
+
+bc_status bc_sparse_layer_norm(const void *d_in, bc_tensor desc, const float *d_gamma,
+                               const float *d_beta, const void *d_residual, float eps,
+                               int32_t relu, void *d_out, bc_grid g, const int32_t *d_idx,
+                               const int32_t *d_count, int32_t capacity, void *stream)
+{
+    if (!d_in || !d_out) return fail(BC_ERR_NULL, "d_in and d_out are required");
+    bc::NormGeom G;
+    bc_status st = norm_geom(desc, eps, G);
+    if (st) return st;
+    if (relu != 0 && relu != 1) return fail(BC_ERR_SHAPE, "relu must be 0 or 1");
+    LayerGeom L;
+    if ((st = block_geom(desc, g, L))) return st;
+    if ((st = check_index(d_idx, d_count, capacity, L.total_blocks))) return st;
+    const size_t bytes = tensor_bytes(desc), cb = (size_t)desc.c * 4;
+    auto bad = [&](const void *p) { return p != d_out && overlap(d_out, bytes, p, bytes); };
+    if (bad(d_in) || bad(d_residual)) return fail(BC_ERR_ALIAS, "d_out partially overlaps an input");
+    if (overlap(d_out, bytes, d_gamma, cb) || overlap(d_out, bytes, d_beta, cb))
+        return fail(BC_ERR_ALIAS, "d_out overlaps gamma or beta");
+    if (d_idx && (overlap(d_out, bytes, d_idx, (size_t)capacity * 4) || overlap(d_out, bytes, d_count, 4)))
+        return fail(BC_ERR_ALIAS, "d_out overlaps the index");
+    if ((st = check_registered(d_out, desc, d_idx != nullptr))) return st;
+    G.relu = relu;
+    G.gh = L.gh; G.gw = L.gw; G.bh = L.bh; G.bw = L.bw;
+    G.idx = d_idx;
+    G.count = d_count;
+    hipError_t e = bc::launch_norm(d_in, d_gamma, d_beta, d_residual, d_out, G, desc.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "layer normalisation launch");
+    if (!d_idx) mark_full(d_out);
+    return ok();
+}
+
+bc_status bc_layer_norm_grad_work(bc_tensor desc, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    bc::NormGeom G;
+    bc_status st = norm_geom(desc, 0.f, G);
+    if (st) return st;
+    *bytes = (int64_t)bc::norm_grad_work(desc.dtype, G.rows, G.c);
+    return ok();
+}
+
+bc_status bc_layer_norm_grad(const void *d_in, bc_tensor desc, const float *d_gamma,
+                             const void *d_y, const void *d_grad_out, float eps,
+                             void *d_grad_in, void *d_grad_res, float *d_dgamma,
+                             float *d_dbeta, int32_t accumulate, void *d_work,
+                             int64_t work_bytes, void *stream)
+{
+    if (!d_in || !d_grad_out || !d_grad_in) return fail(BC_ERR_NULL, "d_in, d_grad_out and d_grad_in are required");
+    bc::NormGeom G;
+    bc_status st = norm_geom(desc, eps, G);
+    if (st) return st;
+    if (accumulate != 0 && accumulate != 1) return fail(BC_ERR_SHAPE, "accumulate must be 0 or 1");
+    const size_t need = bc::norm_grad_work(desc.dtype, G.rows, G.c);
+    if ((st = check_work(d_work, work_bytes, need))) return st;
+    const size_t bytes = tensor_bytes(desc), cb = (size_t)desc.c * 4;
+    const Extent ins[4] = {{d_in, bytes}, {d_y, bytes}, {d_grad_out, bytes}, {d_gamma, cb}};
+    const Extent outs[5] = {{d_grad_in, bytes}, {d_grad_res, bytes}, {d_dgamma, cb}, {d_dbeta, cb}, {d_work, need}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < 4; ++j) {
+            // a pixel's inputs are read before its outputs are written
+            const bool same = outs[i].p == ins[j].p && ((i < 2 && j == 2) || (i == 0 && j == 0));
+            if (!same && overlap(outs[i].p, outs[i].b, ins[j].p, ins[j].b))
+                return fail(BC_ERR_ALIAS, "an output overlaps an input");
+        }
+        for (int j = i + 1; j < 5; ++j)
+            if (overlap(outs[i].p, outs[i].b, outs[j].p, outs[j].b))
+                return fail(BC_ERR_ALIAS, "outputs overlap each other");
+    }
+    const bc::NormGradArgs a = {d_in, d_gamma, d_y, d_grad_out, d_grad_in, d_grad_res};
+    hipError_t e = bc::launch_norm_grad(a, d_dgamma, d_dbeta, accumulate, d_work, G, desc.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "layer normalisation gradient launch");
+    return ok();
+}
+
+// ---------------------------------------------------------------- orthogonalised updates
+
+static bc_status orth_sizes(int32_t batch, int32_t rows, int32_t cols, int32_t steps, const char *name)
+{
+    if (batch < 1 || rows < 1 || cols < 1) return fail(BC_ERR_SHAPE, "%s: sizes must be positive", name);
+    if ((double)batch * rows * cols > 4.0e9) return fail(BC_ERR_SHAPE, "%s: more than 4e9 elements", name);
+    if (std::min(rows, cols) > 16384) return fail(BC_ERR_SHAPE, "%s: the shorter side is above 16384", name);
+    if ((double)batch * bc::orth_tiles(rows, cols) >= (double)(1 << 24))
+        return fail(BC_ERR_SHAPE, "%s: 2^24 or more tiles of 64 x 64", name);
+    if (steps < 1 || steps > 64) return fail(BC_ERR_SHAPE, "steps outside 1..64");
+    return BC_OK;
+}
+
+static bc_status orth_iteration(const bc_newton_schulz &in, bc::NewtonSchulz &ns)
+{
+    ns = {in.steps, in.a, in.b, in.c, in.eps};
+    if (!(ns.eps >= 0.f) || !std::isfinite(ns.eps)) return fail(BC_ERR_SHAPE, "eps must be finite and not negative");
+    const char *why = "";
+    if (!bc::orth_supported(ns, &why)) return fail(BC_ERR_UNSUPPORTED, "%s", why);
+    return BC_OK;
+}
+
+bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32_t steps, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    bc_status st = orth_sizes(batch, rows, cols, steps, "matrices");
+    if (st) return st;
+    *bytes = (int64_t)(bc::orth_work(rows, cols) * (size_t)batch);
+    return ok();
+}
+
+bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int32_t rows,
+                           int32_t cols, const bc_newton_schulz *ns, void *d_out,
+                           int32_t out_dtype, void *d_work, int64_t work_bytes, void *stream)
+{
+    if (!d_g || !ns || !d_out) return fail(BC_ERR_NULL, "d_g, ns and d_out are required");
+    bc_status st = orth_sizes(batch, rows, cols, ns->steps, "matrices");
+    if (st) return st;
+    if (!valid_dtype(in_dtype) || !valid_dtype(out_dtype)) return fail(BC_ERR_DTYPE, "unknown dtype");
+    bc::NewtonSchulz it;
+    if ((st = orth_iteration(*ns, it))) return st;
+    const size_t need = bc::orth_work(rows, cols) * (size_t)batch;
+    if ((st = check_work(d_work, work_bytes, need))) return st;
+    const size_t count = (size_t)batch * rows * cols, ib = count * esize_of(in_dtype), ob = count * esize_of(out_dtype);
+    if (overlap(d_work, need, d_g, ib) || overlap(d_work, need, d_out, ob) ||
+        (overlap(d_g, ib, d_out, ob) && !(d_g == d_out && in_dtype == out_dtype)))
+        return fail(BC_ERR_ALIAS, "the workspace, d_g and d_out overlap");
+    bc::OrthTable T{};
+    T.n = 1;
+    T.work = (uint8_t *)d_work;
+    T.g = d_g;
+    T.out = d_out;
+    T.e[0] = {rows, cols, batch, 0, 0, 0};
+    hipError_t e = bc::launch_orth(T, bc::OrthStep{}, false, in_dtype, out_dtype, it, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "orthogonalisation launch");
+    return ok();
+}
+
+// Sizes of a step's matrices; *need: its workspace.
+static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, size_t *need)
+{
+    if (!params) return fail(BC_ERR_NULL, "params is required");
+    if (n < 1 || n > bc::kMaxParams) return fail(BC_ERR_SHAPE, "n outside 1..%d", bc::kMaxParams);
+    *need = 0;
+    double tiles = 0;
+    for (int t = 0; t < n; ++t) {
+        char name[32];
+        snprintf(name, sizeof name, "params[%d]", t);
+        bc_status st = orth_sizes(1, params[t].rows, params[t].cols, steps, name);
+        if (st) return st;
+        *need += bc::orth_work(params[t].rows, params[t].cols);
+        tiles += bc::orth_tiles(params[t].rows, params[t].cols);
+    }
+    if (tiles >= (double)(1 << 24)) return fail(BC_ERR_SHAPE, "2^24 or more tiles of 64 x 64");
+    return BC_OK;
+}
+
+bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t steps, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    size_t need = 0;
+    bc_status st = muon_sizes(params, n, steps, &need);
+    if (st) return st;
+    *bytes = (int64_t)need;
+    return ok();
+}
+
+bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *muon,
+                            int32_t dtype, void *d_work, int64_t work_bytes, void *stream)
+{
+    if (!params || !muon) return fail(BC_ERR_NULL, "params and muon are required");
+    size_t need = 0;
+    bc_status st = muon_sizes(params, n, muon->ns.steps, &need);
+    if (st) return st;
+    if (!std::isfinite(muon->lr) || !std::isfinite(muon->momentum) || !std::isfinite(muon->weight_decay))
+        return fail(BC_ERR_SHAPE, "lr, momentum and weight_decay must be finite");
+    if (muon->nesterov != 0 && muon->nesterov != 1) return fail(BC_ERR_SHAPE, "nesterov must be 0 or 1");
+    bc::NewtonSchulz it;
+    if ((st = orth_iteration(muon->ns, it))) return st;
+    if ((st = check_work(d_work, work_bytes, need))) return st;
+    bc::OrthTable T{};
+    T.n = n;
+    T.work = (uint8_t *)d_work;
+    std::vector<Extent> all = {{d_work, need}};
+    bool any16 = false;
+    size_t off = 0;
+    for (int t = 0; t < n; ++t) {
+        const bc_matrix &p = params[t];
+        if (!p.w || !p.momentum || !p.grad) return fail(BC_ERR_NULL, "params[%d]: w, momentum and grad are required", t);
+        const size_t count = (size_t)p.rows * p.cols;
+        for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all.push_back({q, count * 4});
+        if (p.w16) all.push_back({p.w16, count * 2});
+        any16 = any16 || p.w16;
+        T.e[t] = {p.rows, p.cols, 1, 0, 0, (uint32_t)(off / 256)};
+        T.p[t] = {p.w, p.momentum, p.grad, (uint16_t *)p.w16};
+        off += bc::orth_work(p.rows, p.cols);
+    }
+    if (any16 && dtype != BC_BF16 && dtype != BC_F16) return fail(BC_ERR_DTYPE, "the copies must be bf16 or f16");
+    if (any_overlap(all)) return fail(BC_ERR_ALIAS, "the optimiser's buffers overlap");
+    const bc::OrthStep h = {muon->lr, muon->momentum, 1.f - muon->lr * muon->weight_decay, muon->nesterov};
+    hipError_t e = bc::launch_orth(T, h, true, BC_F32, dtype == BC_F16 ? BC_F16 : BC_BF16, it, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "orthogonalised step launch");
+    return ok();
+}
+
 }  // extern "C"

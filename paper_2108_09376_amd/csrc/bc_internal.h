@@ -148,4 +148,65 @@ hipError_t launch_rmsprop_many(const RmspropMany &m, float lr, float alpha, floa
 hipError_t launch_rmsprop(float *w, float *v, float *grad, long long count, float lr, float alpha,
                           float eps, float wd, void *w16, bool bf16, hipStream_t s);
 
+// Layer normalisation over channels (k_norm.hip): rows of c elements, every pixel of a
+// channels-last map (idx == nullptr) or the pixels of its active blocks. fmt: a bc_dtype.
+struct NormGeom {
+    uint32_t rows;                             // pixels of the map
+    int c;
+    float inv_c, eps;
+    int relu;
+    int gh, gw, bh, bw;                        // block grid of the map, with an index
+    const int32_t *idx, *count;
+};
+struct NormGradArgs {
+    const void *x;
+    const float *gamma;
+    const void *y, *dy;                        // y: the forward output behind a ReLU, or nullptr
+    void *dx, *dres;
+};
+hipError_t launch_norm(const void *x, const float *gamma, const float *beta, const void *res, void *out,
+                       const NormGeom &g, int fmt, hipStream_t s);
+size_t norm_grad_work(int fmt, uint32_t rows, int c);
+hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, int accumulate, void *work,
+                            const NormGeom &g, int fmt, hipStream_t s);
+
+// Orthogonalised updates (k_orth.hip). A table entry is a shape with its matrices: one of an
+// optimiser's step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the
+// workspace, orth_work(rows, cols) bytes for each matrix. first and per are the launches'.
+struct OrthEntry {
+    int rows, cols, batch;
+    uint32_t first, per;
+    uint32_t off;
+};
+struct OrthParam {
+    float *w, *mom, *grad;
+    uint16_t *w16;
+};
+struct OrthTable {
+    int n;
+    uint8_t *work;
+    const void *g;                             // bc_orthogonalize: [batch][rows][cols]
+    void *out;
+    OrthEntry e[kMaxParams];
+    OrthParam p[kMaxParams];                   // a step's tensors
+};
+struct OrthStep {
+    float lr, momentum, keep;                  // keep = 1 - lr weight_decay
+    int nesterov;
+};
+struct OrthJob {
+    int L, R, E1, E2, D;                       // buffers of a matrix's slot
+    float s1, s2, s3;
+};
+struct OrthJobs { OrthJob job[2]; };
+struct NewtonSchulz {
+    int steps;
+    float a, b, c, eps;
+};
+size_t orth_work(int rows, int cols);
+unsigned orth_tiles(int rows, int cols);       // workgroups of the largest launch, per matrix
+bool orth_supported(const NewtonSchulz &ns, const char **why);
+hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
+                       hipStream_t s);
+
 }  // namespace bc

@@ -1,0 +1,240 @@
+"""Orthogonalised updates on the device against the iteration in 64 bits.
+
+Tolerances, fixed before the kernels ran. The operators promise fp32 accuracy, so the
+measure is what plain fp32 arithmetic does on the same matrix: with e32 the relative error
+(Frobenius norm) of the textbook iteration computed in fp32 on the CPU, the device's fp32
+result may be off by 4 e32 + 2e-6 (4: other orders of summation and rounding; 2e-6: eight
+fp32 roundings of the whole matrix, where e32 happens to vanish). A 16-bit result adds its
+rounding. An optimiser's step scales that error by its rate."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import synth
+from tests._util import TORCH, shifted
+
+pytestmark = pytest.mark.gpu
+
+COEF, EPS = (3.4445, -4.7750, 2.0315), 1e-7
+ROUND = {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def bc(gpu):
+    from paper_2108_09376_amd import bc
+    return bc
+
+
+def iterate(g, steps=5, coef=COEF, eps=EPS, dtype=torch.float64):
+    g = g.detach().cpu().to(dtype)
+    x = g / (torch.sqrt((g.double() ** 2).sum()).to(dtype) + eps)
+    flip = x.shape[0] > x.shape[1]
+    x = x.T.contiguous() if flip else x
+    for _ in range(steps):
+        a = x @ x.T
+        x = coef[0] * x + (coef[1] * a + coef[2] * (a @ a)) @ x
+    return x.T if flip else x
+
+
+def bounds(g, dtype, **kw):
+    want = iterate(g, **kw)
+    e32 = ((iterate(g, dtype=torch.float32, **kw).double() - want).norm() / want.norm().clamp(min=1e-300)).item()
+    return want, 4 * e32 + 2e-6 + ROUND[dtype]
+
+
+def check(got, want, tol, dtype):
+    got = got.detach().double().cpu()
+    assert torch.isfinite(got).all()
+    norm = want.norm().item()
+    assert (got - want).norm().item() <= tol * norm + 1e-30, ((got - want).norm().item() / norm, tol)
+    # no single element far off: within 64 times the bound of the mean element, plus its rounding
+    rms = norm / math.sqrt(want.numel())
+    assert ((got - want).abs() <= 64 * (tol - ROUND[dtype]) * rms + 2 * ROUND[dtype] * (want.abs() + 1e-6)).all()
+
+
+def gradient(seed, m, n, kind="fall"):
+    r = synth.rng(seed)
+    k = max(1, min(m, n) // 2)
+    if kind == "noise":
+        g = r.standard_normal((m, n))
+    elif kind == "rank":                                   # fewer directions than rows
+        g = r.standard_normal((m, k)) @ r.standard_normal((k, n))
+    else:
+        g = (r.standard_normal((m, k)) * np.exp(-np.linspace(0, 3, k))) @ r.standard_normal((k, n)) / math.sqrt(k)
+        g += 0.1 * r.standard_normal((m, n))
+    return torch.from_numpy((1e-3 * g).astype(np.float32))
+
+
+SIZES = [(1, 1), (1, 9), (9, 1), (3, 2), (8, 8), (63, 65), (64, 64), (65, 64), (64, 147), (64, 576), (100, 37), (128, 128),
+         (129, 130), (128, 64), (127, 1152), (256, 256), (256, 129), (193, 301), (300, 257), (256, 1152), (320, 320),
+         (512, 1000), (513, 77), (700, 641)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n", SIZES)
+def test_sizes_and_formats(bc, dtype, m, n):
+    g = gradient(m * 1000 + n, m, n).to(TORCH[dtype]).cuda()
+    out = torch.full_like(g, float("nan"))
+    bc.bc_orthogonalize(g, out)
+    check(out, *bounds(g, dtype), dtype)
+    again = torch.empty_like(out)
+    bc.bc_orthogonalize(g, again)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("m,n", [(64, 64), (96, 512), (256, 256), (300, 90)])
+@pytest.mark.parametrize("kind", ["noise", "rank"])
+def test_spectra(bc, m, n, kind):
+    g = gradient(5, m, n, kind).cuda()
+    out = torch.empty_like(g)
+    bc.bc_orthogonalize(g, out)
+    check(out, *bounds(g, "f32"), "f32")
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7, 9])
+@pytest.mark.parametrize("m,n", [(48, 80), (200, 140)])
+def test_steps(bc, steps, m, n):
+    g = gradient(7, m, n).cuda()
+    out = torch.empty_like(g)
+    bc.bc_orthogonalize(g, out, steps=steps)
+    check(out, *bounds(g, "f32", steps=steps), "f32")
+
+
+@pytest.mark.parametrize("coef", [(1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (1.0, 0.0, 0.0)])
+def test_other_coefficients(bc, coef):
+    g = gradient(8, 70, 150, "noise").cuda()
+    out = torch.empty_like(g)
+    bc.bc_orthogonalize(g, out, steps=4, coef=coef, eps=1e-6)
+    check(out, *bounds(g, "f32", steps=4, coef=coef, eps=1e-6), "f32")
+
+
+@pytest.mark.parametrize("batch,m,n", [(1, 40, 50), (3, 65, 33), (12, 193, 301), (40, 17, 70), (300, 8, 16)])
+def test_batches(bc, batch, m, n):
+    """Each matrix by itself: a matrix of a batch has the bits it has alone; formats may
+    differ; a NaN or zeros stay where they are."""
+    g = torch.stack([gradient(100 + i, m, n) * 4.0 ** (i % 5 - 2) for i in range(batch)]).cuda()
+    out = torch.empty_like(g)
+    bc.bc_orthogonalize(g, out)
+    for i in {0, batch // 2, batch - 1}:
+        check(out[i], *bounds(g[i], "f32"), "f32")
+        alone = torch.empty_like(g[i])
+        bc.bc_orthogonalize(g[i], alone)
+        assert torch.equal(alone, out[i])
+    if batch >= 3:
+        g[0], g[2, m // 2, n // 2] = 0.0, float("nan")
+        half = torch.empty_like(g, dtype=torch.bfloat16)
+        bc.bc_orthogonalize(g, half)
+        assert (half[0] == 0).all() and torch.isnan(half[2]).all()
+        assert torch.equal(half[1], out[1].bfloat16())
+
+
+def test_magnitudes(bc):
+    """The result does not depend on G's scale, from values near fp32's largest to small
+    ones (eps = 0), and eps takes part where the norm is near it."""
+    g = gradient(9, 48, 90)
+    for scale in (1e35, 1.0, 1e-30):
+        s = (g * scale).cuda()
+        out = torch.empty_like(s)
+        bc.bc_orthogonalize(s, out, eps=0.0)
+        check(out, *bounds(s.double(), "f32", eps=0.0), "f32")
+    s = (g * 1e-6).cuda()
+    out = torch.empty_like(s)
+    bc.bc_orthogonalize(s, out, eps=1e-6)
+    check(out, *bounds(s, "f32", eps=1e-6), "f32")
+
+
+def test_in_place_and_unaligned(bc):
+    for dtype in ("f32", "bf16", "f16"):
+        g = gradient(10, 75, 131).to(TORCH[dtype]).cuda()
+        want, over = torch.empty_like(g), g.clone()
+        bc.bc_orthogonalize(g, want)
+        bc.bc_orthogonalize(over, over)
+        out = shifted(torch.zeros_like(g), 3)
+        bc.bc_orthogonalize(shifted(g, 1), out)
+        assert torch.equal(over, want) and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_step_many(bc, nesterov, dtype):
+    shapes = [(64, 288), (64, 9, 64), (128, 64), (1, 5), (5, 1), (130, 3, 3, 20), (256, 129), (33, 70), (300, 40)]
+    lr, mu, wd = 0.02, 0.95, 0.01
+    params, copies = [], []
+    for i, shape in enumerate(shapes):
+        m, n = shape[0], math.prod(shape[1:])
+        r = synth.rng(200 + i)
+        w = torch.from_numpy((r.standard_normal(shape) * math.sqrt(2 / n)).astype(np.float32))
+        copies.append((w, gradient(300 + i, m, n).view(shape) * 5, gradient(400 + i, m, n).view(shape)))
+        p = [t.clone().cuda() for t in copies[-1]]
+        params.append((*p, torch.empty(shape, dtype=TORCH[dtype], device="cuda") if i % 3 else None))
+    bc.bc_muon_step_many(params, lr, mu, wd, nesterov=nesterov)
+    for (w0, m0, g0), (w, m, g, w16) in zip(copies, params):
+        rows, cols = w0.shape[0], w0[0].numel()
+        m1 = mu * m0.double() + g0.double()
+        assert ((m.double().cpu() - m1).abs() <= 2.0 ** -23 * (mu * m0.abs() + g0.abs() + m1.abs())).all()
+        assert (g == 0).all()
+        u = g0.double() + mu * m1 if nesterov else m1
+        o, tol = bounds(u.float().view(rows, cols), "f32")
+        rate = lr * math.sqrt(max(1.0, rows / cols))
+        want = (1 - lr * wd) * w0.double() - rate * o.view(w0.shape)
+        err = (w.double().cpu() - want).norm().item()
+        # u itself is rounded to fp32 (as any fp32 form's is): one part in 2^23 more
+        assert err <= rate * (tol + 2.0 ** -22) * o.norm().item() + 2.0 ** -23 * want.norm().item()
+        if w16 is not None:
+            assert torch.equal(w16, w.to(TORCH[dtype]))
+
+
+def test_step_equals_its_parts(bc):
+    """The step over many matrices takes each as bc_orthogonalize does, and a matrix does not
+    depend on its neighbours."""
+    shapes = [(64, 576), (128, 1152), (200, 31)]
+    make = lambda: [(torch.zeros(s, device="cuda"), torch.zeros(s, device="cuda"), gradient(i, *s).cuda(), None)
+                    for i, s in enumerate(shapes)]
+    a, b = make(), make()
+    outs = []
+    for i, s in enumerate(shapes):
+        outs.append(torch.empty(s, device="cuda"))
+        bc.bc_orthogonalize(gradient(i, *s).cuda(), outs[-1])
+    bc.bc_muon_step_many(a, 1.0, 0.0, 0.0, nesterov=False)
+    for p in b:
+        bc.bc_muon_step_many([p], 1.0, 0.0, 0.0, nesterov=False)
+    for (w, *_), (w1, *_), o in zip(a, b, outs):
+        assert torch.equal(w, w1)
+        rate = math.sqrt(max(1.0, w.shape[0] / w.shape[1]))
+        assert ((w + rate * o).abs() <= 2.0 ** -22 * rate * o.abs()).all()
+
+
+def test_streams_and_graph(bc):
+    """On a stream of its own, and captured: replays equal eager calls on new gradients."""
+    shapes = [(64, 576), (300, 200)]
+    params = [(torch.zeros(s, device="cuda"), torch.zeros(s, device="cuda"), gradient(i, *s).cuda(), None)
+              for i, s in enumerate(shapes)]
+    work = torch.empty(bc.bc_muon_step_many_work(params), dtype=torch.uint8, device="cuda")
+    step = lambda: bc.bc_muon_step_many(params, 0.1, 0.9, 0.0, work=work)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (20, 30, 40):
+        before = [(w.clone(), m.clone()) for w, m, _, _ in params]
+        fresh = [gradient(seed + i, *s).cuda() for i, s in enumerate(shapes)]
+
+        def load():
+            for (w, m, g, _), (w0, m0), f in zip(params, before, fresh):
+                w.copy_(w0), m.copy_(m0), g.copy_(f)
+
+        load()
+        step()
+        torch.cuda.synchronize()
+        want = [(w.clone(), m.clone()) for w, m, _, _ in params]
+        load()
+        graph.replay()
+        torch.cuda.synchronize()
+        for (w, m, g, _), (w1, m1) in zip(params, want):
+            assert torch.equal(w, w1) and torch.equal(m, m1) and (g == 0).all()

@@ -1,0 +1,157 @@
+"""Argument checks of the layer normalisation and the orthogonalised updates, before anything
+is enqueued: no GPU, fake device addresses (see test_abi_host.py)."""
+import ctypes
+
+import pytest
+import torch
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(),
+                            reason="fake device pointers are used only on machines without a GPU")
+pytestmark = no_gpu
+
+A, B_, C, D, E, F, W = (0x10000000 * k for k in range(1, 8))
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2108_09376_amd import bc
+    return bc
+
+
+def test_layer_norm_refusals(B):
+    lib = B.raw()
+
+    def call(x=A, d=(1, 64, 16, 32, 1, 1), gamma=B_, beta=C, res=None, eps=1e-5, relu=0, out=D, grid=(8, 16),
+             idx=E, cnt=F, cap=128):
+        return lib.bc_sparse_layer_norm(x, B.bc_tensor(*d), gamma, beta, res, eps, relu, out, B.bc_grid(*grid), idx,
+                                        cnt, cap, None)
+
+    assert call(x=None) == call(out=None) == call(idx=None) == B.BC_ERR_NULL
+    for bad in (dict(d=(1, 0, 16, 32, 1, 1)), dict(d=(-1, 64, 16, 32, 1, 1)), dict(relu=2), dict(eps=-1.0),
+                dict(eps=NAN), dict(eps=INF), dict(grid=(0, 16)), dict(d=(4000, 4000, 16, 32, 1, 1))):
+        assert call(**bad) == B.BC_ERR_SHAPE, bad
+    assert call(d=(1, 64, 16, 32, 5, 1)) == B.BC_ERR_DTYPE
+    assert call(d=(1, 64, 16, 32, 0, 0)) == call(d=(1, 64, 16, 32, 1, 7)) == B.BC_ERR_LAYOUT
+    assert call(grid=(5, 16)) == B.BC_ERR_NOT_DIVISIBLE
+    assert call(cap=127) == B.BC_ERR_CAPACITY
+    nb = 64 * 16 * 32 * 2
+    for bad in (dict(out=A + 2), dict(out=A - nb + 2), dict(res=D + 16), dict(gamma=D + 8), dict(beta=D + nb - 4),
+                dict(idx=D), dict(cnt=D + 64)):
+        assert call(**bad) == B.BC_ERR_ALIAS, bad
+
+
+def test_layer_norm_grad_refusals(B):
+    lib = B.raw()
+    d = B.bc_tensor(1, 64, 16, 32, 1, 1)
+    n = ctypes.c_int64()
+    assert lib.bc_layer_norm_grad_work(d, None) == B.BC_ERR_NULL
+    assert lib.bc_layer_norm_grad_work(B.bc_tensor(1, 64, 16, 32, 1, 0), ctypes.byref(n)) == B.BC_ERR_LAYOUT
+    assert lib.bc_layer_norm_grad_work(B.bc_tensor(1, 64, 0, 32, 1, 1), ctypes.byref(n)) == B.BC_ERR_SHAPE
+    assert lib.bc_layer_norm_grad_work(d, ctypes.byref(n)) == B.BC_OK and n.value > 0
+    need = n.value
+
+    def call(x=A, d=d, gamma=None, y=None, dy=B_, eps=1e-5, dx=C, dres=None, dg=D, db=E, acc=0, work=W, size=need):
+        return lib.bc_layer_norm_grad(x, d, gamma, y, dy, eps, dx, dres, dg, db, acc, work, size, None)
+
+    assert call(x=None) == call(dy=None) == call(dx=None) == call(work=None) == B.BC_ERR_NULL
+    assert call(acc=2) == call(eps=-1.0) == B.BC_ERR_SHAPE
+    assert call(d=B.bc_tensor(1, 64, 16, 32, 9, 1)) == B.BC_ERR_DTYPE
+    assert call(d=B.bc_tensor(1, 64, 16, 32, 0, 0)) == B.BC_ERR_LAYOUT
+    assert call(size=need - 1) == call(size=-1) == B.BC_ERR_CAPACITY
+    assert call(work=W + 4) == B.BC_ERR_UNSUPPORTED
+    for bad in (dict(dx=A + 2), dict(dx=B_ + 2), dict(y=C), dict(dres=A), dict(dres=C), dict(gamma=C + 64), dict(dg=A),
+                dict(db=D + 4), dict(dg=W), dict(dx=W), dict(work=A), dict(dx=B_, dres=B_)):
+        assert call(**bad) == B.BC_ERR_ALIAS, bad
+
+
+def test_orthogonalize_refusals(B):
+    lib = B.raw()
+    n = ctypes.c_int64()
+    for args in ((0, 64, 64, 5), (1, 0, 64, 5), (1, 64, -1, 5), (1, 64, 64, 0), (1, 64, 64, 65), (1, 20000, 20000, 5),
+                 (1, 1 << 30, 8, 5), (1 << 25, 1, 1, 5), (2000, 2000, 2000, 5)):
+        assert lib.bc_orthogonalize_work(*args, ctypes.byref(n)) == B.BC_ERR_SHAPE, args
+    assert lib.bc_orthogonalize_work(1, 64, 64, 5, None) == B.BC_ERR_NULL
+    assert lib.bc_orthogonalize_work(2, 64, 100, 5, ctypes.byref(n)) == B.BC_OK
+    need = n.value
+    good = (5, 3.4445, -4.7750, 2.0315, 1e-7)
+
+    def call(g=A, dt=0, size=(2, 64, 100), ns=good, out=B_, odt=0, work=W, nb=need):
+        return lib.bc_orthogonalize(g, dt, *size, None if ns is None else ctypes.byref(B.bc_newton_schulz(*ns)), out,
+                                    odt, work, nb, None)
+
+    assert call(g=None) == call(out=None) == call(work=None) == call(ns=None) == B.BC_ERR_NULL
+    assert call(size=(0, 64, 100)) == call(ns=(0,) + good[1:]) == B.BC_ERR_SHAPE
+    assert call(ns=good[:4] + (-1.0,)) == call(ns=good[:4] + (NAN,)) == B.BC_ERR_SHAPE
+    assert call(dt=4) == call(odt=-1) == B.BC_ERR_DTYPE
+    # not positive, not finite, growing without bound, past the entries' range in one step
+    for c in ((0.0, -1.0, 1.0), (-1.0, 0.0, 0.0), (NAN, 0.0, 0.0), (1.0, INF, 0.0), (3.0, 0.0, 0.0), (3.0, 8.0, 8.0)):
+        assert call(ns=(5, *c, 1e-7)) == B.BC_ERR_UNSUPPORTED, c
+    assert call(nb=need - 1) == B.BC_ERR_CAPACITY
+    assert call(work=W + 8) == B.BC_ERR_UNSUPPORTED
+    for bad in (dict(out=A + 4), dict(out=A, odt=1), dict(work=A), dict(out=W + 256)):
+        assert call(**bad) == B.BC_ERR_ALIAS, bad
+
+
+def test_muon_refusals(B):
+    lib = B.raw()
+    ns = (5, 3.4445, -4.7750, 2.0315, 1e-7)
+    n = ctypes.c_int64()
+    good = [(A, B_, C, D, 64, 288), (A + (1 << 20), B_ + (1 << 20), C + (1 << 20), None, 128, 64)]
+
+    def params(rows):
+        arr = (B.bc_matrix * len(rows))()
+        for a, r in zip(arr, rows):
+            a.w, a.momentum, a.grad, a.w16, a.rows, a.cols = r
+        return arr
+
+    assert lib.bc_muon_step_many_work(params(good), 2, 5, ctypes.byref(n)) == B.BC_OK
+    need = n.value
+    assert lib.bc_muon_step_many_work(None, 2, 5, ctypes.byref(n)) == B.BC_ERR_NULL
+    assert lib.bc_muon_step_many_work(params(good), 2, 5, None) == B.BC_ERR_NULL
+    assert lib.bc_muon_step_many_work(params(good), 0, 5, ctypes.byref(n)) == B.BC_ERR_SHAPE
+    assert lib.bc_muon_step_many_work(params(good * 33), 65, 5, ctypes.byref(n)) == B.BC_ERR_SHAPE
+
+    def call(rows=good, lr=0.02, mu=0.95, wd=0.0, nesterov=1, ns=ns, dt=1, work=W, nb=need):
+        h = B.bc_muon(lr, mu, wd, nesterov, B.bc_newton_schulz(*ns))
+        return lib.bc_muon_step_many(params(rows), len(rows), ctypes.byref(h), dt, work, nb, None)
+
+    assert lib.bc_muon_step_many(params(good), 2, None, 1, W, need, None) == B.BC_ERR_NULL
+    for k in range(3):
+        r = list(good[0])
+        r[k] = None
+        assert call(rows=[tuple(r), good[1]]) == B.BC_ERR_NULL
+    assert call(work=None) == B.BC_ERR_NULL
+    assert call(rows=[good[0][:4] + (0, 288)]) == call(lr=NAN) == call(mu=INF) == call(wd=NAN) == B.BC_ERR_SHAPE
+    assert call(nesterov=2) == call(ns=(65,) + ns[1:]) == B.BC_ERR_SHAPE
+    assert call(dt=0) == B.BC_ERR_DTYPE
+    assert call(ns=(5, 3.0, 0.0, 0.0, 1e-7)) == B.BC_ERR_UNSUPPORTED
+    assert call(nb=need - 1) == B.BC_ERR_CAPACITY
+    for k, v in ((0, B_ + 4), (2, A + 64), (3, A), (3, W), (1, good[1][0])):
+        r = list(good[0])
+        r[k] = v
+        assert call(rows=[tuple(r), good[1]]) == B.BC_ERR_ALIAS, (k, v)
+
+
+def test_binding_refuses_mismatched_tensors(B):
+    x = torch.zeros((1, 4, 4, 16), dtype=torch.bfloat16)
+    v, bad = torch.zeros(16), torch.zeros(15)
+    out = torch.empty_like(x)
+    for args in ((x, B.BC_NHWC, bad, v, None, 1e-5, 0, out), (x, B.BC_NHWC, v, v.bfloat16(), None, 1e-5, 0, out),
+                 (x, B.BC_NHWC, v, v, x[:, :2], 1e-5, 0, out), (x, B.BC_NHWC, v, v, None, 1e-5, 0, out.float()),
+                 (x.transpose(1, 2), B.BC_NHWC, v, v, None, 1e-5, 0, out)):
+        with pytest.raises(ValueError):
+            B.bc_sparse_layer_norm(*args, (1, 1), None, None)
+    with pytest.raises(ValueError):
+        B.bc_layer_norm_grad(x, B.BC_NHWC, v, None, x.float(), 1e-5, out, None, v, v)
+    with pytest.raises(ValueError):
+        B.bc_layer_norm_grad(x, B.BC_NHWC, v, None, x, 1e-5, out, None, bad, v)
+    g = torch.zeros(8, 16)
+    with pytest.raises(ValueError):
+        B.bc_orthogonalize(g, torch.zeros(16, 8))
+    with pytest.raises(ValueError):
+        B.bc_orthogonalize(g.T, torch.zeros(16, 8))
+    with pytest.raises(ValueError):
+        B.bc_muon_step_many([(g, g.clone(), g[:4].clone(), None)], 0.1, 0.9, 0.0)
+    with pytest.raises(ValueError):
+        B.bc_muon_step_many([(g, g.clone(), g.double(), None)], 0.1, 0.9, 0.0)
