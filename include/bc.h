@@ -639,8 +639,9 @@ bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32
 
 /*
  * Orthogonalises each of `batch` matrices: d_out = X of the iteration *ns on d_g.
- *   d_g, d_out   [batch][rows][cols] of in_dtype and out_dtype (any dtypes, any sizes >= 1,
- *                any element alignment); d_out may be d_g itself if the dtypes agree.
+ *   d_g, d_out   [batch][rows][cols] of in_dtype and out_dtype (any dtypes, any element
+ *                alignment, any sizes >= 1 up to 16384 for the shorter side, 2^22 for the longer
+ *                and 4e9 elements); d_out may be d_g itself if the dtypes agree.
  * fp32 accuracy whatever the dtypes (operands held as two fp16 numbers, three matrix-core
  * products, fp32 sums; the norm in fp64), one round to out_dtype. A matrix of zeros gives
  * zeros (eps > 0); a NaN or infinity stays within its matrix. Equal inputs give equal bits.

@@ -1157,7 +1157,10 @@ bc_status bc_sparse_layer_norm(const void *d_in, bc_tensor desc, const float *d_
         return fail(BC_ERR_ALIAS, "d_out overlaps the index");
     if ((st = check_registered(d_out, desc, d_idx != nullptr))) return st;
     G.relu = relu;
-    G.gh = L.gh; G.gw = L.gw; G.bh = L.bh; G.bw = L.bw;
+    G.gw = L.gw; G.bh = L.bh; G.bw = L.bw;
+    G.by_block = bc::Divisor((uint32_t)L.bh * (uint32_t)L.bw);
+    G.by_gw = bc::Divisor(L.gw);
+    G.by_bw = bc::Divisor(L.bw);
     G.idx = d_idx;
     G.count = d_count;
     hipError_t e = bc::launch_norm(d_in, d_gamma, d_beta, d_residual, d_out, G, desc.dtype, (hipStream_t)stream);
@@ -1216,6 +1219,7 @@ static bc_status orth_sizes(int32_t batch, int32_t rows, int32_t cols, int32_t s
     if (batch < 1 || rows < 1 || cols < 1) return fail(BC_ERR_SHAPE, "%s: sizes must be positive", name);
     if ((double)batch * rows * cols > 4.0e9) return fail(BC_ERR_SHAPE, "%s: more than 4e9 elements", name);
     if (std::min(rows, cols) > 16384) return fail(BC_ERR_SHAPE, "%s: the shorter side is above 16384", name);
+    if (std::max(rows, cols) > (1 << 22)) return fail(BC_ERR_SHAPE, "%s: the longer side is above 2^22", name);
     if ((double)batch * bc::orth_tiles(rows, cols) >= (double)(1 << 24))
         return fail(BC_ERR_SHAPE, "%s: 2^24 or more tiles of 64 x 64", name);
     if (steps < 1 || steps > 64) return fail(BC_ERR_SHAPE, "steps outside 1..64");
@@ -1231,12 +1235,21 @@ static bc_status orth_iteration(const bc_newton_schulz &in, bc::NewtonSchulz &ns
     return BC_OK;
 }
 
+static size_t orth_need(int32_t batch, int32_t rows, int32_t cols)
+{
+    bc::OrthEntry e{};
+    e.rows = rows;
+    e.cols = cols;
+    e.batch = batch;
+    return bc::orth_shared_work(&e, 1) + bc::orth_work(rows, cols) * (size_t)batch;
+}
+
 bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32_t steps, int64_t *bytes)
 {
     if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
     bc_status st = orth_sizes(batch, rows, cols, steps, "matrices");
     if (st) return st;
-    *bytes = (int64_t)(bc::orth_work(rows, cols) * (size_t)batch);
+    *bytes = (int64_t)orth_need(batch, rows, cols);
     return ok();
 }
 
@@ -1250,7 +1263,7 @@ bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int
     if (!valid_dtype(in_dtype) || !valid_dtype(out_dtype)) return fail(BC_ERR_DTYPE, "unknown dtype");
     bc::NewtonSchulz it;
     if ((st = orth_iteration(*ns, it))) return st;
-    const size_t need = bc::orth_work(rows, cols) * (size_t)batch;
+    const size_t need = orth_need(batch, rows, cols);
     if ((st = check_work(d_work, work_bytes, need))) return st;
     const size_t count = (size_t)batch * rows * cols, ib = count * esize_of(in_dtype), ob = count * esize_of(out_dtype);
     if (overlap(d_work, need, d_g, ib) || overlap(d_work, need, d_out, ob) ||
@@ -1261,7 +1274,7 @@ bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int
     T.work = (uint8_t *)d_work;
     T.g = d_g;
     T.out = d_out;
-    T.e[0] = {rows, cols, batch, 0, 0, 0};
+    T.e[0] = {rows, cols, batch, 0, 0, 0, 1, 0};
     hipError_t e = bc::launch_orth(T, bc::OrthStep{}, false, in_dtype, out_dtype, it, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "orthogonalisation launch");
     return ok();
@@ -1274,15 +1287,20 @@ static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, s
     if (n < 1 || n > bc::kMaxParams) return fail(BC_ERR_SHAPE, "n outside 1..%d", bc::kMaxParams);
     *need = 0;
     double tiles = 0;
+    bc::OrthEntry e[bc::kMaxParams] = {};
     for (int t = 0; t < n; ++t) {
         char name[32];
         snprintf(name, sizeof name, "params[%d]", t);
         bc_status st = orth_sizes(1, params[t].rows, params[t].cols, steps, name);
         if (st) return st;
+        e[t].rows = params[t].rows;
+        e[t].cols = params[t].cols;
+        e[t].batch = 1;
         *need += bc::orth_work(params[t].rows, params[t].cols);
         tiles += bc::orth_tiles(params[t].rows, params[t].cols);
     }
     if (tiles >= (double)(1 << 24)) return fail(BC_ERR_SHAPE, "2^24 or more tiles of 64 x 64");
+    *need += bc::orth_shared_work(e, n);
     return BC_OK;
 }
 
@@ -1322,7 +1340,7 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
         for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all.push_back({q, count * 4});
         if (p.w16) all.push_back({p.w16, count * 2});
         any16 = any16 || p.w16;
-        T.e[t] = {p.rows, p.cols, 1, 0, 0, (uint32_t)(off / 256)};
+        T.e[t] = {p.rows, p.cols, 1, 0, 0, (uint32_t)(off / 256), 1, 0};
         T.p[t] = {p.w, p.momentum, p.grad, (uint16_t *)p.w16};
         off += bc::orth_work(p.rows, p.cols);
     }

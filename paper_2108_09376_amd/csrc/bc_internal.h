@@ -150,12 +150,29 @@ hipError_t launch_rmsprop(float *w, float *v, float *grad, long long count, floa
 
 // Layer normalisation over channels (k_norm.hip): rows of c elements, every pixel of a
 // channels-last map (idx == nullptr) or the pixels of its active blocks. fmt: a bc_dtype.
+// n / d for any 32-bit n as a multiplication (Granlund and Montgomery, 1994): with
+// l = ceil(log2 d), mul = floor(2^32 (2^l - d) / d) + 1, t = high word of mul * n, the
+// quotient is (t + ((n - t) >> min(l, 1))) >> max(l - 1, 0).
+struct Divisor {
+    uint32_t mul;
+    int first, then;
+    Divisor() = default;
+    explicit Divisor(uint32_t d)
+    {
+        int l = 0;
+        while (l < 32 && ((uint64_t)1 << l) < d) ++l;
+        mul = (uint32_t)((((((uint64_t)1 << l) - d) << 32) / d) + 1);
+        first = l < 1 ? l : 1;
+        then = l < 1 ? 0 : l - 1;
+    }
+};
 struct NormGeom {
     uint32_t rows;                             // pixels of the map
     int c;
     float inv_c, eps;
     int relu;
-    int gh, gw, bh, bw;                        // block grid of the map, with an index
+    int gw, bh, bw;                            // block grid of the map, with an index
+    Divisor by_block, by_gw, by_bw;            // bh bw, gw, bw
     const int32_t *idx, *count;
 };
 struct NormGradArgs {
@@ -172,11 +189,13 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
 
 // Orthogonalised updates (k_orth.hip). A table entry is a shape with its matrices: one of an
 // optimiser's step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the
-// workspace, orth_work(rows, cols) bytes for each matrix. first and per are the launches'.
+// workspace (after the shared part), orth_work(rows, cols) bytes for each matrix. first, per
+// and splits are the launches'.
 struct OrthEntry {
     int rows, cols, batch;
     uint32_t first, per;
     uint32_t off;
+    uint16_t splits, direct;                   // K ranges of this launch; which of its plans
 };
 struct OrthParam {
     float *w, *mom, *grad;
@@ -184,7 +203,9 @@ struct OrthParam {
 };
 struct OrthTable {
     int n;
-    uint8_t *work;
+    uint8_t *work;                             // the matrices' parts
+    uint32_t *count;                           // arrivals per tile and partial sums of K ranges
+    float *part;
     const void *g;                             // bc_orthogonalize: [batch][rows][cols]
     void *out;
     OrthEntry e[kMaxParams];
@@ -198,12 +219,20 @@ struct OrthJob {
     int L, R, E1, E2, D;                       // buffers of a matrix's slot
     float s1, s2, s3;
 };
-struct OrthJobs { OrthJob job[2]; };
+struct OrthPlan {                              // one launch's products of a matrix
+    int jobs, sym, last;
+    OrthJob job[2];
+};
+struct OrthStage {
+    OrthPlan plan[2];                          // matrices taken in spans, matrices taken step by step
+    int out, fmt;
+};
 struct NewtonSchulz {
     int steps;
     float a, b, c, eps;
 };
-size_t orth_work(int rows, int cols);
+size_t orth_work(int rows, int cols);         // bytes of a matrix's part
+size_t orth_shared_work(const OrthEntry *e, int n);
 unsigned orth_tiles(int rows, int cols);       // workgroups of the largest launch, per matrix
 bool orth_supported(const NewtonSchulz &ns, const char **why);
 hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,

@@ -37,30 +37,41 @@ __device__ __forceinline__ uint32_t row_count(const NormGeom &g)
     return g.idx ? (uint32_t)*g.count * (uint32_t)(g.bh * g.bw) : g.rows;
 }
 
-// Pixel of row r: itself, or the pixel of an active block.
+__device__ __forceinline__ uint32_t div(uint32_t n, const Divisor &d)
+{
+    const uint32_t t = __umulhi(n, d.mul);
+    return (t + ((n - t) >> d.first)) >> d.then;
+}
+
+// Pixel of row r: itself, or the pixel of an active block. Block rows of all images follow
+// one another (id / gw), and so do their pixel rows.
 __device__ __forceinline__ uint32_t row_pixel(const NormGeom &g, uint32_t r)
 {
     if (!g.idx) return r;
-    const uint32_t bpx = g.bh * g.bw, k = r / bpx, p = r - k * bpx;
-    const uint32_t id = g.idx[k], bpi = g.gh * g.gw;
-    const uint32_t img = id / bpi, b = id - img * bpi, gy = b / g.gw, gx = b - gy * g.gw;
-    const uint32_t py = p / g.bw, px = p - py * g.bw;
-    return (img * (g.gh * g.bh) + gy * g.bh + py) * (g.gw * g.bw) + gx * g.bw + px;
+    const uint32_t k = div(r, g.by_block), p = r - k * (uint32_t)(g.bh * g.bw);
+    const uint32_t id = g.idx[k], row = div(id, g.by_gw), gx = id - row * g.gw;
+    const uint32_t py = div(p, g.by_bw), px = p - py * g.bw;
+    return (row * g.bh + py) * (g.gw * g.bw) + gx * g.bw + px;
 }
 
-// Sum over the L lanes of a row: part of a wave, or the workgroup's four waves (through
-// `lds`, a slot of four floats that is free for reuse two sums later).
-template <int L>
-__device__ __forceinline__ float row_sum(float v, float *lds)
+// Sums of N values over the L lanes of a row: part of a wave, or two or four waves (through
+// `lds`, their slots, free for reuse after the next sum's barrier; the whole workgroup calls).
+template <int L, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (&lds)[N][4])
 {
-    if constexpr (L <= 64) {
-        return lane_sum<L>(v);
-    } else {
-        static_assert(L == kThreads, "a row belongs to a wave's lanes or to the workgroup");
-        v = lane_sum<64>(v);
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lane_sum<(L < 64 ? L : 64)>(v[i]);
+    if constexpr (L > 64) {
+        static_assert(L == 128 || L == 256, "a row belongs to a wave's lanes, to two waves or to four");
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) lds[i][threadIdx.x % L >> 6] = v[i];
         __syncthreads();
-        return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = lds[i][0] + lds[i][1];
+            if constexpr (L == 256) v[i] += lds[i][2] + lds[i][3];
+        }
     }
 }
 
@@ -80,6 +91,40 @@ __device__ __forceinline__ Span span_of(int v, int c)
     return {at, begin - at};
 }
 
+// Gains (or offsets) of a lane's columns. Rows of one vector per lane keep them in registers;
+// longer rows read them again for each row, from the L1, and leave the registers to rows in
+// flight (the pointer is made opaque, or the compiler would keep them all the same).
+template <int VEC>
+__device__ __forceinline__ void load_columns(const float *p, int at, float other, float (&out)[VEC])
+{
+    if (p) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) out[j] = p[at + j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) out[j] = other;
+    }
+}
+
+__device__ __forceinline__ const float *again(const float *p)
+{
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// Rows of several 16-bit vectors stay as stored between the passes: the words are made opaque, or the
+// compiler would keep the converted values too, at twice the registers.
+template <int FMT, int VEC, int NV>
+__device__ __forceinline__ void keep_stored(Raw<FMT, VEC> (&r)[NV])
+{
+    if constexpr (FMT != kF32 && NV >= 2) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(r[v].w[i]));
+    }
+}
+
 // ---------------------------------------------------------------- forward
 
 template <int FMT, int VEC, int L, int NV, bool FULL>
@@ -88,54 +133,65 @@ __global__ __launch_bounds__(kThreads) void k_norm(const void *x, const float *_
                                                    void *out, NormGeom g)
 {
     constexpr int kGroups = kThreads / L;
-    __shared__ float lds[2][4];
+    constexpr bool kKeep = NV <= 2;                       // gains and offsets in registers
+    __shared__ float sums[L > 64 ? kGroups : 1][2][1][4];
     const int group = threadIdx.x / L;
+    auto &lds = sums[L > 64 ? group : 0];
     const uint32_t rows = row_count(g);
     Span sp[NV];
-    float ga[NV][VEC], be[NV][VEC];
+    float ga[kKeep ? NV : 1][VEC], be[kKeep ? NV : 1][VEC];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         sp[v] = span_of<VEC, L, FULL>(v, g.c);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            ga[v][j] = gamma ? gamma[sp[v].at + j] : 1.f;
-            be[v][j] = beta ? beta[sp[v].at + j] : 0.f;
+        if constexpr (kKeep) {
+            load_columns(gamma, sp[v].at, 1.f, ga[v]);
+            load_columns(beta, sp[v].at, 0.f, be[v]);
         }
     }
-    // the workgroup's groups take neighbouring rows
-    for (uint32_t r = blockIdx.x * kGroups + group; r < rows; r += gridDim.x * kGroups) {
-        const size_t base = (size_t)row_pixel(g, r) * g.c;
+    // the workgroup's groups take neighbouring rows, all of them as many turns (a barrier may
+    // be in them): past the last row a group reads the last one again and keeps nothing
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < rows; r0 += gridDim.x * kGroups) {
+        const bool live = r0 + group < rows;
+        const size_t base = (size_t)row_pixel(g, live ? r0 + group : rows - 1) * g.c;
         Raw<FMT, VEC> rx[NV], rr[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) rx[v] = load_raw<FMT, VEC>(x, base + sp[v].at);
         if (res)
 #pragma unroll
             for (int v = 0; v < NV; ++v) rr[v] = load_raw<FMT, VEC>(res, base + sp[v].at);
-        float d[NV][VEC], s = 0.f;
+        float s[1] = {0.f}, q[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) s[0] += FULL || j >= sp[v].skip ? get(rx[v], j) : 0.f;
+        row_sum<L>(s, lds[0]);
+        const float mean = s[0] / (float)g.c;
+        keep_stored(rx);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                d[v][j] = get(rx[v], j);
-                s += FULL || j >= sp[v].skip ? d[v][j] : 0.f;
+                const float d = get(rx[v], j) - mean;
+                q[0] += FULL || j >= sp[v].skip ? d * d : 0.f;
             }
-        const float mean = row_sum<L>(s, lds[0]) / (float)g.c;
-        float q = 0.f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                d[v][j] -= mean;
-                q += FULL || j >= sp[v].skip ? d[v][j] * d[v][j] : 0.f;
-            }
-        const float rstd = 1.f / sqrtf(row_sum<L>(q, lds[1]) * g.inv_c + g.eps);
+        row_sum<L>(q, lds[1]);
+        const float rstd = rsqrtf(q[0] * g.inv_c + g.eps);
+        keep_stored(rx);
+        const float *gp = gamma, *bp = beta;
+        if constexpr (!kKeep) gp = again(gamma), bp = again(beta);
+        if (!live) continue;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if (!FULL && sp[v].skip == VEC) continue;
+            auto &gain = ga[kKeep ? v : 0], &offset = be[kKeep ? v : 0];
+            if constexpr (!kKeep) {
+                load_columns(gp, sp[v].at, 1.f, gain);
+                load_columns(bp, sp[v].at, 0.f, offset);
+            }
             float y[VEC];
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                y[j] = d[v][j] * rstd * ga[v][j] + be[v][j];
+                y[j] = (get(rx[v], j) - mean) * rstd * gain[j] + offset[j];
                 if (res) y[j] += get(rr[v], j);
                 // a NaN passes (fmaxf would drop it)
                 if (g.relu) y[j] = y[j] < 0.f ? 0.f : y[j];
@@ -151,18 +207,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_long(const void *x, const flo
                                                         const float *__restrict__ beta, const void *res,
                                                         void *out, NormGeom g)
 {
-    __shared__ float lds[2][4];
+    __shared__ float lds[2][1][4];
     const uint32_t rows = row_count(g);
     for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const size_t base = (size_t)row_pixel(g, r) * g.c;
-        float s = 0.f, q = 0.f;
-        for (int i = threadIdx.x; i < g.c; i += kThreads) s += get(load_raw<FMT, 1>(x, base + i), 0);
-        const float mean = row_sum<kThreads>(s, lds[0]) / (float)g.c;
+        float s[1] = {0.f}, q[1] = {0.f};
+        for (int i = threadIdx.x; i < g.c; i += kThreads) s[0] += get(load_raw<FMT, 1>(x, base + i), 0);
+        row_sum<kThreads>(s, lds[0]);
+        const float mean = s[0] / (float)g.c;
         for (int i = threadIdx.x; i < g.c; i += kThreads) {
             const float d = get(load_raw<FMT, 1>(x, base + i), 0) - mean;
-            q += d * d;
+            q[0] += d * d;
         }
-        const float rstd = 1.f / sqrtf(row_sum<kThreads>(q, lds[1]) * g.inv_c + g.eps);
+        row_sum<kThreads>(q, lds[1]);
+        const float rstd = rsqrtf(q[0] * g.inv_c + g.eps);
         for (int i = threadIdx.x; i < g.c; i += kThreads) {
             float y[1] = {(get(load_raw<FMT, 1>(x, base + i), 0) - mean) * rstd * (gamma ? gamma[i] : 1.f) +
                           (beta ? beta[i] : 0.f)};
@@ -175,101 +233,189 @@ __global__ __launch_bounds__(kThreads) void k_norm_long(const void *x, const flo
 
 // ---------------------------------------------------------------- backward
 
-// Partial sums of dgamma and dbeta: [workgroup][2][c] in `part`.
-template <int FMT, int VEC, int L, int NV, bool FULL>
-__global__ __launch_bounds__(kThreads) void k_norm_grad(NormGradArgs a, NormGeom g, float *__restrict__ part)
+// dy behind a ReLU: the stored bits where y > 0, zero elsewhere (a NaN there is not used).
+template <int FMT, int VEC>
+__device__ __forceinline__ Raw<FMT, VEC> masked(Raw<FMT, VEC> dy, const Raw<FMT, VEC> &y)
 {
-    constexpr int kGroups = kThreads / L;
-    __shared__ float lds[4][4];
-    const int group = threadIdx.x / L;
-    Span sp[NV];
-    float ga[NV][VEC], sg[NV][VEC], sb[NV][VEC];
+    if constexpr (FMT == kF32 || VEC == 1) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        sp[v] = span_of<VEC, L, FULL>(v, g.c);
+        for (int j = 0; j < VEC; ++j)
+            if (!(get(y, j) > 0.f)) dy.w[j] = 0u;
+    } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            ga[v][j] = a.gamma ? a.gamma[sp[v].at + j] : 1.f;
-            sg[v][j] = sb[v][j] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = get(y, 2 * i) > 0.f ? 0xFFFFu : 0u, hi = get(y, 2 * i + 1) > 0.f ? 0xFFFF0000u : 0u;
+            dy.w[i] &= lo | hi;
         }
     }
-    for (uint32_t r = blockIdx.x * kGroups + group; r < g.rows; r += gridDim.x * kGroups) {
-        const size_t base = (size_t)r * g.c;
-        Raw<FMT, VEC> rx[NV], rd[NV], ry[NV];
+    return dy;
+}
+
+// Threads of a workgroup whose rows take L lanes with NV vectors each
+template <int L, int NV> constexpr int kGradThreads = NV == 8 ? 256 : 512;
+
+// Sum over the lanes of a wave that hold the same columns (groups of L lanes).
+template <int L>
+__device__ __forceinline__ float group_sum(float v)
+{
+    if constexpr (L <= 8) v += dpp<0x128>(v);            // row_ror 8: lane ^ 8
+    if constexpr (L <= 16) {
+        const uint32_t u = __float_as_uint(v);
+        const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (L <= 32) {
+        const uint32_t u = __float_as_uint(v);
+        const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+
+// One row's stored vectors of a lane, requested together.
+template <int FMT, int VEC, int NV>
+struct GradRow {
+    Raw<FMT, VEC> x[NV], dy[NV], y[NV];
+
+    __device__ __forceinline__ void load(const NormGradArgs &a, const Span (&sp)[NV], size_t base)
+    {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            rx[v] = load_raw<FMT, VEC>(a.x, base + sp[v].at);
-            rd[v] = load_raw<FMT, VEC>(a.dy, base + sp[v].at);
+            x[v] = load_raw<FMT, VEC>(a.x, base + sp[v].at);
+            dy[v] = load_raw<FMT, VEC>(a.dy, base + sp[v].at);
         }
         if (a.y)
 #pragma unroll
-            for (int v = 0; v < NV; ++v) ry[v] = load_raw<FMT, VEC>(a.y, base + sp[v].at);
-        float d[NV][VEC], dy[NV][VEC], s = 0.f, t = 0.f;
+            for (int v = 0; v < NV; ++v) y[v] = load_raw<FMT, VEC>(a.y, base + sp[v].at);
+    }
+};
+
+// Partial sums of dgamma and dbeta: [workgroup][2][c] in `part`. The next row is requested
+// before the present one is worked on (but for rows that fill the registers).
+template <int FMT, int VEC, int L, int NV, bool FULL>
+__global__ __launch_bounds__((kGradThreads<L, NV>)) void k_norm_grad(NormGradArgs a, NormGeom g, float *__restrict__ part)
+{
+    constexpr int T = kGradThreads<L, NV>, kGroups = T / L, kWaves = T / 64;
+    constexpr bool kAhead = NV <= 4;
+    constexpr bool kKeep = NV <= 2;                       // gains in registers
+    __shared__ float sum1[L > 64 ? kGroups : 1][1][4], sum3[L > 64 ? kGroups : 1][3][4];
+    const int group = threadIdx.x / L;
+    Span sp[NV];
+    float sg[NV][VEC], sb[NV][VEC], ga[kKeep ? NV : 1][VEC];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        sp[v] = span_of<VEC, L, FULL>(v, g.c);
+        if constexpr (kKeep) load_columns(a.gamma, sp[v].at, 1.f, ga[v]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sg[v][j] = sb[v][j] = 0.f;
+    }
+    // every group takes as many turns as the workgroup (a barrier may be in them); past the
+    // last row a group reads the last one again and keeps nothing
+    auto base_of = [&](uint32_t r) { return (size_t)min(r, g.rows - 1) * g.c; };
+    const uint32_t stride = gridDim.x * kGroups;
+    GradRow<FMT, VEC, NV> row, next;
+    next.load(a, sp, base_of(blockIdx.x * kGroups + group));
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < g.rows; r0 += stride) {
+        const uint32_t r = r0 + group;
+        const size_t base = base_of(r);
+        row = next;
+        if (kAhead && r0 + stride < g.rows) next.load(a, sp, base_of(r + stride));
+        // behind a ReLU: from here on row.dy holds dy'
+        if (a.y)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) row.dy[v] = masked(row.dy[v], row.y[v]);
+        float one[1] = {0.f}, three[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const bool mine = FULL || j >= sp[v].skip;
-                d[v][j] = get(rx[v], j);
-                dy[v][j] = get(rd[v], j);
-                if (a.y && !(get(ry[v], j) > 0.f)) dy[v][j] = 0.f;
-                s += mine ? d[v][j] : 0.f;
-                t += mine ? dy[v][j] * ga[v][j] : 0.f;
-            }
-        const float mean = row_sum<L>(s, lds[0]) / (float)g.c;
-        const float mean_g = row_sum<L>(t, lds[1]) * g.inv_c;
-        float q = 0.f, u = 0.f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const bool mine = FULL || j >= sp[v].skip;
-                d[v][j] -= mean;
-                q += mine ? d[v][j] * d[v][j] : 0.f;
-                u += mine ? dy[v][j] * ga[v][j] * d[v][j] : 0.f;
-            }
-        const float rstd = 1.f / sqrtf(row_sum<L>(q, lds[2]) * g.inv_c + g.eps);
-        const float mean_gx = row_sum<L>(u, lds[3]) * rstd * g.inv_c;
+            for (int j = 0; j < VEC; ++j) one[0] += FULL || j >= sp[v].skip ? get(row.x[v], j) : 0.f;
+        row_sum<L>(one, sum1[L > 64 ? group : 0]);
+        const float mean = one[0] / (float)g.c;
+        keep_stored(row.x);
+        const float *gp = a.gamma;
+        if constexpr (!kKeep) gp = again(gp);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (!FULL && sp[v].skip == VEC) continue;
-            float dx[VEC];
+            auto &gain = ga[kKeep ? v : 0];
+            if constexpr (!kKeep) load_columns(gp, sp[v].at, 1.f, gain);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float xhat = d[v][j] * rstd;
-                dx[j] = rstd * (dy[v][j] * ga[v][j] - mean_g - xhat * mean_gx);
-                sg[v][j] += dy[v][j] * xhat;
-                sb[v][j] += dy[v][j];
+                const bool mine = FULL || j >= sp[v].skip;
+                const float d = mine ? get(row.x[v], j) - mean : 0.f, gr = mine ? get(row.dy[v], j) * gain[j] : 0.f;
+                three[0] += d * d;
+                three[1] += gr;
+                three[2] += gr * d;
             }
-            store_raw<FMT, VEC>(a.dx, base + sp[v].at, pack<FMT, VEC>(dx));
-            if (a.dres) store_raw<FMT, VEC>(a.dres, base + sp[v].at, pack<FMT, VEC>(dy[v]));
         }
+        row_sum<L>(three, sum3[L > 64 ? group : 0]);
+        const float rstd = rsqrtf(three[0] * g.inv_c + g.eps), mean_g = three[1] * g.inv_c;
+        const float mean_gx = three[2] * rstd * g.inv_c;
+        keep_stored(row.x);
+        keep_stored(row.dy);
+        if (r < g.rows) {
+            if constexpr (!kKeep) gp = again(gp);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (!FULL && sp[v].skip == VEC) continue;
+                auto &gain = ga[kKeep ? v : 0];
+                if constexpr (!kKeep) load_columns(gp, sp[v].at, 1.f, gain);
+                float dx[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float xhat = get(row.x[v], j) * rstd - mean * rstd, dy = get(row.dy[v], j);
+                    dx[j] = rstd * (dy * gain[j] - (xhat * mean_gx + mean_g));
+                    sg[v][j] += dy * xhat;
+                    sb[v][j] += dy;
+                }
+                store_raw<FMT, VEC>(a.dx, base + sp[v].at, pack<FMT, VEC>(dx));
+                if (a.dres) store_raw<FMT, VEC>(a.dres, base + sp[v].at, row.dy[v]);
+            }
+        }
+        if (!kAhead && r0 + stride < g.rows) next.load(a, sp, base_of(r + stride));
     }
     if (!part) return;
-    // the groups' sums, one after the other in LDS, then one row of the partial table
-    extern __shared__ float cols[];                       // [2][c]
-    for (int turn = 0; turn < kGroups; ++turn) {
-        __syncthreads();
-        if (group != turn) continue;
+    // a wave's groups by register exchanges, then the waves (or groups) through LDS, in
+    // their order: side by side for one vector per lane, else one after the other
+    extern __shared__ float cols[];                       // [waves or 1][2][c]
+    constexpr bool kApart = NV == 1 && L <= 64;
+    constexpr int kTurns = kApart ? 1 : T / (L < 64 ? 64 : L);
+    const int turn_of = threadIdx.x / (L < 64 ? 64 : L);
+    if constexpr (L < 64)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                sg[v][j] = group_sum<L>(sg[v][j]);
+                sb[v][j] = group_sum<L>(sb[v][j]);
+            }
+    float *mine = cols + (kApart ? (threadIdx.x >> 6) * 2 * g.c : 0);
+    for (int turn = 0; turn < kTurns; ++turn) {
+        if (turn) __syncthreads();
+        if ((!kApart && turn_of != turn) || (L < 64 && (threadIdx.x & 63) >= L)) continue;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 if (!FULL && j < sp[v].skip) continue;
                 const int i = sp[v].at + j;
-                cols[i] = (turn ? cols[i] : 0.f) + sg[v][j];
-                cols[g.c + i] = (turn ? cols[g.c + i] : 0.f) + sb[v][j];
+                mine[i] = (turn ? mine[i] : 0.f) + sg[v][j];
+                mine[g.c + i] = (turn ? mine[g.c + i] : 0.f) + sb[v][j];
             }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * g.c; i += kThreads) part[(size_t)blockIdx.x * 2 * g.c + i] = cols[i];
+    for (int i = threadIdx.x; i < 2 * g.c; i += T) {
+        float s = cols[i];
+        if constexpr (kApart)
+            for (int w = 1; w < kWaves; ++w) s += cols[w * 2 * g.c + i];
+        part[(size_t)blockIdx.x * 2 * g.c + i] = s;
+    }
 }
 
 // Rows longer than a workgroup's registers: their mean, rstd, mean(g) and mean(g xhat) first,
 template <int FMT>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_stats(NormGradArgs a, NormGeom g, float4 *__restrict__ stats)
 {
-    __shared__ float lds[4][4];
+    __shared__ float lds[2][2][4];
     for (uint32_t r = blockIdx.x; r < g.rows; r += gridDim.x) {
         const size_t base = (size_t)r * g.c;
         auto x_at = [&](int i) { return get(load_raw<FMT, 1>(a.x, base + i), 0); };
@@ -277,20 +423,21 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_stats(NormGradArgs a, No
             if (a.y && !(get(load_raw<FMT, 1>(a.y, base + i), 0) > 0.f)) return 0.f;
             return get(load_raw<FMT, 1>(a.dy, base + i), 0) * (a.gamma ? a.gamma[i] : 1.f);
         };
-        float s = 0.f, t = 0.f, q = 0.f, u = 0.f;
+        float one[2] = {0.f, 0.f}, two[2] = {0.f, 0.f};
         for (int i = threadIdx.x; i < g.c; i += kThreads) {
-            s += x_at(i);
-            t += g_at(i);
+            one[0] += x_at(i);
+            one[1] += g_at(i);
         }
-        const float mean = row_sum<kThreads>(s, lds[0]) / (float)g.c;
-        const float mean_g = row_sum<kThreads>(t, lds[1]) * g.inv_c;
+        row_sum<kThreads>(one, lds[0]);
+        const float mean = one[0] / (float)g.c, mean_g = one[1] * g.inv_c;
         for (int i = threadIdx.x; i < g.c; i += kThreads) {
             const float d = x_at(i) - mean;
-            q += d * d;
-            u += g_at(i) * d;
+            two[0] += d * d;
+            two[1] += g_at(i) * d;
         }
-        const float rstd = 1.f / sqrtf(row_sum<kThreads>(q, lds[2]) * g.inv_c + g.eps);
-        const float mean_gx = row_sum<kThreads>(u, lds[3]) * rstd * g.inv_c;
+        row_sum<kThreads>(two, lds[1]);
+        const float rstd = rsqrtf(two[0] * g.inv_c + g.eps);
+        const float mean_gx = two[1] * rstd * g.inv_c;
         if (threadIdx.x == 0) stats[r] = make_float4(mean, rstd, mean_g, mean_gx);
     }
 }
@@ -322,23 +469,25 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_cols(NormGradArgs a, Nor
     }
 }
 
-// Adds the partial rows in their order: 32 columns per workgroup, eight runs of rows each
+// Adds the partial rows in their order: 32 columns per workgroup, 32 runs of rows each
 // (each summed in order), then the runs in order.
-__global__ __launch_bounds__(kThreads) void k_norm_grad_join(const float *__restrict__ part, int parts, int c,
-                                                             float *__restrict__ dgamma, float *__restrict__ dbeta,
-                                                             int accumulate)
+constexpr int kRuns = 32;
+__global__ __launch_bounds__(32 * kRuns) void k_norm_grad_join(const float *__restrict__ part, int parts, int c,
+                                                               float *__restrict__ dgamma, float *__restrict__ dbeta,
+                                                               int accumulate)
 {
-    __shared__ float lds[8][33];
+    __shared__ float lds[kRuns][33];
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const int i = blockIdx.x * 32 + lane;
-    const int each = (parts + 7) / 8, lo = run * each, hi = min(parts, lo + each);
+    const int each = (parts + kRuns - 1) / kRuns, lo = run * each, hi = min(parts, lo + each);
     float s = 0.f;
     if (i < 2 * c)
+#pragma unroll 8
         for (int p = lo; p < hi; ++p) s += part[(size_t)p * 2 * c + i];
     lds[run][lane] = s;
     __syncthreads();
     if (run || i >= 2 * c) return;
-    for (int k = 1; k < 8; ++k) s += lds[k][lane];
+    for (int k = 1; k < kRuns; ++k) s += lds[k][lane];
     float *to = i < c ? dgamma : dbeta;
     if (!to) return;
     to += i < c ? i : i - c;
@@ -364,41 +513,39 @@ bool with_form(int c, F &&f)
         return true;
     }
     const int nv = (c + V - 1) / V;
-    if (nv <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (nv <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (nv <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    else if (nv <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (nv <= 128) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    else if (nv <= 256) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (nv <= 512) go(integral_constant<int, kThreads>{}, integral_constant<int, 2>{});
-    else if (nv <= 1024) go(integral_constant<int, kThreads>{}, integral_constant<int, 4>{});
-    else if (nv <= 2048) go(integral_constant<int, kThreads>{}, integral_constant<int, 8>{});
-    else return false;
-    return true;
+    auto with = [&](auto lanes, auto vecs) { go(lanes, vecs); return true; };
+    using one = integral_constant<int, 1>;
+    using wave = integral_constant<int, 64>;
+    using group = integral_constant<int, 256>;
+    if (nv <= 8) return with(integral_constant<int, 8>{}, one{});
+    if (nv <= 16) return with(integral_constant<int, 16>{}, one{});
+    if (nv <= 32) return with(integral_constant<int, 32>{}, one{});
+    if (nv <= 64) return with(wave{}, one{});
+    if (nv <= 128) return with(integral_constant<int, 128>{}, one{});
+    if (nv <= 256) return with(group{}, one{});
+    if (nv <= 512) return with(group{}, integral_constant<int, 2>{});
+    if (nv <= 1024) return with(group{}, integral_constant<int, 4>{});
+    if (nv <= 2048) return with(group{}, integral_constant<int, 8>{});
+    return false;
 }
 
 constexpr unsigned kMostForward = 2048;      // eight workgroups per CU
-constexpr unsigned kMostBackward = 512;
 constexpr int kLongParts = 64;
 
-// Rows per workgroup and turn of the form for rows of c elements; 0: the long form.
-int row_groups(int fmt, int c)
+// Workgroups of the backward pass, each with a partial row; *held: its form keeps the row.
+unsigned parts_of(int fmt, uint32_t rows, int c, bool *held)
 {
-    const int v = fmt == kF32 ? kVec<kF32> : kVec<kBF16>;
-    if (c < v) return 32;
-    const int nv = (c + v - 1) / v;
-    if (nv <= 8) return 32;
-    if (nv <= 16) return 16;
-    if (nv <= 32) return 8;
-    if (nv <= 256) return 4;
-    return nv <= 2048 ? 1 : 0;
-}
-
-unsigned parts_of(int fmt, uint32_t rows, int c)
-{
-    const int groups = row_groups(fmt, c);
-    if (!groups) return std::min<uint32_t>(rows, kLongParts);
-    return std::min<uint32_t>((rows + groups - 1) / groups, kMostBackward);
+    return with_format(fmt, [&](auto f) {
+        unsigned parts = std::min<uint32_t>(rows, kLongParts);
+        *held = with_form<decltype(f)::value>(c, [&](auto, auto lanes, auto vecs, auto) {
+            constexpr int L = decltype(lanes)::value, kGroups = kGradThreads<L, decltype(vecs)::value> / L;
+            // 512, two per CU, where each has two turns at least (32768 rows of 64: 9.8 us
+            // with 512, 9.0 with 256) and rows leave room for two (4096 of 8192: 74 and 61)
+            const unsigned most = decltype(vecs)::value <= 2 && rows / (2 * kGroups) > 256 ? 512 : 256;
+            parts = std::min<uint32_t>({(rows + kGroups - 1) / kGroups, most, std::max(256u, rows / (2 * kGroups))});
+        });
+        return parts;
+    });
 }
 
 }  // namespace
@@ -423,25 +570,28 @@ hipError_t launch_norm(const void *x, const float *gamma, const float *beta, con
 
 size_t norm_grad_work(int fmt, uint32_t rows, int c)
 {
-    const size_t stats = row_groups(fmt, c) ? 0 : (size_t)rows * sizeof(float4);
-    return stats + (size_t)parts_of(fmt, rows, c) * 2 * c * sizeof(float);
+    bool held = false;
+    const size_t parts = parts_of(fmt, rows, c, &held);
+    return (held ? 0 : (size_t)rows * sizeof(float4)) + parts * 2 * c * sizeof(float);
 }
 
 hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, int accumulate, void *work,
                             const NormGeom &g, int fmt, hipStream_t s)
 {
-    const unsigned parts = parts_of(fmt, g.rows, g.c);
+    bool held = false;
+    const unsigned parts = parts_of(fmt, g.rows, g.c, &held);
     const bool sums = dgamma || dbeta;
     return with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         hipError_t e = hipSuccess;
         float *part = sums ? (float *)work : nullptr;
-        const size_t lds = sums ? (size_t)2 * g.c * sizeof(float) : 0;
-        const bool held = with_form<FMT>(g.c, [&](auto vec, auto lanes, auto vecs, auto full) {
-            auto kern = k_norm_grad<FMT, decltype(vec)::value, decltype(lanes)::value, decltype(vecs)::value,
-                                    decltype(full)::value>;
+        with_form<FMT>(g.c, [&](auto vec, auto lanes, auto vecs, auto full) {
+            constexpr int L = decltype(lanes)::value, NV = decltype(vecs)::value;
+            auto kern = k_norm_grad<FMT, decltype(vec)::value, L, NV, decltype(full)::value>;
+            const size_t tables = !sums ? 0 : NV == 1 && L <= 64 ? kGradThreads<L, NV> / 64 : 1;
+            const size_t lds = tables * 2 * g.c * sizeof(float);
             if ((e = allow_lds((const void *)kern, lds)) == hipSuccess)
-                hipLaunchKernelGGL(kern, dim3(parts), dim3(kThreads), lds, s, a, g, part);
+                hipLaunchKernelGGL(kern, dim3(parts), dim3(kGradThreads<L, NV>), lds, s, a, g, part);
         });
         if (e != hipSuccess) return e;
         if (!held) {
@@ -453,7 +603,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
                                s, a, g, stats, part);
         }
         if (sums)
-            hipLaunchKernelGGL(k_norm_grad_join, dim3((2 * g.c + 31) / 32), dim3(kThreads), 0, s, part, (int)parts,
+            hipLaunchKernelGGL(k_norm_grad_join, dim3((2 * g.c + 31) / 32), dim3(32 * kRuns), 0, s, part, (int)parts,
                                g.c, dgamma, dbeta, accumulate);
         return hipGetLastError();
     });

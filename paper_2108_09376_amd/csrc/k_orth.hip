@@ -26,38 +26,48 @@
 // the coefficients), as |X|_2 <= 1 at the start.
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "bc_internal.h"
+#include "lds_dma.h"
 #include "rows.h"
 
 namespace bc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 64;                      // tile edge; matrices are padded to it with zeros
+constexpr int kTile = 64;                      // edge of small tiles, and of the first kernel's
+constexpr int kBigTile = 128;
 constexpr float kScale = 4096.f;
 constexpr int kSpan = 3;                       // most steps between two A taken from X
 constexpr int kSumParts = 64;                  // partial sums of squares per matrix
+constexpr int kMostSplit = 768;                // workgroups of a launch that splits K
+constexpr int kLeastChunks = 16;               // chunks of K per range at least
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-__host__ __device__ constexpr int padded(int n) { return (n + kTile - 1) / kTile * kTile; }
-
 // A matrix's part of the workspace: partial sums, two X and five squares, each two planes
 // (hi, lo) of halves.
 struct Slot {
-    int m, n;                                  // rows <= columns of X, padded
+    int m, n;                                  // rows <= columns of X, padded with zeros to the tile edge
+    int edge;
     bool flip;                                 // X is the transpose
 };
+
+// Tiles of 128 x 128 read half the bytes per product of 64 x 64 ones but leave CUs idle
+// unless there are hundreds.
+__host__ __device__ constexpr int edge_of(int shorter) { return shorter > 1536 ? kBigTile : kTile; }
 
 __host__ __device__ inline Slot slot_of(int rows, int cols)
 {
     const bool flip = rows > cols;
-    return {padded(flip ? cols : rows), padded(flip ? rows : cols), flip};
+    const int m = flip ? cols : rows, n = flip ? rows : cols, e = edge_of(m);
+    return {(m + e - 1) / e * e, (n + e - 1) / e * e, e, flip};
 }
 
 enum Buf { kX0, kX1, kA, kR, kB0, kB1, kP, kNone };
+enum Out { kResult, kWeights };              // what the last product of a matrix writes
 
 __host__ __device__ inline size_t buf_at(const Slot &s, int b)
 {
@@ -74,10 +84,12 @@ struct Where {
     uint32_t local;
 };
 
+// Every lane looks at one entry: a chain of scalar loads over up to 64 takes microseconds.
 __device__ __forceinline__ Where find(const OrthTable &T, uint32_t at)
 {
-    int t = 0;
-    while (t + 1 < T.n && at >= T.e[t + 1].first) ++t;
+    static_assert(kMaxParams == 64, "one entry per lane");
+    const int lane = threadIdx.x & 63;
+    const int t = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < T.n && T.e[lane].first <= at)) - 1);
     const uint32_t per = T.e[t].per, in = at - T.e[t].first;
     const int img = in / per;
     return {t, img, in - img * per};
@@ -101,6 +113,8 @@ template <bool STEP, int FMT>
 __global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
 {
     __shared__ double lds[4];
+    if (blockIdx.x == 0)                                  // counters of the products
+        for (int i = threadIdx.x; i < kMostSplit; i += kThreads) T.count[i] = 0u;
     const Where w = find(T, blockIdx.x);
     const OrthEntry &e = T.e[w.t];
     const Slot s = slot_of(e.rows, e.cols);
@@ -133,7 +147,15 @@ __device__ __forceinline__ void store_split(_Float16 *hi, size_t plane, size_t a
     hi[at + plane] = (_Float16)(v - (float)h);
 }
 
-// X_0 from G, one padded tile per workgroup.
+__device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
+{
+    const float y[1] = {v};
+    if (fmt == kF32) store_raw<kF32, 1>(p, at, pack<kF32, 1>(y));
+    else if (fmt == kBF16) store_raw<kBF16, 1>(p, at, pack<kBF16, 1>(y));
+    else store_raw<kF16, 1>(p, at, pack<kF16, 1>(y));
+}
+
+// X_0 from G, one 64 x 64 tile per workgroup.
 template <bool STEP, int FMT>
 __global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h, double eps, int parts_each)
 {
@@ -177,117 +199,319 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h
 }
 
 // ---------------------------------------------------------------- products
+//
+// D = s1 E1 + s2 E2 + s3 L R over square tiles of every matrix, two jobs at most per matrix
+// and launch. Symmetric products (all but the last of a span) take L R as L R^T, rows of
+// both, and write a tile on or above the diagonal and its mirror image. The last one takes
+// R = X as it lies, rows along K, and writes X, the result, or the weights.
+//
+//  * A workgroup of four waves owns a tile of 32 F x 32 F, each wave a quarter of it. Chunks
+//    of 32 of K, both planes of both operands, go straight from memory to LDS, kStages deep,
+//    one barrier per chunk; a wave waits for its own requests only.
+//  * L (and R of symmetric products) lies in LDS as rows of 64 bytes, whose 16-byte units
+//    are stored at unit ^ (row / 4): the 16 rows of a fragment read cover all banks. X as R
+//    lies as 32 rows of K; matrix instructions want eight values of K per lane, so it is read
+//    through the transposing ds_read_b64_tr_b16, its 32-byte units exchanged likewise.
+//  * The matrix instruction gets R's fragment first, so that a lane holds four consecutive
+//    columns of a row of D.
+//  * Where tiles are few and K is long (X X^T of a wide matrix), K is split over several
+//    workgroups. Each writes its fp32 sums; the last to arrive (a counter per tile) adds all
+//    of them in order, so that the result does not depend on the order of arrival.
 
-constexpr int kK = 64;                         // depth of a chunk
-constexpr int kPitch = kK + 8;                 // halves per LDS row: reads of 16 rows meet no bank twice
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-// D = s1 E1 + s2 E2 + s3 L R over 64 x 64 tiles of every matrix. Symmetric products take
-// L R as L R^T (rows of both) and write a tile and its mirror image; the last one takes
-// R = X as it lies, and writes X, the result, or the weights.
-enum Out { kPlanes, kResult, kWeights };
+constexpr int kK = 32;                         // depth of a chunk
+constexpr int kStages = 4;
+constexpr int kExtent = 0x7FFFFF00;            // every request lies within its (padded) matrix
 
-template <bool SYM, int OUT, int FMT>
-__global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthJobs J, OrthStep h)
+template <int F> constexpr int kEdge = 32 * F; // edge of a tile
+template <int F> constexpr int kPlane = kEdge<F> * kK * 2;      // bytes of one plane's chunk
+template <int F> constexpr int kStage = 4 * kPlane<F>;          // L hi, L lo, R hi, R lo
+template <int F> constexpr int kFold = 2 * F;                   // chunks between two folds of the running sums
+
+__device__ __forceinline__ f16x8 read_tr(const uint8_t *lo, const uint8_t *hi)
 {
-    __shared__ _Float16 lds[2][2][kTile][kPitch];          // [operand][hi, lo][row][k]
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 *lds_p;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(__attribute__((address_space(3))) uint8_t *)lo);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(__attribute__((address_space(3))) uint8_t *)hi);
+    const f16x4 x = __builtin_bit_cast(f16x4, a), y = __builtin_bit_cast(f16x4, b);
+    return f16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+
+// All of this wave's requests but the youngest N have arrived and its LDS reads are done;
+// past the barrier that holds for every wave.
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
+// Where a tile's operands lie: byte addresses of chunk 0 (hi plane), the distance from hi to
+// lo, and the step from chunk to chunk.
+struct Operand {
+    const uint8_t *at;
+    size_t lo, step;
+    int pitch;                                 // bytes from row to row
+};
+
+// Sums of chunks [c0, c1) of the tile.
+template <int F, bool SYM>
+__device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const Operand &R, int c0, int c1,
+                                         f32x4 (&tot)[F][F])
+{
+    constexpr int kReq = kPlane<F> / 4096;                // requests per wave, plane and chunk
+    constexpr int kPer = 4 * kReq;                        // and per chunk
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+    // the order of X's 32-byte units within row k of a chunk
+    auto mixed = [](int k) { return F == 2 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : (k & 3) | (k >> 3 & 1) << 2; };
+    // this lane's 16 bytes of a request: LDS takes the lanes in order, memory gives the unit
+    // that belongs there
+    int off_l[kReq], off_r[kReq];
+#pragma unroll
+    for (int q = 0; q < kReq; ++q) {
+        const int at = (wave * kReq + q) * 64 + lane;     // 16-byte unit of the plane's chunk
+        const int row = at >> 2, unit = (at & 3) ^ (row >> 2 & 3);
+        off_l[q] = row * L.pitch + unit * 16;
+        const int k = at / (4 * F), u = at % (4 * F);
+        off_r[q] = SYM ? row * R.pitch + unit * 16 : k * R.pitch + ((u >> 1 ^ mixed(k)) * 2 + (u & 1)) * 16;
+    }
+    auto issue = [&](int c) {
+        const uint32_t to = lbase + (c & (kStages - 1)) * kStage<F> + wave * kReq * 1024;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const i32x4 dl = raw_desc(L.at + p * L.lo + c * L.step, kExtent);
+            const i32x4 dr = raw_desc(R.at + p * R.lo + c * R.step, kExtent);
+#pragma unroll
+            for (int q = 0; q < kReq; ++q) {
+                dma16(dl, to + p * kPlane<F> + q * 1024, off_l[q]);
+                dma16(dr, to + (2 + p) * kPlane<F> + q * 1024, off_r[q]);
+            }
+        }
+    };
+    // fragment addresses within a plane's chunk
+    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
+    const int frag = (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 2 & 3)) * 16);
+    int tr[2];                                            // lane = 16 g + 4 j + a: rows 8 g + j, 8 g + 4 + j
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int k = 8 * (lane >> 4) + 4 * h + (lane >> 2 & 3);
+        tr[h] = k * (64 * F) + mixed(k) * 32 + (lane & 3) * 8;    // columns 0-15; others by exclusive or
+    }
+    struct Fragments {
+        f16x8 l[2][F], r[2][F];
+    };
+    auto read = [&](int c, Fragments &f) {
+        const uint8_t *b = smem + (c & (kStages - 1)) * kStage<F>;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                f.l[p][i] = *(const f16x8 *)(b + p * kPlane<F> + (wi + 16 * i) * 64 + frag);
+                const uint8_t *br = b + (2 + p) * kPlane<F>;
+                const int x = ((wj >> 4) + i) * 32;
+                if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (wj + 16 * i) * 64 + frag);
+                else f.r[p][i] = read_tr(br + (tr[0] ^ x), br + (tr[1] ^ x));
+            }
+    };
+    // waits for a chunk behind which `later` more have been requested
+    auto wait = [&](int later) {
+        if (later >= 3) arrived<3 * kPer>();
+        else if (later == 2) arrived<2 * kPer>();
+        else if (later == 1) arrived<kPer>();
+        else arrived<0>();
+    };
+    f32x4 acc[F][F];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[i][j] = tot[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < kStages && c0 + d < c1; ++d) issue(c0 + d);
+    Fragments f[2];
+    wait(c1 - 1 - c0);
+    read(c0, f[0]);
+    // chunk c: its fragments are in `now`; those of c + 1 are read meanwhile. Past the barrier
+    // every wave has read chunk c, so its place in LDS takes chunk c + kStages.
+    auto step = [&](int c, Fragments &now, Fragments &next) {
+        if (c + 1 < c1) {
+            wait(min(c1 - 2 - c, kStages - 2));
+            read(c + 1, next);
+            if (c + kStages < c1) issue(c + kStages);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p)                       // lo hi, hi lo, hi hi
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < F; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
+        if ((c - c0) % kFold<F> == kFold<F> - 1 || c + 1 == c1)
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < F; ++j) {
+                    tot[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+    };
+    for (int c = c0; c < c1; c += 2) {
+        step(c, f[0], f[1]);
+        if (c + 1 < c1) step(c + 1, f[1], f[0]);
+    }
+}
+
+struct alignas(8) F16x4 { _Float16 v[4]; };
+
+template <int F>
+__global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStage S, OrthStep h)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int last;
     const Where w = find(T, blockIdx.x);
-    const OrthJob &job = J.job[blockIdx.y];
     const OrthEntry &e = T.e[w.t];
+    const OrthPlan &plan = S.plan[e.direct];
     const Slot s = slot_of(e.rows, e.cols);
     uint8_t *base = slot_base(T, w, s);
+    constexpr int E = kEdge<F>;
+    // number within the matrix = (job * tiles + tile) * splits + split
+    const uint32_t tiles = e.per / (plan.jobs * e.splits);
+    const int split = w.local % e.splits;
+    const uint32_t jt = w.local / e.splits, tile = jt % tiles;
+    const OrthJob job = plan.job[jt / tiles];
     int ti, tj;
-    if constexpr (SYM) {
+    if (plan.sym) {
         ti = 0;
-        uint32_t t = w.local, row = s.m / kTile;           // row ti holds tiles ti .. m/64 - 1
+        uint32_t t = tile, row = s.m / E;                  // row ti holds tiles ti .. m / E - 1
         while (t >= row) { t -= row--; ++ti; }
         tj = ti + t;
     } else {
-        const int tiles_n = s.n / kTile;
-        ti = w.local / tiles_n;
-        tj = w.local - ti * tiles_n;
+        const int tiles_n = s.n / E;
+        ti = tile / tiles_n;
+        tj = tile - ti * tiles_n;
     }
     const int depth = job.L <= kX1 ? s.n : s.m;            // columns of L
-    const int ld_r = SYM ? depth : s.n;
-    const _Float16 *L = (const _Float16 *)(base + buf_at(s, job.L));
-    const _Float16 *R = (const _Float16 *)(base + buf_at(s, job.R));
-    const size_t plane_l = (size_t)s.m * depth, plane_r = SYM ? plane_l : (size_t)s.m * s.n;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-    f32x4 acc[2][2] = {};
-    for (int k0 = 0; k0 < depth; k0 += kK) {
-        f32x4 part[2][2] = {};
-        __syncthreads();
-        for (int p = 0; p < 2; ++p)
-            for (int q = tid; q < kTile * kK / 8; q += kThreads) {
-                const int r = q / (kK / 8), c = q % (kK / 8) * 8;
-                *(f16x8 *)&lds[0][p][r][c] =
-                    *(const f16x8 *)(L + p * plane_l + (size_t)(ti * kTile + r) * depth + k0 + c);
-                if constexpr (SYM) {
-                    *(f16x8 *)&lds[1][p][r][c] =
-                        *(const f16x8 *)(R + p * plane_r + (size_t)(tj * kTile + r) * ld_r + k0 + c);
-                } else {
-                    const f16x8 v = *(const f16x8 *)(R + p * plane_r + (size_t)(k0 + r) * ld_r + tj * kTile + c);
-                    for (int i = 0; i < 8; ++i) lds[1][p][c + i][r] = v[i];
-                }
-            }
-        __syncthreads();
-        for (int k = 0; k < kK; k += 32) {
-            const int kk = k + (lane >> 4) * 8;
-            f16x8 a[2][2], b[2][2];                        // [hi, lo][tile]
-            for (int p = 0; p < 2; ++p)
-                for (int i = 0; i < 2; ++i) {
-                    a[p][i] = *(const f16x8 *)&lds[0][p][wi + i * 16 + (lane & 15)][kk];
-                    b[p][i] = *(const f16x8 *)&lds[1][p][wj + i * 16 + (lane & 15)][kk];
-                }
-            for (int i = 0; i < 2; ++i)
-                for (int j = 0; j < 2; ++j) {
-                    part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1][i], b[0][j], part[i][j], 0, 0, 0);
-                    part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[1][j], part[i][j], 0, 0, 0);
-                    part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[0][j], part[i][j], 0, 0, 0);
-                }
-        }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j) acc[i][j] += part[i][j];
+    const int chunks = depth / kK, each = (chunks + e.splits - 1) / e.splits;
+    const int c0 = min(chunks, split * each), c1 = min(chunks, c0 + each);
+    Operand L, R;
+    L.pitch = depth * 2;
+    L.at = base + buf_at(s, job.L) + (size_t)ti * E * L.pitch;
+    L.lo = (size_t)s.m * depth * 2;
+    L.step = kK * 2;
+    f32x4 tot[F][F];
+    if (plan.sym) {
+        R = L;
+        R.at = base + buf_at(s, job.R) + (size_t)tj * E * L.pitch;
+        multiply<F, true>(smem, L, R, c0, c1, tot);
+    } else {
+        R.pitch = s.n * 2;
+        R.at = base + buf_at(s, job.R) + (size_t)tj * E * 2;
+        R.lo = (size_t)s.m * s.n * 2;
+        R.step = (size_t)kK * R.pitch;
+        multiply<F, false>(smem, L, R, c0, c1, tot);
     }
-    // acc[i][j][q]: row wi + 16 i + 4 (lane / 16) + q, column wj + 16 j + lane % 16
-    const int ld = SYM ? s.m : s.n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (e.splits > 1) {
+        f32x4 *mine = (f32x4 *)T.part + (size_t)blockIdx.x * (F * F * kThreads);
+#pragma unroll
+        for (int i = 0; i < F * F; ++i) mine[i * kThreads + tid] = tot[i / F][i % F];
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            uint32_t *count = T.count + (blockIdx.x - split);
+            last = atomicAdd(count, 1u) == (uint32_t)e.splits - 1;
+            if (last) *count = 0u;                         // for the next launch
+        }
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        const f32x4 *first = (const f32x4 *)T.part + (size_t)(blockIdx.x - split) * (F * F * kThreads);
+#pragma unroll
+        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = first[i * kThreads + tid];
+        for (int k = 1; k < e.splits; ++k)
+#pragma unroll
+            for (int i = 0; i < F * F; ++i) tot[i / F][i % F] += first[((size_t)k * F * F + i) * kThreads + tid];
+    }
+    // tot[i][j][q]: row wi + 16 i + lane % 16, column wj + 16 j + 4 (lane / 16) + q
+    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
+    const int ld = plan.sym ? s.m : s.n;
     const size_t plane = (size_t)s.m * ld;
-    auto value = [&](int b, size_t at) {
-        const _Float16 *p = (const _Float16 *)(base + buf_at(s, b));
-        return (float)p[at] + (float)p[at + plane];
+    auto planes = [&](int b) { return (_Float16 *)(base + buf_at(s, b)); };
+    auto add = [&](f32x4 &v, float by, int b, size_t at) {
+        const F16x4 hi = *(const F16x4 *)(planes(b) + at), lo = *(const F16x4 *)(planes(b) + at + plane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += by * ((float)hi.v[q] + (float)lo.v[q]);
     };
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j)
-            for (int q = 0; q < 4; ++q) {
-                const int r = ti * kTile + wi + i * 16 + (lane >> 4) * 4 + q, c = tj * kTile + wj + j * 16 + (lane & 15);
-                // on the diagonal the upper half stands for both: what is stored is symmetric
-                if (SYM && c < r) continue;
-                const size_t at = (size_t)r * ld + c;
-                float v = job.s3 * (1.f / kScale) * acc[i][j][q];
-                if (job.E1 != kNone) v += job.s1 * value(job.E1, at);
-                if (job.E2 != kNone) v += job.s2 * value(job.E2, at);
-                if constexpr (OUT == kPlanes) {
-                    _Float16 *d = (_Float16 *)(base + buf_at(s, job.D));
-                    store_split(d, plane, at, v);
-                    if (SYM && c != r) store_split(d, plane, (size_t)c * ld + r, v);
-                } else {
-                    const int row = s.flip ? c : r, col = s.flip ? r : c;
-                    if (row >= e.rows || col >= e.cols) continue;
-                    const size_t o = (size_t)row * e.cols + col;
-                    v *= 1.f / kScale;
-                    if constexpr (OUT == kResult) {
-                        const float y[1] = {v};
-                        store_raw<FMT, 1>(T.out, (size_t)w.img * e.rows * e.cols + o, pack<FMT, 1>(y));
-                    } else {
-                        const OrthParam &p = T.p[w.t];
-                        const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
-                        const float wn = h.keep * p.w[o] - h.lr * sqrtf(tall) * v;
-                        p.w[o] = wn;
-                        const float y[1] = {wn};
-                        if (p.w16) store_raw<FMT, 1>(p.w16, o, pack<FMT, 1>(y));
+    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
+    const float rate = h.lr * sqrtf(tall);
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            const int r = ti * E + wi + i * 16 + (lane & 15), c = tj * E + wj + j * 16 + (lane >> 4) * 4;
+            const size_t at = (size_t)r * ld + c;
+            f32x4 v = tot[i][j] * (job.s3 * (1.f / kScale));
+            if (job.E1 != kNone) add(v, job.s1, job.E1, at);
+            if (job.E2 != kNone) add(v, job.s2, job.E2, at);
+            if (!plan.last) {
+                _Float16 *d = planes(job.D);
+                F16x4 hi, lo;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    hi.v[q] = (_Float16)v[q];
+                    lo.v[q] = (_Float16)(v[q] - (float)hi.v[q]);
+                }
+                if (!plan.sym || ti != tj) {
+                    *(F16x4 *)(d + at) = hi;
+                    *(F16x4 *)(d + at + plane) = lo;
+                }
+                if (!plan.sym) continue;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    // on the diagonal the upper half stands for both: what is stored is symmetric
+                    if (ti == tj && c + q < r) continue;
+                    const size_t mirror = (size_t)(c + q) * ld + r;
+                    d[mirror] = hi.v[q];
+                    d[mirror + plane] = lo.v[q];
+                    if (ti == tj) {
+                        d[at + q] = hi.v[q];
+                        d[at + q + plane] = lo.v[q];
                     }
                 }
+                continue;
             }
+            v *= 1.f / kScale;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = s.flip ? c + q : r, col = s.flip ? r : c + q;
+                if (row >= e.rows || col >= e.cols) continue;
+                const size_t o = (size_t)row * e.cols + col;
+                if (S.out == kResult) {
+                    store_as(S.fmt, T.out, (size_t)w.img * e.rows * e.cols + o, v[q]);
+                } else {
+                    const OrthParam &p = T.p[w.t];
+                    const float wn = h.keep * p.w[o] - rate * v[q];
+                    p.w[o] = wn;
+                    if (p.w16) store_as(S.fmt, p.w16, o, wn);
+                }
+            }
+        }
+}
+
+// ---------------------------------------------------------------- host: what is launched when
+
+constexpr int kSumEach = 4096;
+
+uint32_t sum_parts(const OrthEntry &e)
+{
+    return (uint32_t)std::min<size_t>(((size_t)e.rows * e.cols + kSumEach - 1) / kSumEach, kSumParts);
+}
+
+uint32_t start_tiles(const OrthEntry &e)
+{
+    const Slot s = slot_of(e.rows, e.cols);
+    return (uint32_t)(s.m / kTile) * (uint32_t)(s.n / kTile);
 }
 
 // Numbers the workgroups of a launch: `per` of entry t for each matrix of its batch.
@@ -303,80 +527,114 @@ unsigned number(OrthTable &T, F &&per)
     return (unsigned)at;
 }
 
-constexpr int kSumEach = 4096;
-
-uint32_t sum_parts(const OrthEntry &e)
-{
-    return (uint32_t)std::min<size_t>(((size_t)e.rows * e.cols + kSumEach - 1) / kSumEach, kSumParts);
-}
-
-uint32_t tiles_x(const OrthEntry &e)
-{
-    const Slot s = slot_of(e.rows, e.cols);
-    return (uint32_t)(s.m / kTile) * (uint32_t)(s.n / kTile);
-}
-
-uint32_t tiles_sym(const OrthEntry &e)
-{
-    const uint32_t t = slot_of(e.rows, e.cols).m / kTile;
-    return t * (t + 1) / 2;
-}
-
 // Spans of one step (true) or of 3, 2, 2, ... for a matrix. Difference to 64 bits after five
 // steps, in spans of one / of 3 and 2 / of the textbook form in fp32: 8 x 16 6.8e-7 / 6.7e-6
 // / 6.6e-7, 64 x 147 6.9e-7 / 1.9e-6 / 1.1e-6, 193 x 301 8.3e-7 / 1.5e-6 / 1.6e-6,
 // 512 x 512 6.8e-7 / 1.5e-6 / 2.0e-6: small matrices take the steps one by one.
-bool steps_direct(const OrthEntry &e) { return slot_of(e.rows, e.cols).m <= 128; }
+bool steps_direct(int rows, int cols) { return std::min(rows, cols) <= 128; }
 
-hipError_t launch_steps(OrthTable &T, const OrthStep &h, bool step, int out_fmt, const NewtonSchulz &ns, bool direct,
-                        hipStream_t s)
+// The products of a matrix in order, one entry per launch.
+std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
 {
-    hipError_t e = hipSuccess;
-    const dim3 block(kThreads);
-    const unsigned grid_x = number(T, tiles_x);
-    OrthTable S = T;                           // the same table numbered by symmetric tiles
-    const unsigned grid_s = number(S, tiles_sym);
+    std::vector<OrthPlan> all;
     auto symmetric = [&](std::initializer_list<OrthJob> jobs) {
-        OrthJobs J{};
-        unsigned n = 0;
-        for (const OrthJob &j : jobs) J.job[n++] = j;
-        hipLaunchKernelGGL((k_orth_product<true, kPlanes, kF32>), dim3(grid_s, n), block, 0, s, S, J, h);
-        return hipGetLastError();
+        OrthPlan p{};
+        p.sym = 1;
+        for (const OrthJob &j : jobs) p.job[p.jobs++] = j;
+        all.push_back(p);
     };
     int x = kX0;
     for (int left = ns.steps, most = direct ? 1 : kSpan; left; most = std::min(most, 2)) {
         const int k = std::min(left, most);
         left -= k;
         int p = kNone;
-        if ((e = symmetric({{x, x, kNone, kNone, kA, 0.f, 0.f, 1.f}})) != hipSuccess) return e;
+        symmetric({{x, x, kNone, kNone, kA, 0.f, 0.f, 1.f}});
         for (int i = 0; i < k; ++i) {
             const int b = i & 1 ? kB1 : kB0;
-            if ((e = symmetric({{kA, kA, kA, kNone, b, ns.b / ns.a, 0.f, ns.c / ns.a}})) != hipSuccess) return e;
+            symmetric({{kA, kA, kA, kNone, b, ns.b / ns.a, 0.f, ns.c / ns.a}});
             // P of step 0 is B; then it goes where neither B nor the old P lies
             const int to = i == 1 ? kP : kB1;
             const OrthJob grow = {b, p, p, b, to, 1.f, 1.f, 1.f}, half = {b, kA, kA, kNone, kR, 1.f, 0.f, 1.f};
             const bool last = i + 1 == k;
-            if (i > 0 && !last) e = symmetric({half, grow});
-            else if (i > 0) e = symmetric({grow});
-            else if (!last) e = symmetric({half});
-            if (e != hipSuccess) return e;
+            if (i > 0 && !last) symmetric({half, grow});
+            else if (i > 0) symmetric({grow});
+            else if (!last) symmetric({half});
             p = i == 0 ? b : to;
             const float aa = ns.a * ns.a;
-            if (!last && (e = symmetric({{b, kR, kR, kNone, kA, aa, 0.f, aa}})) != hipSuccess) return e;
+            if (!last) symmetric({{b, kR, kR, kNone, kA, aa, 0.f, aa}});
         }
         const float ak = std::pow(ns.a, (float)k);
-        OrthJobs J{};
-        J.job[0] = {p, x, x, kNone, x == kX0 ? kX1 : kX0, ak, 0.f, ak};
-        if (left) {
-            hipLaunchKernelGGL((k_orth_product<false, kPlanes, kF32>), dim3(grid_x), block, 0, s, T, J, h);
-            x = x == kX0 ? kX1 : kX0;
-        } else {
-            with_format(out_fmt, [&](auto f) {
-                constexpr int FMT = decltype(f)::value;
-                if (step) hipLaunchKernelGGL((k_orth_product<false, kWeights, FMT>), dim3(grid_x), block, 0, s, T, J, h);
-                else hipLaunchKernelGGL((k_orth_product<false, kResult, FMT>), dim3(grid_x), block, 0, s, T, J, h);
-            });
+        const int to = x == kX0 ? kX1 : kX0;
+        OrthPlan q{};
+        q.jobs = 1;
+        q.last = left == 0;
+        q.job[0] = {p, x, x, kNone, to, ak, 0.f, ak};
+        all.push_back(q);
+        x = to;
+    }
+    return all;
+}
+
+// Numbers the product launch S: tiles of each matrix, K split where that helps.
+template <int F>
+unsigned number_products(OrthTable &T, const OrthStage &S)
+{
+    auto chunks = [&](const OrthEntry &e) {
+        const Slot s = slot_of(e.rows, e.cols);
+        return (uint32_t)((S.plan[e.direct].job[0].L <= kX1 ? s.n : s.m) / kK);
+    };
+    auto tiles = [&](const OrthEntry &e) -> uint32_t {
+        const OrthPlan &p = S.plan[e.direct];
+        const Slot s = slot_of(e.rows, e.cols);
+        const uint32_t i = s.m / kEdge<F>, j = s.n / kEdge<F>;
+        return p.jobs * (p.sym ? i * (i + 1) / 2 : i * j);
+    };
+    uint64_t all = 0, work = 0;
+    for (int t = 0; t < T.n; ++t) {
+        all += (uint64_t)tiles(T.e[t]) * T.e[t].batch;
+        work += (uint64_t)tiles(T.e[t]) * T.e[t].batch * chunks(T.e[t]);
+    }
+    // chunks per workgroup
+    const uint32_t each = F > 2 || all > 256 ? 0 : (uint32_t)std::max<uint64_t>(kLeastChunks, (work + 511) / 512);
+    return number(T, [&](OrthEntry &e) {
+        e.splits = !each ? 1 : (chunks(e) + each - 1) / each;
+        return tiles(e) * e.splits;
+    });
+}
+
+template <int F>
+hipError_t launch_products(const OrthTable &all, const OrthStep &h, OrthStage &S, const NewtonSchulz &ns, hipStream_t s)
+{
+    OrthTable T = all;
+    T.n = 0;
+    bool any[2] = {false, false};
+    for (int t = 0; t < all.n; ++t) {
+        if (slot_of(all.e[t].rows, all.e[t].cols).edge != kEdge<F>) continue;
+        T.e[T.n] = all.e[t];
+        T.p[T.n++] = all.p[t];
+        any[all.e[t].direct] = true;
+    }
+    if (!T.n) return hipSuccess;
+    const size_t lds = kStages * kStage<F>;
+    hipError_t e = allow_lds((const void *)k_orth_product<F>, lds);
+    if (e != hipSuccess) return e;
+    std::vector<OrthPlan> plans[2];
+    for (int d = 0; d < 2; ++d)
+        if (any[d]) plans[d] = plans_of(ns, d);
+    const size_t launches = std::max(plans[0].size(), plans[1].size());
+    for (size_t i = 0; i < launches; ++i) {
+        // matrices whose products are all done drop out
+        OrthTable now = T;
+        now.n = 0;
+        for (int t = 0; t < T.n; ++t) {
+            if (i >= plans[T.e[t].direct].size()) continue;
+            now.e[now.n] = T.e[t];
+            now.p[now.n++] = T.p[t];
         }
+        for (int d = 0; d < 2; ++d)
+            if (i < plans[d].size()) S.plan[d] = plans[d][i];
+        const unsigned grid = number_products<F>(now, S);
+        hipLaunchKernelGGL(k_orth_product<F>, dim3(grid), dim3(kThreads), lds, s, now, S, h);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return hipSuccess;
@@ -385,6 +643,24 @@ hipError_t launch_steps(OrthTable &T, const OrthStep &h, bool step, int out_fmt,
 }  // namespace
 
 size_t orth_work(int rows, int cols) { return slot_bytes(slot_of(rows, cols)); }
+
+size_t orth_shared_work(const OrthEntry *e, int n)
+{
+    // every workgroup of a launch that splits K has a place, those of whole tiles too
+    uint64_t wgs = 0;
+    bool any = false;
+    for (int t = 0; t < n; ++t) {
+        const Slot s = slot_of(e[t].rows, e[t].cols);
+        if (s.edge != kTile) continue;
+        const uint64_t i = s.m / kTile, sym = i * (i + 1) / 2;
+        auto ranges = [](int depth) { return (uint64_t)(depth / kK + kLeastChunks - 1) / kLeastChunks; };
+        const uint64_t wide = ranges(s.n), square = ranges(s.m);
+        any = any || wide > 1 || square > 1;
+        wgs += e[t].batch * std::max({sym * wide, 2 * sym * square, i * (s.n / kTile) * square});
+    }
+    return kMostSplit * sizeof(uint32_t) +
+           (any ? std::min<uint64_t>(wgs, kMostSplit) : 0) * (kThreads * 4 * sizeof(f32x4));
+}
 
 unsigned orth_tiles(int rows, int cols)
 {
@@ -434,6 +710,11 @@ hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, i
 {
     hipError_t e = hipSuccess;
     const dim3 block(kThreads);
+    // the shared part of the workspace lies first
+    T.count = (uint32_t *)T.work;
+    T.part = (float *)(T.work + kMostSplit * sizeof(uint32_t));
+    T.work += orth_shared_work(T.e, T.n);
+    for (int t = 0; t < T.n; ++t) T.e[t].direct = steps_direct(T.e[t].rows, T.e[t].cols);
     unsigned grid = number(T, sum_parts);
     if (step) hipLaunchKernelGGL((k_orth_sums<true, kF32>), dim3(grid), block, 0, s, T, h);
     else
@@ -441,27 +722,19 @@ hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, i
             hipLaunchKernelGGL((k_orth_sums<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h);
         });
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const unsigned grid_x = number(T, tiles_x);
-    if (step) hipLaunchKernelGGL((k_orth_start<true, kF32>), dim3(grid_x), block, 0, s, T, h, (double)ns.eps, kSumEach);
+    grid = number(T, start_tiles);
+    if (step) hipLaunchKernelGGL((k_orth_start<true, kF32>), dim3(grid), block, 0, s, T, h, (double)ns.eps, kSumEach);
     else
         with_format(in_fmt, [&](auto f) {
-            hipLaunchKernelGGL((k_orth_start<false, decltype(f)::value>), dim3(grid_x), block, 0, s, T, h, (double)ns.eps,
+            hipLaunchKernelGGL((k_orth_start<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h, (double)ns.eps,
                                kSumEach);
         });
     if ((e = hipGetLastError()) != hipSuccess) return e;
-
-    // the matrices of each way of taking the steps, one after the other
-    for (const bool direct : {true, false}) {
-        OrthTable part = T;
-        part.n = 0;
-        for (int t = 0; t < T.n; ++t) {
-            if (steps_direct(T.e[t]) != direct) continue;
-            part.e[part.n] = T.e[t];
-            part.p[part.n++] = T.p[t];
-        }
-        if (part.n && (e = launch_steps(part, h, step, out_fmt, ns, direct, s)) != hipSuccess) return e;
-    }
-    return hipSuccess;
+    OrthStage S{};
+    S.out = step ? kWeights : kResult;
+    S.fmt = out_fmt;
+    if ((e = launch_products<2>(T, h, S, ns, s)) != hipSuccess) return e;
+    return launch_products<4>(T, h, S, ns, s);
 }
 
 }  // namespace bc
