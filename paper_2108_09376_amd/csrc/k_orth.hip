@@ -40,7 +40,8 @@ constexpr int kTile = 64;                      // edge of small tiles, and of th
 constexpr int kBigTile = 128;
 constexpr float kScale = 4096.f;
 constexpr int kSpan = 3;                       // most steps between two A taken from X
-constexpr int kSumParts = 64;                  // partial sums of squares per matrix
+constexpr int kSumParts = 1024;                // partial sums of squares per matrix at most
+constexpr int kSumEach = 8192;                 // and elements of each at least
 constexpr int kMostSplit = 768;                // workgroups of a launch that splits K
 constexpr int kLeastChunks = 16;               // chunks of K per range at least
 
@@ -77,6 +78,24 @@ __host__ __device__ inline size_t buf_at(const Slot &s, int b)
 
 __host__ __device__ inline size_t slot_bytes(const Slot &s) { return buf_at(s, kNone); }
 
+// Matrices lie in blocks of 32 x 32, row of blocks after row of blocks, each block its hi
+// plane (2 KB), then its lo plane, as LDS holds them: a tile's chunk of K is whole blocks,
+// which requests to LDS take in order, a kilobyte each. Within a plane the four 16-byte units
+// of row r are stored at unit ^ (r / 4): the fragments of 16 rows, and the transposed ones of
+// 16 columns, then meet every bank once.
+constexpr int kBlock = 32, kBlockPlane = kBlock * kBlock * 2, kBlockBytes = 2 * kBlockPlane;
+
+__device__ __forceinline__ int in_block(int r, int c)
+{
+    return (r & 31) * 64 + ((((c & 31) >> 3) ^ (r >> 2 & 3)) << 4) + (c & 7) * 2;
+}
+
+// Byte address of (r, c) of the hi plane in a matrix of ld columns.
+__device__ __forceinline__ size_t blocked(int r, int c, int ld)
+{
+    return ((size_t)(r >> 5) * (ld >> 5) + (c >> 5)) * kBlockBytes + in_block(r, c);
+}
+
 // The matrix that workgroup `at` of a launch works on, and its number within the matrix.
 struct Where {
     int t;                                     // table entry
@@ -108,7 +127,53 @@ __device__ __forceinline__ float look_ahead(const OrthStep &h, float grad, float
     return h.nesterov ? grad + h.momentum * mom : mom;
 }
 
-// Sum of squares of one of a matrix's parts, in 64 bits: no fp32 gradient overflows it.
+// Elements i .. i + 3 of p as fp32 (those below n; p is not read past it).
+template <int FMT>
+__device__ __forceinline__ void load4(const void *p, size_t i, size_t n, float (&v)[4])
+{
+    if (i + 4 <= n) {
+        if constexpr (FMT == kF32) {
+            const Raw<FMT, 4> r = load_raw<FMT, 4>(p, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = get(r, j);
+        } else {
+            struct __attribute__((packed, aligned(2))) Bytes8 { uint32_t w[2]; };
+            const Bytes8 b = *(const Bytes8 *)((const uint8_t *)p + i * 2);
+            Raw<FMT, 8> r{{b.w[0], b.w[1], 0u, 0u}};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = get(r, j);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = i + j < n ? get(load_raw<FMT, 1>(p, i + j), 0) : 0.f;
+    }
+}
+
+__device__ __forceinline__ void store4(float *p, size_t i, size_t n, const float (&v)[4])
+{
+    if (i + 4 <= n) {
+        store_raw<kF32, 4>(p, i, pack<kF32, 4>(v));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j < n) p[i + j] = v[j];
+    }
+}
+
+__host__ __device__ inline int sum_parts(size_t count)
+{
+    const size_t parts = (count + kSumEach - 1) / kSumEach;
+    return (int)(parts < kSumParts ? parts : kSumParts);
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+    for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
+    return v;
+}
+
+// Sum of squares of one of a matrix's parts, in 64 bits: no fp32 gradient overflows it. A
+// step's new momentum is written on the way.
 template <bool STEP, int FMT>
 __global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
 {
@@ -118,33 +183,33 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
     const Where w = find(T, blockIdx.x);
     const OrthEntry &e = T.e[w.t];
     const Slot s = slot_of(e.rows, e.cols);
-    const size_t count = (size_t)e.rows * e.cols;
-    const size_t each = ((count + e.per - 1) / e.per + 3) / 4 * 4;
+    const size_t count = (size_t)e.rows * e.cols, each = ((count + e.per - 1) / e.per + 3) / 4 * 4;
     const size_t lo = w.local * each, hi = lo + each < count ? lo + each : count;
     double sum = 0.0;
-    for (size_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-        float u;
+#pragma unroll 2
+    for (size_t i = lo + threadIdx.x * 4; i < hi; i += kThreads * 4) {
+        float u[4];
         if constexpr (STEP) {
             const OrthParam &p = T.p[w.t];
-            const float g = p.grad[i], m = h.momentum * p.mom[i] + g;
-            p.mom[i] = m;
-            u = look_ahead(h, g, m);
+            float g[4], m[4];
+            load4<kF32>(p.grad, i, hi, g);
+            load4<kF32>(p.mom, i, hi, m);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                m[j] = h.momentum * m[j] + g[j];
+                u[j] = look_ahead(h, g[j], m[j]);
+            }
+            store4(p.mom, i, hi, m);
         } else {
-            u = get(load_raw<FMT, 1>(T.g, w.img * count + i), 0);
+            load4<FMT>((const uint8_t *)T.g + w.img * count * kElem<FMT>, i, hi, u);
         }
-        sum += (double)u * u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += (double)u[j] * u[j];
     }
-    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k, 64);
+    sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) ((double *)slot_base(T, w, s))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
-
-__device__ __forceinline__ void store_split(_Float16 *hi, size_t plane, size_t at, float v)
-{
-    const _Float16 h = (_Float16)v;
-    hi[at] = h;
-    hi[at + plane] = (_Float16)(v - (float)h);
 }
 
 __device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
@@ -157,44 +222,70 @@ __device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
 
 // X_0 from G, one 64 x 64 tile per workgroup.
 template <bool STEP, int FMT>
-__global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h, double eps, int parts_each)
+__global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h, double eps)
 {
     __shared__ float tile[kTile][kTile + 1];
+    __shared__ double lds[4];
     const Where w = find(T, blockIdx.x);
     const OrthEntry &e = T.e[w.t];
     const Slot s = slot_of(e.rows, e.cols);
     uint8_t *base = slot_base(T, w, s);
     const size_t count = (size_t)e.rows * e.cols;
-    const int parts = (int)((count + parts_each - 1) / parts_each < kSumParts ? (count + parts_each - 1) / parts_each : kSumParts);
-    double sum = 0.0;
-    for (int i = 0; i < parts; ++i) sum += ((const double *)base)[i];
-    const double inv = (double)kScale / (sqrt(sum) + eps);
     const int tiles_n = s.n / kTile, ti = w.local / tiles_n, tj = w.local - ti * tiles_n;
-    // the tile of G behind tile (ti, tj) of X
+    // the tile of G behind tile (ti, tj) of X: four elements of a row at a time
     const int r0 = (s.flip ? tj : ti) * kTile, c0 = (s.flip ? ti : tj) * kTile;
-    for (int k = threadIdx.x; k < kTile * kTile; k += kThreads) {
-        const int r = k / kTile, c = k - r * kTile;
-        float u = 0.f;
-        if (r0 + r < e.rows && c0 + c < e.cols) {
-            const size_t i = (size_t)(r0 + r) * e.cols + c0 + c;
-            if constexpr (STEP) {
-                const OrthParam &p = T.p[w.t];
-                u = look_ahead(h, p.grad[i], p.mom[i]);
-                p.grad[i] = 0.f;
-            } else {
-                u = get(load_raw<FMT, 1>(T.g, w.img * count + i), 0);
-            }
-            u = (float)(u * inv);
+    constexpr int kTurns = kTile * kTile / 4 / kThreads;
+    float u[kTurns][4];
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+        const int q = k * kThreads + threadIdx.x, r = r0 + q / (kTile / 4), c = c0 + q % (kTile / 4) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[k][j] = 0.f;
+        if (r >= e.rows || c >= e.cols) continue;
+        const size_t i = (size_t)r * e.cols + c, end = (size_t)(r + 1) * e.cols;
+        if constexpr (STEP) {
+            const OrthParam &p = T.p[w.t];
+            float g[4], m[4], zero[4] = {0.f, 0.f, 0.f, 0.f};
+            load4<kF32>(p.grad, i, end, g);
+            load4<kF32>(p.mom, i, end, m);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[k][j] = look_ahead(h, g[j], m[j]);
+            store4(p.grad, i, end, zero);
+        } else {
+            load4<FMT>((const uint8_t *)T.g + w.img * count * kElem<FMT>, i, end, u[k]);
         }
-        if (s.flip) tile[c][r] = u;
-        else tile[r][c] = u;
+    }
+    // the norm, from the parts in their order
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < sum_parts(count); i += kThreads) sum += ((const double *)base)[i];
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    const double inv = (double)kScale / (sqrt((lds[0] + lds[1]) + (lds[2] + lds[3])) + eps);
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+        const int q = k * kThreads + threadIdx.x, r = q / (kTile / 4), c = q % (kTile / 4) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float v = (float)(u[k][j] * inv);
+            if (s.flip) tile[c + j][r] = v;
+            else tile[r][c + j] = v;
+        }
     }
     __syncthreads();
-    _Float16 *x = (_Float16 *)(base + buf_at(s, kX0));
-    const size_t plane = (size_t)s.m * s.n;
-    for (int k = threadIdx.x; k < kTile * kTile; k += kThreads) {
-        const int r = k / kTile, c = k - r * kTile;
-        store_split(x, plane, (size_t)(ti * kTile + r) * s.n + tj * kTile + c, tile[r][c]);
+    uint8_t *x = base + buf_at(s, kX0);
+    for (int q = threadIdx.x; q < kTile * kTile / 8; q += kThreads) {
+        const int r = q / 8, c = q % 8 * 8;
+        f16x8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float v = tile[r][c + j];
+            hi[j] = (_Float16)v;
+            lo[j] = (_Float16)(v - (float)hi[j]);
+        }
+        uint8_t *to = x + blocked(ti * kTile + r, tj * kTile + c, s.n);
+        *(f16x8 *)to = hi;
+        *(f16x8 *)(to + kBlockPlane) = lo;
     }
 }
 
@@ -206,27 +297,29 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h
 // R = X as it lies, rows along K, and writes X, the result, or the weights.
 //
 //  * A workgroup of four waves owns a tile of 32 F x 32 F, each wave a quarter of it. Chunks
-//    of 32 of K, both planes of both operands, go straight from memory to LDS, kStages deep,
-//    one barrier per chunk; a wave waits for its own requests only.
-//  * L (and R of symmetric products) lies in LDS as rows of 64 bytes, whose 16-byte units
-//    are stored at unit ^ (row / 4): the 16 rows of a fragment read cover all banks. X as R
-//    lies as 32 rows of K; matrix instructions want eight values of K per lane, so it is read
-//    through the transposing ds_read_b64_tr_b16, its 32-byte units exchanged likewise.
+//    of 32 of K, F blocks of either operand, go straight from memory to LDS, kStages deep,
+//    one barrier per chunk; a wave waits for its own requests only, and reads the next
+//    chunk's fragments while the present one's products run.
+//  * Matrix instructions want eight values of K per lane. Rows along K (X as R) are read
+//    through the transposing ds_read_b64_tr_b16.
 //  * The matrix instruction gets R's fragment first, so that a lane holds four consecutive
 //    columns of a row of D.
 //  * Where tiles are few and K is long (X X^T of a wide matrix), K is split over several
-//    workgroups. Each writes its fp32 sums; the last to arrive (a counter per tile) adds all
-//    of them in order, so that the result does not depend on the order of arrival.
+//    workgroups. Each writes its fp32 sums through to the device-coherent level, and the last
+//    to arrive (a counter per tile) adds all of them in order: the result does not depend on
+//    the order of arrival.
+//  * Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, so
+//    that its L2 serves their common rows and columns.
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kK = 32;                         // depth of a chunk
-constexpr int kStages = 4;
+constexpr int kK = kBlock;                     // depth of a chunk
 constexpr int kExtent = 0x7FFFFF00;            // every request lies within its (padded) matrix
+constexpr int kCoherent = 16;                  // cache policy SC1: device-coherent access
 
 template <int F> constexpr int kEdge = 32 * F; // edge of a tile
-template <int F> constexpr int kPlane = kEdge<F> * kK * 2;      // bytes of one plane's chunk
-template <int F> constexpr int kStage = 4 * kPlane<F>;          // L hi, L lo, R hi, R lo
+template <int F> constexpr int kStage = 2 * F * kBlockBytes;    // L's blocks, R's blocks
+template <int F> constexpr int kStages = 4;                   // chunks in LDS
 template <int F> constexpr int kFold = 2 * F;                   // chunks between two folds of the running sums
 
 __device__ __forceinline__ f16x8 read_tr(const uint8_t *lo, const uint8_t *hi)
@@ -247,12 +340,12 @@ __device__ __forceinline__ void arrived()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
 }
 
-// Where a tile's operands lie: byte addresses of chunk 0 (hi plane), the distance from hi to
-// lo, and the step from chunk to chunk.
+// Where a tile's blocks lie: the first of chunk 0, and the distances (in blocks) from one of
+// a chunk's F blocks to the next and from chunk to chunk.
 struct Operand {
     const uint8_t *at;
-    size_t lo, step;
-    int pitch;                                 // bytes from row to row
+    int next;
+    size_t step;
 };
 
 // Sums of chunks [c0, c1) of the tile.
@@ -260,86 +353,68 @@ template <int F, bool SYM>
 __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const Operand &R, int c0, int c1,
                                          f32x4 (&tot)[F][F])
 {
-    constexpr int kReq = kPlane<F> / 4096;                // requests per wave, plane and chunk
-    constexpr int kPer = 4 * kReq;                        // and per chunk
+    constexpr int kReq = F;                               // requests per wave, operand and chunk
+    constexpr int kPer = 2 * kReq;                        // and per chunk
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-    // the order of X's 32-byte units within row k of a chunk
-    auto mixed = [](int k) { return F == 2 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : (k & 3) | (k >> 3 & 1) << 2; };
-    // this lane's 16 bytes of a request: LDS takes the lanes in order, memory gives the unit
-    // that belongs there
-    int off_l[kReq], off_r[kReq];
-#pragma unroll
-    for (int q = 0; q < kReq; ++q) {
-        const int at = (wave * kReq + q) * 64 + lane;     // 16-byte unit of the plane's chunk
-        const int row = at >> 2, unit = (at & 3) ^ (row >> 2 & 3);
-        off_l[q] = row * L.pitch + unit * 16;
-        const int k = at / (4 * F), u = at % (4 * F);
-        off_r[q] = SYM ? row * R.pitch + unit * 16 : k * R.pitch + ((u >> 1 ^ mixed(k)) * 2 + (u & 1)) * 16;
-    }
+    // request q of wave w: kilobyte w (0, 1: hi; 2, 3: lo) of block q; past the range zeros,
+    // from no memory, which nothing uses: every wait counts alike
     auto issue = [&](int c) {
-        const uint32_t to = lbase + (c & (kStages - 1)) * kStage<F> + wave * kReq * 1024;
+        const uint32_t to = lbase + (c & (kStages<F> - 1)) * kStage<F> + wave * 1024;
+        const i32x4 dl = raw_desc(L.at + c * L.step * kBlockBytes, kExtent);
+        const i32x4 dr = raw_desc(R.at + c * R.step * kBlockBytes, kExtent);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const i32x4 dl = raw_desc(L.at + p * L.lo + c * L.step, kExtent);
-            const i32x4 dr = raw_desc(R.at + p * R.lo + c * R.step, kExtent);
-#pragma unroll
-            for (int q = 0; q < kReq; ++q) {
-                dma16(dl, to + p * kPlane<F> + q * 1024, off_l[q]);
-                dma16(dr, to + (2 + p) * kPlane<F> + q * 1024, off_r[q]);
-            }
+        for (int q = 0; q < F; ++q) {
+            const int own = wave * 1024 + lane * 16;
+            dma16(dl, to + q * kBlockBytes, c < c1 ? q * L.next * kBlockBytes + own : kExtent);
+            dma16(dr, to + (F + q) * kBlockBytes, c < c1 ? q * R.next * kBlockBytes + own : kExtent);
         }
     };
-    // fragment addresses within a plane's chunk
-    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
-    const int frag = (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 2 & 3)) * 16);
-    int tr[2];                                            // lane = 16 g + 4 j + a: rows 8 g + j, 8 g + 4 + j
+    // fragment addresses: 16 rows of a block from row 0 (or columns from column 0), wave
+    // quarter wi, wj in units of 16
+    const int wi = (wave >> 1) * F, wj = (wave & 1) * F;
+    const int frag = in_block(lane & 15, (lane >> 4) * 8);
+    int tr[2][2];                                         // [16-column half][k half]
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int k = 8 * (lane >> 4) + 4 * h + (lane >> 2 & 3);
-        tr[h] = k * (64 * F) + mixed(k) * 32 + (lane & 3) * 8;    // columns 0-15; others by exclusive or
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)                       // lane = 16 g + 4 j + a: rows 8 g + j, 8 g + 4 + j
+            tr[h][k] = in_block(8 * (lane >> 4) + 4 * k + (lane >> 2 & 3), 16 * h + (lane & 3) * 4);
     struct Fragments {
         f16x8 l[2][F], r[2][F];
     };
     auto read = [&](int c, Fragments &f) {
-        const uint8_t *b = smem + (c & (kStages - 1)) * kStage<F>;
+        const uint8_t *b = smem + (c & (kStages<F> - 1)) * kStage<F>;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int i = 0; i < F; ++i) {
-                f.l[p][i] = *(const f16x8 *)(b + p * kPlane<F> + (wi + 16 * i) * 64 + frag);
-                const uint8_t *br = b + (2 + p) * kPlane<F>;
-                const int x = ((wj >> 4) + i) * 32;
-                if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (wj + 16 * i) * 64 + frag);
-                else f.r[p][i] = read_tr(br + (tr[0] ^ x), br + (tr[1] ^ x));
+                const int il = wi + i, ir = wj + i;       // 16 rows il, 16 rows or columns ir
+                const uint8_t *bl = b + (il >> 1) * kBlockBytes + p * kBlockPlane;
+                const uint8_t *br = b + (F + (ir >> 1)) * kBlockBytes + p * kBlockPlane;
+                f.l[p][i] = *(const f16x8 *)(bl + (il & 1) * 1024 + frag);
+                // F is even: ir & 1 is i & 1, known at compile time
+                if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (ir & 1) * 1024 + frag);
+                else f.r[p][i] = read_tr(br + tr[i & 1][0], br + tr[i & 1][1]);
             }
     };
-    // waits for a chunk behind which `later` more have been requested
-    auto wait = [&](int later) {
-        if (later >= 3) arrived<3 * kPer>();
-        else if (later == 2) arrived<2 * kPer>();
-        else if (later == 1) arrived<kPer>();
-        else arrived<0>();
-    };
-    f32x4 acc[F][F];
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j) acc[i][j] = tot[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int d = 0; d < kStages && c0 + d < c1; ++d) issue(c0 + d);
+        for (int j = 0; j < F; ++j) tot[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < kStages<F>; ++d) issue(c0 + d);
     Fragments f[2];
-    wait(c1 - 1 - c0);
+    arrived<(kStages<F> - 1) * kPer>();
     read(c0, f[0]);
+    f32x4 acc[F][F];
     // chunk c: its fragments are in `now`; those of c + 1 are read meanwhile. Past the barrier
     // every wave has read chunk c, so its place in LDS takes chunk c + kStages.
     auto step = [&](int c, Fragments &now, Fragments &next) {
-        if (c + 1 < c1) {
-            wait(min(c1 - 2 - c, kStages - 2));
-            read(c + 1, next);
-            if (c + kStages < c1) issue(c + kStages);
-        }
+        arrived<(kStages<F> - 2) * kPer>();
+        read(c + 1, next);
+        issue(c + kStages<F>);
 #pragma unroll
         for (int p = 0; p < 3; ++p)                       // lo hi, hi lo, hi hi
 #pragma unroll
@@ -347,29 +422,34 @@ __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const 
 #pragma unroll
                 for (int j = 0; j < F; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
-        if ((c - c0) % kFold<F> == kFold<F> - 1 || c + 1 == c1)
-#pragma unroll
-            for (int i = 0; i < F; ++i)
-#pragma unroll
-                for (int j = 0; j < F; ++j) {
-                    tot[i][j] += acc[i][j];
-                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                }
     };
-    for (int c = c0; c < c1; c += 2) {
-        step(c, f[0], f[1]);
-        if (c + 1 < c1) step(c + 1, f[1], f[0]);
+    for (int c = c0; c < c1;) {                           // ranges and folds are even
+        const int fold = min(c1, c + kFold<F>);
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (; c < fold; c += 2) {
+            step(c, f[0], f[1]);
+            step(c + 1, f[1], f[0]);
+        }
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) tot[i][j] += acc[i][j];
     }
+    arrived<0>();
 }
-
-struct alignas(8) F16x4 { _Float16 v[4]; };
 
 template <int F>
 __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStage S, OrthStep h)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int last;
-    const Where w = find(T, blockIdx.x);
+    // run of neighbouring tiles for each XCD
+    const uint32_t xcd = blockIdx.x % 8, runs = gridDim.x / 8, longer = gridDim.x % 8;
+    const uint32_t wg = xcd * runs + min(xcd, longer) + blockIdx.x / 8;
+    const Where w = find(T, wg);
     const OrthEntry &e = T.e[w.t];
     const OrthPlan &plan = S.plan[e.direct];
     const Slot s = slot_of(e.rows, e.cols);
@@ -392,56 +472,51 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStag
         tj = tile - ti * tiles_n;
     }
     const int depth = job.L <= kX1 ? s.n : s.m;            // columns of L
-    const int chunks = depth / kK, each = (chunks + e.splits - 1) / e.splits;
+    const int chunks = depth / kK, each = ((chunks + e.splits - 1) / e.splits + 1) & ~1;   // both even
     const int c0 = min(chunks, split * each), c1 = min(chunks, c0 + each);
-    Operand L, R;
-    L.pitch = depth * 2;
-    L.at = base + buf_at(s, job.L) + (size_t)ti * E * L.pitch;
-    L.lo = (size_t)s.m * depth * 2;
-    L.step = kK * 2;
     f32x4 tot[F][F];
+    const Operand L = {base + buf_at(s, job.L) + (size_t)ti * F * chunks * kBlockBytes, chunks, 1};
     if (plan.sym) {
-        R = L;
-        R.at = base + buf_at(s, job.R) + (size_t)tj * E * L.pitch;
+        const Operand R = {base + buf_at(s, job.R) + (size_t)tj * F * chunks * kBlockBytes, chunks, 1};
         multiply<F, true>(smem, L, R, c0, c1, tot);
     } else {
-        R.pitch = s.n * 2;
-        R.at = base + buf_at(s, job.R) + (size_t)tj * E * 2;
-        R.lo = (size_t)s.m * s.n * 2;
-        R.step = (size_t)kK * R.pitch;
+        const Operand R = {base + buf_at(s, job.R) + (size_t)tj * F * kBlockBytes, 1, (size_t)s.n / kBlock};
         multiply<F, false>(smem, L, R, c0, c1, tot);
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (e.splits > 1) {
-        f32x4 *mine = (f32x4 *)T.part + (size_t)blockIdx.x * (F * F * kThreads);
+        const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)((f32x4 *)T.part + (size_t)(wg - split) * (F * F * kThreads)), (short)0,
+            e.splits * F * F * kThreads * 16, kBufferFlags);
+        auto place = [&](int k, int i) { return ((k * F * F + i) * kThreads + tid) * 16; };
 #pragma unroll
-        for (int i = 0; i < F * F; ++i) mine[i * kThreads + tid] = tot[i / F][i % F];
-        __threadfence();
+        for (int i = 0; i < F * F; ++i)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, tot[i / F][i % F]), part, place(split, i), 0, kCoherent);
+        __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (tid == 0) {
-            uint32_t *count = T.count + (blockIdx.x - split);
-            last = atomicAdd(count, 1u) == (uint32_t)e.splits - 1;
-            if (last) *count = 0u;                         // for the next launch
+            uint32_t *count = T.count + (wg - split);
+            last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)e.splits - 1;
+            if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
         }
         __syncthreads();
         if (!last) return;
-        __threadfence();
-        const f32x4 *first = (const f32x4 *)T.part + (size_t)(blockIdx.x - split) * (F * F * kThreads);
 #pragma unroll
-        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = first[i * kThreads + tid];
-        for (int k = 1; k < e.splits; ++k)
+        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int k = 0; k < e.splits; ++k)
 #pragma unroll
-            for (int i = 0; i < F * F; ++i) tot[i / F][i % F] += first[((size_t)k * F * F + i) * kThreads + tid];
+            for (int i = 0; i < F * F; ++i)
+                tot[i / F][i % F] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, place(k, i), 0, kCoherent));
     }
     // tot[i][j][q]: row wi + 16 i + lane % 16, column wj + 16 j + 4 (lane / 16) + q
     const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
     const int ld = plan.sym ? s.m : s.n;
-    const size_t plane = (size_t)s.m * ld;
-    auto planes = [&](int b) { return (_Float16 *)(base + buf_at(s, b)); };
     auto add = [&](f32x4 &v, float by, int b, size_t at) {
-        const F16x4 hi = *(const F16x4 *)(planes(b) + at), lo = *(const F16x4 *)(planes(b) + at + plane);
+        const uint8_t *p = base + buf_at(s, b) + at;
+        const f16x4 hi = *(const f16x4 *)p, lo = *(const f16x4 *)(p + kBlockPlane);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += by * ((float)hi.v[q] + (float)lo.v[q]);
+        for (int q = 0; q < 4; ++q) v[q] += by * ((float)hi[q] + (float)lo[q]);
     };
     const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
     const float rate = h.lr * sqrtf(tall);
@@ -450,33 +525,33 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStag
 #pragma unroll
         for (int j = 0; j < F; ++j) {
             const int r = ti * E + wi + i * 16 + (lane & 15), c = tj * E + wj + j * 16 + (lane >> 4) * 4;
-            const size_t at = (size_t)r * ld + c;
+            const size_t at = blocked(r, c, ld);
             f32x4 v = tot[i][j] * (job.s3 * (1.f / kScale));
             if (job.E1 != kNone) add(v, job.s1, job.E1, at);
             if (job.E2 != kNone) add(v, job.s2, job.E2, at);
             if (!plan.last) {
-                _Float16 *d = planes(job.D);
-                F16x4 hi, lo;
+                uint8_t *d = base + buf_at(s, job.D);
+                f16x4 hi, lo;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    hi.v[q] = (_Float16)v[q];
-                    lo.v[q] = (_Float16)(v[q] - (float)hi.v[q]);
+                    hi[q] = (_Float16)v[q];
+                    lo[q] = (_Float16)(v[q] - (float)hi[q]);
                 }
                 if (!plan.sym || ti != tj) {
-                    *(F16x4 *)(d + at) = hi;
-                    *(F16x4 *)(d + at + plane) = lo;
+                    *(f16x4 *)(d + at) = hi;
+                    *(f16x4 *)(d + at + kBlockPlane) = lo;
                 }
                 if (!plan.sym) continue;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     // on the diagonal the upper half stands for both: what is stored is symmetric
                     if (ti == tj && c + q < r) continue;
-                    const size_t mirror = (size_t)(c + q) * ld + r;
-                    d[mirror] = hi.v[q];
-                    d[mirror + plane] = lo.v[q];
+                    uint8_t *mirror = d + blocked(c + q, r, ld);
+                    *(_Float16 *)mirror = hi[q];
+                    *(_Float16 *)(mirror + kBlockPlane) = lo[q];
                     if (ti == tj) {
-                        d[at + q] = hi.v[q];
-                        d[at + q + plane] = lo.v[q];
+                        *(_Float16 *)(d + at + q * 2) = hi[q];
+                        *(_Float16 *)(d + at + q * 2 + kBlockPlane) = lo[q];
                     }
                 }
                 continue;
@@ -500,13 +575,6 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStag
 }
 
 // ---------------------------------------------------------------- host: what is launched when
-
-constexpr int kSumEach = 4096;
-
-uint32_t sum_parts(const OrthEntry &e)
-{
-    return (uint32_t)std::min<size_t>(((size_t)e.rows * e.cols + kSumEach - 1) / kSumEach, kSumParts);
-}
 
 uint32_t start_tiles(const OrthEntry &e)
 {
@@ -615,7 +683,7 @@ hipError_t launch_products(const OrthTable &all, const OrthStep &h, OrthStage &S
         any[all.e[t].direct] = true;
     }
     if (!T.n) return hipSuccess;
-    const size_t lds = kStages * kStage<F>;
+    const size_t lds = kStages<F> * kStage<F>;
     hipError_t e = allow_lds((const void *)k_orth_product<F>, lds);
     if (e != hipSuccess) return e;
     std::vector<OrthPlan> plans[2];
@@ -715,7 +783,7 @@ hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, i
     T.part = (float *)(T.work + kMostSplit * sizeof(uint32_t));
     T.work += orth_shared_work(T.e, T.n);
     for (int t = 0; t < T.n; ++t) T.e[t].direct = steps_direct(T.e[t].rows, T.e[t].cols);
-    unsigned grid = number(T, sum_parts);
+    unsigned grid = number(T, [](const OrthEntry &e) { return (uint32_t)sum_parts((size_t)e.rows * e.cols); });
     if (step) hipLaunchKernelGGL((k_orth_sums<true, kF32>), dim3(grid), block, 0, s, T, h);
     else
         with_format(in_fmt, [&](auto f) {
@@ -723,11 +791,10 @@ hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, i
         });
     if ((e = hipGetLastError()) != hipSuccess) return e;
     grid = number(T, start_tiles);
-    if (step) hipLaunchKernelGGL((k_orth_start<true, kF32>), dim3(grid), block, 0, s, T, h, (double)ns.eps, kSumEach);
+    if (step) hipLaunchKernelGGL((k_orth_start<true, kF32>), dim3(grid), block, 0, s, T, h, (double)ns.eps);
     else
         with_format(in_fmt, [&](auto f) {
-            hipLaunchKernelGGL((k_orth_start<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h, (double)ns.eps,
-                               kSumEach);
+            hipLaunchKernelGGL((k_orth_start<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h, (double)ns.eps);
         });
     if ((e = hipGetLastError()) != hipSuccess) return e;
     OrthStage S{};
