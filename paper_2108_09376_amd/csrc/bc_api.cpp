@@ -1237,7 +1237,7 @@ static bc_status orth_iteration(const bc_newton_schulz &in, bc::NewtonSchulz &ns
 
 static size_t orth_need(int32_t batch, int32_t rows, int32_t cols)
 {
-    bc::OrthEntry e{};
+    bc::OrthShape e{};
     e.rows = rows;
     e.cols = cols;
     e.batch = batch;
@@ -1274,7 +1274,7 @@ bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int
     T.work = (uint8_t *)d_work;
     T.g = d_g;
     T.out = d_out;
-    T.e[0] = {rows, cols, batch, 0, 0, 0, 1, 0};
+    T.e[0] = {rows, cols, batch, 0};
     hipError_t e = bc::launch_orth(T, bc::OrthStep{}, false, in_dtype, out_dtype, it, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "orthogonalisation launch");
     return ok();
@@ -1287,7 +1287,7 @@ static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, s
     if (n < 1 || n > bc::kMaxParams) return fail(BC_ERR_SHAPE, "n outside 1..%d", bc::kMaxParams);
     *need = 0;
     double tiles = 0;
-    bc::OrthEntry e[bc::kMaxParams] = {};
+    bc::OrthShape e[bc::kMaxParams] = {};
     for (int t = 0; t < n; ++t) {
         char name[32];
         snprintf(name, sizeof name, "params[%d]", t);
@@ -1340,7 +1340,7 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
         for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all.push_back({q, count * 4});
         if (p.w16) all.push_back({p.w16, count * 2});
         any16 = any16 || p.w16;
-        T.e[t] = {p.rows, p.cols, 1, 0, 0, (uint32_t)(off / 256), 1, 0};
+        T.e[t] = {p.rows, p.cols, 1, (uint32_t)(off / 256)};
         T.p[t] = {p.w, p.momentum, p.grad, (uint16_t *)p.w16};
         off += bc::orth_work(p.rows, p.cols);
     }

@@ -187,15 +187,12 @@ size_t norm_grad_work(int fmt, uint32_t rows, int c);
 hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, int accumulate, void *work,
                             const NormGeom &g, int fmt, hipStream_t s);
 
-// Orthogonalised updates (k_orth.hip). A table entry is a shape with its matrices: one of an
-// optimiser's step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the
-// workspace (after the shared part), orth_work(rows, cols) bytes for each matrix. first, per
-// and splits are the launches'.
-struct OrthEntry {
+// Orthogonalised updates (k_orth.hip). A shape with its matrices: one of an optimiser's
+// step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the workspace
+// (after the shared part), orth_work(rows, cols) bytes for each matrix.
+struct OrthShape {
     int rows, cols, batch;
-    uint32_t first, per;
     uint32_t off;
-    uint16_t splits, direct;                   // K ranges of this launch; which of its plans
 };
 struct OrthParam {
     float *w, *mom, *grad;
@@ -203,12 +200,10 @@ struct OrthParam {
 };
 struct OrthTable {
     int n;
-    uint8_t *work;                             // the matrices' parts
-    uint32_t *count;                           // arrivals per tile and partial sums of K ranges
-    float *part;
+    uint8_t *work;
     const void *g;                             // bc_orthogonalize: [batch][rows][cols]
     void *out;
-    OrthEntry e[kMaxParams];
+    OrthShape e[kMaxParams];
     OrthParam p[kMaxParams];                   // a step's tensors
 };
 struct OrthStep {
@@ -216,7 +211,7 @@ struct OrthStep {
     int nesterov;
 };
 struct OrthJob {
-    int L, R, E1, E2, D;                       // buffers of a matrix's slot
+    int L, R, E1, E2, D;                       // buffers of a matrix's part
     float s1, s2, s3;
 };
 struct OrthPlan {                              // one launch's products of a matrix
@@ -225,17 +220,17 @@ struct OrthPlan {                              // one launch's products of a mat
 };
 struct OrthStage {
     OrthPlan plan[2];                          // matrices taken in spans, matrices taken step by step
-    int out, fmt;
+    int each, fmt;                             // chunks per K range (0: whole), the result's format
 };
 struct NewtonSchulz {
     int steps;
     float a, b, c, eps;
 };
 size_t orth_work(int rows, int cols);         // bytes of a matrix's part
-size_t orth_shared_work(const OrthEntry *e, int n);
+size_t orth_shared_work(const OrthShape *e, int n);
 unsigned orth_tiles(int rows, int cols);       // workgroups of the largest launch, per matrix
 bool orth_supported(const NewtonSchulz &ns, const char **why);
-hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
+hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
                        hipStream_t s);
 
 }  // namespace bc

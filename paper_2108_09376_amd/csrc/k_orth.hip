@@ -42,11 +42,17 @@ constexpr float kScale = 4096.f;
 constexpr int kSpan = 3;                       // most steps between two A taken from X
 constexpr int kSumParts = 1024;                // partial sums of squares per matrix at most
 constexpr int kSumEach = 8192;                 // and elements of each at least
-constexpr int kMostSplit = 768;                // workgroups of a launch that splits K
 constexpr int kLeastChunks = 16;               // chunks of K per range at least
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// The workspace's shared part; the fp32 sums of K ranges follow it.
+constexpr int kMostSplit = 768;                // workgroups of a launch that splits K
+struct OrthHead {
+    uint32_t count[kMostSplit];                // arrivals per tile
+};
+static_assert(sizeof(OrthHead) % 256 == 0, "what follows is aligned");
 
 // A matrix's part of the workspace: partial sums, two X and five squares, each two planes
 // (hi, lo) of halves.
@@ -68,7 +74,6 @@ __host__ __device__ inline Slot slot_of(int rows, int cols)
 }
 
 enum Buf { kX0, kX1, kA, kR, kB0, kB1, kP, kNone };
-enum Out { kResult, kWeights };              // what the last product of a matrix writes
 
 __host__ __device__ inline size_t buf_at(const Slot &s, int b)
 {
@@ -96,27 +101,68 @@ __device__ __forceinline__ size_t blocked(int r, int c, int ld)
     return ((size_t)(r >> 5) * (ld >> 5) + (c >> 5)) * kBlockBytes + in_block(r, c);
 }
 
+// Spans of one step (true) or of 3, 2, 2, ... for a matrix. Difference to 64 bits after five
+// steps, in spans of one / of 3 and 2 / of the textbook form in fp32: 8 x 16 6.8e-7 / 6.7e-6
+// / 6.6e-7, 64 x 147 6.9e-7 / 1.9e-6 / 1.1e-6, 193 x 301 8.3e-7 / 1.5e-6 / 1.6e-6,
+// 512 x 512 6.8e-7 / 1.5e-6 / 2.0e-6: small matrices take the steps one by one.
+__host__ __device__ inline bool steps_direct(int rows, int cols) { return (rows < cols ? rows : cols) <= 128; }
+
+// The same value in every lane, told to the compiler.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
+{
+    const uint64_t u = (uint64_t)p;
+    return (const uint8_t *)((uint64_t)(uint32_t)uniform((int)(u >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)u));
+}
+
+// What a kernel's launch is about, in its arguments: one shape with its batch, or a table. A
+// chain of reads of the arguments costs a microsecond each, so every lane reads its entry of
+// the whole table at once.
+template <bool MANY>
+struct Matrices {
+    OrthShape e[MANY ? kMaxParams : 1];
+    OrthParam p[MANY ? kMaxParams : 1];
+    uint32_t first[MANY ? kMaxParams : 1];     // first workgroup of an entry; behind the last: their number
+    uint8_t *work;                             // the matrices' parts
+    const void *g;                             // bc_orthogonalize's tensors
+    void *out;
+};
+
 // The matrix that workgroup `at` of a launch works on, and its number within the matrix.
 struct Where {
-    int t;                                     // table entry
-    int img;                                   // matrix of the entry's batch
+    OrthShape e;
+    int t, img;                                // place in the table, matrix of the batch
     uint32_t local;
 };
 
-// Every lane looks at one entry: a chain of scalar loads over up to 64 takes microseconds.
-__device__ __forceinline__ Where find(const OrthTable &T, uint32_t at)
+// per: workgroups of each matrix of a batch.
+template <bool MANY>
+__device__ __forceinline__ Where find(const Matrices<MANY> &M, uint32_t at, uint32_t per)
 {
-    static_assert(kMaxParams == 64, "one entry per lane");
-    const int lane = threadIdx.x & 63;
-    const int t = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < T.n && T.e[lane].first <= at)) - 1);
-    const uint32_t per = T.e[t].per, in = at - T.e[t].first;
-    const int img = in / per;
-    return {t, img, in - img * per};
+    Where w;
+    if constexpr (MANY) {
+        static_assert(kMaxParams == 64, "one entry per lane");
+        const int lane = threadIdx.x & 63;
+        const OrthShape mine = M.e[lane];
+        const uint32_t first = M.first[lane];
+        w.t = uniform(__popcll(__ballot(first <= at)) - 1);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, w.t); };
+        w.e = {of(mine.rows), of(mine.cols), 1, (uint32_t)of(mine.off)};
+        w.img = 0;
+        w.local = at - (uint32_t)of(first);
+    } else {
+        w.e = M.e[0];
+        w.t = 0;
+        w.img = M.e[0].batch == 1 ? 0 : at / per;
+        w.local = at - w.img * per;
+    }
+    return w;
 }
 
-__device__ __forceinline__ uint8_t *slot_base(const OrthTable &T, const Where &w, const Slot &s)
+template <bool MANY>
+__device__ __forceinline__ uint8_t *slot_base(const Matrices<MANY> &M, const Where &w, const Slot &s)
 {
-    return T.work + T.e[w.t].off * 256 + (size_t)w.img * slot_bytes(s);
+    return M.work + w.e.off * (size_t)256 + (size_t)w.img * slot_bytes(s);
 }
 
 // ---------------------------------------------------------------- the start: momentum, norm, X_0
@@ -166,6 +212,12 @@ __host__ __device__ inline int sum_parts(size_t count)
     return (int)(parts < kSumParts ? parts : kSumParts);
 }
 
+__host__ __device__ inline uint32_t start_tiles(const OrthShape &e)
+{
+    const Slot s = slot_of(e.rows, e.cols);
+    return (uint32_t)(s.m / kTile) * (uint32_t)(s.n / kTile);
+}
+
 __device__ __forceinline__ double wave_sum(double v)
 {
     for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
@@ -174,23 +226,23 @@ __device__ __forceinline__ double wave_sum(double v)
 
 // Sum of squares of one of a matrix's parts, in 64 bits: no fp32 gradient overflows it. A
 // step's new momentum is written on the way.
-template <bool STEP, int FMT>
-__global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
+template <bool MANY, int FMT>
+__global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHead *head, OrthStep h, uint32_t per)
 {
     __shared__ double lds[4];
-    if (blockIdx.x == 0)                                  // counters of the products
-        for (int i = threadIdx.x; i < kMostSplit; i += kThreads) T.count[i] = 0u;
-    const Where w = find(T, blockIdx.x);
-    const OrthEntry &e = T.e[w.t];
+    if (blockIdx.x == 0)                                  // for the launches after this one
+        for (int i = threadIdx.x; i < kMostSplit; i += kThreads) head->count[i] = 0u;
+    const Where w = find(M, blockIdx.x, per);
+    const OrthShape &e = w.e;
     const Slot s = slot_of(e.rows, e.cols);
-    const size_t count = (size_t)e.rows * e.cols, each = ((count + e.per - 1) / e.per + 3) / 4 * 4;
+    const size_t count = (size_t)e.rows * e.cols, parts = sum_parts(count), each = ((count + parts - 1) / parts + 3) / 4 * 4;
     const size_t lo = w.local * each, hi = lo + each < count ? lo + each : count;
     double sum = 0.0;
 #pragma unroll 2
     for (size_t i = lo + threadIdx.x * 4; i < hi; i += kThreads * 4) {
         float u[4];
-        if constexpr (STEP) {
-            const OrthParam &p = T.p[w.t];
+        if constexpr (MANY) {
+            const OrthParam &p = M.p[w.t];
             float g[4], m[4];
             load4<kF32>(p.grad, i, hi, g);
             load4<kF32>(p.mom, i, hi, m);
@@ -201,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
             }
             store4(p.mom, i, hi, m);
         } else {
-            load4<FMT>((const uint8_t *)T.g + w.img * count * kElem<FMT>, i, hi, u);
+            load4<FMT>((const uint8_t *)M.g + w.img * count * kElem<FMT>, i, hi, u);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum += (double)u[j] * u[j];
@@ -209,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(OrthTable T, OrthStep h)
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) ((double *)slot_base(T, w, s))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    if (threadIdx.x == 0) ((double *)slot_base(M, w, s))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
 __device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
@@ -221,15 +273,15 @@ __device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
 }
 
 // X_0 from G, one 64 x 64 tile per workgroup.
-template <bool STEP, int FMT>
-__global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h, double eps)
+template <bool MANY, int FMT>
+__global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthStep h, double eps, uint32_t per)
 {
     __shared__ float tile[kTile][kTile + 1];
     __shared__ double lds[4];
-    const Where w = find(T, blockIdx.x);
-    const OrthEntry &e = T.e[w.t];
+    const Where w = find(M, blockIdx.x, per);
+    const OrthShape &e = w.e;
     const Slot s = slot_of(e.rows, e.cols);
-    uint8_t *base = slot_base(T, w, s);
+    uint8_t *base = slot_base(M, w, s);
     const size_t count = (size_t)e.rows * e.cols;
     const int tiles_n = s.n / kTile, ti = w.local / tiles_n, tj = w.local - ti * tiles_n;
     // the tile of G behind tile (ti, tj) of X: four elements of a row at a time
@@ -243,8 +295,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h
         for (int j = 0; j < 4; ++j) u[k][j] = 0.f;
         if (r >= e.rows || c >= e.cols) continue;
         const size_t i = (size_t)r * e.cols + c, end = (size_t)(r + 1) * e.cols;
-        if constexpr (STEP) {
-            const OrthParam &p = T.p[w.t];
+        if constexpr (MANY) {
+            const OrthParam &p = M.p[w.t];
             float g[4], m[4], zero[4] = {0.f, 0.f, 0.f, 0.f};
             load4<kF32>(p.grad, i, end, g);
             load4<kF32>(p.mom, i, end, m);
@@ -252,7 +304,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(OrthTable T, OrthStep h
             for (int j = 0; j < 4; ++j) u[k][j] = look_ahead(h, g[j], m[j]);
             store4(p.grad, i, end, zero);
         } else {
-            load4<FMT>((const uint8_t *)T.g + w.img * count * kElem<FMT>, i, end, u[k]);
+            load4<FMT>((const uint8_t *)M.g + w.img * count * kElem<FMT>, i, end, u[k]);
         }
     }
     // the norm, from the parts in their order
@@ -320,7 +372,7 @@ constexpr int kCoherent = 16;                  // cache policy SC1: device-coher
 template <int F> constexpr int kEdge = 32 * F; // edge of a tile
 template <int F> constexpr int kStage = 2 * F * kBlockBytes;    // L's blocks, R's blocks
 template <int F> constexpr int kStages = 4;                   // chunks in LDS
-template <int F> constexpr int kFold = 2 * F;                   // chunks between two folds of the running sums
+constexpr int kFold = 4;                       // chunks with running sums of their own
 
 __device__ __forceinline__ f16x8 read_tr(const uint8_t *lo, const uint8_t *hi)
 {
@@ -408,10 +460,9 @@ __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const 
     Fragments f[2];
     arrived<(kStages<F> - 1) * kPer>();
     read(c0, f[0]);
-    f32x4 acc[F][F];
     // chunk c: its fragments are in `now`; those of c + 1 are read meanwhile. Past the barrier
     // every wave has read chunk c, so its place in LDS takes chunk c + kStages.
-    auto step = [&](int c, Fragments &now, Fragments &next) {
+    auto step = [&](int c, Fragments &now, Fragments &next, f32x4 (&acc)[F][F]) {
         arrived<(kStages<F> - 2) * kPer>();
         read(c + 1, next);
         issue(c + kStages<F>);
@@ -423,71 +474,131 @@ __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const 
                 for (int j = 0; j < F; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
     };
-    for (int c = c0; c < c1;) {                           // ranges and folds are even
-        const int fold = min(c1, c + kFold<F>);
+    // N chunks with sums of their own, written out: sums carried around a loop would be moved
+    // between registers in every turn
+    auto fold = [&](int c, auto n) {
+        constexpr int N = decltype(n)::value;
+        f32x4 acc[F][F];
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll
             for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (; c < fold; c += 2) {
-            step(c, f[0], f[1]);
-            step(c + 1, f[1], f[0]);
-        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) step(c + k, f[k & 1], f[~k & 1], acc);
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll
             for (int j = 0; j < F; ++j) tot[i][j] += acc[i][j];
-    }
+    };
+    int c = c0;
+    for (; c + kFold <= c1; c += kFold) fold(c, std::integral_constant<int, kFold>{});
+    if (c < c1) fold(c, std::integral_constant<int, 2>{});        // ranges are even
     arrived<0>();
 }
 
+// Chunks of K of a product, tiles of a matrix with `jobs` of them, and K ranges of about
+// `each` chunks (0: whole).
+__host__ __device__ inline int chunks_of(const OrthPlan &p, const Slot &s) { return (p.job[0].L <= kX1 ? s.n : s.m) / kK; }
+
 template <int F>
-__global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStage S, OrthStep h)
+__host__ __device__ inline uint32_t tiles_of(const OrthPlan &p, const Slot &s)
+{
+    const uint32_t i = s.m / kEdge<F>, j = s.n / kEdge<F>;
+    return p.sym ? i * (i + 1) / 2 : i * j;
+}
+
+__host__ __device__ inline int ranges_of(int chunks, int each) { return each ? (chunks + each - 1) / each : 1; }
+
+template <int F>
+__host__ __device__ inline uint32_t products_of(const OrthPlan &p, const OrthShape &e, int each)
+{
+    const Slot s = slot_of(e.rows, e.cols);
+    if (s.edge != kEdge<F> || !p.jobs) return 0;
+    return p.jobs * tiles_of<F>(p, s) * ranges_of(chunks_of(p, s), each);
+}
+
+// What a lane adds to its part of a tile: s E, of both planes, in the layout of the sums.
+template <int F>
+struct Addend {
+    f16x4 hi[F][F], lo[F][F];
+};
+
+template <int F, bool MANY>
+__global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, OrthStage S, OrthHead *head, OrthStep h, uint32_t per)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int last;
     // run of neighbouring tiles for each XCD
     const uint32_t xcd = blockIdx.x % 8, runs = gridDim.x / 8, longer = gridDim.x % 8;
     const uint32_t wg = xcd * runs + min(xcd, longer) + blockIdx.x / 8;
-    const Where w = find(T, wg);
-    const OrthEntry &e = T.e[w.t];
-    const OrthPlan &plan = S.plan[e.direct];
+    auto plan_of = [&](const OrthShape &e) -> const OrthPlan & {
+        return S.plan[MANY && steps_direct(e.rows, e.cols)];
+    };
+    const Where w = find(M, wg, per);
+    const OrthShape &e = w.e;
+    const OrthPlan &plan = plan_of(e);
     const Slot s = slot_of(e.rows, e.cols);
-    uint8_t *base = slot_base(T, w, s);
+    uint8_t *base = slot_base(M, w, s);
     constexpr int E = kEdge<F>;
-    // number within the matrix = (job * tiles + tile) * splits + split
-    const uint32_t tiles = e.per / (plan.jobs * e.splits);
-    const int split = w.local % e.splits;
-    const uint32_t jt = w.local / e.splits, tile = jt % tiles;
-    const OrthJob job = plan.job[jt / tiles];
+    // number within the matrix = (job * tiles + tile) * ranges + range
+    const int chunks = chunks_of(plan, s), ranges = ranges_of(chunks, S.each);
+    uint32_t tile = w.local, split = 0;
+    if (ranges > 1) {
+        tile = w.local / ranges;
+        split = w.local - tile * ranges;
+    }
+    const uint32_t tiles = tiles_of<F>(plan, s);
+    const int second = tile >= tiles;
+    const OrthJob job = plan.job[second];
+    tile -= second * tiles;
     int ti, tj;
     if (plan.sym) {
         ti = 0;
-        uint32_t t = tile, row = s.m / E;                  // row ti holds tiles ti .. m / E - 1
-        while (t >= row) { t -= row--; ++ti; }
-        tj = ti + t;
+        uint32_t row = s.m / E;                            // row ti holds tiles ti .. m / E - 1
+        while (tile >= row) { tile -= row--; ++ti; }
+        tj = ti + tile;
     } else {
         const int tiles_n = s.n / E;
         ti = tile / tiles_n;
         tj = tile - ti * tiles_n;
     }
-    const int depth = job.L <= kX1 ? s.n : s.m;            // columns of L
-    const int chunks = depth / kK, each = ((chunks + e.splits - 1) / e.splits + 1) & ~1;   // both even
-    const int c0 = min(chunks, split * each), c1 = min(chunks, c0 + each);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // a lane's part of the tile: [i][j][q] is row wi + 16 i + lane % 16, column
+    // wj + 16 j + 4 (lane / 16) + q
+    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
+    const int ld = plan.sym ? s.m : s.n;
+    auto load = [&](Addend<F> &a, int b) {
+        const uint8_t *p = base + buf_at(s, b);
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+                const uint8_t *at = p + blocked(ti * E + wi + i * 16 + (lane & 15), tj * E + wj + j * 16 + (lane >> 4) * 4, ld);
+                a.hi[i][j] = *(const f16x4 *)at;
+                a.lo[i][j] = *(const f16x4 *)(at + kBlockPlane);
+            }
+    };
+    // small tiles ask for what they add before the product, large ones have no registers left
+    Addend<F> e1, e2;
+    if constexpr (F == 2) {
+        if (job.E1 != kNone) load(e1, job.E1);
+        if (job.E2 != kNone) load(e2, job.E2);
+    }
+    const int each = ((chunks + ranges - 1) / ranges + 1) & ~1;       // chunks are even, so are ranges
+    const int c0 = uniform(min(chunks, (int)split * each)), c1 = uniform(min(chunks, c0 + each));
     f32x4 tot[F][F];
-    const Operand L = {base + buf_at(s, job.L) + (size_t)ti * F * chunks * kBlockBytes, chunks, 1};
-    if (plan.sym) {
-        const Operand R = {base + buf_at(s, job.R) + (size_t)tj * F * chunks * kBlockBytes, chunks, 1};
+    const Operand L = {uniform(base + buf_at(s, job.L) + (size_t)ti * F * chunks * kBlockBytes), chunks, 1};
+    if (uniform(plan.sym)) {
+        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * chunks * kBlockBytes), chunks, 1};
         multiply<F, true>(smem, L, R, c0, c1, tot);
     } else {
-        const Operand R = {base + buf_at(s, job.R) + (size_t)tj * F * kBlockBytes, 1, (size_t)s.n / kBlock};
+        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * kBlockBytes), 1, (size_t)s.n / kBlock};
         multiply<F, false>(smem, L, R, c0, c1, tot);
     }
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (e.splits > 1) {
+    if (ranges > 1) {
         const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)((f32x4 *)T.part + (size_t)(wg - split) * (F * F * kThreads)), (short)0,
-            e.splits * F * F * kThreads * 16, kBufferFlags);
+            (void *)((f32x4 *)(head + 1) + (size_t)(wg - split) * (F * F * kThreads)), (short)0,
+            ranges * F * F * kThreads * 16, kBufferFlags);
         auto place = [&](int k, int i) { return ((k * F * F + i) * kThreads + tid) * 16; };
 #pragma unroll
         for (int i = 0; i < F * F; ++i)
@@ -495,8 +606,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStag
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (tid == 0) {
-            uint32_t *count = T.count + (wg - split);
-            last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)e.splits - 1;
+            uint32_t *count = head->count + (wg - split);
+            last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)ranges - 1;
             if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
         }
         __syncthreads();
@@ -504,102 +615,107 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(OrthTable T, OrthStag
 #pragma unroll
         for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int k = 0; k < e.splits; ++k)
+        for (int k = 0; k < ranges; ++k)
 #pragma unroll
             for (int i = 0; i < F * F; ++i)
                 tot[i / F][i % F] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, place(k, i), 0, kCoherent));
     }
-    // tot[i][j][q]: row wi + 16 i + lane % 16, column wj + 16 j + 4 (lane / 16) + q
-    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
-    const int ld = plan.sym ? s.m : s.n;
-    auto add = [&](f32x4 &v, float by, int b, size_t at) {
-        const uint8_t *p = base + buf_at(s, b) + at;
-        const f16x4 hi = *(const f16x4 *)p, lo = *(const f16x4 *)(p + kBlockPlane);
+    auto add = [&](const Addend<F> &a, float by) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += by * ((float)hi[q] + (float)lo[q]);
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tot[i][j][q] += by * ((float)a.hi[i][j][q] + (float)a.lo[i][j][q]);
     };
-    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
-    const float rate = h.lr * sqrtf(tall);
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] *= job.s3 * (1.f / kScale);
+    if constexpr (F == 2) {
+        if (job.E1 != kNone) add(e1, job.s1);
+        if (job.E2 != kNone) add(e2, job.s2);
+    } else {
+        if (job.E1 != kNone) {
+            load(e1, job.E1);
+            add(e1, job.s1);
+        }
+        if (job.E2 != kNone) {
+            load(e1, job.E2);
+            add(e1, job.s2);
+        }
+    }
+    if (!plan.last) {
+        // through LDS, in blocks as memory holds them: the tile, then its mirror image. On the
+        // diagonal the upper half stands for both: what is stored is symmetric.
+        constexpr int kTileBytes = F * F * kBlockBytes;
+        const bool diagonal = plan.sym && ti == tj, mirror = plan.sym && ti != tj;
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
-            const int r = ti * E + wi + i * 16 + (lane & 15), c = tj * E + wj + j * 16 + (lane >> 4) * 4;
-            const size_t at = blocked(r, c, ld);
-            f32x4 v = tot[i][j] * (job.s3 * (1.f / kScale));
-            if (job.E1 != kNone) add(v, job.s1, job.E1, at);
-            if (job.E2 != kNone) add(v, job.s2, job.E2, at);
-            if (!plan.last) {
-                uint8_t *d = base + buf_at(s, job.D);
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+                const int r = wi + i * 16 + (lane & 15), c = wj + j * 16 + (lane >> 4) * 4;
                 f16x4 hi, lo;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    hi[q] = (_Float16)v[q];
-                    lo[q] = (_Float16)(v[q] - (float)hi[q]);
+                    hi[q] = (_Float16)tot[i][j][q];
+                    lo[q] = (_Float16)(tot[i][j][q] - (float)hi[q]);
                 }
-                if (!plan.sym || ti != tj) {
-                    *(f16x4 *)(d + at) = hi;
-                    *(f16x4 *)(d + at + kBlockPlane) = lo;
+                uint8_t *at = smem + blocked(r, c, E);
+                if (!diagonal) {
+                    *(f16x4 *)at = hi;
+                    *(f16x4 *)(at + kBlockPlane) = lo;
                 }
-                if (!plan.sym) continue;
+                if (diagonal || mirror)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    // on the diagonal the upper half stands for both: what is stored is symmetric
-                    if (ti == tj && c + q < r) continue;
-                    uint8_t *mirror = d + blocked(c + q, r, ld);
-                    *(_Float16 *)mirror = hi[q];
-                    *(_Float16 *)(mirror + kBlockPlane) = lo[q];
-                    if (ti == tj) {
-                        *(_Float16 *)(d + at + q * 2) = hi[q];
-                        *(_Float16 *)(d + at + q * 2 + kBlockPlane) = lo[q];
+                    for (int q = 0; q < 4; ++q) {
+                        if (diagonal && c + q < r) continue;
+                        uint8_t *to = smem + (mirror ? kTileBytes : 0) + blocked(c + q, r, E);
+                        *(_Float16 *)to = hi[q];
+                        *(_Float16 *)(to + kBlockPlane) = lo[q];
+                        if (diagonal) {
+                            *(_Float16 *)(at + q * 2) = hi[q];
+                            *(_Float16 *)(at + q * 2 + kBlockPlane) = lo[q];
+                        }
                     }
-                }
-                continue;
             }
-            v *= 1.f / kScale;
+        __syncthreads();
+        // a row of F blocks of the tile is one run of memory
+        uint8_t *d = base + buf_at(s, job.D);
+        auto copy = [&](const uint8_t *from, int bi, int bj) {
+#pragma unroll
+            for (int k = 0; k < kTileBytes / 16 / kThreads; ++k) {
+                const int q = (k * kThreads + tid) * 16, row = q / (F * kBlockBytes), in = q % (F * kBlockBytes);
+                *(f16x8 *)(d + ((size_t)(bi * F + row) * (ld / kBlock) + bj * F) * kBlockBytes + in) = *(const f16x8 *)(from + q);
+            }
+        };
+        copy(smem, ti, tj);
+        if (mirror) copy(smem + kTileBytes, tj, ti);
+        return;
+    }
+    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
+    const float rate = h.lr * sqrtf(tall);
+    auto write = [&](size_t o, float v) {
+        if constexpr (MANY) {
+            const OrthParam &p = M.p[w.t];
+            const float wn = h.keep * p.w[o] - rate * v;
+            p.w[o] = wn;
+            if (p.w16) store_as(S.fmt, p.w16, o, wn);
+        } else {
+            store_as(S.fmt, M.out, (size_t)w.img * e.rows * e.cols + o, v);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int row = s.flip ? c + q : r, col = s.flip ? r : c + q;
-                if (row >= e.rows || col >= e.cols) continue;
-                const size_t o = (size_t)row * e.cols + col;
-                if (S.out == kResult) {
-                    store_as(S.fmt, T.out, (size_t)w.img * e.rows * e.cols + o, v[q]);
-                } else {
-                    const OrthParam &p = T.p[w.t];
-                    const float wn = h.keep * p.w[o] - rate * v[q];
-                    p.w[o] = wn;
-                    if (p.w16) store_as(S.fmt, p.w16, o, wn);
-                }
+                const int r = ti * E + wi + i * 16 + (lane & 15), c = tj * E + wj + j * 16 + (lane >> 4) * 4 + q;
+                const int row = s.flip ? c : r, col = s.flip ? r : c;
+                if (row < e.rows && col < e.cols) write((size_t)row * e.cols + col, tot[i][j][q] * (1.f / kScale));
             }
-        }
 }
 
 // ---------------------------------------------------------------- host: what is launched when
-
-uint32_t start_tiles(const OrthEntry &e)
-{
-    const Slot s = slot_of(e.rows, e.cols);
-    return (uint32_t)(s.m / kTile) * (uint32_t)(s.n / kTile);
-}
-
-// Numbers the workgroups of a launch: `per` of entry t for each matrix of its batch.
-template <typename F>
-unsigned number(OrthTable &T, F &&per)
-{
-    uint64_t at = 0;
-    for (int t = 0; t < T.n; ++t) {
-        T.e[t].first = (uint32_t)at;
-        T.e[t].per = per(T.e[t]);
-        at += (uint64_t)T.e[t].per * T.e[t].batch;
-    }
-    return (unsigned)at;
-}
-
-// Spans of one step (true) or of 3, 2, 2, ... for a matrix. Difference to 64 bits after five
-// steps, in spans of one / of 3 and 2 / of the textbook form in fp32: 8 x 16 6.8e-7 / 6.7e-6
-// / 6.6e-7, 64 x 147 6.9e-7 / 1.9e-6 / 1.1e-6, 193 x 301 8.3e-7 / 1.5e-6 / 1.6e-6,
-// 512 x 512 6.8e-7 / 1.5e-6 / 2.0e-6: small matrices take the steps one by one.
-bool steps_direct(int rows, int cols) { return std::min(rows, cols) <= 128; }
 
 // The products of a matrix in order, one entry per launch.
 std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
@@ -643,66 +759,53 @@ std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
     return all;
 }
 
-// Numbers the product launch S: tiles of each matrix, K split where that helps.
-template <int F>
-unsigned number_products(OrthTable &T, const OrthStage &S)
+// Numbers a launch: count(shape) workgroups for each matrix. *per: of the first entry's.
+template <bool MANY, typename F>
+unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
 {
-    auto chunks = [&](const OrthEntry &e) {
-        const Slot s = slot_of(e.rows, e.cols);
-        return (uint32_t)((S.plan[e.direct].job[0].L <= kX1 ? s.n : s.m) / kK);
-    };
-    auto tiles = [&](const OrthEntry &e) -> uint32_t {
-        const OrthPlan &p = S.plan[e.direct];
-        const Slot s = slot_of(e.rows, e.cols);
-        const uint32_t i = s.m / kEdge<F>, j = s.n / kEdge<F>;
-        return p.jobs * (p.sym ? i * (i + 1) / 2 : i * j);
-    };
-    uint64_t all = 0, work = 0;
+    uint64_t at = 0;
     for (int t = 0; t < T.n; ++t) {
-        all += (uint64_t)tiles(T.e[t]) * T.e[t].batch;
-        work += (uint64_t)tiles(T.e[t]) * T.e[t].batch * chunks(T.e[t]);
+        const uint32_t c = count(T.e[t]);
+        if (t == 0) *per = c;
+        M.first[t] = (uint32_t)at;
+        at += (uint64_t)c * T.e[t].batch;
     }
-    // chunks per workgroup
-    const uint32_t each = F > 2 || all > 256 ? 0 : (uint32_t)std::max<uint64_t>(kLeastChunks, (work + 511) / 512);
-    return number(T, [&](OrthEntry &e) {
-        e.splits = !each ? 1 : (chunks(e) + each - 1) / each;
-        return tiles(e) * e.splits;
-    });
+    if constexpr (MANY)
+        for (int t = T.n; t < kMaxParams; ++t) M.first[t] = (uint32_t)at;
+    return (unsigned)at;
 }
 
-template <int F>
-hipError_t launch_products(const OrthTable &all, const OrthStep &h, OrthStage &S, const NewtonSchulz &ns, hipStream_t s)
+template <int F, bool MANY>
+hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, OrthStage &S,
+                           const NewtonSchulz &ns, hipStream_t s)
 {
-    OrthTable T = all;
-    T.n = 0;
     bool any[2] = {false, false};
-    for (int t = 0; t < all.n; ++t) {
-        if (slot_of(all.e[t].rows, all.e[t].cols).edge != kEdge<F>) continue;
-        T.e[T.n] = all.e[t];
-        T.p[T.n++] = all.p[t];
-        any[all.e[t].direct] = true;
-    }
-    if (!T.n) return hipSuccess;
+    for (int t = 0; t < T.n; ++t)
+        if (slot_of(T.e[t].rows, T.e[t].cols).edge == kEdge<F>) any[steps_direct(T.e[t].rows, T.e[t].cols)] = true;
+    if (!any[0] && !any[1]) return hipSuccess;
     const size_t lds = kStages<F> * kStage<F>;
-    hipError_t e = allow_lds((const void *)k_orth_product<F>, lds);
+    hipError_t e = allow_lds((const void *)k_orth_product<F, MANY>, lds);
     if (e != hipSuccess) return e;
+    // one shape has its plan in the first place
     std::vector<OrthPlan> plans[2];
     for (int d = 0; d < 2; ++d)
-        if (any[d]) plans[d] = plans_of(ns, d);
+        if (any[d]) plans[MANY ? d : 0] = plans_of(ns, d);
     const size_t launches = std::max(plans[0].size(), plans[1].size());
+    auto plan = [&](const OrthShape &e) -> const OrthPlan & { return S.plan[MANY && steps_direct(e.rows, e.cols)]; };
     for (size_t i = 0; i < launches; ++i) {
-        // matrices whose products are all done drop out
-        OrthTable now = T;
-        now.n = 0;
+        // a plan that is done has no jobs, and its matrices no workgroups
+        for (int d = 0; d < 2; ++d) S.plan[d] = i < plans[d].size() ? plans[d][i] : OrthPlan{};
+        // K in ranges where tiles are few
+        uint64_t all = 0, work = 0;
         for (int t = 0; t < T.n; ++t) {
-            if (i >= plans[T.e[t].direct].size()) continue;
-            now.e[now.n] = T.e[t];
-            now.p[now.n++] = T.p[t];
+            const uint64_t wgs = (uint64_t)products_of<F>(plan(T.e[t]), T.e[t], 0) * T.e[t].batch;
+            all += wgs;
+            work += wgs * chunks_of(plan(T.e[t]), slot_of(T.e[t].rows, T.e[t].cols));
         }
-        for (int d = 0; d < 2; ++d)
-            if (i < plans[d].size()) S.plan[d] = plans[d][i];
-        const unsigned grid = number_products<F>(now, S);
-        hipLaunchKernelGGL(k_orth_product<F>, dim3(grid), dim3(kThreads), lds, s, now, S, h);
+        S.each = F > 2 || all > 256 ? 0 : (int)std::max<uint64_t>(kLeastChunks, (work + 511) / 512);
+        uint32_t per = 0;
+        const unsigned grid = number(M, T, &per, [&](const OrthShape &e) { return products_of<F>(plan(e), e, S.each); });
+        hipLaunchKernelGGL((k_orth_product<F, MANY>), dim3(grid), dim3(kThreads), lds, s, M, S, head, h, per);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return hipSuccess;
@@ -712,7 +815,7 @@ hipError_t launch_products(const OrthTable &all, const OrthStep &h, OrthStage &S
 
 size_t orth_work(int rows, int cols) { return slot_bytes(slot_of(rows, cols)); }
 
-size_t orth_shared_work(const OrthEntry *e, int n)
+size_t orth_shared_work(const OrthShape *e, int n)
 {
     // every workgroup of a launch that splits K has a place, those of whole tiles too
     uint64_t wgs = 0;
@@ -726,7 +829,7 @@ size_t orth_shared_work(const OrthEntry *e, int n)
         any = any || wide > 1 || square > 1;
         wgs += e[t].batch * std::max({sym * wide, 2 * sym * square, i * (s.n / kTile) * square});
     }
-    return kMostSplit * sizeof(uint32_t) +
+    return sizeof(OrthHead) +
            (any ? std::min<uint64_t>(wgs, kMostSplit) : 0) * (kThreads * 4 * sizeof(f32x4));
 }
 
@@ -773,35 +876,41 @@ bool orth_supported(const NewtonSchulz &ns, const char **why)
     return true;
 }
 
-hipError_t launch_orth(OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
-                       hipStream_t s)
+template <bool MANY>
+static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int out_fmt, const NewtonSchulz &ns, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    const dim3 block(kThreads);
-    // the shared part of the workspace lies first
-    T.count = (uint32_t *)T.work;
-    T.part = (float *)(T.work + kMostSplit * sizeof(uint32_t));
-    T.work += orth_shared_work(T.e, T.n);
-    for (int t = 0; t < T.n; ++t) T.e[t].direct = steps_direct(T.e[t].rows, T.e[t].cols);
-    unsigned grid = number(T, [](const OrthEntry &e) { return (uint32_t)sum_parts((size_t)e.rows * e.cols); });
-    if (step) hipLaunchKernelGGL((k_orth_sums<true, kF32>), dim3(grid), block, 0, s, T, h);
-    else
-        with_format(in_fmt, [&](auto f) {
-            hipLaunchKernelGGL((k_orth_sums<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h);
-        });
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    grid = number(T, start_tiles);
-    if (step) hipLaunchKernelGGL((k_orth_start<true, kF32>), dim3(grid), block, 0, s, T, h, (double)ns.eps);
-    else
-        with_format(in_fmt, [&](auto f) {
-            hipLaunchKernelGGL((k_orth_start<false, decltype(f)::value>), dim3(grid), block, 0, s, T, h, (double)ns.eps);
-        });
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    OrthHead *head = (OrthHead *)T.work;
+    Matrices<MANY> M{};
+    M.work = T.work + orth_shared_work(T.e, T.n);
+    M.g = T.g;
+    M.out = T.out;
+    for (int t = 0; t < T.n; ++t) {
+        M.e[t] = T.e[t];
+        M.p[t] = T.p[t];
+    }
+    with_format(in_fmt, [&](auto f) {
+        constexpr int FMT = decltype(f)::value;
+        if constexpr (!MANY || FMT == kF32) {                 // gradients and momentum are fp32
+            uint32_t per = 0;
+            unsigned grid = number(M, T, &per, [](const OrthShape &e) { return (uint32_t)sum_parts((size_t)e.rows * e.cols); });
+            hipLaunchKernelGGL((k_orth_sums<MANY, FMT>), dim3(grid), dim3(kThreads), 0, s, M, head, h, per);
+            if ((e = hipGetLastError()) != hipSuccess) return;
+            grid = number(M, T, &per, start_tiles);
+            hipLaunchKernelGGL((k_orth_start<MANY, FMT>), dim3(grid), dim3(kThreads), 0, s, M, h, (double)ns.eps, per);
+        }
+    });
+    if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
     OrthStage S{};
-    S.out = step ? kWeights : kResult;
     S.fmt = out_fmt;
-    if ((e = launch_products<2>(T, h, S, ns, s)) != hipSuccess) return e;
-    return launch_products<4>(T, h, S, ns, s);
+    if ((e = launch_products<2, MANY>(T, M, head, h, S, ns, s)) != hipSuccess) return e;
+    return launch_products<4, MANY>(T, M, head, h, S, ns, s);
+}
+
+hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
+                       hipStream_t s)
+{
+    return step ? launch<true>(T, h, in_fmt, out_fmt, ns, s) : launch<false>(T, h, in_fmt, out_fmt, ns, s);
 }
 
 }  // namespace bc
