@@ -350,8 +350,13 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //
 //  * A workgroup of four waves owns a tile of 32 F x 32 F, each wave a quarter of it. Chunks
 //    of 32 of K, F blocks of either operand, go straight from memory to LDS, kStages deep,
-//    one barrier per chunk; a wave waits for its own requests only, and reads the next
-//    chunk's fragments while the present one's products run.
+//    one barrier per chunk; a wave waits for its own requests only. Between the matrix
+//    instructions of a chunk lie the reads of the next chunk's fragments and the requests of
+//    the chunk kStages ahead, evenly: a wave that does one after the other leaves its matrix
+//    core idle (2048 x 2048, 128 x 128 tiles: 38 us a product, 24 of them the instructions).
+//  * What is added to the product, E1 and E2, follows the last chunk into LDS. The finished
+//    tile takes E1's place there and goes to memory in whole blocks, its mirror image through
+//    transposing reads.
 //  * Matrix instructions want eight values of K per lane. Rows along K (X as R) are read
 //    through the transposing ds_read_b64_tr_b16.
 //  * The matrix instruction gets R's fragment first, so that a lane holds four consecutive
@@ -400,79 +405,103 @@ struct Operand {
     size_t step;
 };
 
-// Sums of chunks [c0, c1) of the tile.
-template <int F, bool SYM>
-__device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const Operand &R, int c0, int c1,
-                                         f32x4 (&tot)[F][F])
+// The tile's blocks of E1 and E2 (nullptr: none), `pitch` blocks from row to row.
+struct Addends {
+    const uint8_t *at[2];
+    int pitch;
+};
+
+// A lane's address in a 32 x 32 block for transposed reads: it gets rows 8 g + 4 k .. + 3
+// (g = lane / 16) of column 16 h + lane % 16 from what its group of 16 lanes points to,
+// lane 16 g + 4 j + a to row 8 g + 4 k + j, columns 16 h + 4 a .. + 3.
+__device__ __forceinline__ int transposed(int lane, int h, int k)
 {
-    constexpr int kReq = F;                               // requests per wave, operand and chunk
-    constexpr int kPer = 2 * kReq;                        // and per chunk
+    return in_block(8 * (lane >> 4) + 4 * k + (lane >> 2 & 3), 16 * h + (lane & 3) * 4);
+}
+
+template <int F>
+struct Fragments {
+    f16x8 l[2][F], r[2][F];                               // [hi, lo][16 rows or columns]
+};
+
+// Sums of chunks [c0, c1) (both even) of the tile; E1 and E2 are left in LDS, in the stages
+// from c1 on (see stage_of).
+template <int F, bool SYM>
+__device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const Operand &R, const Addends &X, int c0,
+                                         int c1, f32x4 (&tot)[F][F])
+{
+    constexpr int kPer = 2 * F;                           // requests per wave and chunk
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t lbase = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-    // request q of wave w: kilobyte w (0, 1: hi; 2, 3: lo) of block q; past the range zeros,
-    // from no memory, which nothing uses: every wait counts alike
-    auto issue = [&](int c) {
-        const uint32_t to = lbase + (c & (kStages<F> - 1)) * kStage<F> + wave * 1024;
-        const i32x4 dl = raw_desc(L.at + c * L.step * kBlockBytes, kExtent);
-        const i32x4 dr = raw_desc(R.at + c * R.step * kBlockBytes, kExtent);
-#pragma unroll
-        for (int q = 0; q < F; ++q) {
-            const int own = wave * 1024 + lane * 16;
-            dma16(dl, to + q * kBlockBytes, c < c1 ? q * L.next * kBlockBytes + own : kExtent);
-            dma16(dr, to + (F + q) * kBlockBytes, c < c1 ? q * R.next * kBlockBytes + own : kExtent);
-        }
+    const int wave = uniform(tid >> 6);
+    const uint32_t lbase = uniform((int)lds_addr(smem));
+    const int own = wave * 1024 + lane * 16;
+    // request q of wave w: kilobyte w (0, 1: hi; 2, 3: lo) of L's block q or R's block q - F.
+    // Past the range come two rows of a tile's blocks per stage, E1's, then E2's; what is not
+    // there is zeros, from no memory: every wait counts alike.
+    struct Source {
+        i32x4 l, r;
+        int next_l, next_r;
+        uint32_t to;
     };
-    // fragment addresses: 16 rows of a block from row 0 (or columns from column 0), wave
-    // quarter wi, wj in units of 16
+    auto source = [&](int c) {
+        const bool in = c < c1;
+        const int x = c - c1, e = F == 2 ? x : x >> 1, row = F == 2 ? 0 : (x & 1) * 2;
+        const uint8_t *add = e == 0 ? X.at[0] : e == 1 ? X.at[1] : nullptr;
+        const uint8_t *l = in ? L.at + c * L.step * kBlockBytes : add + (size_t)row * X.pitch * kBlockBytes;
+        const uint8_t *r = in ? R.at + c * R.step * kBlockBytes : add + (size_t)(row + 1) * X.pitch * kBlockBytes;
+        const int bytes = in || add ? kExtent : 0;
+        return Source{raw_desc(l, bytes), raw_desc(r, bytes), in ? L.next : 1, in ? R.next : 1,
+                      lbase + (c & (kStages<F> - 1)) * kStage<F> + wave * 1024};
+    };
+    auto request = [&](const Source &s, int q) {
+        if (q < F) dma16(s.l, s.to + q * kBlockBytes, q * s.next_l * kBlockBytes + own);
+        else dma16(s.r, s.to + q * kBlockBytes, (q - F) * s.next_r * kBlockBytes + own);
+    };
+    // fragment q of a chunk: plane q / F, 16 rows (or columns) q % F of this wave's
     const int wi = (wave >> 1) * F, wj = (wave & 1) * F;
     const int frag = in_block(lane & 15, (lane >> 4) * 8);
-    int tr[2][2];                                         // [16-column half][k half]
+    int tr[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)                       // lane = 16 g + 4 j + a: rows 8 g + j, 8 g + 4 + j
-            tr[h][k] = in_block(8 * (lane >> 4) + 4 * k + (lane >> 2 & 3), 16 * h + (lane & 3) * 4);
-    struct Fragments {
-        f16x8 l[2][F], r[2][F];
-    };
-    auto read = [&](int c, Fragments &f) {
-        const uint8_t *b = smem + (c & (kStages<F> - 1)) * kStage<F>;
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int i = 0; i < F; ++i) {
-                const int il = wi + i, ir = wj + i;       // 16 rows il, 16 rows or columns ir
-                const uint8_t *bl = b + (il >> 1) * kBlockBytes + p * kBlockPlane;
-                const uint8_t *br = b + (F + (ir >> 1)) * kBlockBytes + p * kBlockPlane;
-                f.l[p][i] = *(const f16x8 *)(bl + (il & 1) * 1024 + frag);
-                // F is even: ir & 1 is i & 1, known at compile time
-                if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (ir & 1) * 1024 + frag);
-                else f.r[p][i] = read_tr(br + tr[i & 1][0], br + tr[i & 1][1]);
-            }
+        for (int k = 0; k < 2; ++k) tr[h][k] = transposed(lane, h, k);
+    auto read = [&](int c, Fragments<F> &f, int q) {
+        const int p = q / F, i = q % F, il = wi + i, ir = wj + i;
+        const uint8_t *b = smem + (c & (kStages<F> - 1)) * kStage<F> + p * kBlockPlane;
+        const uint8_t *bl = b + (il >> 1) * kBlockBytes, *br = b + (F + (ir >> 1)) * kBlockBytes;
+        f.l[p][i] = *(const f16x8 *)(bl + (i & 1) * 1024 + frag);     // F is even: il & 1 is i & 1
+        if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (i & 1) * 1024 + frag);
+        else f.r[p][i] = read_tr(br + tr[i & 1][0], br + tr[i & 1][1]);
     };
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < F; ++j) tot[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < kStages<F>; ++d) {
+        const Source s = source(c0 + d);
 #pragma unroll
-    for (int d = 0; d < kStages<F>; ++d) issue(c0 + d);
-    Fragments f[2];
+        for (int q = 0; q < kPer; ++q) request(s, q);
+    }
+    Fragments<F> f[2];
     arrived<(kStages<F> - 1) * kPer>();
-    read(c0, f[0]);
+#pragma unroll
+    for (int q = 0; q < 2 * F; ++q) read(c0, f[0], q);
     // chunk c: its fragments are in `now`; those of c + 1 are read meanwhile. Past the barrier
     // every wave has read chunk c, so its place in LDS takes chunk c + kStages.
-    auto step = [&](int c, Fragments &now, Fragments &next, f32x4 (&acc)[F][F]) {
+    auto step = [&](int c, Fragments<F> &now, Fragments<F> &next, f32x4 (&acc)[F][F]) {
         arrived<(kStages<F> - 2) * kPer>();
-        read(c + 1, next);
-        issue(c + kStages<F>);
+        const Source s = source(c + kStages<F>);
+        constexpr int kEach = 3 * F * F / (2 * F);        // matrix instructions per group
 #pragma unroll
-        for (int p = 0; p < 3; ++p)                       // lo hi, hi lo, hi hi
+        for (int q = 0; q < 2 * F; ++q) {
+            read(c + 1, next, q);
+            request(s, q);
 #pragma unroll
-            for (int i = 0; i < F; ++i)
-#pragma unroll
-                for (int j = 0; j < F; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
+            for (int k = q * kEach; k < (q + 1) * kEach; ++k) {
+                const int p = k / (F * F), i = k / F % F, j = k % F;      // lo hi, hi lo, hi hi
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     // N chunks with sums of their own, written out: sums carried around a loop would be moved
     // between registers in every turn
@@ -480,19 +509,15 @@ __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const 
         constexpr int N = decltype(n)::value;
         f32x4 acc[F][F];
 #pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < F * F; ++i) acc[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < N; ++k) step(c + k, f[k & 1], f[~k & 1], acc);
 #pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) tot[i][j] += acc[i][j];
+        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] += acc[i / F][i % F];
     };
     int c = c0;
     for (; c + kFold <= c1; c += kFold) fold(c, std::integral_constant<int, kFold>{});
-    if (c < c1) fold(c, std::integral_constant<int, 2>{});        // ranges are even
+    if (c < c1) fold(c, std::integral_constant<int, 2>{});
     arrived<0>();
 }
 
@@ -517,12 +542,6 @@ __host__ __device__ inline uint32_t products_of(const OrthPlan &p, const OrthSha
     return p.jobs * tiles_of<F>(p, s) * ranges_of(chunks_of(p, s), each);
 }
 
-// What a lane adds to its part of a tile: s E, of both planes, in the layout of the sums.
-template <int F>
-struct Addend {
-    f16x4 hi[F][F], lo[F][F];
-};
-
 template <int F, bool MANY>
 __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, OrthStage S, OrthHead *head, OrthStep h, uint32_t per)
 {
@@ -540,17 +559,18 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
     const Slot s = slot_of(e.rows, e.cols);
     uint8_t *base = slot_base(M, w, s);
     constexpr int E = kEdge<F>;
-    // number within the matrix = (job * tiles + tile) * ranges + range
+    // number within the matrix = (range * jobs + job) * tiles + tile, so that neighbours read
+    // the same columns of X
     const int chunks = chunks_of(plan, s), ranges = ranges_of(chunks, S.each);
-    uint32_t tile = w.local, split = 0;
+    const uint32_t tiles = tiles_of<F>(plan, s), all = tiles * plan.jobs;
+    uint32_t which = w.local, split = 0;
     if (ranges > 1) {
-        tile = w.local / ranges;
-        split = w.local - tile * ranges;
+        split = w.local / all;
+        which = w.local - split * all;
     }
-    const uint32_t tiles = tiles_of<F>(plan, s);
-    const int second = tile >= tiles;
+    const int second = which >= tiles;
     const OrthJob job = plan.job[second];
-    tile -= second * tiles;
+    uint32_t tile = which - second * tiles;
     int ti, tj;
     if (plan.sym) {
         ti = 0;
@@ -558,46 +578,35 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
         while (tile >= row) { tile -= row--; ++ti; }
         tj = ti + tile;
     } else {
-        const int tiles_n = s.n / E;
-        ti = tile / tiles_n;
-        tj = tile - ti * tiles_n;
+        const int tiles_m = s.m / E;                       // down the columns of X
+        tj = tile / tiles_m;
+        ti = tile - tj * tiles_m;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // a lane's part of the tile: [i][j][q] is row wi + 16 i + lane % 16, column
     // wj + 16 j + 4 (lane / 16) + q
     const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
     const int ld = plan.sym ? s.m : s.n;
-    auto load = [&](Addend<F> &a, int b) {
-        const uint8_t *p = base + buf_at(s, b);
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) {
-                const uint8_t *at = p + blocked(ti * E + wi + i * 16 + (lane & 15), tj * E + wj + j * 16 + (lane >> 4) * 4, ld);
-                a.hi[i][j] = *(const f16x4 *)at;
-                a.lo[i][j] = *(const f16x4 *)(at + kBlockPlane);
-            }
+    auto tile_at = [&](int b, int bi, int bj) {            // tile (bi, bj) of a buffer
+        return base + buf_at(s, b) + ((size_t)bi * F * (ld / kBlock) + bj * F) * kBlockBytes;
     };
-    // small tiles ask for what they add before the product, large ones have no registers left
-    Addend<F> e1, e2;
-    if constexpr (F == 2) {
-        if (job.E1 != kNone) load(e1, job.E1);
-        if (job.E2 != kNone) load(e2, job.E2);
-    }
+    const Addends X = {{job.E1 == kNone ? nullptr : uniform(tile_at(job.E1, ti, tj)),
+                        job.E2 == kNone ? nullptr : uniform(tile_at(job.E2, ti, tj))}, ld / kBlock};
     const int each = ((chunks + ranges - 1) / ranges + 1) & ~1;       // chunks are even, so are ranges
     const int c0 = uniform(min(chunks, (int)split * each)), c1 = uniform(min(chunks, c0 + each));
     f32x4 tot[F][F];
     const Operand L = {uniform(base + buf_at(s, job.L) + (size_t)ti * F * chunks * kBlockBytes), chunks, 1};
     if (uniform(plan.sym)) {
         const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * chunks * kBlockBytes), chunks, 1};
-        multiply<F, true>(smem, L, R, c0, c1, tot);
+        multiply<F, true>(smem, L, R, X, c0, c1, tot);
     } else {
         const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * kBlockBytes), 1, (size_t)s.n / kBlock};
-        multiply<F, false>(smem, L, R, c0, c1, tot);
+        multiply<F, false>(smem, L, R, X, c0, c1, tot);
     }
     if (ranges > 1) {
+        const uint32_t slot = wg - w.local + which * ranges;   // the tile's first place
         const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)((f32x4 *)(head + 1) + (size_t)(wg - split) * (F * F * kThreads)), (short)0,
+            (void *)((f32x4 *)(head + 1) + (size_t)slot * (F * F * kThreads)), (short)0,
             ranges * F * F * kThreads * 16, kBufferFlags);
         auto place = [&](int k, int i) { return ((k * F * F + i) * kThreads + tid) * 16; };
 #pragma unroll
@@ -606,7 +615,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (tid == 0) {
-            uint32_t *count = head->count + (wg - split);
+            uint32_t *count = head->count + slot;
             last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)ranges - 1;
             if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
         }
@@ -620,75 +629,68 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
             for (int i = 0; i < F * F; ++i)
                 tot[i / F][i % F] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, place(k, i), 0, kCoherent));
     }
-    auto add = [&](const Addend<F> &a, float by) {
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tot[i][j][q] += by * ((float)a.hi[i][j][q] + (float)a.lo[i][j][q]);
-    };
-#pragma unroll
-    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] *= job.s3 * (1.f / kScale);
-    if constexpr (F == 2) {
-        if (job.E1 != kNone) add(e1, job.s1);
-        if (job.E2 != kNone) add(e2, job.s2);
-    } else {
-        if (job.E1 != kNone) {
-            load(e1, job.E1);
-            add(e1, job.s1);
-        }
-        if (job.E2 != kNone) {
-            load(e1, job.E2);
-            add(e1, job.s2);
-        }
-    }
-    if (!plan.last) {
-        // through LDS, in blocks as memory holds them: the tile, then its mirror image. On the
-        // diagonal the upper half stands for both: what is stored is symmetric.
-        constexpr int kTileBytes = F * F * kBlockBytes;
-        const bool diagonal = plan.sym && ti == tj, mirror = plan.sym && ti != tj;
+    // E1 and E2 lie in the two halves of LDS behind the last chunk; E1's place takes the result
+    constexpr int kTileBytes = F * F * kBlockBytes;
+    uint8_t *first = smem + (c1 & (kStages<F> - 1)) * kStage<F>;
+    const uint8_t *next = smem + ((c1 + F / 2) & (kStages<F> - 1)) * kStage<F>;
+    static_assert(kTileBytes == F / 2 * kStage<F> && kStages<F> == 4, "a tile takes one or two stages");
+    auto add = [&](const uint8_t *from, float by) {
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll
             for (int j = 0; j < F; ++j) {
-                const int r = wi + i * 16 + (lane & 15), c = wj + j * 16 + (lane >> 4) * 4;
+                const uint8_t *at = from + blocked(wi + i * 16 + (lane & 15), wj + j * 16 + (lane >> 4) * 4, E);
+                const f16x4 hi = *(const f16x4 *)at, lo = *(const f16x4 *)(at + kBlockPlane);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tot[i][j][q] += by * ((float)hi[q] + (float)lo[q]);
+            }
+    };
+#pragma unroll
+    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] *= job.s3 * (1.f / kScale);
+    if (job.E1 != kNone) add(first, job.s1);
+    if (job.E2 != kNone) add(next, job.s2);
+    if (!plan.last) {
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
                 f16x4 hi, lo;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     hi[q] = (_Float16)tot[i][j][q];
                     lo[q] = (_Float16)(tot[i][j][q] - (float)hi[q]);
                 }
-                uint8_t *at = smem + blocked(r, c, E);
-                if (!diagonal) {
-                    *(f16x4 *)at = hi;
-                    *(f16x4 *)(at + kBlockPlane) = lo;
-                }
-                if (diagonal || mirror)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (diagonal && c + q < r) continue;
-                        uint8_t *to = smem + (mirror ? kTileBytes : 0) + blocked(c + q, r, E);
-                        *(_Float16 *)to = hi[q];
-                        *(_Float16 *)(to + kBlockPlane) = lo[q];
-                        if (diagonal) {
-                            *(_Float16 *)(at + q * 2) = hi[q];
-                            *(_Float16 *)(at + q * 2 + kBlockPlane) = lo[q];
-                        }
-                    }
+                uint8_t *at = first + blocked(wi + i * 16 + (lane & 15), wj + j * 16 + (lane >> 4) * 4, E);
+                *(f16x4 *)at = hi;
+                *(f16x4 *)(at + kBlockPlane) = lo;
             }
         __syncthreads();
-        // a row of F blocks of the tile is one run of memory
-        uint8_t *d = base + buf_at(s, job.D);
-        auto copy = [&](const uint8_t *from, int bi, int bj) {
+        // half a plane of a block per wave and turn: 16 rows, a unit of 16 bytes per lane
+        uint8_t *d = tile_at(job.D, ti, tj), *mirror = tile_at(job.D, tj, ti);
+        const int u = lane >> 4;
 #pragma unroll
-            for (int k = 0; k < kTileBytes / 16 / kThreads; ++k) {
-                const int q = (k * kThreads + tid) * 16, row = q / (F * kBlockBytes), in = q % (F * kBlockBytes);
-                *(f16x8 *)(d + ((size_t)(bi * F + row) * (ld / kBlock) + bj * F) * kBlockBytes + in) = *(const f16x8 *)(from + q);
+        for (int k = 0; k < F * F; ++k) {
+            const int piece = k * 4 + wave, h = piece & 1, p = piece >> 1 & 1, b = piece >> 2, bi = b / F, bj = b % F;
+            const uint8_t *from = first + b * kBlockBytes + p * kBlockPlane;
+            const size_t row = (size_t)(ld / kBlock) * kBlockBytes, in = p * kBlockPlane + in_block(16 * h + (lane & 15), 8 * u);
+            f16x8 v = *(const f16x8 *)(from + in_block(16 * h + (lane & 15), 8 * u));
+            if (!plan.sym) {
+                *(f16x8 *)(d + bi * row + bj * kBlockBytes + in) = v;
+                continue;
             }
-        };
-        copy(smem, ti, tj);
-        if (mirror) copy(smem + kTileBytes, tj, ti);
+            // on the diagonal the upper half stands for both: what is stored is symmetric
+            const bool diagonal = ti == tj;
+            if (diagonal && bi > bj) continue;
+            const f16x8 m = read_tr(from + transposed(lane, h, 0), from + transposed(lane, h, 1));
+            if (diagonal && bi == bj) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (8 * u + q < 16 * h + (lane & 15)) v[q] = m[q];
+            } else {
+                *(f16x8 *)(mirror + bj * row + bi * kBlockBytes + in) = m;
+            }
+            *(f16x8 *)(d + bi * row + bj * kBlockBytes + in) = v;
+        }
         return;
     }
     const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
