@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = 64;                      // edge of small tiles, and of the first kernel's
-constexpr int kBigTile = 128;
+constexpr int kPad = 128;                      // matrices are padded to it with zeros
 constexpr float kScale = 4096.f;
 constexpr int kSpan = 3;                       // most steps between two A taken from X
 constexpr int kSumParts = 1024;                // partial sums of squares per matrix at most
@@ -57,20 +57,15 @@ static_assert(sizeof(OrthHead) % 256 == 0, "what follows is aligned");
 // A matrix's part of the workspace: partial sums, two X and five squares, each two planes
 // (hi, lo) of halves.
 struct Slot {
-    int m, n;                                  // rows <= columns of X, padded with zeros to the tile edge
-    int edge;
+    int m, n;                                  // rows <= columns of X, padded
     bool flip;                                 // X is the transpose
 };
-
-// Tiles of 128 x 128 read half the bytes per product of 64 x 64 ones but leave CUs idle
-// unless there are hundreds.
-__host__ __device__ constexpr int edge_of(int shorter) { return shorter > 1536 ? kBigTile : kTile; }
 
 __host__ __device__ inline Slot slot_of(int rows, int cols)
 {
     const bool flip = rows > cols;
-    const int m = flip ? cols : rows, n = flip ? rows : cols, e = edge_of(m);
-    return {(m + e - 1) / e * e, (n + e - 1) / e * e, e, flip};
+    const int m = flip ? cols : rows, n = flip ? rows : cols, e = kPad;
+    return {(m + e - 1) / e * e, (n + e - 1) / e * e, flip};
 }
 
 enum Buf { kX0, kX1, kA, kR, kB0, kB1, kP, kNone };
@@ -348,11 +343,11 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 // both, and write a tile on or above the diagonal and its mirror image. The last one takes
 // R = X as it lies, rows along K, and writes X, the result, or the weights.
 //
-//  * A workgroup of four waves owns a tile of 32 F x 32 F, each wave a quarter of it. Chunks
-//    of 32 of K, F blocks of either operand, go straight from memory to LDS, kStages deep,
-//    one barrier per chunk; a wave waits for its own requests only. Between the matrix
+//  * A workgroup of four waves owns a tile of 32 FI x 32 FJ, each wave a quarter of it. Chunks
+//    of 32 of K, FI blocks of L and FJ of R, go straight from memory to LDS, a few deep, one
+//    barrier per chunk; a wave waits for its own requests only. Between the matrix
 //    instructions of a chunk lie the reads of the next chunk's fragments and the requests of
-//    the chunk kStages ahead, evenly: a wave that does one after the other leaves its matrix
+//    the chunk that takes the present one's place, evenly: a wave that does one after the other leaves its matrix
 //    core idle (2048 x 2048, 128 x 128 tiles: 38 us a product, 24 of them the instructions).
 //  * What is added to the product, E1 and E2, follows the last chunk into LDS. The finished
 //    tile takes E1's place there and goes to memory in whole blocks, its mirror image through
@@ -371,13 +366,22 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kK = kBlock;                     // depth of a chunk
+constexpr int kFold = 4;                       // chunks with running sums of their own
 constexpr int kExtent = 0x7FFFFF00;            // every request lies within its (padded) matrix
 constexpr int kCoherent = 16;                  // cache policy SC1: device-coherent access
 
-template <int F> constexpr int kEdge = 32 * F; // edge of a tile
-template <int F> constexpr int kStage = 2 * F * kBlockBytes;    // L's blocks, R's blocks
-template <int F> constexpr int kStages = 4;                   // chunks in LDS
-constexpr int kFold = 4;                       // chunks with running sums of their own
+// A tile's form: FI x FJ fragments of 16 x 16 per wave. LDS for two workgroups per CU.
+template <int FI, int FJ>
+struct Tile {
+    static constexpr int I = 32 * FI, J = 32 * FJ;        // rows, columns
+    static constexpr int kPer = FI + FJ;                  // blocks of a chunk, requests of a wave for it
+    static constexpr int kStages = FI + FJ > 4 ? 3 : 4;   // chunks in LDS
+    static constexpr int kStage = kPer * kBlockBytes;
+    static constexpr int kBlocks = FI * FJ;               // of the tile
+    static constexpr int kRing = kStages * kPer;          // blocks of LDS
+    static constexpr size_t kLds = (size_t)kStages * kStage;
+    static_assert(2 * kBlocks <= kRing, "two addends fit where the chunks were");
+};
 
 __device__ __forceinline__ f16x8 read_tr(const uint8_t *lo, const uint8_t *hi)
 {
@@ -398,11 +402,10 @@ __device__ __forceinline__ void arrived()
 }
 
 // Where a tile's blocks lie: the first of chunk 0, and the distances (in blocks) from one of
-// a chunk's F blocks to the next and from chunk to chunk.
+// a chunk's blocks to the next and from chunk to chunk.
 struct Operand {
     const uint8_t *at;
-    int next;
-    size_t step;
+    size_t next, step;
 };
 
 // The tile's blocks of E1 and E2 (nullptr: none), `pitch` blocks from row to row.
@@ -419,130 +422,144 @@ __device__ __forceinline__ int transposed(int lane, int h, int k)
     return in_block(8 * (lane >> 4) + 4 * k + (lane >> 2 & 3), 16 * h + (lane & 3) * 4);
 }
 
-template <int F>
+template <int FI, int FJ>
 struct Fragments {
-    f16x8 l[2][F], r[2][F];                               // [hi, lo][16 rows or columns]
+    f16x8 l[2][FI], r[2][FJ];                             // [hi, lo][16 rows or columns]
 };
 
-// Sums of chunks [c0, c1) (both even) of the tile; E1 and E2 are left in LDS, in the stages
-// from c1 on (see stage_of).
-template <int F, bool SYM>
+// Sums of chunks [c0, c1) of the tile, a multiple of kFold and at least one fold. E1's blocks,
+// then E2's, are left in LDS behind the last chunk, from block *behind of the ring on.
+template <int FI, int FJ, bool SYM>
 __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const Operand &R, const Addends &X, int c0,
-                                         int c1, f32x4 (&tot)[F][F])
+                                         int c1, f32x4 (&tot)[FI][FJ], int *behind)
 {
-    constexpr int kPer = 2 * F;                           // requests per wave and chunk
+    using T = Tile<FI, FJ>;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = uniform(tid >> 6);
     const uint32_t lbase = uniform((int)lds_addr(smem));
-    const int own = wave * 1024 + lane * 16;
-    // request q of wave w: kilobyte w (0, 1: hi; 2, 3: lo) of L's block q or R's block q - F.
-    // Past the range come two rows of a tile's blocks per stage, E1's, then E2's; what is not
-    // there is zeros, from no memory: every wait counts alike.
-    struct Source {
-        i32x4 l, r;
-        int next_l, next_r;
-        uint32_t to;
+    // request q of wave w: kilobyte w (0, 1: hi; 2, 3: lo) of L's block q or R's block q - FI
+    int off[T::kPer];
+#pragma unroll
+    for (int q = 0; q < T::kPer; ++q)
+        off[q] = (int)(q < FI ? q * L.next : (q - FI) * R.next) * kBlockBytes + wave * 1024 + lane * 16;
+    const uint8_t *pl = L.at + c0 * L.step * kBlockBytes, *pr = R.at + c0 * R.step * kBlockBytes;
+    i32x4 dl, dr;
+    auto next_chunk = [&] {
+        dl = raw_desc(pl, kExtent);
+        dr = raw_desc(pr, kExtent);
+        pl += L.step * kBlockBytes;
+        pr += R.step * kBlockBytes;
     };
-    auto source = [&](int c) {
-        const bool in = c < c1;
-        const int x = c - c1, e = F == 2 ? x : x >> 1, row = F == 2 ? 0 : (x & 1) * 2;
-        const uint8_t *add = e == 0 ? X.at[0] : e == 1 ? X.at[1] : nullptr;
-        const uint8_t *l = in ? L.at + c * L.step * kBlockBytes : add + (size_t)row * X.pitch * kBlockBytes;
-        const uint8_t *r = in ? R.at + c * R.step * kBlockBytes : add + (size_t)(row + 1) * X.pitch * kBlockBytes;
-        const int bytes = in || add ? kExtent : 0;
-        return Source{raw_desc(l, bytes), raw_desc(r, bytes), in ? L.next : 1, in ? R.next : 1,
-                      lbase + (c & (kStages<F> - 1)) * kStage<F> + wave * 1024};
+    auto request = [&](uint32_t to, int q) { dma16(q < FI ? dl : dr, to + q * kBlockBytes, off[q]); };
+    // block x of the addends; one that is not there is zeros, from no memory
+    auto request_addend = [&](uint32_t to, int q, int x) {
+        const int b = x % T::kBlocks;
+        const uint8_t *e = x < T::kBlocks ? X.at[0] : x < 2 * T::kBlocks ? X.at[1] : nullptr;
+        dma16(raw_desc(e, e ? kExtent : 0), to + q * kBlockBytes,
+              ((b / FJ) * X.pitch + b % FJ) * kBlockBytes + wave * 1024 + lane * 16);
     };
-    auto request = [&](const Source &s, int q) {
-        if (q < F) dma16(s.l, s.to + q * kBlockBytes, q * s.next_l * kBlockBytes + own);
-        else dma16(s.r, s.to + q * kBlockBytes, (q - F) * s.next_r * kBlockBytes + own);
-    };
-    // fragment q of a chunk: plane q / F, 16 rows (or columns) q % F of this wave's
-    const int wi = (wave >> 1) * F, wj = (wave & 1) * F;
+    // fragments of a chunk, 2 (FI + FJ): plane, 16 rows (or columns) of this wave's
+    const int wi = (wave >> 1) * FI, wj = (wave & 1) * FJ;
     const int frag = in_block(lane & 15, (lane >> 4) * 8);
     int tr[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < 2; ++k) tr[h][k] = transposed(lane, h, k);
-    auto read = [&](int c, Fragments<F> &f, int q) {
-        const int p = q / F, i = q % F, il = wi + i, ir = wj + i;
-        const uint8_t *b = smem + (c & (kStages<F> - 1)) * kStage<F> + p * kBlockPlane;
-        const uint8_t *bl = b + (il >> 1) * kBlockBytes, *br = b + (F + (ir >> 1)) * kBlockBytes;
-        f.l[p][i] = *(const f16x8 *)(bl + (i & 1) * 1024 + frag);     // F is even: il & 1 is i & 1
-        if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (i & 1) * 1024 + frag);
-        else f.r[p][i] = read_tr(br + tr[i & 1][0], br + tr[i & 1][1]);
+    auto read = [&](const uint8_t *b, Fragments<FI, FJ> &f, int q) {
+        if (q < 2 * FI) {                                 // FI and FJ are even: the half of a block is i & 1
+            const int p = q / FI, i = q % FI;
+            f.l[p][i] = *(const f16x8 *)(b + ((wi + i) >> 1) * kBlockBytes + p * kBlockPlane + (i & 1) * 1024 + frag);
+        } else {
+            const int p = (q - 2 * FI) / FJ, i = (q - 2 * FI) % FJ;
+            const uint8_t *br = b + (FI + ((wj + i) >> 1)) * kBlockBytes + p * kBlockPlane;
+            if constexpr (SYM) f.r[p][i] = *(const f16x8 *)(br + (i & 1) * 1024 + frag);
+            else f.r[p][i] = read_tr(br + tr[i & 1][0], br + tr[i & 1][1]);
+        }
     };
 #pragma unroll
-    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < FI * FJ; ++i) tot[i / FJ][i % FJ] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int d = 0; d < kStages<F>; ++d) {
-        const Source s = source(c0 + d);
+    for (int d = 0; d < T::kStages; ++d) {
+        next_chunk();
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) request(s, q);
+        for (int q = 0; q < T::kPer; ++q) request(lbase + d * T::kStage + wave * 1024, q);
     }
-    Fragments<F> f[2];
-    arrived<(kStages<F> - 1) * kPer>();
+    Fragments<FI, FJ> f[2];
+    arrived<(T::kStages - 1) * T::kPer>();
 #pragma unroll
-    for (int q = 0; q < 2 * F; ++q) read(c0, f[0], q);
-    // chunk c: its fragments are in `now`; those of c + 1 are read meanwhile. Past the barrier
-    // every wave has read chunk c, so its place in LDS takes chunk c + kStages.
-    auto step = [&](int c, Fragments<F> &now, Fragments<F> &next, f32x4 (&acc)[F][F]) {
-        arrived<(kStages<F> - 2) * kPer>();
-        const Source s = source(c + kStages<F>);
-        constexpr int kEach = 3 * F * F / (2 * F);        // matrix instructions per group
+    for (int q = 0; q < 2 * T::kPer; ++q) read(smem, f[0], q);
+    int at = 0;                                           // byte of LDS where chunk c lies
+    // a chunk: its fragments are in `now`; the next one's are read meanwhile. Past the barrier
+    // every wave has read the present chunk, so its place in LDS takes the chunk kStages ahead,
+    // or the addends' blocks from AHEAD on.
+    auto step = [&](Fragments<FI, FJ> &now, Fragments<FI, FJ> &next, f32x4 (&acc)[FI][FJ], auto ahead) {
+        constexpr int kAhead = decltype(ahead)::value;
+        arrived<(T::kStages - 2) * T::kPer>();
+        const uint32_t to = lbase + at + wave * 1024;
+        at = at + T::kStage == (int)T::kLds ? 0 : at + T::kStage;
+        const uint8_t *b = smem + at;
+        if constexpr (kAhead < 0) next_chunk();
+        constexpr int kEach = 3 * FI * FJ / T::kPer;      // matrix instructions per group
+        static_assert(kEach * T::kPer == 3 * FI * FJ, "groups are equal");
 #pragma unroll
-        for (int q = 0; q < 2 * F; ++q) {
-            read(c + 1, next, q);
-            request(s, q);
+        for (int q = 0; q < T::kPer; ++q) {
+            read(b, next, 2 * q);
+            read(b, next, 2 * q + 1);
+            if constexpr (kAhead < 0) request(to, q);
+            else request_addend(to, q, kAhead + q);
 #pragma unroll
             for (int k = q * kEach; k < (q + 1) * kEach; ++k) {
-                const int p = k / (F * F), i = k / F % F, j = k % F;      // lo hi, hi lo, hi hi
+                const int p = k / (FI * FJ), i = k / FJ % FI, j = k % FJ;      // lo hi, hi lo, hi hi
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.r[p == 1][j], now.l[p == 0][i], acc[i][j], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // N chunks with sums of their own, written out: sums carried around a loop would be moved
-    // between registers in every turn
-    auto fold = [&](int c, auto n) {
-        constexpr int N = decltype(n)::value;
-        f32x4 acc[F][F];
+    // kFold chunks with sums of their own, written out: sums carried around a loop would be
+    // moved between registers in every turn
+    auto fold = [&](auto last) {
+        f32x4 acc[FI][FJ];
 #pragma unroll
-        for (int i = 0; i < F * F; ++i) acc[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < FI * FJ; ++i) acc[i / FJ][i % FJ] = f32x4{0.f, 0.f, 0.f, 0.f};
+        static_assert(kFold == 4 && T::kStages <= 4, "the last fold's requests reach the addends");
+        constexpr int kFirst = decltype(last)::value ? (T::kStages - kFold) * T::kPer : -4 * T::kPer;
+        step(f[0], f[1], acc, std::integral_constant<int, kFirst>{});
+        step(f[1], f[0], acc, std::integral_constant<int, kFirst + T::kPer>{});
+        step(f[0], f[1], acc, std::integral_constant<int, kFirst + 2 * T::kPer>{});
+        step(f[1], f[0], acc, std::integral_constant<int, kFirst + 3 * T::kPer>{});
 #pragma unroll
-        for (int k = 0; k < N; ++k) step(c + k, f[k & 1], f[~k & 1], acc);
-#pragma unroll
-        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] += acc[i / F][i % F];
+        for (int i = 0; i < FI * FJ; ++i) tot[i / FJ][i % FJ] += acc[i / FJ][i % FJ];
     };
-    int c = c0;
-    for (; c + kFold <= c1; c += kFold) fold(c, std::integral_constant<int, kFold>{});
-    if (c < c1) fold(c, std::integral_constant<int, 2>{});
+    for (int c = c0 + kFold; c < c1; c += kFold) fold(std::false_type{});
+    fold(std::true_type{});
     arrived<0>();
+    *behind = at / kBlockBytes;
 }
 
 // Chunks of K of a product, tiles of a matrix with `jobs` of them, and K ranges of about
 // `each` chunks (0: whole).
 __host__ __device__ inline int chunks_of(const OrthPlan &p, const Slot &s) { return (p.job[0].L <= kX1 ? s.n : s.m) / kK; }
 
-template <int F>
+// Row i of a symmetric product's tiles holds those that reach the diagonal: i I / J .. m / J - 1.
+template <int FI, int FJ>
 __host__ __device__ inline uint32_t tiles_of(const OrthPlan &p, const Slot &s)
 {
-    const uint32_t i = s.m / kEdge<F>, j = s.n / kEdge<F>;
-    return p.sym ? i * (i + 1) / 2 : i * j;
+    static_assert(FI % FJ == 0, "whole tiles left of the diagonal");
+    const uint32_t i = s.m / (32 * FI), j = p.sym ? s.m / (32 * FJ) : s.n / (32 * FJ);
+    return p.sym ? i * j - FI / FJ * (i * (i - 1) / 2) : i * j;
 }
 
 __host__ __device__ inline int ranges_of(int chunks, int each) { return each ? (chunks + each - 1) / each : 1; }
 
-template <int F>
+template <int FI, int FJ>
 __host__ __device__ inline uint32_t products_of(const OrthPlan &p, const OrthShape &e, int each)
 {
     const Slot s = slot_of(e.rows, e.cols);
-    if (s.edge != kEdge<F> || !p.jobs) return 0;
-    return p.jobs * tiles_of<F>(p, s) * ranges_of(chunks_of(p, s), each);
+    return p.jobs ? p.jobs * tiles_of<FI, FJ>(p, s) * ranges_of(chunks_of(p, s), each) : 0;
 }
 
-template <int F, bool MANY>
+template <int FI, int FJ, bool MANY>
 __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, OrthStage S, OrthHead *head, OrthStep h, uint32_t per)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -558,11 +575,11 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
     const OrthPlan &plan = plan_of(e);
     const Slot s = slot_of(e.rows, e.cols);
     uint8_t *base = slot_base(M, w, s);
-    constexpr int E = kEdge<F>;
+    using Form = Tile<FI, FJ>;
     // number within the matrix = (range * jobs + job) * tiles + tile, so that neighbours read
     // the same columns of X
     const int chunks = chunks_of(plan, s), ranges = ranges_of(chunks, S.each);
-    const uint32_t tiles = tiles_of<F>(plan, s), all = tiles * plan.jobs;
+    const uint32_t tiles = tiles_of<FI, FJ>(plan, s), all = tiles * plan.jobs;
     uint32_t which = w.local, split = 0;
     if (ranges > 1) {
         split = w.local / all;
@@ -574,44 +591,45 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
     int ti, tj;
     if (plan.sym) {
         ti = 0;
-        uint32_t row = s.m / E;                            // row ti holds tiles ti .. m / E - 1
-        while (tile >= row) { tile -= row--; ++ti; }
-        tj = ti + tile;
+        uint32_t row = s.m / Form::J;                      // tiles of row ti
+        for (; tile >= row; row -= FI / FJ, ++ti) tile -= row;
+        tj = ti * (FI / FJ) + tile;
     } else {
-        const int tiles_m = s.m / E;                       // down the columns of X
+        const int tiles_m = s.m / Form::I;                 // down the columns of X
         tj = tile / tiles_m;
         ti = tile - tj * tiles_m;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // a lane's part of the tile: [i][j][q] is row wi + 16 i + lane % 16, column
     // wj + 16 j + 4 (lane / 16) + q
-    const int wi = (wave >> 1) * 16 * F, wj = (wave & 1) * 16 * F;
+    const int wi = (wave >> 1) * 16 * FI, wj = (wave & 1) * 16 * FJ;
     const int ld = plan.sym ? s.m : s.n;
-    auto tile_at = [&](int b, int bi, int bj) {            // tile (bi, bj) of a buffer
-        return base + buf_at(s, b) + ((size_t)bi * F * (ld / kBlock) + bj * F) * kBlockBytes;
+    const int gi = ti * FI, gj = tj * FJ;                  // the tile's first block
+    auto block_at = [&](int b, int bi, int bj) {           // block (bi, bj) of a buffer
+        return base + buf_at(s, b) + ((size_t)bi * (ld / kBlock) + bj) * kBlockBytes;
     };
-    const Addends X = {{job.E1 == kNone ? nullptr : uniform(tile_at(job.E1, ti, tj)),
-                        job.E2 == kNone ? nullptr : uniform(tile_at(job.E2, ti, tj))}, ld / kBlock};
-    const int each = ((chunks + ranges - 1) / ranges + 1) & ~1;       // chunks are even, so are ranges
-    const int c0 = uniform(min(chunks, (int)split * each)), c1 = uniform(min(chunks, c0 + each));
-    f32x4 tot[F][F];
-    const Operand L = {uniform(base + buf_at(s, job.L) + (size_t)ti * F * chunks * kBlockBytes), chunks, 1};
+    const Addends X = {{job.E1 == kNone ? nullptr : uniform(block_at(job.E1, gi, gj)),
+                        job.E2 == kNone ? nullptr : uniform(block_at(job.E2, gi, gj))}, ld / kBlock};
+    const int c0 = uniform(split * S.each), c1 = uniform(ranges > 1 ? min(chunks, c0 + S.each) : chunks);
+    f32x4 tot[FI][FJ];
+    int behind;
+    const Operand L = {uniform(base + buf_at(s, job.L) + (size_t)gi * chunks * kBlockBytes), (size_t)chunks, 1};
     if (uniform(plan.sym)) {
-        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * chunks * kBlockBytes), chunks, 1};
-        multiply<F, true>(smem, L, R, X, c0, c1, tot);
+        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)gj * chunks * kBlockBytes), (size_t)chunks, 1};
+        multiply<FI, FJ, true>(smem, L, R, X, c0, c1, tot, &behind);
     } else {
-        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)tj * F * kBlockBytes), 1, (size_t)s.n / kBlock};
-        multiply<F, false>(smem, L, R, X, c0, c1, tot);
+        const Operand R = {uniform(base + buf_at(s, job.R) + (size_t)gj * kBlockBytes), 1, (size_t)s.n / kBlock};
+        multiply<FI, FJ, false>(smem, L, R, X, c0, c1, tot, &behind);
     }
     if (ranges > 1) {
         const uint32_t slot = wg - w.local + which * ranges;   // the tile's first place
         const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)((f32x4 *)(head + 1) + (size_t)slot * (F * F * kThreads)), (short)0,
-            ranges * F * F * kThreads * 16, kBufferFlags);
-        auto place = [&](int k, int i) { return ((k * F * F + i) * kThreads + tid) * 16; };
+            (void *)((f32x4 *)(head + 1) + (size_t)slot * (FI * FJ * kThreads)), (short)0,
+            ranges * FI * FJ * kThreads * 16, kBufferFlags);
+        auto place = [&](int k, int i) { return ((k * FI * FJ + i) * kThreads + tid) * 16; };
 #pragma unroll
-        for (int i = 0; i < F * F; ++i)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, tot[i / F][i % F]), part, place(split, i), 0, kCoherent);
+        for (int i = 0; i < FI * FJ; ++i)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, tot[i / FJ][i % FJ]), part, place(split, i), 0, kCoherent);
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (tid == 0) {
@@ -622,74 +640,79 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
         __syncthreads();
         if (!last) return;
 #pragma unroll
-        for (int i = 0; i < F * F; ++i) tot[i / F][i % F] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < FI * FJ; ++i) tot[i / FJ][i % FJ] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int k = 0; k < ranges; ++k)
 #pragma unroll
-            for (int i = 0; i < F * F; ++i)
-                tot[i / F][i % F] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, place(k, i), 0, kCoherent));
+            for (int i = 0; i < FI * FJ; ++i)
+                tot[i / FJ][i % FJ] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, place(k, i), 0, kCoherent));
     }
-    // E1 and E2 lie in the two halves of LDS behind the last chunk; E1's place takes the result
-    constexpr int kTileBytes = F * F * kBlockBytes;
-    uint8_t *first = smem + (c1 & (kStages<F> - 1)) * kStage<F>;
-    const uint8_t *next = smem + ((c1 + F / 2) & (kStages<F> - 1)) * kStage<F>;
-    static_assert(kTileBytes == F / 2 * kStage<F> && kStages<F> == 4, "a tile takes one or two stages");
-    auto add = [&](const uint8_t *from, float by) {
+    // behind the last chunk LDS holds E1's blocks, which the result replaces, then E2's
+    auto in_lds = [&](int b) {                             // block b of them
+        const int at = behind + b;
+        return smem + (at < Form::kRing ? at : at - Form::kRing) * kBlockBytes;
+    };
+    // where a lane's [i][j] lies in block (wi + 16 i) / 32, (wj + 16 j) / 32 of the tile
+    auto mine = [&](int i, int j, int add) {
+        const int r = wi + i * 16, c = wj + j * 16;
+        return in_lds(add * Form::kBlocks + (r >> 5) * FJ + (c >> 5)) + in_block(r + (lane & 15), c + (lane >> 4) * 4);
+    };
+    auto add = [&](int which, float by) {
 #pragma unroll
-        for (int i = 0; i < F; ++i)
+        for (int i = 0; i < FI; ++i)
 #pragma unroll
-            for (int j = 0; j < F; ++j) {
-                const uint8_t *at = from + blocked(wi + i * 16 + (lane & 15), wj + j * 16 + (lane >> 4) * 4, E);
+            for (int j = 0; j < FJ; ++j) {
+                const uint8_t *at = mine(i, j, which);
                 const f16x4 hi = *(const f16x4 *)at, lo = *(const f16x4 *)(at + kBlockPlane);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) tot[i][j][q] += by * ((float)hi[q] + (float)lo[q]);
             }
     };
 #pragma unroll
-    for (int i = 0; i < F * F; ++i) tot[i / F][i % F] *= job.s3 * (1.f / kScale);
-    if (job.E1 != kNone) add(first, job.s1);
-    if (job.E2 != kNone) add(next, job.s2);
+    for (int i = 0; i < FI * FJ; ++i) tot[i / FJ][i % FJ] *= job.s3 * (1.f / kScale);
+    if (job.E1 != kNone) add(0, job.s1);
+    if (job.E2 != kNone) add(1, job.s2);
     if (!plan.last) {
 #pragma unroll
-        for (int i = 0; i < F; ++i)
+        for (int i = 0; i < FI; ++i)
 #pragma unroll
-            for (int j = 0; j < F; ++j) {
+            for (int j = 0; j < FJ; ++j) {
                 f16x4 hi, lo;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     hi[q] = (_Float16)tot[i][j][q];
                     lo[q] = (_Float16)(tot[i][j][q] - (float)hi[q]);
                 }
-                uint8_t *at = first + blocked(wi + i * 16 + (lane & 15), wj + j * 16 + (lane >> 4) * 4, E);
+                uint8_t *at = mine(i, j, 0);
                 *(f16x4 *)at = hi;
                 *(f16x4 *)(at + kBlockPlane) = lo;
             }
         __syncthreads();
         // half a plane of a block per wave and turn: 16 rows, a unit of 16 bytes per lane
-        uint8_t *d = tile_at(job.D, ti, tj), *mirror = tile_at(job.D, tj, ti);
-        const int u = lane >> 4;
+        const int r = lane & 15, u = lane >> 4;
 #pragma unroll
-        for (int k = 0; k < F * F; ++k) {
-            const int piece = k * 4 + wave, h = piece & 1, p = piece >> 1 & 1, b = piece >> 2, bi = b / F, bj = b % F;
-            const uint8_t *from = first + b * kBlockBytes + p * kBlockPlane;
-            const size_t row = (size_t)(ld / kBlock) * kBlockBytes, in = p * kBlockPlane + in_block(16 * h + (lane & 15), 8 * u);
-            f16x8 v = *(const f16x8 *)(from + in_block(16 * h + (lane & 15), 8 * u));
+        for (int k = 0; k < Form::kBlocks; ++k) {
+            const int h = wave & 1, p = wave >> 1, bi = gi + k / FJ, bj = gj + k % FJ;
+            const uint8_t *from = in_lds(k) + p * kBlockPlane;
+            const int in = p * kBlockPlane + in_block(16 * h + r, 8 * u);
+            uint8_t *d = block_at(job.D, bi, bj) + in;
+            f16x8 v = *(const f16x8 *)(from + in_block(16 * h + r, 8 * u));
             if (!plan.sym) {
-                *(f16x8 *)(d + bi * row + bj * kBlockBytes + in) = v;
+                *(f16x8 *)d = v;
                 continue;
             }
-            // on the diagonal the upper half stands for both: what is stored is symmetric
-            const bool diagonal = ti == tj;
-            if (diagonal && bi > bj) continue;
+            // the blocks above the diagonal, and their mirror images; on it the upper half stands
+            // for both: what is stored is symmetric
+            if (bi > bj) continue;
             const f16x8 m = read_tr(from + transposed(lane, h, 0), from + transposed(lane, h, 1));
-            if (diagonal && bi == bj) {
+            if (bi == bj) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if (8 * u + q < 16 * h + (lane & 15)) v[q] = m[q];
+                    if (8 * u + q < 16 * h + r) v[q] = m[q];
             } else {
-                *(f16x8 *)(mirror + bj * row + bi * kBlockBytes + in) = m;
+                *(f16x8 *)(block_at(job.D, bj, bi) + in) = m;
             }
-            *(f16x8 *)(d + bi * row + bj * kBlockBytes + in) = v;
+            *(f16x8 *)d = v;
         }
         return;
     }
@@ -706,12 +729,12 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
         }
     };
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FI; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+        for (int j = 0; j < FJ; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = ti * E + wi + i * 16 + (lane & 15), c = tj * E + wj + j * 16 + (lane >> 4) * 4 + q;
+                const int r = ti * Form::I + wi + i * 16 + (lane & 15), c = tj * Form::J + wj + j * 16 + (lane >> 4) * 4 + q;
                 const int row = s.flip ? c : r, col = s.flip ? r : c;
                 if (row < e.rows && col < e.cols) write((size_t)row * e.cols + col, tot[i][j][q] * (1.f / kScale));
             }
@@ -777,38 +800,55 @@ unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
     return (unsigned)at;
 }
 
-template <int F, bool MANY>
+// Tiles of 128 x 64 read three quarters of the bytes of 64 x 64 ones per product, where they
+// are enough for the chip.
+constexpr uint64_t kEnough = 192;
+
+template <int FI, int FJ, bool MANY>
+hipError_t launch_product(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, const OrthStage &S,
+                          hipStream_t s)
+{
+    uint32_t per = 0;
+    const unsigned grid = number(M, T, &per, [&](const OrthShape &e) {
+        return products_of<FI, FJ>(S.plan[MANY && steps_direct(e.rows, e.cols)], e, S.each);
+    });
+    const hipError_t e = allow_lds((const void *)k_orth_product<FI, FJ, MANY>, Tile<FI, FJ>::kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_orth_product<FI, FJ, MANY>), dim3(grid), dim3(kThreads), (unsigned)(Tile<FI, FJ>::kLds), s, M, S,
+                       head, h, per);
+    return hipGetLastError();
+}
+
+template <bool MANY>
 hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, OrthStage &S,
                            const NewtonSchulz &ns, hipStream_t s)
 {
-    bool any[2] = {false, false};
-    for (int t = 0; t < T.n; ++t)
-        if (slot_of(T.e[t].rows, T.e[t].cols).edge == kEdge<F>) any[steps_direct(T.e[t].rows, T.e[t].cols)] = true;
-    if (!any[0] && !any[1]) return hipSuccess;
-    const size_t lds = kStages<F> * kStage<F>;
-    hipError_t e = allow_lds((const void *)k_orth_product<F, MANY>, lds);
-    if (e != hipSuccess) return e;
     // one shape has its plan in the first place
     std::vector<OrthPlan> plans[2];
-    for (int d = 0; d < 2; ++d)
-        if (any[d]) plans[MANY ? d : 0] = plans_of(ns, d);
+    for (int t = 0; t < T.n; ++t) {
+        const bool direct = steps_direct(T.e[t].rows, T.e[t].cols);
+        if (plans[MANY && direct].empty()) plans[MANY && direct] = plans_of(ns, direct);
+    }
     const size_t launches = std::max(plans[0].size(), plans[1].size());
-    auto plan = [&](const OrthShape &e) -> const OrthPlan & { return S.plan[MANY && steps_direct(e.rows, e.cols)]; };
     for (size_t i = 0; i < launches; ++i) {
         // a plan that is done has no jobs, and its matrices no workgroups
         for (int d = 0; d < 2; ++d) S.plan[d] = i < plans[d].size() ? plans[d][i] : OrthPlan{};
-        // K in ranges where tiles are few
-        uint64_t all = 0, work = 0;
+        // large tiles where they are enough, K in ranges where even small ones are few
+        uint64_t large = 0, small = 0, work = 0;
         for (int t = 0; t < T.n; ++t) {
-            const uint64_t wgs = (uint64_t)products_of<F>(plan(T.e[t]), T.e[t], 0) * T.e[t].batch;
-            all += wgs;
-            work += wgs * chunks_of(plan(T.e[t]), slot_of(T.e[t].rows, T.e[t].cols));
+            const OrthPlan &p = S.plan[MANY && steps_direct(T.e[t].rows, T.e[t].cols)];
+            const Slot slot = slot_of(T.e[t].rows, T.e[t].cols);
+            if (!p.jobs) continue;
+            const uint64_t b = T.e[t].batch, wgs = products_of<2, 2>(p, T.e[t], 0) * b;
+            large += products_of<4, 2>(p, T.e[t], 0) * b;
+            small += wgs;
+            work += wgs * chunks_of(p, slot);
         }
-        S.each = F > 2 || all > 256 ? 0 : (int)std::max<uint64_t>(kLeastChunks, (work + 511) / 512);
-        uint32_t per = 0;
-        const unsigned grid = number(M, T, &per, [&](const OrthShape &e) { return products_of<F>(plan(e), e, S.each); });
-        hipLaunchKernelGGL((k_orth_product<F, MANY>), dim3(grid), dim3(kThreads), lds, s, M, S, head, h, per);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        const bool use_large = large >= kEnough;
+        S.each = small > 256 ? 0 : (int)std::max<uint64_t>(kLeastChunks, ((work + 511) / 512 + kFold - 1) / kFold * kFold);
+        const hipError_t e = use_large ? launch_product<4, 2, MANY>(T, M, head, h, S, s)
+                                       : launch_product<2, 2, MANY>(T, M, head, h, S, s);
+        if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
@@ -824,7 +864,6 @@ size_t orth_shared_work(const OrthShape *e, int n)
     bool any = false;
     for (int t = 0; t < n; ++t) {
         const Slot s = slot_of(e[t].rows, e[t].cols);
-        if (s.edge != kTile) continue;
         const uint64_t i = s.m / kTile, sym = i * (i + 1) / 2;
         auto ranges = [](int depth) { return (uint64_t)(depth / kK + kLeastChunks - 1) / kLeastChunks; };
         const uint64_t wide = ranges(s.n), square = ranges(s.m);
@@ -905,8 +944,7 @@ static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int 
     if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
     OrthStage S{};
     S.fmt = out_fmt;
-    if ((e = launch_products<2, MANY>(T, M, head, h, S, ns, s)) != hipSuccess) return e;
-    return launch_products<4, MANY>(T, M, head, h, S, ns, s);
+    return launch_products<MANY>(T, M, head, h, S, ns, s);
 }
 
 hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
