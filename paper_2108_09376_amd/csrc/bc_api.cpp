@@ -1235,13 +1235,12 @@ static bc_status orth_iteration(const bc_newton_schulz &in, bc::NewtonSchulz &ns
     return BC_OK;
 }
 
-static size_t orth_need(int32_t batch, int32_t rows, int32_t cols)
+static size_t orth_need(int32_t batch, int32_t rows, int32_t cols, int32_t steps)
 {
-    bc::OrthShape e{};
-    e.rows = rows;
-    e.cols = cols;
-    e.batch = batch;
-    return bc::orth_shared_work(&e, 1) + bc::orth_work(rows, cols) * (size_t)batch;
+    bc::OrthTable T{};
+    T.n = 1;
+    T.e[0] = {rows, cols, batch, 0};
+    return bc::orth_shared_work(T, steps) + bc::orth_work(rows, cols) * (size_t)batch;
 }
 
 bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32_t steps, int64_t *bytes)
@@ -1249,7 +1248,7 @@ bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32
     if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
     bc_status st = orth_sizes(batch, rows, cols, steps, "matrices");
     if (st) return st;
-    *bytes = (int64_t)orth_need(batch, rows, cols);
+    *bytes = (int64_t)orth_need(batch, rows, cols, steps);
     return ok();
 }
 
@@ -1263,7 +1262,7 @@ bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int
     if (!valid_dtype(in_dtype) || !valid_dtype(out_dtype)) return fail(BC_ERR_DTYPE, "unknown dtype");
     bc::NewtonSchulz it;
     if ((st = orth_iteration(*ns, it))) return st;
-    const size_t need = orth_need(batch, rows, cols);
+    const size_t need = orth_need(batch, rows, cols, ns->steps);
     if ((st = check_work(d_work, work_bytes, need))) return st;
     const size_t count = (size_t)batch * rows * cols, ib = count * esize_of(in_dtype), ob = count * esize_of(out_dtype);
     if (overlap(d_work, need, d_g, ib) || overlap(d_work, need, d_out, ob) ||
@@ -1287,20 +1286,19 @@ static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, s
     if (n < 1 || n > bc::kMaxParams) return fail(BC_ERR_SHAPE, "n outside 1..%d", bc::kMaxParams);
     *need = 0;
     double tiles = 0;
-    bc::OrthShape e[bc::kMaxParams] = {};
+    bc::OrthTable T{};
+    T.n = n;
     for (int t = 0; t < n; ++t) {
         char name[32];
         snprintf(name, sizeof name, "params[%d]", t);
         bc_status st = orth_sizes(1, params[t].rows, params[t].cols, steps, name);
         if (st) return st;
-        e[t].rows = params[t].rows;
-        e[t].cols = params[t].cols;
-        e[t].batch = 1;
+        T.e[t] = {params[t].rows, params[t].cols, 1, 0};
         *need += bc::orth_work(params[t].rows, params[t].cols);
         tiles += bc::orth_tiles(params[t].rows, params[t].cols);
     }
     if (tiles >= (double)(1 << 24)) return fail(BC_ERR_SHAPE, "2^24 or more tiles of 64 x 64");
-    *need += bc::orth_shared_work(e, n);
+    *need += bc::orth_shared_work(T, steps);
     return BC_OK;
 }
 

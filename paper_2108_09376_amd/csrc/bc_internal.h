@@ -227,7 +227,7 @@ struct NewtonSchulz {
     float a, b, c, eps;
 };
 size_t orth_work(int rows, int cols);         // bytes of a matrix's part
-size_t orth_shared_work(const OrthShape *e, int n);
+size_t orth_shared_work(const OrthTable &T, int steps);
 unsigned orth_tiles(int rows, int cols);       // workgroups of the largest launch, per matrix
 bool orth_supported(const NewtonSchulz &ns, const char **why);
 hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,

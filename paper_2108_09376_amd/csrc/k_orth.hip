@@ -48,7 +48,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // The workspace's shared part; the fp32 sums of K ranges follow it.
-constexpr int kMostSplit = 768;                // workgroups of a launch that splits K
+constexpr int kMostSplit = 1024;               // workgroups of a launch that splits K: 512 and one more per tile
 struct OrthHead {
     uint32_t count[kMostSplit];                // arrivals per tile
 };
@@ -81,13 +81,14 @@ __host__ __device__ inline size_t slot_bytes(const Slot &s) { return buf_at(s, k
 // Matrices lie in blocks of 32 x 32, row of blocks after row of blocks, each block its hi
 // plane (2 KB), then its lo plane, as LDS holds them: a tile's chunk of K is whole blocks,
 // which requests to LDS take in order, a kilobyte each. Within a plane the four 16-byte units
-// of row r are stored at unit ^ (r / 4): the fragments of 16 rows, and the transposed ones of
-// 16 columns, then meet every bank once.
+// of row r are stored at unit ^ (-(r / 4) mod 4). A read of 16 bytes per lane is served for
+// rows 0-3 and 12-15 of one unit with rows 4-11 of the next (and the other way round), a
+// transposing one for rows 0-3 and 8-11 (4-7 and 12-15): both then meet every bank once.
 constexpr int kBlock = 32, kBlockPlane = kBlock * kBlock * 2, kBlockBytes = 2 * kBlockPlane;
 
 __device__ __forceinline__ int in_block(int r, int c)
 {
-    return (r & 31) * 64 + ((((c & 31) >> 3) ^ (r >> 2 & 3)) << 4) + (c & 7) * 2;
+    return (r & 31) * 64 + ((((c & 31) >> 3) ^ (-(r >> 2) & 3)) << 4) + (c & 7) * 2;
 }
 
 // Byte address of (r, c) of the hi plane in a matrix of ld columns.
@@ -259,12 +260,27 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHe
     if (threadIdx.x == 0) ((double *)slot_base(M, w, s))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-__device__ __forceinline__ void store_as(int fmt, void *p, size_t at, float v)
+// Elements i .. i + 3 (those below n) rounded to a 16-bit format, or as they are.
+__device__ __forceinline__ void store4_as(int fmt, void *p, size_t i, size_t n, const float (&v)[4])
 {
-    const float y[1] = {v};
-    if (fmt == kF32) store_raw<kF32, 1>(p, at, pack<kF32, 1>(y));
-    else if (fmt == kBF16) store_raw<kBF16, 1>(p, at, pack<kBF16, 1>(y));
-    else store_raw<kF16, 1>(p, at, pack<kF16, 1>(y));
+    if (fmt == kF32) {
+        store4((float *)p, i, n, v);
+        return;
+    }
+    struct __attribute__((packed, aligned(2))) Halves { uint16_t h[4]; } o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float one[1] = {v[j]};
+        o.h[j] = (uint16_t)(fmt == kBF16 ? pack<kBF16, 1>(one).w[0] : pack<kF16, 1>(one).w[0]);
+    }
+    uint16_t *to = (uint16_t *)p + i;
+    if (i + 4 <= n) {
+        *(Halves *)to = o;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j < n) to[j] = o.h[j];
+    }
 }
 
 // X_0 from G, one 64 x 64 tile per workgroup.
@@ -716,28 +732,49 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
         }
         return;
     }
-    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
-    const float rate = h.lr * sqrtf(tall);
-    auto write = [&](size_t o, float v) {
-        if constexpr (MANY) {
-            const OrthParam &p = M.p[w.t];
-            const float wn = h.keep * p.w[o] - rate * v;
-            p.w[o] = wn;
-            if (p.w16) store_as(S.fmt, p.w16, o, wn);
-        } else {
-            store_as(S.fmt, M.out, (size_t)w.img * e.rows * e.cols + o, v);
-        }
-    };
+    // the result: in fp32 through LDS, in rows of the result (columns of X where that is the
+    // transpose), four elements per thread and turn
+    static_assert((size_t)Form::I * (Form::J + 4) * 4 <= Form::kLds && (size_t)Form::J * (Form::I + 4) * 4 <= Form::kLds,
+                  "the tile fits");
+    float *rows = (float *)smem;
+    __syncthreads();                                       // E1 and E2 have been read
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
-        for (int j = 0; j < FJ; ++j)
+        for (int j = 0; j < FJ; ++j) {
+            const int r = wi + i * 16 + (lane & 15), c = wj + j * 16 + (lane >> 4) * 4;
+            tot[i][j] *= 1.f / kScale;
+            if (!s.flip) {
+                *(f32x4 *)(rows + r * (Form::J + 4) + c) = tot[i][j];
+            } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = ti * Form::I + wi + i * 16 + (lane & 15), c = tj * Form::J + wj + j * 16 + (lane >> 4) * 4 + q;
-                const int row = s.flip ? c : r, col = s.flip ? r : c;
-                if (row < e.rows && col < e.cols) write((size_t)row * e.cols + col, tot[i][j][q] * (1.f / kScale));
+                for (int q = 0; q < 4; ++q) rows[(c + q) * (Form::I + 4) + r] = tot[i][j][q];
             }
+        }
+    __syncthreads();
+    const int width = s.flip ? Form::I : Form::J;
+    const int row0 = s.flip ? tj * Form::J : ti * Form::I, col0 = s.flip ? ti * Form::I : tj * Form::J;
+    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
+    const float rate = h.lr * sqrtf(tall);
+#pragma unroll
+    for (int k = 0; k < Form::I * Form::J / 4 / kThreads; ++k) {
+        const int q = (k * kThreads + tid) * 4, r = q / width, c = q - r * width;
+        if (row0 + r >= e.rows || col0 + c >= e.cols) continue;
+        const f32x4 x = *(const f32x4 *)(rows + r * (width + 4) + c);
+        const size_t o = (size_t)(row0 + r) * e.cols + col0 + c, end = (size_t)(row0 + r + 1) * e.cols;
+        float v[4] = {x[0], x[1], x[2], x[3]};
+        if constexpr (MANY) {
+            const OrthParam &p = M.p[w.t];
+            float was[4];
+            load4<kF32>(p.w, o, end, was);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = h.keep * was[j] - rate * v[j];
+            store4(p.w, o, end, v);
+            if (p.w16) store4_as(S.fmt, p.w16, o, end, v);
+        } else {
+            store4_as(S.fmt, (uint8_t *)M.out + (size_t)w.img * e.rows * e.cols * (S.fmt == kF32 ? 4 : 2), o, end, v);
+        }
+    }
 }
 
 // ---------------------------------------------------------------- host: what is launched when
@@ -804,6 +841,57 @@ unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
 // are enough for the chip.
 constexpr uint64_t kEnough = 192;
 
+// The products of one launch: the plans of its matrices (those taken in spans, those taken step
+// by step; a plan that is done has no jobs), the tiles, and the K ranges.
+struct Launch {
+    OrthPlan plan[2];
+    bool large;
+    int each;
+    size_t part_bytes;                         // of the sums of K ranges
+};
+
+std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
+{
+    std::vector<OrthPlan> plans[2];
+    for (int t = 0; t < T.n; ++t) {
+        const bool direct = steps_direct(T.e[t].rows, T.e[t].cols);
+        if (plans[direct].empty()) plans[direct] = plans_of(ns, direct);
+    }
+    std::vector<Launch> all(std::max(plans[0].size(), plans[1].size()));
+    for (size_t i = 0; i < all.size(); ++i) {
+        Launch &l = all[i];
+        for (int d = 0; d < 2; ++d) l.plan[d] = i < plans[d].size() ? plans[d][i] : OrthPlan{};
+        auto total = [&](auto count) {
+            uint64_t n = 0;
+            for (int t = 0; t < T.n; ++t) {
+                const OrthPlan &p = l.plan[steps_direct(T.e[t].rows, T.e[t].cols)];
+                if (p.jobs) n += (uint64_t)count(p, T.e[t]) * T.e[t].batch;
+            }
+            return n;
+        };
+        auto chunks = [](const OrthPlan &p, const OrthShape &e) { return (uint64_t)chunks_of(p, slot_of(e.rows, e.cols)); };
+        const uint64_t large = total([](const OrthPlan &p, const OrthShape &e) { return products_of<4, 2>(p, e, 0); });
+        l.large = large >= kEnough;
+        auto tiles = [&](const OrthPlan &p, const OrthShape &e, int each) {
+            return l.large ? products_of<4, 2>(p, e, each) : products_of<2, 2>(p, e, each);
+        };
+        const uint64_t wgs = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, 0); });
+        const uint64_t work = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, 0) * chunks(p, e); });
+        uint64_t longest = 0;
+        for (int t = 0; t < T.n; ++t) {
+            const OrthPlan &p = l.plan[steps_direct(T.e[t].rows, T.e[t].cols)];
+            if (p.jobs) longest = std::max(longest, chunks(p, T.e[t]));
+        }
+        // K in ranges, of whole folds, where the longest workgroup would far outlast the chip's
+        // share of the work (twice as long: 1024 x 2048 254 us whole, 265 in ranges)
+        const uint64_t share = std::max<uint64_t>(kLeastChunks, ((work + 511) / 512 + kFold - 1) / kFold * kFold);
+        l.each = longest >= 3 * share && wgs <= 512 ? (int)share : 0;
+        const uint64_t places = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, l.each); });
+        l.part_bytes = l.each ? places * kThreads * sizeof(f32x4) * (l.large ? 8 : 4) : 0;
+    }
+    return all;
+}
+
 template <int FI, int FJ, bool MANY>
 hipError_t launch_product(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, const OrthStage &S,
                           hipStream_t s)
@@ -820,34 +908,17 @@ hipError_t launch_product(const OrthTable &T, Matrices<MANY> &M, OrthHead *head,
 }
 
 template <bool MANY>
-hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, OrthStage &S,
+hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head, const OrthStep &h, int out_fmt,
                            const NewtonSchulz &ns, hipStream_t s)
 {
-    // one shape has its plan in the first place
-    std::vector<OrthPlan> plans[2];
-    for (int t = 0; t < T.n; ++t) {
-        const bool direct = steps_direct(T.e[t].rows, T.e[t].cols);
-        if (plans[MANY && direct].empty()) plans[MANY && direct] = plans_of(ns, direct);
-    }
-    const size_t launches = std::max(plans[0].size(), plans[1].size());
-    for (size_t i = 0; i < launches; ++i) {
-        // a plan that is done has no jobs, and its matrices no workgroups
-        for (int d = 0; d < 2; ++d) S.plan[d] = i < plans[d].size() ? plans[d][i] : OrthPlan{};
-        // large tiles where they are enough, K in ranges where even small ones are few
-        uint64_t large = 0, small = 0, work = 0;
-        for (int t = 0; t < T.n; ++t) {
-            const OrthPlan &p = S.plan[MANY && steps_direct(T.e[t].rows, T.e[t].cols)];
-            const Slot slot = slot_of(T.e[t].rows, T.e[t].cols);
-            if (!p.jobs) continue;
-            const uint64_t b = T.e[t].batch, wgs = products_of<2, 2>(p, T.e[t], 0) * b;
-            large += products_of<4, 2>(p, T.e[t], 0) * b;
-            small += wgs;
-            work += wgs * chunks_of(p, slot);
-        }
-        const bool use_large = large >= kEnough;
-        S.each = small > 256 ? 0 : (int)std::max<uint64_t>(kLeastChunks, ((work + 511) / 512 + kFold - 1) / kFold * kFold);
-        const hipError_t e = use_large ? launch_product<4, 2, MANY>(T, M, head, h, S, s)
-                                       : launch_product<2, 2, MANY>(T, M, head, h, S, s);
+    OrthStage S{};
+    S.fmt = out_fmt;
+    for (const Launch &l : launches_of(T, ns)) {
+        S.each = l.each;
+        for (int d = 0; d < 2; ++d) S.plan[d] = l.plan[d];
+        if (!MANY && !S.plan[0].jobs) S.plan[0] = S.plan[1];      // one shape has its plan in the first place
+        const hipError_t e = l.large ? launch_product<4, 2, MANY>(T, M, head, h, S, s)
+                                     : launch_product<2, 2, MANY>(T, M, head, h, S, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -857,21 +928,11 @@ hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head
 
 size_t orth_work(int rows, int cols) { return slot_bytes(slot_of(rows, cols)); }
 
-size_t orth_shared_work(const OrthShape *e, int n)
+size_t orth_shared_work(const OrthTable &T, int steps)
 {
-    // every workgroup of a launch that splits K has a place, those of whole tiles too
-    uint64_t wgs = 0;
-    bool any = false;
-    for (int t = 0; t < n; ++t) {
-        const Slot s = slot_of(e[t].rows, e[t].cols);
-        const uint64_t i = s.m / kTile, sym = i * (i + 1) / 2;
-        auto ranges = [](int depth) { return (uint64_t)(depth / kK + kLeastChunks - 1) / kLeastChunks; };
-        const uint64_t wide = ranges(s.n), square = ranges(s.m);
-        any = any || wide > 1 || square > 1;
-        wgs += e[t].batch * std::max({sym * wide, 2 * sym * square, i * (s.n / kTile) * square});
-    }
-    return sizeof(OrthHead) +
-           (any ? std::min<uint64_t>(wgs, kMostSplit) : 0) * (kThreads * 4 * sizeof(f32x4));
+    size_t part = 0;
+    for (const Launch &l : launches_of(T, NewtonSchulz{steps, 1.f, 1.f, 1.f, 0.f})) part = std::max(part, l.part_bytes);
+    return sizeof(OrthHead) + part;
 }
 
 unsigned orth_tiles(int rows, int cols)
@@ -923,7 +984,7 @@ static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int 
     hipError_t e = hipSuccess;
     OrthHead *head = (OrthHead *)T.work;
     Matrices<MANY> M{};
-    M.work = T.work + orth_shared_work(T.e, T.n);
+    M.work = T.work + orth_shared_work(T, ns.steps);
     M.g = T.g;
     M.out = T.out;
     for (int t = 0; t < T.n; ++t) {
@@ -942,9 +1003,7 @@ static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int 
         }
     });
     if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
-    OrthStage S{};
-    S.fmt = out_fmt;
-    return launch_products<MANY>(T, M, head, h, S, ns, s);
+    return launch_products<MANY>(T, M, head, h, out_fmt, ns, s);
 }
 
 hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
