@@ -1235,20 +1235,15 @@ static bc_status orth_iteration(const bc_newton_schulz &in, bc::NewtonSchulz &ns
     return BC_OK;
 }
 
-static size_t orth_need(int32_t batch, int32_t rows, int32_t cols, int32_t steps)
-{
-    bc::OrthTable T{};
-    T.n = 1;
-    T.e[0] = {rows, cols, batch, 0};
-    return bc::orth_shared_work(T, steps) + bc::orth_work(rows, cols) * (size_t)batch;
-}
-
 bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32_t steps, int64_t *bytes)
 {
     if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
     bc_status st = orth_sizes(batch, rows, cols, steps, "matrices");
     if (st) return st;
-    *bytes = (int64_t)orth_need(batch, rows, cols, steps);
+    bc::OrthTable T{};
+    T.n = 1;
+    T.e[0] = {rows, cols, batch, 0};
+    *bytes = (int64_t)bc::orth_layout(T, steps);
     return ok();
 }
 
@@ -1262,31 +1257,29 @@ bc_status bc_orthogonalize(const void *d_g, int32_t in_dtype, int32_t batch, int
     if (!valid_dtype(in_dtype) || !valid_dtype(out_dtype)) return fail(BC_ERR_DTYPE, "unknown dtype");
     bc::NewtonSchulz it;
     if ((st = orth_iteration(*ns, it))) return st;
-    const size_t need = orth_need(batch, rows, cols, ns->steps);
+    bc::OrthTable T{};
+    T.n = 1;
+    T.e[0] = {rows, cols, batch, 0};
+    const size_t need = bc::orth_layout(T, ns->steps);
     if ((st = check_work(d_work, work_bytes, need))) return st;
     const size_t count = (size_t)batch * rows * cols, ib = count * esize_of(in_dtype), ob = count * esize_of(out_dtype);
     if (overlap(d_work, need, d_g, ib) || overlap(d_work, need, d_out, ob) ||
         (overlap(d_g, ib, d_out, ob) && !(d_g == d_out && in_dtype == out_dtype)))
         return fail(BC_ERR_ALIAS, "the workspace, d_g and d_out overlap");
-    bc::OrthTable T{};
-    T.n = 1;
     T.work = (uint8_t *)d_work;
     T.g = d_g;
     T.out = d_out;
-    T.e[0] = {rows, cols, batch, 0};
     hipError_t e = bc::launch_orth(T, bc::OrthStep{}, false, in_dtype, out_dtype, it, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "orthogonalisation launch");
     return ok();
 }
 
-// Sizes of a step's matrices; *need: its workspace.
-static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, size_t *need)
+// Sizes of a step's matrices and their places in the workspace; *need: its bytes.
+static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, bc::OrthTable &T, size_t *need)
 {
     if (!params) return fail(BC_ERR_NULL, "params is required");
     if (n < 1 || n > bc::kMaxParams) return fail(BC_ERR_SHAPE, "n outside 1..%d", bc::kMaxParams);
-    *need = 0;
     double tiles = 0;
-    bc::OrthTable T{};
     T.n = n;
     for (int t = 0; t < n; ++t) {
         char name[32];
@@ -1294,11 +1287,10 @@ static bc_status muon_sizes(const bc_matrix *params, int32_t n, int32_t steps, s
         bc_status st = orth_sizes(1, params[t].rows, params[t].cols, steps, name);
         if (st) return st;
         T.e[t] = {params[t].rows, params[t].cols, 1, 0};
-        *need += bc::orth_work(params[t].rows, params[t].cols);
         tiles += bc::orth_tiles(params[t].rows, params[t].cols);
     }
     if (tiles >= (double)(1 << 24)) return fail(BC_ERR_SHAPE, "2^24 or more tiles of 64 x 64");
-    *need += bc::orth_shared_work(T, steps);
+    *need = bc::orth_layout(T, steps);
     return BC_OK;
 }
 
@@ -1306,7 +1298,8 @@ bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t ste
 {
     if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
     size_t need = 0;
-    bc_status st = muon_sizes(params, n, steps, &need);
+    bc::OrthTable T{};
+    bc_status st = muon_sizes(params, n, steps, T, &need);
     if (st) return st;
     *bytes = (int64_t)need;
     return ok();
@@ -1317,7 +1310,8 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
 {
     if (!params || !muon) return fail(BC_ERR_NULL, "params and muon are required");
     size_t need = 0;
-    bc_status st = muon_sizes(params, n, muon->ns.steps, &need);
+    bc::OrthTable T{};
+    bc_status st = muon_sizes(params, n, muon->ns.steps, T, &need);
     if (st) return st;
     if (!std::isfinite(muon->lr) || !std::isfinite(muon->momentum) || !std::isfinite(muon->weight_decay))
         return fail(BC_ERR_SHAPE, "lr, momentum and weight_decay must be finite");
@@ -1325,12 +1319,9 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
     bc::NewtonSchulz it;
     if ((st = orth_iteration(muon->ns, it))) return st;
     if ((st = check_work(d_work, work_bytes, need))) return st;
-    bc::OrthTable T{};
-    T.n = n;
     T.work = (uint8_t *)d_work;
     std::vector<Extent> all = {{d_work, need}};
     bool any16 = false;
-    size_t off = 0;
     for (int t = 0; t < n; ++t) {
         const bc_matrix &p = params[t];
         if (!p.w || !p.momentum || !p.grad) return fail(BC_ERR_NULL, "params[%d]: w, momentum and grad are required", t);
@@ -1338,9 +1329,7 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
         for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all.push_back({q, count * 4});
         if (p.w16) all.push_back({p.w16, count * 2});
         any16 = any16 || p.w16;
-        T.e[t] = {p.rows, p.cols, 1, (uint32_t)(off / 256)};
         T.p[t] = {p.w, p.momentum, p.grad, (uint16_t *)p.w16};
-        off += bc::orth_work(p.rows, p.cols);
     }
     if (any16 && dtype != BC_BF16 && dtype != BC_F16) return fail(BC_ERR_DTYPE, "the copies must be bf16 or f16");
     if (any_overlap(all)) return fail(BC_ERR_ALIAS, "the optimiser's buffers overlap");

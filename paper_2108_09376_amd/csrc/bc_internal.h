@@ -188,8 +188,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
                             const NormGeom &g, int fmt, hipStream_t s);
 
 // Orthogonalised updates (k_orth.hip). A shape with its matrices: one of an optimiser's
-// step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the workspace
-// (after the shared part), orth_work(rows, cols) bytes for each matrix.
+// step, or a batch of equal ones; `off` (units of 256 bytes) is its part of the workspace.
 struct OrthShape {
     int rows, cols, batch;
     uint32_t off;
@@ -201,6 +200,7 @@ struct OrthParam {
 struct OrthTable {
     int n;
     uint8_t *work;
+    size_t parts;                              // byte of the workspace where the matrices' parts begin
     const void *g;                             // bc_orthogonalize: [batch][rows][cols]
     void *out;
     OrthShape e[kMaxParams];
@@ -226,8 +226,7 @@ struct NewtonSchulz {
     int steps;
     float a, b, c, eps;
 };
-size_t orth_work(int rows, int cols);         // bytes of a matrix's part
-size_t orth_shared_work(const OrthTable &T, int steps);
+size_t orth_layout(OrthTable &T, int steps);   // sets T.parts and each off; bytes of the workspace
 unsigned orth_tiles(int rows, int cols);       // workgroups of the largest launch, per matrix
 bool orth_supported(const NewtonSchulz &ns, const char **why);
 hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,

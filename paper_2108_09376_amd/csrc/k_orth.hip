@@ -14,7 +14,7 @@
 // 3 n/m + 7, in spans of one (products on X in every step) 7.5 n/m + 2.5. Directions of X
 // that are small beside the largest lose digits in A as the square of their size, and a
 // step multiplies such an error by up to a^2, so a new A is taken from X after three steps,
-// and after two once the small directions have grown (spans_of has the figures).
+// and after two once the small directions have grown (steps_direct and plans_of have the figures).
 //
 // Arithmetic: an fp32 value x is held as two fp16 numbers, hi = half(x), lo = half(x - hi),
 // about 22 bits, all scaled by 2^12, and a product is hi hi + hi lo + lo hi on the matrix
@@ -103,6 +103,40 @@ __device__ __forceinline__ size_t blocked(int r, int c, int ld)
 // 512 x 512 6.8e-7 / 1.5e-6 / 2.0e-6: small matrices take the steps one by one.
 __host__ __device__ inline bool steps_direct(int rows, int cols) { return (rows < cols ? rows : cols) <= 128; }
 
+// Small matrices: M x C of X in LDS, hi and lo. kR x kC fragments of 16 x 16 of X per wave,
+// kWR x kWC waves; kAR x kAC fragments of A.
+template <int M_, int C_>
+struct Fused {
+    static constexpr int M = M_, C = C_;
+    static constexpr int kThreads = 512, kWaves = 8;
+    static constexpr int kB = M / kBlock, kCB = C / kBlock;
+    static constexpr int kWC = M == 128 ? 2 : C == 512 ? 8 : 4, kWR = kWaves / kWC;
+    static constexpr int kR = M / 16 / kWR, kC = C / 16 / kWC;
+    static constexpr int kAR = M == 128 ? 2 : 1, kAC = M == 128 ? 4 : 2;
+    static constexpr int kX = M * C * 4, kSquare = M * M * 4;
+    static constexpr int kLds = kX + kSquare * (M == 128 ? 1 : 2);
+    static_assert(kLds <= 160 * 1024, "one workgroup per CU");
+};
+
+// Whether a matrix fits one of the forms.
+__host__ __device__ inline bool fits(const OrthShape &e, int m, int c)
+{
+    return (e.rows < e.cols ? e.rows : e.cols) <= m && (e.rows < e.cols ? e.cols : e.rows) <= c;
+}
+
+// v as hi + lo, to 22 bits. The compiler must see one v: an instruction that rounds a product
+// or a sum to 16 bits at once would make a hi that differs, now and then, from v rounded twice,
+// and lo would then miss by an ulp of hi.
+struct Halves {
+    _Float16 hi, lo;
+};
+__device__ __forceinline__ Halves halves_of(float v)
+{
+    asm("" : "+v"(v));
+    const _Float16 hi = (_Float16)v;
+    return {hi, (_Float16)(v - (float)hi)};
+}
+
 // The same value in every lane, told to the compiler.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
@@ -163,10 +197,33 @@ __device__ __forceinline__ uint8_t *slot_base(const Matrices<MANY> &M, const Whe
 
 // ---------------------------------------------------------------- the start: momentum, norm, X_0
 
-// u of the momentum form: nesterov ? grad + mu m : m, m the new momentum
+// Several kernels compute these, and what a matrix becomes does not depend on which: fused
+// operations are written as such, here and in the products' last steps.
+//
+// mom <- mu mom + grad, and u of the momentum form: nesterov ? grad + mu mom : mom.
+__device__ __forceinline__ float moved(const OrthStep &h, float grad, float mom) { return __builtin_fmaf(h.momentum, mom, grad); }
 __device__ __forceinline__ float look_ahead(const OrthStep &h, float grad, float mom)
 {
-    return h.nesterov ? grad + h.momentum * mom : mom;
+    return h.nesterov ? __builtin_fmaf(h.momentum, mom, grad) : mom;
+}
+
+// The start's factor kScale / (norm + eps) as f 2^x: in 32 bits no step leaves their range.
+struct Factor {
+    float f;
+    int x;
+};
+__device__ __forceinline__ Factor factor_of(double squares, double eps)
+{
+    Factor r;
+    r.f = (float)frexp((double)kScale / (sqrt(squares) + eps), &r.x);
+    return r;
+}
+__device__ __forceinline__ float scaled(float u, const Factor &by) { return ldexpf(u, by.x) * by.f; }
+
+// The element behind a step: decay and update.
+__device__ __forceinline__ float stepped(const OrthStep &h, float rate, float was, float x)
+{
+    return __builtin_fmaf(-rate, x, h.keep * was);
 }
 
 // Elements i .. i + 3 of p as fp32 (those below n; p is not read past it).
@@ -230,7 +287,6 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHe
         for (int i = threadIdx.x; i < kMostSplit; i += kThreads) head->count[i] = 0u;
     const Where w = find(M, blockIdx.x, per);
     const OrthShape &e = w.e;
-    const Slot s = slot_of(e.rows, e.cols);
     const size_t count = (size_t)e.rows * e.cols, parts = sum_parts(count), each = ((count + parts - 1) / parts + 3) / 4 * 4;
     const size_t lo = w.local * each, hi = lo + each < count ? lo + each : count;
     double sum = 0.0;
@@ -244,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHe
             load4<kF32>(p.mom, i, hi, m);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                m[j] = h.momentum * m[j] + g[j];
+                m[j] = moved(h, g[j], m[j]);
                 u[j] = look_ahead(h, g[j], m[j]);
             }
             store4(p.mom, i, hi, m);
@@ -257,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHe
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) ((double *)slot_base(M, w, s))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    if (threadIdx.x == 0) ((double *)slot_base(M, w, slot_of(e.rows, e.cols)))[w.local] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
 // Elements i .. i + 3 (those below n) rounded to a 16-bit format, or as they are.
@@ -324,13 +380,13 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
-    const double inv = (double)kScale / (sqrt((lds[0] + lds[1]) + (lds[2] + lds[3])) + eps);
+    const Factor by = factor_of((lds[0] + lds[1]) + (lds[2] + lds[3]), eps);
 #pragma unroll
     for (int k = 0; k < kTurns; ++k) {
         const int q = k * kThreads + threadIdx.x, r = q / (kTile / 4), c = q % (kTile / 4) * 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float v = (float)(u[k][j] * inv);
+            const float v = scaled(u[k][j], by);
             if (s.flip) tile[c + j][r] = v;
             else tile[r][c + j] = v;
         }
@@ -343,8 +399,9 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float v = tile[r][c + j];
-            hi[j] = (_Float16)v;
-            lo[j] = (_Float16)(v - (float)hi[j]);
+            const Halves part = halves_of(v);
+            hi[j] = part.hi;
+            lo[j] = part.lo;
         }
         uint8_t *to = x + blocked(ti * kTile + r, tj * kTile + c, s.n);
         *(f16x8 *)to = hi;
@@ -681,7 +738,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
                 const uint8_t *at = mine(i, j, which);
                 const f16x4 hi = *(const f16x4 *)at, lo = *(const f16x4 *)(at + kBlockPlane);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tot[i][j][q] += by * ((float)hi[q] + (float)lo[q]);
+                for (int q = 0; q < 4; ++q) tot[i][j][q] = __builtin_fmaf(by, (float)hi[q] + (float)lo[q], tot[i][j][q]);
             }
     };
 #pragma unroll
@@ -696,8 +753,9 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
                 f16x4 hi, lo;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    hi[q] = (_Float16)tot[i][j][q];
-                    lo[q] = (_Float16)(tot[i][j][q] - (float)hi[q]);
+                    const Halves part = halves_of(tot[i][j][q]);
+                    hi[q] = part.hi;
+                    lo[q] = part.lo;
                 }
                 uint8_t *at = mine(i, j, 0);
                 *(f16x4 *)at = hi;
@@ -768,13 +826,345 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
             float was[4];
             load4<kF32>(p.w, o, end, was);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = h.keep * was[j] - rate * v[j];
+            for (int j = 0; j < 4; ++j) v[j] = stepped(h, rate, was[j], v[j]);
             store4(p.w, o, end, v);
             if (p.w16) store4_as(S.fmt, p.w16, o, end, v);
         } else {
             store4_as(S.fmt, (uint8_t *)M.out + (size_t)w.img * e.rows * e.cols * (S.fmt == kF32 ? 4 : 2), o, end, v);
         }
     }
+}
+
+// ---------------------------------------------------------------- small matrices, in one launch
+//
+// The products of small matrices are shorter than the launches for them. Here a workgroup of
+// eight waves keeps 64 or 128 rows of X in LDS, with A and B beside it, and runs a matrix from
+// G to the result in one launch.
+//
+// X' = a (X + B X), B = (b/a) A + (c/a) A^2, as the products above in spans of one step, and
+// with their sums, order and roundings: the same bits. (Products this short are never split
+// over K.) The workgroup's latency bounds it: of a step of 64 x 64 (6500 cycles) the matrix
+// instructions take some 1500, the rest is fragments on their way from LDS, the split into
+// halves, and four barriers.
+struct FusedStage {
+    float a, b, c;                             // a, b / a, c / a
+    double eps;
+    int steps, fmt;
+};
+
+// acc += product t of the three of halves, l r^T of one block of K: lo hi, hi lo, hi hi. The
+// mirror image of a fragment has the first two the other way round.
+__device__ __forceinline__ void multiply(f32x4 &acc, const f16x8 (&l)[2], const f16x8 (&r)[2], int t)
+{
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[t == 1], l[t == 0], acc, 0, 0, 0);
+}
+__device__ __forceinline__ int mirrored(int t) { return t == 2 ? 2 : 1 - t; }
+
+template <typename F, bool MANY, int FMT>
+__global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, FusedStage S, OrthStep h, uint32_t per)
+{
+    constexpr int M = F::M, kR = F::kR, kC = F::kC, kAR = F::kAR, kAC = F::kAC;
+    extern __shared__ __align__(16) uint8_t smem[];
+    // X, A, and B: in A's place with 128 rows
+    uint8_t *const X = smem, *const A = smem + F::kX, *const B = M == 128 ? A : A + F::kSquare;
+    const Where w = find(Ms, blockIdx.x, per);
+    const OrthShape &e = w.e;
+    const bool flip = e.rows > e.cols;
+    const int m = flip ? e.cols : e.rows, n = flip ? e.rows : e.cols;      // of X, not padded
+    const int cols = (n + kBlock - 1) / kBlock * kBlock;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const size_t count = (size_t)e.rows * e.cols;
+    const int frag = in_block(lane & 15, (lane >> 4) * 8);
+    const int rr = lane & 15, cc = (lane >> 4) * 4;        // a lane's place in a fragment of sums
+    // 16 rows of a block (half hf) as they lie, 16 columns of a block transposed
+    auto rows_of = [&](const uint8_t *b, int p, int hf) { return *(const f16x8 *)(b + p * kBlockPlane + hf * 1024 + frag); };
+    auto columns_of = [&](const uint8_t *b, int p, int hf) {
+        return read_tr(b + p * kBlockPlane + transposed(lane, hf, 0), b + p * kBlockPlane + transposed(lane, hf, 1));
+    };
+    // fragment (i, j) of a matrix of ld blocks per row
+    auto place = [&](uint8_t *at, int i, int j, int ld) {
+        return at + ((i >> 1) * ld + (j >> 1)) * kBlockBytes + in_block((i & 1) * 16 + rr, (j & 1) * 16 + cc);
+    };
+    // four values of a row to hi and lo, and what these hold
+    auto put = [](uint8_t *at, f32x4 &v) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const Halves part = halves_of(v[q]);
+            hi[q] = part.hi;
+            lo[q] = part.lo;
+        }
+        *(f16x4 *)at = hi;
+        *(f16x4 *)(at + kBlockPlane) = lo;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)hi[q] + (float)lo[q];
+    };
+    auto take = [](const uint8_t *at) {
+        const f16x4 hi = *(const f16x4 *)at, lo = *(const f16x4 *)(at + kBlockPlane);
+        f32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)hi[q] + (float)lo[q];
+        return v;
+    };
+
+    // X to LDS: eight columns of a row of a block per thread and turn
+    constexpr int kTurns = M * F::C / 8 / F::kThreads;
+    static_assert(kTurns >= 1 && F::kThreads == 512, "four blocks a turn");
+    {
+        float u[kTurns][8];
+        int at[kTurns];
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int blk = t * 4 + wave / 2, bi = blk / F::kCB, bj = blk % F::kCB, k = tid & 127;
+            // neighbours along a row of G
+            const int r = flip ? k & 31 : k >> 2, c = (flip ? k >> 5 : k & 3) * 8;
+            at[t] = bj * kBlock < cols ? (bi * F::kCB + bj) * kBlockBytes + in_block(r, c) : -1;
+            const int xr = bi * kBlock + r, xc = bj * kBlock + c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[t][j] = 0.f;
+            if (xr >= m || xc >= n) continue;
+            if (flip) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (xc + j >= n) continue;
+                    const size_t i = (size_t)(xc + j) * e.cols + xr;
+                    if constexpr (MANY) {
+                        const OrthParam &p = Ms.p[w.t];
+                        const float g = p.grad[i], mom = moved(h, g, p.mom[i]);
+                        u[t][j] = look_ahead(h, g, mom);
+                        p.mom[i] = mom;
+                        p.grad[i] = 0.f;
+                    } else {
+                        u[t][j] = get(load_raw<FMT, 1>(Ms.g, w.img * count + i), 0);
+                    }
+                }
+                continue;
+            }
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const size_t i = (size_t)xr * e.cols + xc + v * 4, end = (size_t)(xr + 1) * e.cols;
+                if (i >= end) continue;
+                float g[4];
+                if constexpr (MANY) {
+                    const OrthParam &p = Ms.p[w.t];
+                    float mom[4], zero[4] = {0.f, 0.f, 0.f, 0.f};
+                    load4<kF32>(p.grad, i, end, g);
+                    load4<kF32>(p.mom, i, end, mom);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        mom[j] = moved(h, g[j], mom[j]);
+                        g[j] = look_ahead(h, g[j], mom[j]);
+                    }
+                    store4(p.mom, i, end, mom);
+                    store4(p.grad, i, end, zero);
+                } else {
+                    load4<FMT>((const uint8_t *)Ms.g + w.img * count * kElem<FMT>, i, end, g);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[t][v * 4 + j] = g[j];
+            }
+        }
+        double *const sums = (double *)A;
+        double sum = 0.0;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += (double)u[t][j] * u[t][j];
+        sum = wave_sum(sum);
+        if (lane == 0) sums[wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+        for (int i = 0; i < F::kWaves; ++i) sum += sums[i];
+        const Factor by = factor_of(sum, S.eps);
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            f16x8 hi, lo;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = scaled(u[t][j], by);
+                const Halves part = halves_of(v);
+                hi[j] = part.hi;
+                lo[j] = part.lo;
+            }
+            if (at[t] < 0) continue;
+            *(f16x8 *)(X + at[t]) = hi;
+            *(f16x8 *)(X + at[t] + kBlockPlane) = lo;
+        }
+    }
+    __syncthreads();
+
+    // The wave's part of X, as it lies in LDS: both terms of X + B X have the same X.
+    const int x_i = wave / F::kWC * kR, x_j = wave % F::kWC * kC;
+    f32x4 x[kR][kC];
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int j = 0; j < kC; ++j)
+            x[i][j] = (x_j + j) * 16 < cols ? take(place(X, x_i + i, x_j + j, F::kCB)) : f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // Sums of S S^T over `blocks` of K for the wave's part of A, the upper half standing for both:
+    // below the diagonal the products come in the order that makes them its mirror image, and
+    // fragments on the diagonal in either.
+    const int a_i = M == 128 ? wave / 2 * 2 : wave / 2, a_j = M == 128 ? wave % 2 * 4 : wave % 2 * 2;
+    auto square = [&](const uint8_t *from, int ld, int blocks, f32x4 (&tot)[kAR][kAC]) {
+#pragma unroll
+        for (int i = 0; i < kAR * kAC; ++i) tot[i / kAC][i % kAC] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k0 = 0; k0 < blocks; k0 += kFold) {
+            f32x4 acc[kAR][kAC], other[kAR];               // other: fragment (i, i) in the other order
+#pragma unroll
+            for (int i = 0; i < kAR * kAC; ++i) acc[i / kAC][i % kAC] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kAR; ++i) other[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int k = k0; k < min(k0 + kFold, blocks); ++k) {
+                f16x8 l[kAR][2], r[kAC][2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+#pragma unroll
+                    for (int i = 0; i < kAR; ++i) l[i][p] = rows_of(from + (((a_i + i) >> 1) * ld + k) * kBlockBytes, p, (a_i + i) & 1);
+#pragma unroll
+                    for (int j = 0; j < kAC; ++j) r[j][p] = rows_of(from + (((a_j + j) >> 1) * ld + k) * kBlockBytes, p, j & 1);
+                }
+#pragma unroll
+                for (int j0 = 0; j0 < kAC; j0 += 2) {      // a block of 32 columns, one branch for it
+                    // below(i, j): fragments below the diagonal; diagonal(i): a row's fragment on it
+                    auto block = [&](auto below, auto diagonal) {
+#pragma unroll
+                        for (int t = 0; t < 3; ++t)
+#pragma unroll
+                            for (int i = 0; i < kAR; ++i) {
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+                                    multiply(acc[i][j0 + j], l[i], r[j0 + j], below(i, j) ? mirrored(t) : t);
+                                if (diagonal(i) >= 0) multiply(other[i], l[i], r[j0 + diagonal(i)], mirrored(t));
+                            }
+                    };
+                    const int d = (a_i >> 1) - ((a_j + j0) >> 1);
+                    constexpr auto none = [](int) { return -1; };
+                    if (d < 0) block([](int, int) { return false; }, none);
+                    else if (d > 0) block([](int, int) { return true; }, none);
+                    else if (kAR == 2) block([](int i, int j) { return i > j; }, [](int i) { return i; });
+                    else if (a_i & 1) block([](int, int j) { return j == 0; }, [](int) { return 1; });
+                    else block([](int, int) { return false; }, [](int) { return 0; });
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAR; ++i)
+#pragma unroll
+                for (int j = 0; j < kAC; ++j) {
+                    if (a_i + i == a_j + j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[i][j][q] = rr > cc + q ? other[i][q] : acc[i][j][q];
+                    tot[i][j] += acc[i][j];
+                }
+        }
+    };
+    f32x4 sq[kAR][kAC];
+    auto gram = [&] {
+        square(X, F::kCB, cols / kBlock, sq);
+#pragma unroll
+        for (int i = 0; i < kAR * kAC; ++i) sq[i / kAC][i % kAC] *= 1.f / kScale;
+    };
+
+    gram();
+    for (int step = 0; step < S.steps; ++step) {
+#pragma unroll
+        for (int i = 0; i < kAR; ++i)
+#pragma unroll
+            for (int j = 0; j < kAC; ++j) put(place(A, a_i + i, a_j + j, F::kB), sq[i][j]);
+        __syncthreads();
+        // B = (b/a) A + (c/a) A^2
+        f32x4 b[kAR][kAC];
+        square(A, F::kB, F::kB, b);
+        if constexpr (M == 128) __syncthreads();           // B replaces A
+#pragma unroll
+        for (int i = 0; i < kAR; ++i)
+#pragma unroll
+            for (int j = 0; j < kAC; ++j) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) b[i][j][q] = __builtin_fmaf(S.b, sq[i][j][q], b[i][j][q] * (S.c * (1.f / kScale)));
+                put(place(B, a_i + i, a_j + j, F::kB), b[i][j]);
+            }
+        __syncthreads();
+        // X' = a (X + B X)
+        constexpr int kJ = kR * kC > 8 ? 2 : kC;           // at once: registers for the sums
+#pragma unroll
+        for (int j0 = 0; j0 < kC; j0 += kJ) {
+            if ((x_j + j0) * 16 >= cols) continue;
+            f32x4 acc[kR][kJ];
+#pragma unroll
+            for (int i = 0; i < kR * kJ; ++i) acc[i / kJ][i % kJ] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int k = 0; k < F::kB; ++k) {
+                f16x8 l[kR][2], r[kJ][2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+#pragma unroll
+                    for (int i = 0; i < kR; ++i) l[i][p] = rows_of(B + (((x_i + i) >> 1) * F::kB + k) * kBlockBytes, p, (x_i + i) & 1);
+#pragma unroll
+                    for (int j = 0; j < kJ; ++j) r[j][p] = columns_of(X + (k * F::kCB + ((x_j + j0 + j) >> 1)) * kBlockBytes, p, j & 1);
+                }
+#pragma unroll
+                for (int t = 0; t < 3; ++t)
+#pragma unroll
+                    for (int i = 0; i < kR; ++i)
+#pragma unroll
+                        for (int j = 0; j < kJ; ++j) multiply(acc[i][j], l[i], r[j], t);
+            }
+#pragma unroll
+            for (int i = 0; i < kR; ++i)
+#pragma unroll
+                for (int j = 0; j < kJ; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        x[i][j0 + j][q] = __builtin_fmaf(S.a, x[i][j0 + j][q], acc[i][j][q] * (S.a * (1.f / kScale)));
+        }
+        if (step + 1 == S.steps) break;
+        if constexpr (F::kWR > 1) __syncthreads();         // other waves read these columns too
+#pragma unroll
+        for (int i = 0; i < kR; ++i)
+#pragma unroll
+            for (int j = 0; j < kC; ++j)
+                if ((x_j + j) * 16 < cols) put(place(X, x_i + i, x_j + j, F::kCB), x[i][j]);
+        __syncthreads();
+        gram();
+    }
+    const float tall = e.rows > e.cols ? (float)e.rows / (float)e.cols : 1.f;
+    const float rate = h.lr * sqrtf(tall);
+    auto write = [&](size_t i, size_t end, float (&v)[4]) {      // elements i .. i + 3 below end
+        if constexpr (MANY) {
+            const OrthParam &p = Ms.p[w.t];
+            float was[4];
+            load4<kF32>(p.w, i, end, was);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = stepped(h, rate, was[q], v[q]);
+            store4(p.w, i, end, v);
+            if (p.w16) store4_as(S.fmt, p.w16, i, end, v);
+        } else {
+            store4_as(S.fmt, (uint8_t *)Ms.out + w.img * count * (S.fmt == kF32 ? 4 : 2), i, end, v);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int j = 0; j < kC; ++j) {
+            const int r = (x_i + i) * 16 + rr, c = (x_j + j) * 16 + cc;
+            if (r >= m || c >= n) continue;
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = x[i][j][q] * (1.f / kScale);
+            if (!flip) {
+                write((size_t)r * e.cols + c, (size_t)(r + 1) * e.cols, v);
+                continue;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (c + q < n) {
+                    float one[4] = {v[q], 0.f, 0.f, 0.f};
+                    const size_t to = (size_t)(c + q) * e.cols + r;
+                    write(to, to + 1, one);
+                }
+        }
 }
 
 // ---------------------------------------------------------------- host: what is launched when
@@ -838,7 +1228,8 @@ unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
 }
 
 // Tiles of 128 x 64 read three quarters of the bytes of 64 x 64 ones per product, where they
-// are enough for the chip.
+// are enough for the chip (2048 x 2048 837 us with the small ones, 746 with the large; with
+// 128 x 128, one workgroup per CU, 1173). 1500 x 1700, 156 large tiles: 415 and 414.
 constexpr uint64_t kEnough = 192;
 
 // The products of one launch: the plans of its matrices (those taken in spans, those taken step
@@ -870,13 +1261,16 @@ std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
             return n;
         };
         auto chunks = [](const OrthPlan &p, const OrthShape &e) { return (uint64_t)chunks_of(p, slot_of(e.rows, e.cols)); };
-        const uint64_t large = total([](const OrthPlan &p, const OrthShape &e) { return products_of<4, 2>(p, e, 0); });
-        l.large = large >= kEnough;
-        auto tiles = [&](const OrthPlan &p, const OrthShape &e, int each) {
-            return l.large ? products_of<4, 2>(p, e, each) : products_of<2, 2>(p, e, each);
+        auto tiles = [&](bool large, int each) {
+            return total([&](const OrthPlan &p, const OrthShape &e) {
+                return large ? products_of<4, 2>(p, e, each) : products_of<2, 2>(p, e, each);
+            });
         };
-        const uint64_t wgs = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, 0); });
-        const uint64_t work = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, 0) * chunks(p, e); });
+        l.large = tiles(true, 0) >= kEnough;
+        const uint64_t wgs = tiles(l.large, 0);
+        const uint64_t work = total([&](const OrthPlan &p, const OrthShape &e) {
+            return (l.large ? products_of<4, 2>(p, e, 0) : products_of<2, 2>(p, e, 0)) * chunks(p, e);
+        });
         uint64_t longest = 0;
         for (int t = 0; t < T.n; ++t) {
             const OrthPlan &p = l.plan[steps_direct(T.e[t].rows, T.e[t].cols)];
@@ -886,7 +1280,7 @@ std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
         // share of the work (twice as long: 1024 x 2048 254 us whole, 265 in ranges)
         const uint64_t share = std::max<uint64_t>(kLeastChunks, ((work + 511) / 512 + kFold - 1) / kFold * kFold);
         l.each = longest >= 3 * share && wgs <= 512 ? (int)share : 0;
-        const uint64_t places = total([&](const OrthPlan &p, const OrthShape &e) { return tiles(p, e, l.each); });
+        const uint64_t places = tiles(l.large, l.each);
         l.part_bytes = l.each ? places * kThreads * sizeof(f32x4) * (l.large ? 8 : 4) : 0;
     }
     return all;
@@ -924,15 +1318,54 @@ hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head
     return hipSuccess;
 }
 
+// Whether all matrices are small. With larger ones beside them their products share the
+// larger ones' launches and cost nothing. By themselves, us in the launches of products and
+// here: 64 x 64 69 and 17, 64 x 147 75 and 27, 64 x 512 79 and 51, 128 x 128 70 and 53,
+// 256 of 64 x 64 164 and 18. (In a launch per step with chunks of 256 columns 64 x 2048 took
+// 64 for 91, but not to the same bits.)
+bool all_fused(const OrthTable &T)
+{
+    for (int t = 0; t < T.n; ++t)
+        if (!fits(T.e[t], 64, 512) && !fits(T.e[t], 128, 128)) return false;
+    return true;
+}
+
+template <typename F, bool MANY, int FMT>
+hipError_t launch_fused(const OrthTable &T, Matrices<MANY> &Ms, const OrthStep &h, int out_fmt, const NewtonSchulz &ns,
+                        hipStream_t s)
+{
+    const hipError_t e = allow_lds((const void *)k_orth_fused<F, MANY, FMT>, F::kLds);
+    if (e != hipSuccess) return e;
+    uint32_t per = 0;
+    const unsigned grid = number(Ms, T, &per, [&](const OrthShape &e) {
+        // the smallest form that fits
+        const bool is = fits(e, 64, 128)   ? F::M == 64 && F::C == 128
+                        : fits(e, 64, 256) ? F::C == 256
+                        : fits(e, 64, 512) ? F::C == 512
+                                           : F::M == 128;
+        return (uint32_t)is;
+    });
+    if (!grid) return hipSuccess;
+    const FusedStage S = {ns.a, ns.b / ns.a, ns.c / ns.a, (double)ns.eps, ns.steps, out_fmt};
+    hipLaunchKernelGGL((k_orth_fused<F, MANY, FMT>), dim3(grid), dim3(F::kThreads), (unsigned)F::kLds, s, Ms, S, h, per);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t orth_work(int rows, int cols) { return slot_bytes(slot_of(rows, cols)); }
-
-size_t orth_shared_work(const OrthTable &T, int steps)
+size_t orth_layout(OrthTable &T, int steps)
 {
-    size_t part = 0;
-    for (const Launch &l : launches_of(T, NewtonSchulz{steps, 1.f, 1.f, 1.f, 0.f})) part = std::max(part, l.part_bytes);
-    return sizeof(OrthHead) + part;
+    const bool fused = all_fused(T);
+    size_t at = sizeof(OrthHead), part = 0;
+    if (!fused)
+        for (const Launch &l : launches_of(T, NewtonSchulz{steps, 1.f, 1.f, 1.f, 0.f})) part = std::max(part, l.part_bytes);
+    T.parts = at + part;                       // where the matrices' parts begin
+    at = 0;
+    for (int t = 0; t < T.n; ++t) {
+        T.e[t].off = (uint32_t)(at / 256);
+        if (!fused) at += slot_bytes(slot_of(T.e[t].rows, T.e[t].cols)) * T.e[t].batch;
+    }
+    return T.parts + at;
 }
 
 unsigned orth_tiles(int rows, int cols)
@@ -982,9 +1415,10 @@ template <bool MANY>
 static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int out_fmt, const NewtonSchulz &ns, hipStream_t s)
 {
     hipError_t e = hipSuccess;
+    const bool fused = all_fused(T);
     OrthHead *head = (OrthHead *)T.work;
     Matrices<MANY> M{};
-    M.work = T.work + orth_shared_work(T, ns.steps);
+    M.work = T.work + T.parts;
     M.g = T.g;
     M.out = T.out;
     for (int t = 0; t < T.n; ++t) {
@@ -994,15 +1428,23 @@ static hipError_t launch(const OrthTable &T, const OrthStep &h, int in_fmt, int 
     with_format(in_fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if constexpr (!MANY || FMT == kF32) {                 // gradients and momentum are fp32
+            if (fused) {
+                e = launch_fused<Fused<64, 128>, MANY, FMT>(T, M, h, out_fmt, ns, s);
+                if (e == hipSuccess) e = launch_fused<Fused<64, 256>, MANY, FMT>(T, M, h, out_fmt, ns, s);
+                if (e == hipSuccess) e = launch_fused<Fused<64, 512>, MANY, FMT>(T, M, h, out_fmt, ns, s);
+                if (e == hipSuccess) e = launch_fused<Fused<128, 128>, MANY, FMT>(T, M, h, out_fmt, ns, s);
+                return;
+            }
             uint32_t per = 0;
             unsigned grid = number(M, T, &per, [](const OrthShape &e) { return (uint32_t)sum_parts((size_t)e.rows * e.cols); });
             hipLaunchKernelGGL((k_orth_sums<MANY, FMT>), dim3(grid), dim3(kThreads), 0, s, M, head, h, per);
             if ((e = hipGetLastError()) != hipSuccess) return;
             grid = number(M, T, &per, start_tiles);
             hipLaunchKernelGGL((k_orth_start<MANY, FMT>), dim3(grid), dim3(kThreads), 0, s, M, h, (double)ns.eps, per);
+            e = hipGetLastError();
         }
     });
-    if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
+    if (e != hipSuccess || fused) return e;
     return launch_products<MANY>(T, M, head, h, out_fmt, ns, s);
 }
 

@@ -206,6 +206,29 @@ def test_step_equals_its_parts(bc):
         assert ((w + rate * o).abs() <= 2.0 ** -22 * rate * o.abs()).all()
 
 
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_small_matrices_alone_and_among_large(bc, nesterov):
+    """Small matrices take one launch by themselves and the products' launches beside larger ones:
+    the same result either way, to the bit."""
+    shapes = [(1, 1), (5, 3), (64, 64), (64, 147), (147, 64), (30, 129), (64, 512), (500, 33), (128, 128), (65, 128), (128, 97)]
+    def make():
+        return [(gradient(i + 50, *s).cuda(), gradient(i + 20, *s).cuda(), gradient(i, *s, "noise").cuda(),
+                 torch.empty(s, dtype=torch.bfloat16, device="cuda")) for i, s in enumerate(shapes)]
+    large = lambda: [(torch.zeros(300, 400, device="cuda"), torch.zeros(300, 400, device="cuda"), gradient(9, 300, 400).cuda(), None)]
+    among, together, alone = make(), make(), make()
+    for _ in range(2):                                     # two steps: the momentum as well
+        bc.bc_muon_step_many(among + large(), 0.1, 0.9, 0.01, nesterov=nesterov)
+        bc.bc_muon_step_many(together, 0.1, 0.9, 0.01, nesterov=nesterov)
+        for p in alone:
+            bc.bc_muon_step_many([p], 0.1, 0.9, 0.01, nesterov=nesterov)
+        for p, q, r, s in zip(among, together, alone, shapes):
+            for x, y, z in zip(p, q, r):
+                assert torch.equal(x, y) and torch.equal(x, z), s
+            for x in (p, q, r):
+                assert not x[2].any()                      # the gradient has been taken
+                x[2].copy_(gradient(77, *s))
+
+
 def test_streams_and_graph(bc):
     """On a stream of its own, and captured: replays equal eager calls on new gradients."""
     shapes = [(64, 576), (300, 200)]
