@@ -207,12 +207,22 @@ class PolicyNet:
     """The policy network's forward pass on the device (Section 3.3, Eq. 2): S_t
     assembled by bc_policy_input, the convolutions on the dense path (every block; each
     layer on a grid of at most 8x8-pixel blocks), P_t by bc_policy_probabilities.
-    h, w: frame size; block: block edge in frame pixels (the head ends on that grid)."""
+    h, w: frame size; block: block edge in frame pixels (the head ends on that grid).
+    norm: None, or "layer": every convolution but the last is followed by layer
+    normalisation over its channels (the biases become its offsets; gains start at 1), and
+    the online update moves those convolutions' weight matrices by orthogonalised momentum
+    (bc_muon_step_many), the rest by RMSprop. The network learns from one frame at a time,
+    where batch statistics are not to be had and the few rewards make the gradient's
+    directions very unequal."""
+
+    NORM_EPS = 1e-5
 
     def __init__(self, h: int, w: int, block: int = 128, classes: int = 19, params=None,
-                 dtype=torch.bfloat16, device="cuda", seed0: int = 3000):
+                 dtype=torch.bfloat16, device="cuda", seed0: int = 3000, norm: str | None = None):
         if h % block or w % block or block != 128:
             raise ValueError("the head reduces the frame by 128: blocks of 128 pixels")
+        if norm not in (None, "layer"):
+            raise ValueError("norm is None or 'layer'")
         self.layers = build_policy_layers()
         self.classes, self.dtype, self.device = classes, dtype, torch.device(device)
         self.grid = (h // block, w // block)
@@ -224,6 +234,11 @@ class PolicyNet:
                         for (oh, ow, c) in self.shapes]
         self.grids = [(oh // min(8, oh), ow // min(8, ow)) for (oh, ow, _) in self.shapes]
         self.prob = torch.empty((1,) + self.grid, dtype=torch.float32, device=self.device)
+        self.norm = norm
+        # layers behind which the norm stands; their convolutions' outputs before it
+        self.normed = range(len(self.layers) - 1) if norm else range(0)
+        self.raw = [torch.empty_like(self.buffers[i]) for i in self.normed]
+        self.gains = [torch.ones_like(self.biases[i]) for i in self.normed]
 
     def macs(self) -> float:
         return float(sum(l.cin * l.cout * l.k * l.k * oh * ow
@@ -237,6 +252,12 @@ class PolicyNet:
         for i, l in enumerate(self.layers):
             src = self.input if l.src < 0 else self.buffers[l.src]
             res = None if l.res is None else self.buffers[l.res]
+            if i in self.normed:
+                bc.bc_sparse_conv2d((l.k, l.k, l.stride, l.pad, 0), src, bc.BC_NHWC, self.weights[i],
+                                    None, None, self.raw[i], self.grids[i], None, None, stream)
+                bc.bc_sparse_layer_norm(self.raw[i], bc.BC_NHWC, self.gains[i], self.biases[i], res,
+                                        self.NORM_EPS, l.relu, self.buffers[i], self.grids[i], None, None, stream)
+                continue
             bc.bc_sparse_conv2d((l.k, l.k, l.stride, l.pad, int(l.relu)), src, bc.BC_NHWC,
                                 self.weights[i], self.biases[i], res, self.buffers[i],
                                 self.grids[i], None, None, stream)
@@ -245,8 +266,9 @@ class PolicyNet:
 
     # ------------------------------------------------------------------ online update
     def _init_training(self):
-        """fp32 master weights ([cout][k][k][cin], the layout the convolutions read),
-        RMSprop state and gradient accumulators, and two gradient maps per layer."""
+        """fp32 master weights ([cout][k][k][cin], the layout the convolutions read), the
+        updates' state (RMSprop's, or the momentum of a matrix) and gradient accumulators, two
+        gradient maps per layer, and the workspaces."""
         dev, dt = self.device, self.dtype
         self.master, self.v_w, self.dw, self.v_b, self.db = [], [], [], [], []
         for wt in self.weights:
@@ -259,11 +281,20 @@ class PolicyNet:
             self.db.append(torch.zeros_like(b))
         self.gbufs = [[torch.empty((1, oh, ow, c), dtype=dt, device=dev) for _ in range(2)]
                       for (oh, ow, c) in self.shapes]
+        self.v_g = [torch.zeros_like(g) for g in self.gains]
+        self.dg = [torch.zeros_like(g) for g in self.gains]
+        if self.norm:
+            need = [bc.bc_layer_norm_grad_work(x, bc.BC_NHWC) for x in self.raw]
+            need.append(bc.bc_muon_step_many_work(self._matrices()))
+            self.work = torch.empty(max(need), dtype=torch.uint8, device=dev)
+
+    def _matrices(self):
+        return [(self.master[i], self.v_w[i], self.dw[i], self.weights[i]) for i in self.normed]
 
     def backward(self, reward, mask, prob, stream=None):
         """Adds the gradients of L = -sum_b R_b log pi(a_b) at the last forward pass to
-        self.dw / self.db. reward, prob float32 [1, gh, gw]; mask uint8 (the executed
-        grid a_b)."""
+        self.dw / self.db (and the norms' gains' to self.dg). reward, prob float32
+        [1, gh, gw]; mask uint8 (the executed grid a_b)."""
         if not hasattr(self, "master"):
             self._init_training()
         last = len(self.layers) - 1
@@ -272,15 +303,21 @@ class PolicyNet:
         for li in range(last, -1, -1):
             l = self.layers[li]
             gp = cur.pop(li)                          # complete: every consumer came later
-            if l.relu:
-                bc.bc_grad_combine(gp, None, self.buffers[li], gp, stream)
             geom = (l.k, l.k, l.stride, l.pad, 0)
             src = self.input if l.src < 0 else self.buffers[l.src]
-            bc.bc_conv2d_weight_grad(geom, src, gp, self.dw[li], self.db[li], stream)
+            dy = gp                                   # of the convolution's own output
+            if li in self.normed:
+                dy = self.gbufs[li][1] if gp is self.gbufs[li][0] else self.gbufs[li][0]
+                bc.bc_layer_norm_grad(self.raw[li], bc.BC_NHWC, self.gains[li], self.buffers[li] if l.relu else None,
+                                      gp, self.NORM_EPS, dy, gp if l.res is not None else None, self.dg[li],
+                                      self.db[li], True, self.work, stream)
+            elif l.relu:
+                bc.bc_grad_combine(gp, None, self.buffers[li], gp, stream)
+            bc.bc_conv2d_weight_grad(geom, src, dy, self.dw[li], None if li in self.normed else self.db[li], stream)
             if l.src >= 0:
                 acc = cur.get(l.src)
                 out = self.gbufs[l.src][1] if acc is self.gbufs[l.src][0] else self.gbufs[l.src][0]
-                bc.bc_conv2d_input_grad(geom, gp, self.weights[li], acc, out, stream)
+                bc.bc_conv2d_input_grad(geom, dy, self.weights[li], acc, out, stream)
                 cur[l.src] = out
             if l.res is not None:
                 acc = cur.get(l.res)
@@ -291,20 +328,26 @@ class PolicyNet:
                 else:
                     bc.bc_grad_combine(acc, gp, None, acc, stream)
 
-    def update(self, lr=1e-4, alpha=0.99, eps=1e-8, weight_decay=1e-3, stream=None):
+    def update(self, lr=1e-4, alpha=0.99, eps=1e-8, weight_decay=1e-3, stream=None, matrix_lr=2e-3, momentum=0.95):
         """One RMSprop step on every weight and bias with the accumulated gradients (which
-        it resets); the 16-bit weights the convolutions read are rewritten."""
+        it resets); the 16-bit weights the convolutions read are rewritten. With norm="layer"
+        the normalised convolutions' weights take an orthogonalised step of matrix_lr and
+        momentum instead."""
         params = []
         for i in range(len(self.layers)):
-            params.append((self.master[i], self.v_w[i], self.dw[i], self.weights[i]))
+            if i not in self.normed:
+                params.append((self.master[i], self.v_w[i], self.dw[i], self.weights[i]))
             params.append((self.biases[i], self.v_b[i], self.db[i], None))
+        params += [(self.gains[i], self.v_g[i], self.dg[i], None) for i in self.normed]
+        if self.normed:
+            bc.bc_muon_step_many(self._matrices(), matrix_lr, momentum, weight_decay, work=self.work, stream=stream)
         bc.bc_rmsprop_step_many(params, lr, alpha, eps, weight_decay, stream)
 
-    def train_step(self, reward, mask, prob, stream=None, **rmsprop):
+    def train_step(self, reward, mask, prob, stream=None, **hyper):
         """The online update of Section 4: backward pass at the last forward pass, then one
-        RMSprop step."""
+        step of update(**hyper)."""
         self.backward(reward, mask, prob, stream)
-        self.update(stream=stream, **rmsprop)
+        self.update(stream=stream, **hyper)
 
 
 def layer_shapes(layers: list[Layer], h: int, w: int) -> list[tuple[int, int, int]]:

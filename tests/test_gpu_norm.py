@@ -281,3 +281,30 @@ def test_streams_and_graph(bc):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dg, db), want))
+
+
+def test_offsets_past_32_bits(bc):
+    """A map of more than 2^31 elements, forward and backward: pixels at both ends and on both
+    sides of 2^31 elements against the formulas in 64 bits."""
+    h, w, c = 16400, 1024, 128                             # 2.15e9 elements, 4.3 GB a map
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty((1, h, w, c), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    gy = torch.empty_like(x).normal_(generator=gen)
+    gamma = torch.rand(c, device="cuda", generator=gen) + 0.5
+    beta = torch.rand(c, device="cuda", generator=gen) - 0.5
+    y, gx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    bc.bc_sparse_layer_norm(x, bc.BC_NHWC, gamma, beta, None, 1e-5, True, y, (h // 8, w // 8), None, None)
+    bc.bc_layer_norm_grad(x, bc.BC_NHWC, gamma, y, gy, 1e-5, gx, None, None, None)
+    row = 2 ** 31 // (w * c)
+    for r in (0, 1, row - 1, row, row + 1, h - 1):
+        at = slice(r, r + 1)
+        xd, gd, gm = x[0, at].double(), gy[0, at].double(), gamma.double()
+        mean = xd.mean(-1, keepdim=True)
+        rstd = ((xd - mean) ** 2).mean(-1, keepdim=True).add(1e-5).rsqrt()
+        hat = (xd - mean) * rstd
+        want = torch.relu(hat * gm + beta.double())
+        assert ((y[0, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all(), r
+        g = gd * (y[0, at] > 0) * gm
+        want = (g - g.mean(-1, keepdim=True) - hat * (g * hat).mean(-1, keepdim=True)) * rstd
+        assert ((gx[0, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all(), r
+    assert not y.isnan().any() and not gx.isnan().any()

@@ -261,3 +261,38 @@ def test_streams_and_graph(bc):
         torch.cuda.synchronize()
         for (w, m, g, _), (w1, m1) in zip(params, want):
             assert torch.equal(w, w1) and torch.equal(m, m1) and (g == 0).all()
+
+
+def test_offsets_past_32_bits(bc):
+    """A matrix whose X passes 2^32 bytes, with one element per row: its singular values are
+    those elements, and each becomes what the iteration makes of it alone."""
+    m, n = 300, 2 ** 22
+    cols = [0, 1, 31, 32, n // 2 - 1, n // 2, n - 129, n - 64, n - 2, n - 1]
+    g = torch.zeros(m, n, device="cuda")
+    values = [0.3 + 0.05 * i for i in range(len(cols))]
+    rows = [i * (m - 1) // (len(cols) - 1) for i in range(len(cols))]
+    for r, c, v in zip(rows, cols, values):
+        g[r, c] = v
+    norm = math.sqrt(sum(float(np.float32(v)) ** 2 for v in values)) + EPS
+    out = torch.full_like(g, float("nan"))
+    bc.bc_orthogonalize(g, out)
+    for r, c, v in zip(rows, cols, values):
+        s = float(np.float32(v)) / norm
+        for _ in range(5):
+            s = COEF[0] * s + COEF[1] * s ** 3 + COEF[2] * s ** 5
+        assert abs(out[r, c].item() - s) <= 1e-5 * abs(s), (r, c)
+        out[r, c] = 0.0
+    assert not out.any()
+
+
+def test_batches_past_32_bits(bc):
+    """More than 2^31 elements in a batch: the last matrices as by themselves."""
+    g = torch.empty((66000, 64, 512), dtype=torch.float16, device="cuda")
+    g.normal_(generator=torch.Generator(device="cuda").manual_seed(4))
+    out = torch.full_like(g, float("nan"))
+    bc.bc_orthogonalize(g, out)
+    for i in (0, 65535, 65536, 65999):
+        alone = torch.empty_like(out[i])
+        bc.bc_orthogonalize(g[i], alone)
+        assert torch.equal(alone, out[i]), i
+    assert not out.isnan().any()

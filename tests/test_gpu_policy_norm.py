@@ -1,0 +1,161 @@
+"""The policy network with layer normalisation and orthogonalised updates.
+
+* Forward pass and gradients against the same network in float64 by torch's autograd, which
+  rounds to bf16 where the device stores (the convolution's output and the normalised map;
+  the gradient passes the rounding unchanged). Norm-wise within 1e-1 per parameter: the
+  network without norms is held to 5e-2 for one stored map per layer (ReLU gates flipped
+  where device and reference round to different neighbours), and here each layer has two.
+* One update against its definition: the matrices by their momentum's orthogonal factor,
+  everything else by RMSprop.
+* Several updates raise the probability of the rewarded decisions."""
+import numpy as np
+import pytest
+import torch
+import torch.nn.functional as F
+
+import synth
+from oracle import policy as P
+from tests._util import max_abs_rel, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def R(gpu):
+    from paper_2108_09376_amd import bc, resnet
+    return bc, resnet
+
+
+def inputs(seed, h=256, w=512):
+    r = synth.rng(seed)
+    bits = lambda shape, s=1.0: to_dev(synth.to_storage_bits(synth.normal(r, shape, s), "bf16"), "bf16")
+    frame, state, scores = bits((1, 3, h, w)), bits((1, 3, h, w)), bits((1, 64, h // 4, w // 4), 3.0)
+    reward = torch.from_numpy(r.normal(0, 1, (1, h // 128, w // 128)).astype(np.float32)).cuda()
+    mask = torch.from_numpy(synth.bernoulli_mask(r, 1, h // 128, w // 128, 0.5)).cuda()
+    return frame, state, scores, reward, mask
+
+
+def stored(a):
+    """bf16 values of a, with the gradient of a."""
+    return a + (a.detach().bfloat16().double() - a.detach())
+
+
+def reference(net):
+    """(parameters, layer outputs) of the network's forward pass in float64 on the CPU."""
+    leaf = lambda t: t.detach().double().cpu().requires_grad_()
+    ws = [leaf(w) for w in net.weights]
+    bs = [leaf(b) for b in net.biases]
+    gs = [leaf(g) for g in net.gains]
+    x0, ys = net.input.double().cpu().permute(0, 3, 1, 2), []
+    for i, l in enumerate(net.layers):
+        src = x0 if l.src < 0 else ys[l.src]
+        y = F.conv2d(src, ws[i].permute(0, 3, 1, 2), None if i in net.normed else bs[i], l.stride, l.pad)
+        if i in net.normed:
+            y = stored(y)
+            mean = y.mean(1, keepdim=True)
+            var = ((y - mean) ** 2).mean(1, keepdim=True)
+            y = (y - mean) / torch.sqrt(var + net.NORM_EPS) * gs[i].view(1, -1, 1, 1) + bs[i].view(1, -1, 1, 1)
+        if l.res is not None:
+            y = y + ys[l.res]
+        ys.append(stored(torch.relu(y) if l.relu else y))
+    return (ws, bs, gs), ys
+
+
+def test_forward_and_gradients(R):
+    bc, resnet = R
+    net = resnet.PolicyNet(256, 512, norm="layer")
+    r = synth.rng(610)
+    for g, b in zip(net.gains, net.biases):
+        g.copy_(torch.from_numpy(r.uniform(0.5, 1.5, g.numel()).astype(np.float32)))
+        b.copy_(torch.from_numpy(r.normal(0, 0.2, b.numel()).astype(np.float32)))
+    frame, state, scores, reward, mask = inputs(611)
+    prob = net.forward(frame, state, scores, mask).clone()
+    net.backward(reward, mask, prob)
+    (ws, bs, gs), ys = reference(net)
+    z = ys[-1][:, 0]
+    assert (prob.cpu().double() - torch.sigmoid(z)).abs().max().item() <= 2e-2
+    dz = P.logit_grad(reward.cpu().numpy(), mask.cpu().numpy(), prob.cpu().numpy())
+    (z * torch.from_numpy(dz)).sum().backward()
+    for name, got, want in (("w", net.dw, ws), ("b", net.db, bs), ("g", net.dg, gs)):
+        for i, (a, b) in enumerate(zip(got, want)):
+            a, b = a.double().cpu(), b.grad
+            assert (a - b).norm() <= 1e-1 * b.norm(), (name, i, ((a - b).norm() / b.norm()).item())
+
+
+def test_update(R):
+    bc, resnet = R
+    net = resnet.PolicyNet(256, 512, norm="layer")
+    frame, state, scores, reward, mask = inputs(620)
+    prob = net.forward(frame, state, scores, None)
+    net.backward(reward, mask, prob)
+    before = [(m.clone(), d.clone()) for m, d in zip(net.master, net.dw)]
+    small = [(t.clone().cpu().numpy(), d.clone().cpu().numpy())
+             for t, d in zip(net.biases + net.gains, net.db + net.dg)]
+    net.update(lr=1e-2, weight_decay=1e-3, matrix_lr=5e-2, momentum=0.9)
+    for i, (w0, d) in enumerate(before):
+        assert not net.dw[i].any()
+        if i in net.normed:
+            rows = d.shape[0]
+            u = (d + 0.9 * d).reshape(rows, -1)
+            x = torch.empty_like(u)
+            bc.bc_orthogonalize(u, x)
+            rate = 5e-2 * max(1.0, rows / u.shape[1]) ** 0.5
+            want = (1 - 5e-2 * 1e-3) * w0.double() - rate * x.double().view_as(w0)
+            # u rounded once or twice: within a few units of fp32 accuracy of the step
+            assert (net.master[i].double() - want).norm() <= 1e-5 * rate * x.double().norm() + 2.0 ** -23 * w0.double().norm()
+            assert torch.equal(net.v_w[i], d)              # the momentum
+        else:
+            want, _ = P.rmsprop_step(w0.cpu().numpy(), np.zeros(w0.shape), d.cpu().numpy(), lr=1e-2)
+            assert max_abs_rel(net.master[i].cpu().numpy(), want) <= 1e-5
+        assert torch.equal(net.weights[i], net.master[i].to(net.dtype))
+    for (w0, d), got in zip(small, net.biases + net.gains):
+        want, _ = P.rmsprop_step(w0, np.zeros(w0.shape), d, lr=1e-2)
+        assert np.abs(got.cpu().numpy() - want).max() <= 1e-5 * max(1.0, np.abs(want).max())
+    assert not any(d.any() for d in net.db + net.dg)
+
+
+def test_learns(R):
+    """Blocks rewarded for being executed, the others for not: after updates on one frame the
+    policy prefers them so."""
+    bc, resnet = R
+    net = resnet.PolicyNet(256, 512, norm="layer")
+    frame, state, scores, _, want = inputs(630)
+    sign = want.float() * 2 - 1
+    gap = lambda p: ((p - 0.5) * sign).mean().item()
+    start = gap(net.forward(frame, state, scores, None).clone())
+    for _ in range(20):
+        prob = net.forward(frame, state, scores, None)
+        net.train_step(torch.ones_like(prob), want, prob, lr=1e-3, matrix_lr=1e-2)
+    end = gap(net.forward(frame, state, scores, None))
+    assert np.isfinite(end) and end > start + 0.1, (start, end)
+
+
+def test_graph(R):
+    """Forward pass and update captured once: replays equal eager calls on the same gradients.
+    (The convolutions' weight gradients are sums in no fixed order, so each replay is given
+    gradients instead of computing them.)"""
+    bc, resnet = R
+    a, b = (resnet.PolicyNet(256, 512, norm="layer") for _ in range(2))
+    frame, state, scores, reward, mask = inputs(640)
+
+    def step(net):
+        net.forward(frame, state, scores, mask)
+        net.update(lr=1e-3, matrix_lr=1e-2)
+    for net in (a, b):
+        net.train_step(reward, mask, net.forward(frame, state, scores, mask), lr=0.0, weight_decay=0.0, matrix_lr=0.0)
+        for t in net.v_w + net.v_b + net.v_g:
+            t.zero_()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(a)
+    for k in range(3):
+        for x, y in zip(a.dw + a.db + a.dg, b.dw + b.db + b.dg):
+            x.normal_()
+            y.copy_(x)
+        torch.cuda.synchronize()
+        g.replay()
+        step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(a.prob, b.prob)
+        assert all(torch.equal(x, y) for x, y in zip(a.master + a.gains + a.biases, b.master + b.gains + b.biases))

@@ -155,3 +155,9 @@ def test_binding_refuses_mismatched_tensors(B):
         B.bc_muon_step_many([(g, g.clone(), g[:4].clone(), None)], 0.1, 0.9, 0.0)
     with pytest.raises(ValueError):
         B.bc_muon_step_many([(g, g.clone(), g.double(), None)], 0.1, 0.9, 0.0)
+
+
+def test_policy_norm_refusal(B):
+    from paper_2108_09376_amd import resnet
+    with pytest.raises(ValueError):
+        resnet.PolicyNet(256, 512, norm="batch", device="cpu")
