@@ -22,6 +22,11 @@
 // Weight gradients: a workgroup keeps the sums of its rows in registers (a lane has the same
 // columns in every row), its groups meet in LDS, each workgroup writes one partial row, and
 // a second kernel adds those in their order: no atomics, equal bits in every run.
+//
+// Measured: forward 5.1 to 5.5 TB/s on maps of 50 MB and more (16384 x 4096 in fp16 49 us,
+// 8191 x 1001 in fp32 12.3), backward 4.5 to 4.9 (16384 x 4096 84 us and 4 for the partial
+// rows; 16384 x 1024 in fp32 41.5), where a large copy reaches 4.9. Calls of a few hundred
+// rows take 2.7 us forward and 5.6 backward, launches of which little is work.
 #include <algorithm>
 
 #include "bc_internal.h"
@@ -497,7 +502,11 @@ __global__ __launch_bounds__(32 * kRuns) void k_norm_grad_join(const float *__re
 // ---------------------------------------------------------------- choice of form
 
 // Calls f(vector elements, lanes per row, vectors per lane, full) with the form for rows of
-// c elements, or returns false where a row exceeds a workgroup's registers.
+// c elements, or returns false where a row exceeds a workgroup's registers. The fewest lanes
+// that hold a row in one vector each, or 256 lanes with the fewest vectors. With other forms,
+// us forward and backward: 32768 rows of 64 in bf16 with 8 lanes 3.9 and 8.8, with 64 lanes
+// 11.9 and 23.1; 16384 of 1024 with 128 lanes 13.4 and 27.3, with 256 21.0 and 42.4; 16384 of
+// 4096 held in registers 49 and 88, in three passes 168 and 399.
 template <int FMT, typename F>
 bool with_form(int c, F &&f)
 {
@@ -529,7 +538,10 @@ bool with_form(int c, F &&f)
     return false;
 }
 
-constexpr unsigned kMostForward = 2048;      // eight workgroups per CU
+// Workgroups of the forward pass at most: 32 per CU, of which eight run (16384 rows of 4096 in
+// fp16 57 us with 2048 workgroups, 51 with 4096, 49 with 8192, 53 with one per row; 30000 of
+// 3000 88, 76, 71 and 80).
+constexpr unsigned kMostForward = 8192;
 constexpr int kLongParts = 64;
 
 // Workgroups of the backward pass, each with a partial row; *held: its form keeps the row.

@@ -42,7 +42,10 @@ constexpr float kScale = 4096.f;
 constexpr int kSpan = 3;                       // most steps between two A taken from X
 constexpr int kSumParts = 1024;                // partial sums of squares per matrix at most
 constexpr int kSumEach = 8192;                 // and elements of each at least
-constexpr int kLeastChunks = 16;               // chunks of K per range at least
+// Chunks of K per range at least: the sums of a range cost as much as some of its chunks. 8 / 16
+// / 32, us: 64 x 4096 99 / 95 / 107, 256 x 2304 106 / 105 / 120, the policy network's step 143
+// / 143 / 179; 128 x 1024 84 / 93 / 93, 512 x 4608 158 / 158 / 156.
+constexpr int kLeastChunks = 16;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -420,8 +423,9 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //    of 32 of K, FI blocks of L and FJ of R, go straight from memory to LDS, a few deep, one
 //    barrier per chunk; a wave waits for its own requests only. Between the matrix
 //    instructions of a chunk lie the reads of the next chunk's fragments and the requests of
-//    the chunk that takes the present one's place, evenly: a wave that does one after the other leaves its matrix
-//    core idle (2048 x 2048, 128 x 128 tiles: 38 us a product, 24 of them the instructions).
+//    the chunk that takes the present one's place, evenly: a wave that does one after the other
+//    leaves its matrix core idle (2048 x 2048, 128 x 128 tiles: 38 us a product, 24 of them
+//    the instructions).
 //  * What is added to the product, E1 and E2, follows the last chunk into LDS. The finished
 //    tile takes E1's place there and goes to memory in whole blocks, its mirror image through
 //    transposing reads.
@@ -434,7 +438,19 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //    to arrive (a counter per tile) adds all of them in order: the result does not depend on
 //    the order of arrival.
 //  * Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, so
-//    that its L2 serves their common rows and columns.
+//    that its L2 serves their common rows and columns (in turn through all matrices of a step
+//    instead, which evens the load out: ResNet-50's 948 us for 917, the policy network's 154
+//    for 143).
+//
+// What bounds them: 2048 x 2048, 750 us, is 230 TFLOP/s of the textbook's products (three
+// fp16 products each, fewer in the form computed: some 620 on the matrix cores), 272 tiles on
+// 256 CUs, one wave per SIMD with its chunks' way through LDS exposed. ResNet-50's step, 915 us:
+// 100 for the two passes over momentum and gradients, which memory bounds, 420 for the four
+// products along n, 390 for thirteen products of 432 to 578 tiles, 27 to 34 us each and for
+// two thirds the start and the end of their one round of workgroups. Small matrices: 5 to 9 us
+// for each of 17 products, a launch, the way to LDS and the tile's way out. (Eight chunks in
+// LDS with a workgroup per CU, where the tiles are that few, are slower than four: 512 x 4608
+// 169 for 157, the policy network's step 154 for 143.)
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
