@@ -538,10 +538,13 @@ bool with_form(int c, F &&f)
     return false;
 }
 
-// Workgroups of the forward pass at most: 32 per CU, of which eight run (16384 rows of 4096 in
-// fp16 57 us with 2048 workgroups, 51 with 4096, 49 with 8192, 53 with one per row; 30000 of
-// 3000 88, 76, 71 and 80).
-constexpr unsigned kMostForward = 8192;
+// Workgroups of the forward pass at most. Every pixel: 32 per CU, of which eight run (16384 rows
+// of 4096 in fp16 57 us with 2048 workgroups, 51 with 4096, 49 with 8192, 53 with one per
+// row; 30000 of 3000 88, 76, 71 and 80). Active blocks, whose number only the device knows:
+// 8 per CU, for those without work cost more than they bring (38 of 128 blocks of
+// 32 x 32 x 256: 11.0 us with 2048, 12.4 with 8192).
+unsigned most_groups(const NormGeom &g) { return g.idx ? 2048 : 8192; }
+
 constexpr int kLongParts = 64;
 
 // Workgroups of the backward pass, each with a partial row; *held: its form keeps the row.
@@ -569,12 +572,12 @@ hipError_t launch_norm(const void *x, const float *gamma, const float *beta, con
         constexpr int FMT = decltype(f)::value;
         const bool held = with_form<FMT>(g.c, [&](auto vec, auto lanes, auto vecs, auto full) {
             constexpr int L = decltype(lanes)::value;
-            const unsigned grid = std::min<uint32_t>((g.rows + kThreads / L - 1) / (kThreads / L), kMostForward);
+            const unsigned grid = std::min<uint32_t>((g.rows + kThreads / L - 1) / (kThreads / L), most_groups(g));
             hipLaunchKernelGGL((k_norm<FMT, decltype(vec)::value, L, decltype(vecs)::value, decltype(full)::value>),
                                dim3(grid), dim3(kThreads), 0, s, x, gamma, beta, res, out, g);
         });
         if (!held)
-            hipLaunchKernelGGL(k_norm_long<FMT>, dim3(std::min<uint32_t>(g.rows, kMostForward)), dim3(kThreads), 0, s,
+            hipLaunchKernelGGL(k_norm_long<FMT>, dim3(std::min<uint32_t>(g.rows, most_groups(g))), dim3(kThreads), 0, s,
                                x, gamma, beta, res, out, g);
         return hipGetLastError();
     });
@@ -609,7 +612,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
         if (!held) {
             float4 *stats = (float4 *)work;
             part = sums ? (float *)(stats + g.rows) : nullptr;
-            hipLaunchKernelGGL(k_norm_grad_stats<FMT>, dim3(std::min<uint32_t>(g.rows, kMostForward)), dim3(kThreads), 0,
+            hipLaunchKernelGGL(k_norm_grad_stats<FMT>, dim3(std::min<uint32_t>(g.rows, most_groups(g))), dim3(kThreads), 0,
                                s, a, g, stats);
             hipLaunchKernelGGL(k_norm_grad_cols<FMT>, dim3((g.c + kThreads - 1) / kThreads, parts), dim3(kThreads), 0,
                                s, a, g, stats, part);
