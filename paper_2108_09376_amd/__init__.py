@@ -7,7 +7,8 @@ method for AMD Instinct MI355X (gfx950):
 
 * ``libblockcopy.so`` -- hand-written HIP kernels behind the C ABI of ``include/bc.h``
   (block index compaction, halo gather, block scatter, matrix-core sparse
-  convolution with fused epilogue, sparse max pooling);
+  convolution with fused epilogue, sparse max pooling, layer normalisation and its
+  gradient, orthogonalised weight updates, and the policy's steps);
 * :mod:`paper_2108_09376_amd.bc` -- the ctypes binding (same names as the C ABI);
 * :mod:`paper_2108_09376_amd.resnet` -- a frame-by-frame ResNet-18/50 runner that
   keeps one persistent buffer per layer;
