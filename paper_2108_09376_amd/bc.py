@@ -469,20 +469,18 @@ def bc_block_rewards(ig, mask, prob, grid, tau, gamma, mu, mavg, reward, cost=No
     _check(st, "bc_block_rewards")
 
 
-def _work(work, need, device):
-    """The caller's workspace, or a new one of need() bytes on the current stream."""
-    if work is None:
-        import torch
-        work = torch.empty(need(), dtype=torch.uint8, device=device)
-    return work
+def _work(nbytes, like):
+    """A workspace where the caller has none, from the current stream's memory."""
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 
 def _nbytes(t) -> int:
     return t.numel() * t.element_size()
 
 
-def _alike(t, like, name):
-    if t is not None and (t.shape != like.shape or t.dtype != like.dtype or not t.is_contiguous()):
+def _alike(t, shape, dtype, name):
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_contiguous()):
         raise ValueError(f"{name} must be contiguous and shaped and typed like the map")
 
 
@@ -492,7 +490,7 @@ def _is_f32(t) -> bool:
 
 def _per_channel(t, c, name):
     """An fp32 vector of one value per channel (or None)."""
-    if t is not None and (t.numel() != c or not _is_f32(t)):
+    if t is not None and not (t.numel() == c and _TORCH_DT.get(t.dtype) == BC_F32 and t.is_contiguous()):
         raise ValueError(f"{name} must be {c} contiguous float32 values")
 
 
@@ -501,10 +499,11 @@ def bc_sparse_layer_norm(x, layout, gamma, beta, residual, eps, relu, out, grid,
     x, residual and out [n, h, w, c] (layout BC_NHWC), gamma and beta float32 [c] or None."""
     cap = 0 if idx is None else int(idx.numel())
     d = _desc(x, layout)
-    _alike(out, x, "out")
-    _alike(residual, x, "residual")
-    _per_channel(gamma, d.c, "gamma")
-    _per_channel(beta, d.c, "beta")
+    shape, dtype, c = x.shape, x.dtype, d.c
+    _alike(out, shape, dtype, "out")
+    _alike(residual, shape, dtype, "residual")
+    _per_channel(gamma, c, "gamma")
+    _per_channel(beta, c, "beta")
     st = _lib.bc_sparse_layer_norm(_ptr(x), d, _ptr(gamma), _ptr(beta), _ptr(residual), float(eps), int(relu),
                                    _ptr(out), _grid(grid), _ptr(idx), _ptr(count), cap, _stream(stream))
     _check(st, "bc_sparse_layer_norm")
@@ -524,11 +523,16 @@ def bc_layer_norm_grad(x, layout, gamma, y, grad_out, eps, grad_in, grad_res, dg
     written, or added to with accumulate. work: a uint8 device tensor that the caller keeps
     (None: allocated here, for work enqueued on torch's current stream)."""
     d = _desc(x, layout)
-    for t, name in ((y, "y"), (grad_out, "grad_out"), (grad_in, "grad_in"), (grad_res, "grad_res")):
-        _alike(t, x, name)
-    for t, name in ((gamma, "gamma"), (dgamma, "dgamma"), (dbeta, "dbeta")):
-        _per_channel(t, d.c, name)
-    work = _work(work, lambda: bc_layer_norm_grad_work(x, layout), x.device)
+    shape, dtype, c = x.shape, x.dtype, d.c
+    _alike(y, shape, dtype, "y")
+    _alike(grad_out, shape, dtype, "grad_out")
+    _alike(grad_in, shape, dtype, "grad_in")
+    _alike(grad_res, shape, dtype, "grad_res")
+    _per_channel(gamma, c, "gamma")
+    _per_channel(dgamma, c, "dgamma")
+    _per_channel(dbeta, c, "dbeta")
+    if work is None:
+        work = _work(bc_layer_norm_grad_work(x, layout), x)
     st = _lib.bc_layer_norm_grad(_ptr(x), d, _ptr(gamma), _ptr(y), _ptr(grad_out), float(eps), _ptr(grad_in),
                                  _ptr(grad_res), _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(work),
                                  _nbytes(work), _stream(stream))
@@ -561,7 +565,8 @@ def bc_orthogonalize(g, out, steps=NS_STEPS, coef=NS_COEF, eps=NS_EPS, work=None
     itself), any dtypes. work as for bc_layer_norm_grad."""
     if out.shape != g.shape or not out.is_contiguous():
         raise ValueError("out must be contiguous and shaped like g")
-    work = _work(work, lambda: bc_orthogonalize_work(g, steps), g.device)
+    if work is None:
+        work = _work(bc_orthogonalize_work(g, steps), g)
     st = _lib.bc_orthogonalize(_ptr(g), _dtype_code(g), *_matrices(g),
                                ctypes.byref(_newton_schulz(steps, tuple(coef), eps)), _ptr(out),
                                _dtype_code(out), _ptr(work), _nbytes(work), _stream(stream))
@@ -599,7 +604,8 @@ def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=N
     ...], float32, grad reset to 0; the 16-bit copies share one dtype). work as for
     bc_layer_norm_grad."""
     arr, dt = _matrix_array(params)
-    work = _work(work, lambda: bc_muon_step_many_work(params, steps), params[0][0].device)
+    if work is None:
+        work = _work(bc_muon_step_many_work(params, steps), params[0][0])
     h = bc_muon(float(lr), float(momentum), float(weight_decay), int(nesterov),
                 _newton_schulz(steps, tuple(coef), eps))
     st = _lib.bc_muon_step_many(arr, len(params), ctypes.byref(h), dt, _ptr(work), _nbytes(work), _stream(stream))
