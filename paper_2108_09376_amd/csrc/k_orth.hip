@@ -1245,8 +1245,11 @@ unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
 
 // Tiles of 128 x 64 read three quarters of the bytes of 64 x 64 ones per product, where they
 // are enough for the chip (2048 x 2048 837 us with the small ones, 746 with the large; with
-// 128 x 128, one workgroup per CU, 1173). 1500 x 1700, 156 large tiles: 415 and 414.
-constexpr uint64_t kEnough = 192;
+// 128 x 128, one workgroup per CU, 1173; 1500 x 1700, 156 large tiles: 415 and 414). Where some
+// products are twice as long as the mean, small tiles even the load out and more large ones
+// are needed (ResNet-50's step, launches of 386 to 578 large tiles: 894 us with those from 192
+// on large, 875 from 500 on).
+constexpr uint64_t kEnough = 192, kEnoughUneven = 500;
 
 // The products of one launch: the plans of its matrices (those taken in spans, those taken step
 // by step; a plan that is done has no jobs), the tiles, and the K ranges.
@@ -1282,19 +1285,22 @@ std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
                 return large ? products_of<4, 2>(p, e, each) : products_of<2, 2>(p, e, each);
             });
         };
-        l.large = tiles(true, 0) >= kEnough;
-        const uint64_t wgs = tiles(l.large, 0);
-        const uint64_t work = total([&](const OrthPlan &p, const OrthShape &e) {
-            return (l.large ? products_of<4, 2>(p, e, 0) : products_of<2, 2>(p, e, 0)) * chunks(p, e);
-        });
+        auto work = [&](bool large) {
+            return total([&](const OrthPlan &p, const OrthShape &e) {
+                return (large ? products_of<4, 2>(p, e, 0) : products_of<2, 2>(p, e, 0)) * chunks(p, e);
+            });
+        };
         uint64_t longest = 0;
         for (int t = 0; t < T.n; ++t) {
             const OrthPlan &p = l.plan[steps_direct(T.e[t].rows, T.e[t].cols)];
             if (p.jobs) longest = std::max(longest, chunks(p, T.e[t]));
         }
+        const uint64_t large = tiles(true, 0);
+        l.large = large >= (longest * large >= 2 * work(true) ? kEnoughUneven : kEnough);
+        const uint64_t wgs = tiles(l.large, 0);
         // K in ranges, of whole folds, where the longest workgroup would far outlast the chip's
         // share of the work (twice as long: 1024 x 2048 254 us whole, 265 in ranges)
-        const uint64_t share = std::max<uint64_t>(kLeastChunks, ((work + 511) / 512 + kFold - 1) / kFold * kFold);
+        const uint64_t share = std::max<uint64_t>(kLeastChunks, ((work(l.large) + 511) / 512 + kFold - 1) / kFold * kFold);
         l.each = longest >= 3 * share && wgs <= 512 ? (int)share : 0;
         const uint64_t places = tiles(l.large, l.each);
         l.part_bytes = l.each ? places * kThreads * sizeof(f32x4) * (l.large ? 8 : 4) : 0;
