@@ -444,11 +444,11 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //
 // What bounds them: 2048 x 2048, 750 us, is 230 TFLOP/s of the textbook's products (three
 // fp16 products each, fewer in the form computed: some 620 on the matrix cores), 272 tiles on
-// 256 CUs, one wave per SIMD with its chunks' way through LDS exposed. ResNet-50's step, 915 us:
-// 100 for the two passes over momentum and gradients, which memory bounds, 420 for the four
-// products along n, 390 for thirteen products of 432 to 578 tiles, 27 to 34 us each and for
-// two thirds the start and the end of their one round of workgroups. Small matrices: 5 to 9 us
-// for each of 17 products, a launch, the way to LDS and the tile's way out. (Eight chunks in
+// 256 CUs, one wave per SIMD with its chunks' way through LDS exposed. ResNet-50's step, 870 us:
+// 100 for the two passes over momentum and gradients, which memory bounds, 405 for the four
+// products along n, 365 for thirteen products of m x m, 25 to 52 us each and for two thirds the
+// start and the end of their one or two rounds of workgroups. Small matrices: 5 to 9 us for
+// each of 17 products, a launch, the way to LDS and the tile's way out. (Eight chunks in
 // LDS with a workgroup per CU, where the tiles are that few, are slower than four: 512 x 4608
 // 169 for 157, the policy network's step 154 for 143.)
 
