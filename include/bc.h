@@ -678,7 +678,9 @@ bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t ste
  *   w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) X(u);  grad = 0;
  * X(u) as bc_orthogonalize gives it in fp32, and w16, if not NULL, the weights rounded to
  * `dtype` (BC_BF16 or BC_F16). `params` is a host array read during the call. No two buffers
- * may overlap. d_work as for bc_orthogonalize, bc_muon_step_many_work bytes.
+ * may overlap. d_work as for bc_orthogonalize, bc_muon_step_many_work bytes. Equal calls give
+ * equal bits. The order of a long product's sums (over 1536 elements and more) depends on the
+ * sizes of all matrices of the call: alone and among others such a matrix agrees to rounding.
  * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_CAPACITY, BC_ERR_ALIAS,
  * BC_ERR_UNSUPPORTED, BC_ERR_HIP.
  */
