@@ -100,11 +100,20 @@ __device__ __forceinline__ size_t blocked(int r, int c, int ld)
     return ((size_t)(r >> 5) * (ld >> 5) + (c >> 5)) * kBlockBytes + in_block(r, c);
 }
 
-// Spans of one step (true) or of 3, 2, 2, ... for a matrix. Difference to 64 bits after five
-// steps, in spans of one / of 3 and 2 / of the textbook form in fp32: 8 x 16 6.8e-7 / 6.7e-6
-// / 6.6e-7, 64 x 147 6.9e-7 / 1.9e-6 / 1.1e-6, 193 x 301 8.3e-7 / 1.5e-6 / 1.6e-6,
-// 512 x 512 6.8e-7 / 1.5e-6 / 2.0e-6: small matrices take the steps one by one.
-__host__ __device__ inline bool steps_direct(int rows, int cols) { return (rows < cols ? rows : cols) <= 128; }
+// Spans of one step (true) or of 3, 2, 2, ... for a matrix. Spans save products along n and cost
+// accuracy. Difference to 64 bits after five steps on normal values, one by one / in spans / the
+// textbook form in fp32: 140 x 200 9.8e-7 / 2.0e-6 / 1.6e-6, 256 x 256 8.6e-7 / 2.5e-6 / 1.8e-6,
+// 320 x 5000 1.5e-6 / 3.6e-6 / 2.7e-6, 384 x 1536 1.3e-6 / 2.9e-6 / 3.0e-6, 512 x 512 8.2e-7 /
+// 2.8e-6 / 2.3e-6, 512 x 4608 1.5e-6 / 3.5e-6 / 4.4e-6, 1024 x 4096 9.1e-7 / 2.0e-6 / 3.7e-6. So
+// they are left to matrices on which they stay with fp32: both sides above 384, one of them well
+// above the other; near squares have nothing to save either. us one by one / in spans: 512 x 640
+// 117 / 129, 1024 x 1280 189 / 197, 1024 x 2048 243 / 218, 2048 x 2048 664 / 740, 512 x 4608
+// 187 / 157; 256 x 2304 107 / 105 and ResNet-50's step 972 / 888, the price of the accuracy.
+__host__ __device__ inline bool steps_direct(int rows, int cols)
+{
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    return m <= 384 || (long long)4 * n <= (long long)5 * m;
+}
 
 // Small matrices: M x C of X in LDS, hi and lo. kR x kC fragments of 16 x 16 of X per wave,
 // kWR x kWC waves; kAR x kAC fragments of A.

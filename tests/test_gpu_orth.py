@@ -130,6 +130,23 @@ def test_batches(bc, batch, m, n):
         assert torch.equal(half[1], out[1].bfloat16())
 
 
+@pytest.mark.parametrize("m,n", [(140, 200), (193, 301), (256, 256), (256, 2304), (4000, 150), (320, 1000), (512, 512),
+                                 (640, 512)])
+@pytest.mark.parametrize("kind", ["fall", "noise", "rank"])
+def test_no_further_off_than_fp32(bc, m, n, kind):
+    """What is promised as fp32 accuracy is no worse than plain fp32 arithmetic: the mean
+    difference to 64 bits over three matrices is at most that of the textbook form in fp32."""
+    here = fp32 = 0.0
+    for seed in (11, 12, 13):
+        g = gradient(seed, m, n, kind)
+        want = iterate(g)
+        out = torch.empty_like(g, device="cuda")
+        bc.bc_orthogonalize(g.cuda(), out)
+        here += ((out.double().cpu() - want).norm() / want.norm()).item()
+        fp32 += ((iterate(g, dtype=torch.float32).double() - want).norm() / want.norm()).item()
+    assert here <= fp32, (here / 3, fp32 / 3)
+
+
 def test_magnitudes(bc):
     """The result does not depend on G's scale, from values near fp32's largest to small
     ones (eps = 0), and eps takes part where the norm is near it."""
