@@ -367,7 +367,9 @@ __global__ __launch_bounds__((kGradThreads<L, NV>)) void k_norm_grad(NormGradArg
                 float dx[VEC];
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float xhat = get(row.x[v], j) * rstd - mean * rstd, dy = get(row.dy[v], j);
+                    // the difference first: x rstd - mean rstd would leave the rounding of mean rstd
+                    // in xhat (0.06 in a row of one value 4096.3), or pass fp32's range
+                    const float xhat = (get(row.x[v], j) - mean) * rstd, dy = get(row.dy[v], j);
                     dx[j] = rstd * (dy * gain[j] - (xhat * mean_gx + mean_g));
                     sg[v][j] += dy * xhat;
                     sb[v][j] += dy;

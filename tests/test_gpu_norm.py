@@ -222,6 +222,30 @@ def test_backward_in_place_and_unaligned(bc, dtype, c):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("c", [1, 7, 64, 100, 255, 1001, 4096, 20001])
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+def test_backward_flat_rows(bc, dtype, c, eps):
+    """Rows of one value each (of so few bits that their sums are exact): x - mean is 0, so they
+    add exactly nothing to dgamma, and dx is (g - mean(g)) / sqrt(eps)."""
+    values = [3.25, -100.0, 4160.0, 30720.0] + ([2.0 ** 120, -(2.0 ** 120)] if c <= 255 and dtype != "f16" else [])
+    n = 7 * len(values)
+    x = torch.tensor(values, device="cuda").repeat(7).view(1, n, 1, 1).expand(1, n, 1, c).to(TORCH[dtype]).contiguous()
+    dy, gamma = maps(90, (1, n, 1, c), dtype, 2.0 ** -8), vectors(91, c)[0]
+    dx = torch.full_like(x, float("nan"))
+    dgamma, dbeta = torch.full((c,), float("nan"), device="cuda"), torch.full((c,), float("nan"), device="cuda")
+    bc.bc_layer_norm_grad(x, bc.BC_NHWC, gamma, None, dy, eps, dx, None, dgamma, dbeta)
+    assert (dgamma == 0).all()
+    flat = dy.double().reshape(-1, c)
+    assert ((dbeta.double() - flat.sum(0)).abs() <= (n / 32 + 700) * U * flat.abs().sum(0)).all()
+    g = dy.double() * gamma.double()
+    rstd = 1 / np.sqrt(np.float64(np.float32(eps)))
+    tol = rstd * (c / 8 + 28) * U * (g.abs() + g.abs().mean(-1, keepdim=True))
+    want = rstd * (g - g.mean(-1, keepdim=True))
+    inside = want.abs() < torch.finfo(TORCH[dtype]).max / 2
+    check(torch.where(inside, dx.double(), 0), torch.where(inside, want, 0), tol, dtype)
+
+
 def test_backward_against_differences(bc):
     """Directional derivatives of the forward pass in fp32, with central differences in 64
     bits on the same formula: d/dt loss(x + t v) = sum grad_in v, likewise gamma and beta."""
