@@ -476,30 +476,39 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_cols(NormGradArgs a, Nor
     }
 }
 
-// Adds the partial rows in their order: 32 columns per workgroup, 32 runs of rows each
+// Adds the partial rows in their order: 32 columns per workgroup and turn, 32 runs of rows each
 // (each summed in order), then the runs in order.
 constexpr int kRuns = 32;
-__global__ __launch_bounds__(32 * kRuns) void k_norm_grad_join(const float *__restrict__ part, int parts, int c,
+__global__ __launch_bounds__(32 * kRuns) void k_norm_grad_join(const float *__restrict__ part, int parts, uint32_t c,
                                                                float *__restrict__ dgamma, float *__restrict__ dbeta,
                                                                int accumulate)
 {
     __shared__ float lds[kRuns][33];
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
-    const int i = blockIdx.x * 32 + lane;
     const int each = (parts + kRuns - 1) / kRuns, lo = run * each, hi = min(parts, lo + each);
-    float s = 0.f;
-    if (i < 2 * c)
+    const size_t cols = (size_t)2 * c;
+    for (size_t at = (size_t)blockIdx.x * 32; at < cols; at += (size_t)gridDim.x * 32) {
+        const size_t i = at + lane;
+        float s = 0.f;
+        if (i < cols)
 #pragma unroll 8
-        for (int p = lo; p < hi; ++p) s += part[(size_t)p * 2 * c + i];
-    lds[run][lane] = s;
-    __syncthreads();
-    if (run || i >= 2 * c) return;
-    for (int k = 1; k < kRuns; ++k) s += lds[k][lane];
-    float *to = i < c ? dgamma : dbeta;
-    if (!to) return;
-    to += i < c ? i : i - c;
-    *to = accumulate ? *to + s : s;
+            for (int p = lo; p < hi; ++p) s += part[p * cols + i];
+        lds[run][lane] = s;
+        __syncthreads();
+        if (run == 0 && i < cols) {
+            for (int k = 1; k < kRuns; ++k) s += lds[k][lane];
+            float *to = i < c ? dgamma : dbeta;
+            if (to) {
+                to += i < c ? i : i - c;
+                *to = accumulate ? *to + s : s;
+            }
+        }
+        __syncthreads();                                  // the sums have been read
+    }
 }
+
+// Workgroups of it: a launch of 2^32 threads or more does not take place.
+unsigned join_groups(uint32_t c) { return (unsigned)std::min<size_t>(((size_t)2 * c + 31) / 32, 1 << 20); }
 
 // ---------------------------------------------------------------- choice of form
 
@@ -620,8 +629,8 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
                                s, a, g, stats, part);
         }
         if (sums)
-            hipLaunchKernelGGL(k_norm_grad_join, dim3((2 * g.c + 31) / 32), dim3(32 * kRuns), 0, s, part, (int)parts,
-                               g.c, dgamma, dbeta, accumulate);
+            hipLaunchKernelGGL(k_norm_grad_join, dim3(join_groups(g.c)), dim3(32 * kRuns), 0, s, part, (int)parts,
+                               (uint32_t)g.c, dgamma, dbeta, accumulate);
         return hipGetLastError();
     });
 }

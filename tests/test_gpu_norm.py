@@ -332,3 +332,38 @@ def test_offsets_past_32_bits(bc):
         want = (g - g.mean(-1, keepdim=True) - hat * (g * hat).mean(-1, keepdim=True)) * rstd
         assert ((gx[0, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all(), r
     assert not y.isnan().any() and not gx.isnan().any()
+
+
+@pytest.mark.parametrize("rows,c", [(2, 2 ** 26 + 5), (1, 2 ** 30 + 9)])
+def test_backward_more_channels_than_threads(bc, rows, c):
+    """The sums over pixels of 2^27 and 2^31 columns: more than a launch has threads, more than
+    31 bits count. Values of -1 and 1 and small integers: every sum over channels is exact in
+    fp32 but for the last additions (4 u), xhat = x / sqrt(var + eps) to 8 u."""
+    i = torch.arange(c, device="cuda", dtype=torch.int32)
+    x = torch.empty((1, 1, rows, c), dtype=torch.bfloat16, device="cuda")
+    dy, dx = torch.empty_like(x), torch.full_like(x, float("nan"))
+    for r in range(rows):
+        x[0, 0, r] = 1 - 2 * ((i + r) & 1)
+        dy[0, 0, r] = (i * 5 + r * 3 >> 2) % 4 - 1
+    del i
+    dgamma, dbeta = torch.full((c,), float("nan"), device="cuda"), torch.full((c,), float("nan"), device="cuda")
+    bc.bc_layer_norm_grad(x, bc.BC_NHWC, None, None, dy, EPS, dx, None, dgamma, dbeta)
+    means = []
+    for r in range(rows):
+        sx = sxg = sg = 0.0
+        for a in range(0, c, 1 << 27):
+            xr, gr = x[0, 0, r, a:a + (1 << 27)].double(), dy[0, 0, r, a:a + (1 << 27)].double()
+            sx, sg, sxg = sx + xr.sum().item(), sg + gr.sum().item(), sxg + (gr * xr).sum().item()
+        mean = sx / c
+        rstd = (1 - mean * mean + EPS) ** -0.5
+        means.append((mean, rstd, sg / c, (sxg / c - mean * sg / c) * rstd))
+    for a in range(0, c, 1 << 27):
+        at = slice(a, min(c, a + (1 << 27)))
+        wg = wb = 0.0
+        for r, (mean, rstd, mg, mgx) in enumerate(means):
+            g, xhat = dy[0, 0, r, at].double(), (x[0, 0, r, at].double() - mean) * rstd
+            wg, wb = wg + g * xhat, wb + g
+            want = rstd * (g - mg - xhat * mgx)
+            assert ((dx[0, 0, r, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 64 * U).all()
+        assert ((dgamma[at].double() - wg).abs() <= 8 * U * 2 * rows).all()
+        assert torch.equal(dbeta[at].double(), wb)
