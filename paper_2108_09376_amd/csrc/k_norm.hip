@@ -213,20 +213,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_long(const void *x, const flo
                                                         void *out, NormGeom g)
 {
     __shared__ float lds[2][1][4];
-    const uint32_t rows = row_count(g);
+    const uint32_t rows = row_count(g), c = g.c;           // i passes 31 bits behind the last channels
     for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const size_t base = (size_t)row_pixel(g, r) * g.c;
         float s[1] = {0.f}, q[1] = {0.f};
-        for (int i = threadIdx.x; i < g.c; i += kThreads) s[0] += get(load_raw<FMT, 1>(x, base + i), 0);
+        for (uint32_t i = threadIdx.x; i < c; i += kThreads) s[0] += get(load_raw<FMT, 1>(x, base + i), 0);
         row_sum<kThreads>(s, lds[0]);
         const float mean = s[0] / (float)g.c;
-        for (int i = threadIdx.x; i < g.c; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < c; i += kThreads) {
             const float d = get(load_raw<FMT, 1>(x, base + i), 0) - mean;
             q[0] += d * d;
         }
         row_sum<kThreads>(q, lds[1]);
         const float rstd = rsqrtf(q[0] * g.inv_c + g.eps);
-        for (int i = threadIdx.x; i < g.c; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < c; i += kThreads) {
             float y[1] = {(get(load_raw<FMT, 1>(x, base + i), 0) - mean) * rstd * (gamma ? gamma[i] : 1.f) +
                           (beta ? beta[i] : 0.f)};
             if (res) y[0] += get(load_raw<FMT, 1>(res, base + i), 0);
@@ -423,21 +423,22 @@ template <int FMT>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_stats(NormGradArgs a, NormGeom g, float4 *__restrict__ stats)
 {
     __shared__ float lds[2][2][4];
+    const uint32_t c = g.c;
     for (uint32_t r = blockIdx.x; r < g.rows; r += gridDim.x) {
         const size_t base = (size_t)r * g.c;
-        auto x_at = [&](int i) { return get(load_raw<FMT, 1>(a.x, base + i), 0); };
-        auto g_at = [&](int i) {
+        auto x_at = [&](uint32_t i) { return get(load_raw<FMT, 1>(a.x, base + i), 0); };
+        auto g_at = [&](uint32_t i) {
             if (a.y && !(get(load_raw<FMT, 1>(a.y, base + i), 0) > 0.f)) return 0.f;
             return get(load_raw<FMT, 1>(a.dy, base + i), 0) * (a.gamma ? a.gamma[i] : 1.f);
         };
         float one[2] = {0.f, 0.f}, two[2] = {0.f, 0.f};
-        for (int i = threadIdx.x; i < g.c; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < c; i += kThreads) {
             one[0] += x_at(i);
             one[1] += g_at(i);
         }
         row_sum<kThreads>(one, lds[0]);
         const float mean = one[0] / (float)g.c, mean_g = one[1] * g.inv_c;
-        for (int i = threadIdx.x; i < g.c; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < c; i += kThreads) {
             const float d = x_at(i) - mean;
             two[0] += d * d;
             two[1] += g_at(i) * d;
@@ -454,8 +455,8 @@ template <int FMT>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_cols(NormGradArgs a, NormGeom g,
                                                              const float4 *__restrict__ stats, float *__restrict__ part)
 {
-    const int i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= g.c) return;
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+    if (i >= (uint32_t)g.c) return;
     const float ga = a.gamma ? a.gamma[i] : 1.f;
     float sg = 0.f, sb = 0.f;
     for (uint32_t r = blockIdx.y; r < g.rows; r += gridDim.y) {
@@ -532,7 +533,7 @@ bool with_form(int c, F &&f)
         f(integral_constant<int, 1>{}, integral_constant<int, 8>{}, integral_constant<int, 1>{}, std::false_type{});
         return true;
     }
-    const int nv = (c + V - 1) / V;
+    const int nv = c / V + (c % V != 0);
     auto with = [&](auto lanes, auto vecs) { go(lanes, vecs); return true; };
     using one = integral_constant<int, 1>;
     using wave = integral_constant<int, 64>;
@@ -625,7 +626,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, float *dgamma, float *dbeta, 
             part = sums ? (float *)(stats + g.rows) : nullptr;
             hipLaunchKernelGGL(k_norm_grad_stats<FMT>, dim3(std::min<uint32_t>(g.rows, most_groups(g))), dim3(kThreads), 0,
                                s, a, g, stats);
-            hipLaunchKernelGGL(k_norm_grad_cols<FMT>, dim3((g.c + kThreads - 1) / kThreads, parts), dim3(kThreads), 0,
+            hipLaunchKernelGGL(k_norm_grad_cols<FMT>, dim3(((uint32_t)g.c + kThreads - 1) / kThreads, parts), dim3(kThreads), 0,
                                s, a, g, stats, part);
         }
         if (sums)

@@ -334,7 +334,7 @@ def test_offsets_past_32_bits(bc):
     assert not y.isnan().any() and not gx.isnan().any()
 
 
-@pytest.mark.parametrize("rows,c", [(2, 2 ** 26 + 5), (1, 2 ** 30 + 9)])
+@pytest.mark.parametrize("rows,c", [(2, 2 ** 26 + 5), (1, 2 ** 30 + 9), (1, 2 ** 31 - 1)])
 def test_backward_more_channels_than_threads(bc, rows, c):
     """The sums over pixels of 2^27 and 2^31 columns: more than a launch has threads, more than
     31 bits count. Values of -1 and 1 and small integers: every sum over channels is exact in
@@ -367,3 +367,15 @@ def test_backward_more_channels_than_threads(bc, rows, c):
             assert ((dx[0, 0, r, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 64 * U).all()
         assert ((dgamma[at].double() - wg).abs() <= 8 * U * 2 * rows).all()
         assert torch.equal(dbeta[at].double(), wb)
+
+
+def test_forward_most_channels(bc):
+    """A row of 2^31 - 1 channels, as many as a size can say: -1 and 1 in turn."""
+    c = 2 ** 31 - 1
+    x = torch.empty((1, 1, 1, c), dtype=torch.bfloat16, device="cuda")
+    x.view(-1)[0::2], x.view(-1)[1::2] = 1.0, -1.0
+    out = torch.full_like(x, float("nan"))
+    bc.bc_sparse_layer_norm(x, bc.BC_NHWC, None, None, None, 0.5, False, out, (1, 1), None, None)
+    want = (1 / 1.5 ** 0.5) * torch.tensor([1.0, -1.0], dtype=torch.float64, device="cuda")
+    for k in (0, 1):                                       # the mean is 1 / c, the variance 1 - 1 / c^2
+        assert ((out.view(-1)[k::2].float() - want[k]).abs() <= 2.0 ** -8 * want[k].abs() + 8 * U).all()
