@@ -469,10 +469,16 @@ def bc_block_rewards(ig, mask, prob, grid, tau, gamma, mu, mavg, reward, cost=No
     _check(st, "bc_block_rewards")
 
 
-def _work(nbytes, like):
-    """A workspace where the caller has none, from the current stream's memory."""
+def _work(nbytes, like, stream):
+    """A workspace where the caller has none: memory of the stream that the call runs on, which
+    no other stream is given while that one's work may still use it."""
     import torch
-    return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 
 def _nbytes(t) -> int:
@@ -521,7 +527,7 @@ def bc_layer_norm_grad(x, layout, gamma, y, grad_out, eps, grad_in, grad_res, dg
     """grad_in (and grad_res, the residual's gradient, if not None) from grad_out, with the
     ReLU's mask from the forward output y (None: no ReLU); dgamma, dbeta float32 [c] (or None)
     written, or added to with accumulate. work: a uint8 device tensor that the caller keeps
-    (None: allocated here, for work enqueued on torch's current stream)."""
+    (None: allocated here, from the memory of the call's stream)."""
     d = _desc(x, layout)
     shape, dtype, c = x.shape, x.dtype, d.c
     _alike(y, shape, dtype, "y")
@@ -532,7 +538,7 @@ def bc_layer_norm_grad(x, layout, gamma, y, grad_out, eps, grad_in, grad_res, dg
     _per_channel(dgamma, c, "dgamma")
     _per_channel(dbeta, c, "dbeta")
     if work is None:
-        work = _work(bc_layer_norm_grad_work(x, layout), x)
+        work = _work(bc_layer_norm_grad_work(x, layout), x, stream)
     st = _lib.bc_layer_norm_grad(_ptr(x), d, _ptr(gamma), _ptr(y), _ptr(grad_out), float(eps), _ptr(grad_in),
                                  _ptr(grad_res), _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(work),
                                  _nbytes(work), _stream(stream))
@@ -566,7 +572,7 @@ def bc_orthogonalize(g, out, steps=NS_STEPS, coef=NS_COEF, eps=NS_EPS, work=None
     if out.shape != g.shape or not out.is_contiguous():
         raise ValueError("out must be contiguous and shaped like g")
     if work is None:
-        work = _work(bc_orthogonalize_work(g, steps), g)
+        work = _work(bc_orthogonalize_work(g, steps), g, stream)
     st = _lib.bc_orthogonalize(_ptr(g), _dtype_code(g), *_matrices(g),
                                ctypes.byref(_newton_schulz(steps, tuple(coef), eps)), _ptr(out),
                                _dtype_code(out), _ptr(work), _nbytes(work), _stream(stream))
@@ -605,7 +611,7 @@ def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=N
     bc_layer_norm_grad."""
     arr, dt = _matrix_array(params)
     if work is None:
-        work = _work(bc_muon_step_many_work(params, steps), params[0][0])
+        work = _work(bc_muon_step_many_work(params, steps), params[0][0], stream)
     h = bc_muon(float(lr), float(momentum), float(weight_decay), int(nesterov),
                 _newton_schulz(steps, tuple(coef), eps))
     st = _lib.bc_muon_step_many(arr, len(params), ctypes.byref(h), dt, _ptr(work), _nbytes(work), _stream(stream))

@@ -280,6 +280,40 @@ def test_streams_and_graph(bc):
             assert torch.equal(w, w1) and torch.equal(m, m1) and (g == 0).all()
 
 
+@pytest.mark.parametrize("by_handle", [False, True])
+def test_workspace_belongs_to_the_stream(bc, monkeypatch, by_handle):
+    """Calls on a stream that is not torch's current one and bring no workspace: what they take
+    is not given to the current stream, whose work is not ordered with theirs, behind them."""
+    made, real = [], bc._work
+
+    def spy(*args):
+        t = real(*args)
+        made.append((t.data_ptr(), t.numel()))
+        return t
+
+    monkeypatch.setattr(bc, "_work", spy)
+    g = gradient(11, 300, 400).cuda()
+    params = [(g.clone(), g.clone(), g.clone(), None)]
+    x, gamma = torch.randn(1, 32, 32, 4096, device="cuda"), torch.rand(4096, device="cuda")
+    dx, dg = torch.empty_like(x), torch.empty_like(gamma)
+    out, want = torch.empty_like(g), torch.empty_like(g)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    at = side.cuda_stream if by_handle else side
+    for call in (lambda s: bc.bc_orthogonalize(g, out, stream=s),
+                 lambda s: bc.bc_muon_step_many(params, 0.1, 0.9, 0.0, stream=s),
+                 lambda s: bc.bc_layer_norm_grad(x, bc.BC_NHWC, gamma, None, x, 1e-5, dx, None, dg, None, stream=s)):
+        torch.cuda.empty_cache()
+        call(at)
+        begin, size = made[-1]
+        assert size > 1 << 20
+        others = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        assert all(t.data_ptr() >= begin + size or t.data_ptr() + size <= begin for t in others)
+        side.synchronize()
+    bc.bc_orthogonalize(g, want)
+    assert torch.equal(out, want)
+
+
 def test_offsets_past_32_bits(bc):
     """A matrix whose X passes 2^32 bytes, with one element per row: its singular values are
     those elements, and each becomes what the iteration makes of it alone."""
