@@ -436,6 +436,14 @@ def bc_conv2d_weight_grad(geom, x, grad_out, dw, db=None, stream=None):
     _check(st, "bc_conv2d_weight_grad")
 
 
+def _copies_dtype(params) -> int:
+    """The dtype that all 16-bit copies, the last of each of `params`, share (bf16 without any)."""
+    dts = {_dtype_code(p[3]) for p in params if p[3] is not None}
+    if len(dts) > 1:
+        raise ValueError("the 16-bit copies must share one dtype")
+    return dts.pop() if dts else BC_BF16
+
+
 def bc_rmsprop_step(w, v, grad, lr, alpha, eps, weight_decay, w16=None, stream=None):
     """One RMSprop step on float32 tensors w, v, grad (grad reset to 0), and the 16-bit
     copy w16 (same element count) if given."""
@@ -449,11 +457,9 @@ def bc_rmsprop_step_many(params, lr, alpha, eps, weight_decay, stream=None):
     """bc_rmsprop_step on every (w, v, grad, w16 or None) of `params` in one launch; the
     16-bit copies share one dtype."""
     arr = (bc_param * len(params))()
-    dt = BC_BF16
+    dt = _copies_dtype(params)
     for i, (w, v, grad, w16) in enumerate(params):
         arr[i] = bc_param(_ptr(w), _ptr(v), _ptr(grad), _ptr(w16), int(w.numel()))
-        if w16 is not None:
-            dt = _dtype_code(w16)
     st = _lib.bc_rmsprop_step_many(arr, len(params), float(lr), float(alpha), float(eps),
                                    float(weight_decay), dt, _stream(stream))
     _check(st, "bc_rmsprop_step_many")
@@ -581,7 +587,7 @@ def bc_orthogonalize(g, out, steps=NS_STEPS, coef=NS_COEF, eps=NS_EPS, work=None
 
 def _matrix_array(params):
     arr = (bc_matrix * len(params))()
-    dt = BC_BF16
+    dt = _copies_dtype(params)
     for a, (w, m, grad, w16) in zip(arr, params):
         count, rows = w.numel(), w.shape[0]
         for t in (w, m, grad):
@@ -592,7 +598,7 @@ def _matrix_array(params):
         if w16 is not None:
             if w16.numel() != count or not w16.is_contiguous():
                 raise ValueError("the 16-bit copy must be contiguous and as large as the weights")
-            a.w16, dt = w16.data_ptr(), _dtype_code(w16)
+            a.w16 = w16.data_ptr()
     return arr, dt
 
 

@@ -157,6 +157,24 @@ def test_binding_refuses_mismatched_tensors(B):
         B.bc_muon_step_many([(g, g.clone(), g.double(), None)], 0.1, 0.9, 0.0)
 
 
+def test_copies_of_two_dtypes(B):
+    """All 16-bit copies of a step are written in one format: two are refused, in any order."""
+    def param(dt):
+        w = torch.zeros(8, 16)
+        return w, torch.zeros_like(w), torch.zeros_like(w), None if dt is None else torch.zeros(8, 16, dtype=dt)
+
+    bf16, f16, f32 = torch.bfloat16, torch.float16, torch.float32
+    for dts in ((bf16, f16), (f16, None, bf16), (f32, bf16), (bf16, bf16, f16, bf16)):
+        params = [param(d) for d in dts]
+        with pytest.raises(ValueError):
+            B.bc_muon_step_many(params, 0.1, 0.9, 0.0)
+        with pytest.raises(ValueError):
+            B.bc_muon_step_many_work(params)
+        with pytest.raises(ValueError):
+            B.bc_rmsprop_step_many(params, 0.1, 0.9, 1e-8, 0.0)
+    assert B.bc_muon_step_many_work([param(f16), param(None), param(f16)]) > 0
+
+
 def test_policy_norm_refusal(B):
     from paper_2108_09376_amd import resnet
     with pytest.raises(ValueError):
