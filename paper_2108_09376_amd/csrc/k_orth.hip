@@ -1194,6 +1194,9 @@ __global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, F
 
 // ---------------------------------------------------------------- host: what is launched when
 
+// Steps of the span that begins at step `at` of `steps`.
+int span_steps(int at, int steps, bool direct) { return std::min(steps - at, direct ? 1 : at == 0 ? kSpan : 2); }
+
 // The products of a matrix in order, one entry per launch.
 std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
 {
@@ -1205,9 +1208,8 @@ std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
         all.push_back(p);
     };
     int x = kX0;
-    for (int left = ns.steps, most = direct ? 1 : kSpan; left; most = std::min(most, 2)) {
-        const int k = std::min(left, most);
-        left -= k;
+    for (int at = 0, k; at < ns.steps; at += k) {
+        k = span_steps(at, ns.steps, direct);
         int p = kNone;
         symmetric({{x, x, kNone, kNone, kA, 0.f, 0.f, 1.f}});
         for (int i = 0; i < k; ++i) {
@@ -1228,7 +1230,7 @@ std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
         const int to = x == kX0 ? kX1 : kX0;
         OrthPlan q{};
         q.jobs = 1;
-        q.last = left == 0;
+        q.last = at + k == ns.steps;
         q.job[0] = {p, x, x, kNone, to, ak, 0.f, ak};
         all.push_back(q);
         x = to;
@@ -1414,9 +1416,13 @@ bool orth_supported(const NewtonSchulz &ns, const char **why)
     }
     // Bounds over the singular values in [0, top]: 1 + B at the ends and the vertex of its
     // parabola, the step's polynomial at the ends and where its derivative is zero.
+    // The factors of a span's steps multiply up in P.
     double top = 1.0, factors = 1.0;
-    for (int i = 0; i < ns.steps; ++i) {
-        if (i % kSpan == 0) factors = 1.0;
+    for (int i = 0, next_span = 0; i < ns.steps; ++i) {
+        if (i == next_span) {
+            factors = 1.0;
+            next_span += span_steps(i, ns.steps, false);
+        }
         const double lam = top * top;
         auto factor = [&](double t) { return 1.0 + (b * t + c * t * t) / a; };
         double f = std::max(1.0, std::fabs(factor(lam)));

@@ -110,6 +110,32 @@ def test_other_coefficients(bc, coef):
     check(out, *bounds(g, "f32", steps=4, coef=coef, eps=1e-6), "f32")
 
 
+@pytest.mark.parametrize("coef", [COEF, (1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5)])
+@pytest.mark.parametrize("steps", [2, 4, 5, 7, 8])
+def test_other_coefficients_in_spans(bc, coef, steps):
+    g = gradient(12, 400, 600, "noise").cuda()
+    out = torch.empty_like(g)
+    bc.bc_orthogonalize(g, out, steps=steps, coef=coef)
+    check(out, *bounds(g, "f32", steps=steps, coef=coef), "f32")
+
+
+def test_one_value_in_spans(bc):
+    """One element, whose singular value is 1: the factors of a span are as large as the check of
+    the coefficients counts them (2.19 three times, 10.5, in the first)."""
+    coef = (0.45704228, -0.49950711, 1.04263144)
+    g = torch.zeros(500, 1000, device="cuda")
+    g[3, 5] = 1.0
+    out = torch.empty_like(g)
+    for steps in (3, 5, 6):
+        bc.bc_orthogonalize(g, out, steps=steps, coef=coef, eps=0.0)
+        s = 1.0
+        for _ in range(steps):                             # an error grows less than fivefold a step, on the mean
+            s = coef[0] * s + coef[1] * s ** 3 + coef[2] * s ** 5
+        assert abs(out[3, 5].item() - s) <= 2e-6 * 5.0 ** steps * s
+        out[3, 5] = 0.0
+        assert not out.any()
+
+
 @pytest.mark.parametrize("batch,m,n", [(1, 40, 50), (3, 65, 33), (12, 193, 301), (40, 17, 70), (300, 8, 16)])
 def test_batches(bc, batch, m, n):
     """Each matrix by itself: a matrix of a batch has the bits it has alone; formats may

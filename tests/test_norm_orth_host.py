@@ -93,6 +93,22 @@ def test_orthogonalize_refusals(B):
         assert call(**bad) == B.BC_ERR_ALIAS, bad
 
 
+def test_coefficients_of_late_spans(B):
+    """Steps 5 and 6 (from 0) are one span. With these coefficients a singular value of 1 stays
+    near 1 until step 5 and grows by 2.73 and 6.31 there: their product, 17.2, is beyond the 16
+    bits that the span's factor is held in. Fewer steps stay within, in any span."""
+    def call(steps, c):
+        return B.raw().bc_orthogonalize(A, 0, 1, 500, 1000, ctypes.byref(B.bc_newton_schulz(steps, *c, 0.0)), B_, 0, W,
+                                        0, None)
+
+    for c in ((0.45704228, -0.49950711, 1.04263144), (0.45456629, -0.77823198, -0.67638974)):
+        assert call(7, c) == B.BC_ERR_UNSUPPORTED, c
+        for steps in range(1, 7):                          # the check behind theirs: no workspace
+            assert call(steps, c) == B.BC_ERR_CAPACITY, (steps, c)
+    for steps in range(1, 65):
+        assert call(steps, (3.4445, -4.7750, 2.0315)) == call(steps, (1.5, -0.5, 0.0)) == B.BC_ERR_CAPACITY
+
+
 def test_muon_refusals(B):
     lib = B.raw()
     ns = (5, 3.4445, -4.7750, 2.0315, 1e-7)
