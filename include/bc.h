@@ -644,7 +644,8 @@ bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32
  *                and 4e9 elements); d_out may be d_g itself if the dtypes agree.
  * fp32 accuracy whatever the dtypes (operands held as two fp16 numbers, three matrix-core
  * products, fp32 sums; the norm in fp64), one round to out_dtype. A matrix of zeros gives
- * zeros (eps > 0); a NaN or infinity stays within its matrix. Equal inputs give equal bits.
+ * zeros (eps > 0); a NaN or infinity stays within its matrix. Equal inputs give equal bits; a
+ * matrix of a batch has the bits it has alone, or, with a side above 1408, agrees to rounding.
  *   ns       a > 0, and coefficients under which no value of the iteration passes 15 for
  *            singular values in [0, 1] (else BC_ERR_UNSUPPORTED).
  *   d_work   as for bc_layer_norm_grad, bc_orthogonalize_work bytes.
@@ -679,8 +680,9 @@ bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t ste
  * X(u) as bc_orthogonalize gives it in fp32, and w16, if not NULL, the weights rounded to
  * `dtype` (BC_BF16 or BC_F16). `params` is a host array read during the call. No two buffers
  * may overlap. d_work as for bc_orthogonalize, bc_muon_step_many_work bytes. Equal calls give
- * equal bits. The order of a long product's sums (over 1536 elements and more) depends on the
- * sizes of all matrices of the call: alone and among others such a matrix agrees to rounding.
+ * equal bits, and a matrix has the bits it has alone, but where its longer side is above 1408:
+ * the order of sums that long depends on the sizes of all matrices of the call, and alone and
+ * among others such a matrix agrees to rounding.
  * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_CAPACITY, BC_ERR_ALIAS,
  * BC_ERR_UNSUPPORTED, BC_ERR_HIP.
  */

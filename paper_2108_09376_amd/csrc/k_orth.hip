@@ -635,8 +635,10 @@ __device__ __forceinline__ void multiply(uint8_t *smem, const Operand &L, const 
     *behind = at / kBlockBytes;
 }
 
-// Chunks of K of a product, tiles of a matrix with `jobs` of them, and K ranges of about
-// `each` chunks (0: whole).
+// Chunks of K of a product, tiles of a matrix with `jobs` of them, and K ranges of `each` chunks
+// (0: whole) where there are three at least: a shorter product is whole in every launch, so its
+// bits do not depend on the longer ones beside it (in ranges as well: the policy network's step
+// 144 us for 150, steps of other networks 0 to 2 % slower).
 __host__ __device__ inline int chunks_of(const OrthPlan &p, const Slot &s) { return (p.job[0].L <= kX1 ? s.n : s.m) / kK; }
 
 // Row i of a symmetric product's tiles holds those that reach the diagonal: i I / J .. m / J - 1.
@@ -648,7 +650,7 @@ __host__ __device__ inline uint32_t tiles_of(const OrthPlan &p, const Slot &s)
     return p.sym ? i * j - FI / FJ * (i * (i - 1) / 2) : i * j;
 }
 
-__host__ __device__ inline int ranges_of(int chunks, int each) { return each ? (chunks + each - 1) / each : 1; }
+__host__ __device__ inline int ranges_of(int chunks, int each) { return each && chunks >= 3 * each ? (chunks + each - 1) / each : 1; }
 
 template <int FI, int FJ>
 __host__ __device__ inline uint32_t products_of(const OrthPlan &p, const OrthShape &e, int each)

@@ -249,6 +249,30 @@ def test_step_equals_its_parts(bc):
         assert ((w + rate * o).abs() <= 2.0 ** -22 * rate * o.abs()).all()
 
 
+@pytest.mark.parametrize("shapes,long", [([(64, 576), (128, 1152), (576, 64), (200, 1408)], (64, 2304)),
+                                         ([(64, 1000), (1400, 130), (300, 900)], (4000, 100)),
+                                         ([(64, 640), (150, 800)], (300, 4608))])
+def test_step_beside_long_products(bc, shapes, long):
+    """A product along more than 1408 elements may be summed in ranges. The matrices beside it have
+    the bits they have alone; it agrees with itself to rounding."""
+    make = lambda ss: [(gradient(i + 60, *s).cuda(), torch.zeros(s, device="cuda"), gradient(i, *s).cuda(), None)
+                       for i, s in enumerate(ss)]
+    together, alone = make(shapes + [long]), make(shapes + [long])
+    before = [p[0].double().cpu() for p in alone]
+    bc.bc_muon_step_many(together, 0.1, 0.9, 0.0)
+    for p in alone:
+        bc.bc_muon_step_many([p], 0.1, 0.9, 0.0)
+    for i, (p, q) in enumerate(zip(together, alone)):
+        if i < len(shapes):
+            assert torch.equal(p[0], q[0]), shapes[i]
+    g = gradient(len(shapes), *long)
+    o, tol = bounds(g.double() * 1.9, "f32")
+    rate = 0.1 * math.sqrt(max(1.0, long[0] / long[1]))
+    for p in (together[-1], alone[-1]):
+        err = (p[0].double().cpu() - (before[-1] - rate * o)).norm().item()
+        assert err <= rate * (tol + 2.0 ** -22) * o.norm().item() + 2.0 ** -23 * before[-1].norm().item()
+
+
 @pytest.mark.parametrize("nesterov", [False, True])
 def test_small_matrices_alone_and_among_large(bc, nesterov):
     """Small matrices take one launch by themselves and the products' launches beside larger ones:
