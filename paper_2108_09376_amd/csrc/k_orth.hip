@@ -277,6 +277,13 @@ __host__ __device__ inline int sum_parts(size_t count)
     return (int)(parts < kSumParts ? parts : kSumParts);
 }
 
+// Elements of each part: four per thread and turn, so the last part may be short or empty.
+__host__ __device__ inline size_t sum_each(size_t count)
+{
+    const size_t parts = sum_parts(count);
+    return ((count + parts - 1) / parts + 3) / 4 * 4;
+}
+
 __host__ __device__ inline uint32_t start_tiles(const OrthShape &e)
 {
     const Slot s = slot_of(e.rows, e.cols);
@@ -299,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_sums(Matrices<MANY> M, OrthHe
         for (int i = threadIdx.x; i < kMostSplit; i += kThreads) head->count[i] = 0u;
     const Where w = find(M, blockIdx.x, per);
     const OrthShape &e = w.e;
-    const size_t count = (size_t)e.rows * e.cols, parts = sum_parts(count), each = ((count + parts - 1) / parts + 3) / 4 * 4;
+    const size_t count = (size_t)e.rows * e.cols, each = sum_each(count);
     const size_t lo = w.local * each, hi = lo + each < count ? lo + each : count;
     double sum = 0.0;
 #pragma unroll 2
@@ -939,14 +946,60 @@ __global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, F
     static_assert(kTurns >= 1 && F::kThreads == 512, "four blocks a turn");
     {
         float u[kTurns][8];
-        int at[kTurns];
+        // row and first column of X, neighbours along a row of G
+        struct Cell {
+            int r, c;
+        };
+        auto cell = [&](int t) -> Cell {
+            const int blk = t * 4 + wave / 2, k = tid & 127;
+            return {blk / F::kCB * kBlock + (flip ? k & 31 : k >> 2), blk % F::kCB * kBlock + (flip ? k >> 5 : k & 3) * 8};
+        };
+        // The norm: the squares in the order in which k_orth_sums and k_orth_start take them, four
+        // waves for each of four parts at most, or the last bits would depend on the kernel. The
+        // elements are read again for it, all at once (through LDS instead, from the lanes that
+        // hold them: 64 x 147 30.3 us, 64 x 512 58.7).
+        double *const sums = (double *)A;                  // [part][wave of four]
+        constexpr int kParts = M * F::C <= kSumEach ? 1 : M * F::C / kSumEach, kReads = kSumEach / 1024;
+        static_assert(kParts <= 4 && M * F::C <= kParts * kSumEach, "parts of a matrix");
+        auto squares = [&] {
+            const int each = (int)sum_each(count);
+#pragma unroll 1
+            for (int part = wave >> 2; part < kParts; part += 2) {
+                const int lo = part * each + (tid & 255) * 4, hi = min((int)count, (part + 1) * each);
+                float v[kReads][4];
+#pragma unroll
+                for (int k = 0; k < kReads; ++k) {
+                    const int i = lo + k * 1024;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[k][j] = 0.f;
+                    if (i >= hi) continue;
+                    if constexpr (MANY) {
+                        const OrthParam &p = Ms.p[w.t];
+                        float g[4], mom[4];
+                        load4<kF32>(p.grad, i, hi, g);
+                        load4<kF32>(p.mom, i, hi, mom);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[k][j] = look_ahead(h, g[j], moved(h, g[j], mom[j]));
+                    } else {
+                        load4<FMT>((const uint8_t *)Ms.g + w.img * count * kElem<FMT>, i, hi, v[k]);
+                    }
+                }
+                double sum = 0.0;
+#pragma unroll
+                for (int k = 0; k < kReads; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum += (double)v[k][j] * v[k][j];
+                sum = wave_sum(sum);
+                if (lane == 0) sums[part * 4 + (wave & 3)] = sum;
+            }
+        };
+        if constexpr (MANY) {                              // before the gradients and momenta are written
+            squares();
+            __syncthreads();
+        }
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
-            const int blk = t * 4 + wave / 2, bi = blk / F::kCB, bj = blk % F::kCB, k = tid & 127;
-            // neighbours along a row of G
-            const int r = flip ? k & 31 : k >> 2, c = (flip ? k >> 5 : k & 3) * 8;
-            at[t] = bj * kBlock < cols ? (bi * F::kCB + bj) * kBlockBytes + in_block(r, c) : -1;
-            const int xr = bi * kBlock + r, xc = bj * kBlock + c;
+            const auto [xr, xc] = cell(t);
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[t][j] = 0.f;
             if (xr >= m || xc >= n) continue;
@@ -991,17 +1044,12 @@ __global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, F
                 for (int j = 0; j < 4; ++j) u[t][v * 4 + j] = g[j];
             }
         }
-        double *const sums = (double *)A;
-        double sum = 0.0;
-#pragma unroll
-        for (int t = 0; t < kTurns; ++t)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += (double)u[t][j] * u[t][j];
-        sum = wave_sum(sum);
-        if (lane == 0) sums[wave] = sum;
+        if constexpr (!MANY) squares();
         __syncthreads();
-        sum = 0.0;
-        for (int i = 0; i < F::kWaves; ++i) sum += sums[i];
+        auto part_sum = [&](int k) {
+            return k < kParts ? (sums[4 * k] + sums[4 * k + 1]) + (sums[4 * k + 2] + sums[4 * k + 3]) : 0.0;
+        };
+        const double sum = (part_sum(0) + part_sum(2)) + (part_sum(1) + part_sum(3));
         const Factor by = factor_of(sum, S.eps);
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
@@ -1013,9 +1061,11 @@ __global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, F
                 hi[j] = part.hi;
                 lo[j] = part.lo;
             }
-            if (at[t] < 0) continue;
-            *(f16x8 *)(X + at[t]) = hi;
-            *(f16x8 *)(X + at[t] + kBlockPlane) = lo;
+            const auto [xr, xc] = cell(t);
+            if (xc / kBlock * kBlock >= cols) continue;
+            uint8_t *at = X + ((xr >> 5) * F::kCB + (xc >> 5)) * kBlockBytes + in_block(xr, xc);
+            *(f16x8 *)at = hi;
+            *(f16x8 *)(at + kBlockPlane) = lo;
         }
     }
     __syncthreads();

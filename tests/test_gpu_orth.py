@@ -296,6 +296,27 @@ def test_small_matrices_alone_and_among_large(bc, nesterov):
                 x[2].copy_(gradient(77, *s))
 
 
+# Normal values (8 x 16 by seed) with two of them set so that the sum of squares lies where its
+# last bit in 64 bits, that is the order of summation, decides on the norm's rounding to 32.
+EDGES = [(0, "0x1.e7dab4p-1", "0x1.6ef872p-13"), (1, "0x1.d1f888p-1", "0x1.2a1f0cp-12"),
+         (2, "0x1.ed6dc6p-1", "0x1.8cc1e0p-13"), (4, "0x1.0016c4p+0", "0x1.c7fd54p-13"),
+         (9, "0x1.0a11d8p+0", "0x1.69c1a4p-13"), (12, "0x1.e3d394p-1", "0x1.0075cep-12"),
+         (17, "0x1.0a327ep+0", "0x1.5b1508p-12"), (18, "0x1.e9e41ep-1", "0x1.441b9cp-12")]
+
+
+@pytest.mark.parametrize("seed,first,last", EDGES)
+def test_norm_in_one_order(bc, seed, first, last):
+    """The norm's sum is taken in one order, whichever kernel takes it: the bits are the same alone
+    and beside a larger matrix."""
+    g = np.random.default_rng(seed).standard_normal((8, 16)).astype(np.float32)
+    g[0, 0], g[7, 15] = float.fromhex(first), float.fromhex(last)
+    make = lambda a: (torch.zeros(a.shape, device="cuda"), torch.zeros(a.shape, device="cuda"), torch.from_numpy(a).cuda(), None)
+    alone, beside = make(g), make(g)
+    bc.bc_muon_step_many([alone], 1.0, 0.0, 0.0, nesterov=False, eps=0.0)
+    bc.bc_muon_step_many([beside, make(np.ones((300, 400), np.float32))], 1.0, 0.0, 0.0, nesterov=False, eps=0.0)
+    assert torch.equal(alone[0], beside[0])
+
+
 def test_streams_and_graph(bc):
     """On a stream of its own, and captured: replays equal eager calls on new gradients."""
     shapes = [(64, 576), (300, 200)]
