@@ -640,8 +640,10 @@ bc_status bc_orthogonalize_work(int32_t batch, int32_t rows, int32_t cols, int32
 /*
  * Orthogonalises each of `batch` matrices: d_out = X of the iteration *ns on d_g.
  *   d_g, d_out   [batch][rows][cols] of in_dtype and out_dtype (any dtypes, any element
- *                alignment, any sizes >= 1 up to 16384 for the shorter side, 2^22 for the longer
- *                and 4e9 elements); d_out may be d_g itself if the dtypes agree.
+ *                alignment, any sizes >= 1 up to 16384 for the shorter side, 2^22 for the longer,
+ *                4e9 elements, and fewer than 2^24 tiles of 64 x 64 in all matrices of the
+ *                call, each padded to multiples of 128: 2^22 - 1 matrices of 30 x 31, 127
+ *                of 1 x 2^22); d_out may be d_g itself if the dtypes agree.
  * fp32 accuracy whatever the dtypes (operands held as two fp16 numbers, three matrix-core
  * products, fp32 sums; the norm in fp64), one round to out_dtype. A matrix of zeros gives
  * zeros (eps > 0); a NaN or infinity stays within its matrix. Equal inputs give equal bits; a
@@ -674,7 +676,8 @@ bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t ste
                                  int64_t *bytes);
 
 /*
- * One orthogonalised step of n weight matrices (1 <= n <= 64), all in the same launches:
+ * One orthogonalised step of n weight matrices (1 <= n <= 64, sizes and tiles together within
+ * bc_orthogonalize's limits), all in the same launches:
  *   m = momentum m + grad;  u = nesterov ? grad + momentum m : m;
  *   w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) X(u);  grad = 0;
  * X(u) as bc_orthogonalize gives it in fp32, and w16, if not NULL, the weights rounded to

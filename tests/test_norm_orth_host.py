@@ -93,6 +93,19 @@ def test_orthogonalize_refusals(B):
         assert call(**bad) == B.BC_ERR_ALIAS, bad
 
 
+def test_tiles_of_a_call(B):
+    """As many matrices as the header promises, and not one more."""
+    n = ctypes.c_int64()
+    for most, rows, cols in ((2 ** 22 - 1, 1, 1), (2 ** 22 - 1, 30, 31), (127, 1, 2 ** 22), (127, 2 ** 22, 5)):
+        assert B.raw().bc_orthogonalize_work(most, rows, cols, 5, ctypes.byref(n)) == B.BC_OK and n.value > 0
+        assert B.raw().bc_orthogonalize_work(most + 1, rows, cols, 5, ctypes.byref(n)) == B.BC_ERR_SHAPE
+    params = (B.bc_matrix * 64)()
+    for p in params:
+        p.rows, p.cols = 2 ** 22, 200                      # 2^18 tiles each
+    assert B.raw().bc_muon_step_many_work(params, 63, 5, ctypes.byref(n)) == B.BC_OK and n.value > 0
+    assert B.raw().bc_muon_step_many_work(params, 64, 5, ctypes.byref(n)) == B.BC_ERR_SHAPE
+
+
 def test_coefficients_of_late_spans(B):
     """Steps 5 and 6 (from 0) are one span. With these coefficients a singular value of 1 stays
     near 1 until step 5 and grows by 2.73 and 6.31 there: their product, 17.2, is beyond the 16
