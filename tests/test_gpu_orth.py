@@ -84,6 +84,56 @@ def test_sizes_and_formats(bc, dtype, m, n):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("m,n", [(1800, 2000), (2000, 1800), (1700, 2300), (300, 4608), (4608, 300), (64, 4096), (512, 4608),
+                                 (700, 2100)])
+@pytest.mark.parametrize("kind", ["fall", "noise"])
+def test_large_and_long(bc, m, n, kind):
+    """Dense matrices of enough tiles for the large ones in every product, step by step and in
+    spans (two jobs and two addends in a launch), and products long enough for ranges of K, whose
+    sums meet in no fixed order of arrival: the same bits in every run."""
+    g = gradient(m + n, m, n, kind)
+    out, again = torch.empty_like(g, device="cuda"), torch.empty_like(g, device="cuda")
+    g = g.cuda()
+    bc.bc_orthogonalize(g, out)
+    check(out, *bounds(g, "f32"), "f32")
+    for _ in range(3):
+        bc.bc_orthogonalize(g, again)
+        assert torch.equal(out, again)
+
+
+def test_batch_in_large_tiles(bc):
+    """40 matrices of 193 x 301 take the large tiles, one of them the small ones: the same bits."""
+    g = torch.stack([gradient(500 + i, 193, 301) for i in range(40)]).cuda()
+    out, alone = torch.empty_like(g), torch.empty_like(g[0])
+    bc.bc_orthogonalize(g, out)
+    for i in (0, 1, 19, 39):
+        bc.bc_orthogonalize(g[i], alone)
+        assert torch.equal(out[i], alone)
+        check(out[i], *bounds(g[i], "f32"), "f32")
+
+
+@pytest.mark.parametrize("shapes", [[(1800, 2000), (600, 700), (64, 2304)],               # large tiles, 48 chunks and more whole
+                                    [(300, 400)] * 40,                                    # large tiles, many matrices
+                                    [(700, 5000), (400, 1200), (2304, 64), (128, 1152)]])  # in ranges beside short ones
+def test_step_of_large_and_long(bc, shapes):
+    """The step over many matrices against each by itself: to the bit up to 1408, else to rounding."""
+    params = [(torch.zeros(s, device="cuda"), torch.zeros(s, device="cuda"), gradient(i + 600, *s).cuda(), None)
+              for i, s in enumerate(shapes)]
+    alone = [tuple(None if t is None else t.clone() for t in p) for p in params]
+    again = [tuple(None if t is None else t.clone() for t in p) for p in params]
+    bc.bc_muon_step_many(params, 1.0, 0.0, 0.0, nesterov=False)
+    bc.bc_muon_step_many(again, 1.0, 0.0, 0.0, nesterov=False)
+    for i, (p, a, b) in enumerate(zip(params, alone, again)):
+        assert torch.equal(p[0], b[0])
+        if i % 13 == 0 or len(shapes) < 13:
+            bc.bc_muon_step_many([a], 1.0, 0.0, 0.0, nesterov=False)
+            if max(shapes[i]) <= 1408:
+                assert torch.equal(p[0], a[0])
+            rate = math.sqrt(max(1.0, shapes[i][0] / shapes[i][1]))
+            for w in (p[0], a[0]):
+                check(w / -rate, *bounds(gradient(i + 600, *shapes[i]), "f32"), "f32")
+
+
 @pytest.mark.parametrize("m,n", [(64, 64), (96, 512), (256, 256), (300, 90)])
 @pytest.mark.parametrize("kind", ["noise", "rank"])
 def test_spectra(bc, m, n, kind):
