@@ -1127,10 +1127,10 @@ struct Extent {
     size_t b;
 };
 
-static bool any_overlap(std::vector<Extent> &v)
+static bool any_overlap(Extent *v, int n)
 {
-    std::sort(v.begin(), v.end(), [](const Extent &x, const Extent &y) { return (uintptr_t)x.p < (uintptr_t)y.p; });
-    for (size_t i = 0; i + 1 < v.size(); ++i)
+    std::sort(v, v + n, [](const Extent &x, const Extent &y) { return (uintptr_t)x.p < (uintptr_t)y.p; });
+    for (int i = 0; i + 1 < n; ++i)
         if (overlap(v[i].p, v[i].b, v[i + 1].p, v[i + 1].b)) return true;
     return false;
 }
@@ -1320,19 +1320,20 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
     if ((st = orth_iteration(muon->ns, it))) return st;
     if ((st = check_work(d_work, work_bytes, need))) return st;
     T.work = (uint8_t *)d_work;
-    std::vector<Extent> all = {{d_work, need}};
+    Extent all[4 * bc::kMaxParams + 1] = {{d_work, need}};
+    int extents = 1;
     bool any16 = false;
     for (int t = 0; t < n; ++t) {
         const bc_matrix &p = params[t];
         if (!p.w || !p.momentum || !p.grad) return fail(BC_ERR_NULL, "params[%d]: w, momentum and grad are required", t);
         const size_t count = (size_t)p.rows * p.cols;
-        for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all.push_back({q, count * 4});
-        if (p.w16) all.push_back({p.w16, count * 2});
+        for (const void *q : {(const void *)p.w, (const void *)p.momentum, (const void *)p.grad}) all[extents++] = {q, count * 4};
+        if (p.w16) all[extents++] = {p.w16, count * 2};
         any16 = any16 || p.w16;
         T.p[t] = {p.w, p.momentum, p.grad, (uint16_t *)p.w16};
     }
     if (any16 && dtype != BC_BF16 && dtype != BC_F16) return fail(BC_ERR_DTYPE, "the copies must be bf16 or f16");
-    if (any_overlap(all)) return fail(BC_ERR_ALIAS, "the optimiser's buffers overlap");
+    if (any_overlap(all, extents)) return fail(BC_ERR_ALIAS, "the optimiser's buffers overlap");
     const bc::OrthStep h = {muon->lr, muon->momentum, 1.f - muon->lr * muon->weight_decay, muon->nesterov};
     hipError_t e = bc::launch_orth(T, h, true, BC_F32, dtype == BC_F16 ? BC_F16 : BC_BF16, it, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "orthogonalised step launch");

@@ -26,7 +26,6 @@
 // the coefficients), as |X|_2 <= 1 at the start.
 #include <algorithm>
 #include <cmath>
-#include <vector>
 
 #include "bc_internal.h"
 #include "lds_dma.h"
@@ -1246,18 +1245,33 @@ __global__ __launch_bounds__(F::kThreads) void k_orth_fused(Matrices<MANY> Ms, F
 
 // ---------------------------------------------------------------- host: what is launched when
 
+// A list of at most N, in place: nothing here allocates, so no call can end in an exception.
+template <typename T, int N>
+struct List {
+    T at[N];
+    int n = 0;
+
+    void add(const T &x) { at[n++] = x; }
+    const T *begin() const { return at; }
+    const T *end() const { return at + n; }
+};
+
+// Launches of products at most: 64 steps in spans of 3, 2, 2, ... take 10 + 30 * 7 + 3, one by
+// one 3 each.
+constexpr int kMostLaunches = 224;
+
 // Steps of the span that begins at step `at` of `steps`.
 int span_steps(int at, int steps, bool direct) { return std::min(steps - at, direct ? 1 : at == 0 ? kSpan : 2); }
 
 // The products of a matrix in order, one entry per launch.
-std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
+List<OrthPlan, kMostLaunches> plans_of(const NewtonSchulz &ns, bool direct)
 {
-    std::vector<OrthPlan> all;
+    List<OrthPlan, kMostLaunches> all;
     auto symmetric = [&](std::initializer_list<OrthJob> jobs) {
         OrthPlan p{};
         p.sym = 1;
         for (const OrthJob &j : jobs) p.job[p.jobs++] = j;
-        all.push_back(p);
+        all.add(p);
     };
     int x = kX0;
     for (int at = 0, k; at < ns.steps; at += k) {
@@ -1284,7 +1298,7 @@ std::vector<OrthPlan> plans_of(const NewtonSchulz &ns, bool direct)
         q.jobs = 1;
         q.last = at + k == ns.steps;
         q.job[0] = {p, x, x, kNone, to, ak, 0.f, ak};
-        all.push_back(q);
+        all.add(q);
         x = to;
     }
     return all;
@@ -1323,17 +1337,17 @@ struct Launch {
     size_t part_bytes;                         // of the sums of K ranges
 };
 
-std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
+List<Launch, kMostLaunches> launches_of(const OrthTable &T, const NewtonSchulz &ns)
 {
-    std::vector<OrthPlan> plans[2];
+    List<OrthPlan, kMostLaunches> plans[2];
     for (int t = 0; t < T.n; ++t) {
         const bool direct = steps_direct(T.e[t].rows, T.e[t].cols);
-        if (plans[direct].empty()) plans[direct] = plans_of(ns, direct);
+        if (!plans[direct].n) plans[direct] = plans_of(ns, direct);
     }
-    std::vector<Launch> all(std::max(plans[0].size(), plans[1].size()));
-    for (size_t i = 0; i < all.size(); ++i) {
-        Launch &l = all[i];
-        for (int d = 0; d < 2; ++d) l.plan[d] = i < plans[d].size() ? plans[d][i] : OrthPlan{};
+    List<Launch, kMostLaunches> all;
+    for (int i = 0; i < std::max(plans[0].n, plans[1].n); ++i) {
+        Launch l{};
+        for (int d = 0; d < 2; ++d) l.plan[d] = i < plans[d].n ? plans[d].at[i] : OrthPlan{};
         auto total = [&](auto count) {
             uint64_t n = 0;
             for (int t = 0; t < T.n; ++t) {
@@ -1367,6 +1381,7 @@ std::vector<Launch> launches_of(const OrthTable &T, const NewtonSchulz &ns)
         l.each = longest >= 3 * share && wgs <= 512 ? (int)share : 0;
         const uint64_t places = tiles(l.large, l.each);
         l.part_bytes = l.each ? places * kThreads * sizeof(f32x4) * (l.large ? 8 : 4) : 0;
+        all.add(l);
     }
     return all;
 }

@@ -1,6 +1,10 @@
 """Argument checks of the layer normalisation and the orthogonalised updates, before anything
 is enqueued: no GPU, fake device addresses (see test_abi_host.py)."""
 import ctypes
+import os
+import shutil
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -202,6 +206,59 @@ def test_copies_of_two_dtypes(B):
         with pytest.raises(ValueError):
             B.bc_rmsprop_step_many(params, 0.1, 0.9, 1e-8, 0.0)
     assert B.bc_muon_step_many_work([param(f16), param(None), param(f16)]) > 0
+
+
+NO_MEMORY = """
+#include <cstdlib>
+#include <new>
+static thread_local bool none;
+extern "C" void no_memory(int on) { none = on; }
+void *operator new(std::size_t n)
+{
+    void *p = none ? nullptr : std::malloc(n ? n : 1);
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, std::size_t) noexcept { std::free(p); }
+"""
+
+CALLS = """
+import ctypes
+from paper_2108_09376_amd import bc as B
+none = ctypes.CDLL(None).no_memory
+lib, n = B.raw(), ctypes.c_int64()
+ns = B.bc_newton_schulz(64, 1.5, -0.5, 0.0, 1e-7)
+h = B.bc_muon(0.1, 0.9, 0.0, 1, ns)
+params = (B.bc_matrix * 64)()
+for i, p in enumerate(params):
+    p.w, p.momentum, p.grad, p.w16 = (0x10000000 * (4 * i + k + 1) for k in range(4))
+    p.rows, p.cols = 500 + i, 1000
+params[63].grad = params[0].w
+for on in (0, 1):                              # without first: the error text has its room then
+    none(on)
+    got = (lib.bc_orthogonalize_work(3, 1000, 2000, 64, ctypes.byref(n)),
+           lib.bc_muon_step_many_work(params, 64, 64, ctypes.byref(n)),
+           lib.bc_muon_step_many(params, 64, ctypes.byref(h), 1, 0x7000000000, n.value, None),
+           lib.bc_orthogonalize(params[0].w, 0, 3, 1000, 2000, ctypes.byref(ns), params[1].w, 0, None, 0, None))
+    none(0)
+    assert got == (B.BC_OK, B.BC_OK, B.BC_ERR_ALIAS, B.BC_ERR_NULL), got
+"""
+
+
+def test_no_exception_without_memory(B, tmp_path):
+    """The orthogonalising calls allocate nothing on the host: with an operator new that throws
+    they check, plan and answer as ever."""
+    cxx = shutil.which("g++")
+    if not cxx:
+        pytest.skip("g++ not found")
+    src, lib = tmp_path / "no_memory.cpp", tmp_path / "no_memory.so"
+    src.write_text(NO_MEMORY)
+    subprocess.check_call([cxx, "-O1", "-shared", "-fPIC", "-o", str(lib), str(src)])
+    env = dict(os.environ, LD_PRELOAD=" ".join(filter(None, [str(lib), os.environ.get("LD_PRELOAD")])))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", CALLS], env=env, cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
 
 
 def test_policy_norm_refusal(B):
