@@ -488,6 +488,8 @@ def _work(nbytes, like, stream):
 
 
 def _nbytes(t) -> int:
+    if not t.is_contiguous():
+        raise ValueError("a workspace must be contiguous")
     return t.numel() * t.element_size()
 
 

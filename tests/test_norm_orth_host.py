@@ -190,6 +190,19 @@ def test_binding_refuses_mismatched_tensors(B):
         B.bc_muon_step_many([(g, g.clone(), g.double(), None)], 0.1, 0.9, 0.0)
 
 
+def test_workspace_of_fewer_bytes_than_elements(B):
+    """A view's elements are not its memory: one element expanded to as many as are needed."""
+    x, v, g = torch.zeros((1, 4, 4, 16)), torch.zeros(16), torch.zeros(8, 16)
+    params = [(g, g.clone(), g.clone(), None)]
+    for work in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(2 << 20, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            B.bc_layer_norm_grad(x, B.BC_NHWC, v, None, x, 1e-5, torch.empty_like(x), None, v, v, work=work)
+        with pytest.raises(ValueError):
+            B.bc_orthogonalize(g, torch.empty_like(g), work=work)
+        with pytest.raises(ValueError):
+            B.bc_muon_step_many(params, 0.1, 0.9, 0.0, work=work)
+
+
 def test_copies_of_two_dtypes(B):
     """All 16-bit copies of a step are written in one format: two are refused, in any order."""
     def param(dt):
