@@ -591,7 +591,10 @@ def _matrix_array(params):
     arr = (bc_matrix * len(params))()
     dt = _copies_dtype(params)
     for a, (w, m, grad, w16) in zip(arr, params):
-        count, rows = w.numel(), w.shape[0]
+        count = w.numel()
+        if not count or not w.dim():
+            raise ValueError("weights are [rows, ...], with at least one element")
+        rows = w.shape[0]
         for t in (w, m, grad):
             if t.numel() != count or not _is_f32(t):
                 raise ValueError("weights, momentum and gradient are contiguous float32 of one size")

@@ -203,6 +203,15 @@ def test_workspace_of_fewer_bytes_than_elements(B):
             B.bc_muon_step_many(params, 0.1, 0.9, 0.0, work=work)
 
 
+@pytest.mark.parametrize("shape", [(), (0, 16), (4, 0), (0,)])
+def test_weights_without_elements(B, shape):
+    w = torch.zeros(shape)
+    with pytest.raises(ValueError):
+        B.bc_muon_step_many([(w, w.clone(), w.clone(), None)], 0.1, 0.9, 0.0)
+    with pytest.raises(ValueError):
+        B.bc_muon_step_many_work([(w, w.clone(), w.clone(), None)])
+
+
 def test_copies_of_two_dtypes(B):
     """All 16-bit copies of a step are written in one format: two are refused, in any order."""
     def param(dt):
