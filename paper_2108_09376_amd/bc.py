@@ -475,15 +475,21 @@ def bc_block_rewards(ig, mask, prob, grid, tau, gamma, mu, mavg, reward, cost=No
     _check(st, "bc_block_rewards")
 
 
+def torch_stream(stream, device):
+    """torch's object for a stream argument (an object or a handle; not None)."""
+    import torch
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream), device=device)
+
+
 def _work(nbytes, like, stream):
     """A workspace where the caller has none: memory of the stream that the call runs on, which
     no other stream is given while that one's work may still use it."""
     import torch
     if stream is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(_stream(stream), device=like.device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(torch_stream(stream, like.device)):
         return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 

@@ -297,6 +297,8 @@ class PolicyNet:
         [1, gh, gw]; mask uint8 (the executed grid a_b)."""
         if not hasattr(self, "master"):
             self._init_training()
+            if stream is not None:                    # the state was filled on torch's current stream
+                bc.torch_stream(stream, self.device).wait_stream(torch.cuda.current_stream(self.device))
         last = len(self.layers) - 1
         cur = {last: self.gbufs[last][0]}
         bc.bc_policy_logit_grad(reward, mask, prob, cur[last], stream)

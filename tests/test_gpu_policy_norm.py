@@ -130,6 +130,29 @@ def test_learns(R):
     assert np.isfinite(end) and end > start + 0.1, (start, end)
 
 
+@pytest.mark.parametrize("norm", [None, "layer"])
+@pytest.mark.parametrize("by_handle", [False, True])
+def test_first_update_on_another_stream(R, norm, by_handle):
+    """The first backward pass makes its state on torch's current stream, here still busy, and
+    runs on another: the gradients are those of a pass on one stream. (Within 1e-3 norm-wise:
+    the weight gradients' fp32 sums are in no fixed order.)"""
+    bc, resnet = R
+    a, b = (resnet.PolicyNet(256, 512, norm=norm) for _ in range(2))
+    frame, state, scores, reward, mask = inputs(650)
+    prob = b.forward(frame, state, scores, mask)
+    b.backward(reward, mask, prob)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    at = side.cuda_stream if by_handle else side
+    prob = a.forward(frame, state, scores, mask, stream=at)
+    side.synchronize()
+    torch.cuda._sleep(20_000_000)                          # some 10 ms of the current stream
+    a.backward(reward, mask, prob, stream=at)
+    torch.cuda.synchronize()
+    for x, y in zip(a.dw + a.db + a.dg, b.dw + b.db + b.dg):
+        assert (x - y).norm() <= 1e-3 * y.norm()
+
+
 def test_graph(R):
     """Forward pass and update captured once: replays equal eager calls on the same gradients.
     (The convolutions' weight gradients are sums in no fixed order, so each replay is given
