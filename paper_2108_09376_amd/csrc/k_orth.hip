@@ -13,17 +13,18 @@
 // and written twice. In units of 2 m^3 operations, five steps in spans of 3 and 2 take
 // 3 n/m + 7, in spans of one (products on X in every step) 7.5 n/m + 2.5. Directions of X
 // that are small beside the largest lose digits in A as the square of their size, and a
-// step multiplies such an error by up to a^2, so a new A is taken from X after three steps,
-// and after two once the small directions have grown (steps_direct and plans_of have the figures).
+// step multiplies such an error by up to a^2, so a new A is taken from X after three steps, after
+// two once the small directions have grown, and after every step where that would still be less
+// exact than plain fp32 (steps_direct has the figures).
 //
 // Arithmetic: an fp32 value x is held as two fp16 numbers, hi = half(x), lo = half(x - hi),
 // about 22 bits, all scaled by 2^12, and a product is hi hi + hi lo + lo hi on the matrix
 // cores: fp32 accuracy at a third of the fp16 rate, five times the fp32 rate. What is left
 // out, lo lo, is below 2^-22 of the product. A matrix instruction rounds its running sum by
-// more than an ulp, so the sums of each chunk of K start at zero and join the tile's totals
-// in fp32 (512 x 4608, five steps, difference to 64 bits: 1.5e-6, with one running sum
-// 3.3e-6; the textbook form in fp32 3.2e-6). Entries stay within 16 (the host has checked
-// the coefficients), as |X|_2 <= 1 at the start.
+// more than an ulp, so the sums of every four chunks of K start at zero and join the tile's
+// totals in fp32 (512 x 4608, five steps, difference to 64 bits: 1.7e-6; the textbook form in
+// fp32 3.2e-6). Entries stay within 16 (the host has checked the coefficients), as |X|_2 <= 1 at
+// the start.
 #include <algorithm>
 #include <cmath>
 
@@ -42,8 +43,8 @@ constexpr int kSpan = 3;                       // most steps between two A taken
 constexpr int kSumParts = 1024;                // partial sums of squares per matrix at most
 constexpr int kSumEach = 8192;                 // and elements of each at least
 // Chunks of K per range at least: the sums of a range cost as much as some of its chunks. 8 / 16
-// / 32, us: 64 x 4096 99 / 95 / 107, 256 x 2304 106 / 105 / 120, the policy network's step 143
-// / 143 / 179; 128 x 1024 84 / 93 / 93, 512 x 4608 158 / 158 / 156.
+// / 32, us: 64 x 4096 100 / 96 / 107, 64 x 2048 88 / 91 / 121, 256 x 2304 108 / 108 / 143, the
+// policy network's step 146 / 149 / 175; 128 x 1024 84 / 92 / 93, 1024 x 1280 221 / 191 / 191.
 constexpr int kLeastChunks = 16;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -453,19 +454,19 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //    to arrive (a counter per tile) adds all of them in order: the result does not depend on
 //    the order of arrival.
 //  * Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, so
-//    that its L2 serves their common rows and columns (in turn through all matrices of a step
-//    instead, which evens the load out: ResNet-50's 948 us for 917, the policy network's 154
-//    for 143).
+//    that its L2 serves their common rows and columns. us so and with neighbours on different
+//    XCDs: ResNet-50's step 988 and 1036, 512 x 4608 157 and 171, 12 of 193 x 301 102 and 122,
+//    2048 x 2048 681 and 676. The runs are equal in tiles, not in work: in ResNet-50's launches
+//    one XCD gets 1.4 to 2.3 times the mean's chunks.
 //
-// What bounds them: 2048 x 2048, 750 us, is 230 TFLOP/s of the textbook's products (three
-// fp16 products each, fewer in the form computed: some 620 on the matrix cores), 272 tiles on
-// 256 CUs, one wave per SIMD with its chunks' way through LDS exposed. ResNet-50's step, 870 us:
-// 100 for the two passes over momentum and gradients, which memory bounds, 405 for the four
-// products along n, 365 for thirteen products of m x m, 25 to 52 us each and for two thirds the
-// start and the end of their one or two rounds of workgroups. Small matrices: 5 to 9 us for
-// each of 17 products, a launch, the way to LDS and the tile's way out. (Eight chunks in
-// LDS with a workgroup per CU, where the tiles are that few, are slower than four: 512 x 4608
-// 169 for 157, the policy network's step 154 for 143.)
+// What bounds them is the latency of a workgroup's waves, not a unit. A symmetric product of
+// 2048 x 2048 (272 tiles on 256 CUs, 41 to 55 us) keeps the matrix cores busy for 26000 cycles
+// of each SIMD, LDS for 14000 of each CU, and the waves alive for 58000: one wave per SIMD waits
+// out its chunks' way; the product with X, two waves per SIMD, 49000 of 88000. In all 2048 x 2048,
+// 680 us, is 255 TFLOP/s of the textbook's products, three fp16 products each. ResNet-50's step,
+// 980 us: 100 for the two passes over momentum and gradients, which memory bounds, the rest the
+// products, 24 to 125 us each, with XCDs that end early. Few tiles: 5 to 11 us for each of 15 or
+// 17 products, a launch, the way to LDS and the tile's way out.
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
@@ -875,8 +876,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_product(Matrices<MANY> M, Ort
 // G to the result in one launch.
 //
 // X' = a (X + B X), B = (b/a) A + (c/a) A^2, as the products above in spans of one step, and
-// with their sums, order and roundings: the same bits. (Products this short are never split
-// over K.) The workgroup's latency bounds it: of a step of 64 x 64 (6500 cycles) the matrix
+// with their sums, order and roundings, the norm's among them: the same bits. (Products this
+// short are never split over K.) The workgroup's latency bounds it: of a step of 64 x 64 (6500 cycles) the matrix
 // instructions take some 1500, the rest is fragments on their way from LDS, the split into
 // halves, and four barriers.
 struct FusedStage {
@@ -1321,12 +1322,11 @@ unsigned number(Matrices<MANY> &M, const OrthTable &T, uint32_t *per, F &&count)
 }
 
 // Tiles of 128 x 64 read three quarters of the bytes of 64 x 64 ones per product, where they
-// are enough for the chip (2048 x 2048 837 us with the small ones, 746 with the large; with
-// 128 x 128, one workgroup per CU, 1173; 1500 x 1700, 156 large tiles: 415 and 414). Where some
-// products are twice as long as the mean, small tiles even the load out and more large ones
-// are needed (ResNet-50's step, launches of 386 to 578 large tiles: 894 us with those from 192
-// on large, 875 from 500 on).
-constexpr uint64_t kEnough = 192, kEnoughUneven = 500;
+// are enough for the chip. us with the large ones and with the small ones only: 2048 x 2048 681
+// and 811, ResNet-50's step 981 and 1011, 1024 x 2048 219 and 224; 1500 x 1700, 156 large tiles
+// in its symmetric products, 395 and 408; the policy network's step, where only the products
+// along n take them, 149 and 145. (128 x 128, one workgroup per CU: 2048 x 2048 half as slow again.)
+constexpr uint64_t kEnough = 192;
 
 // The products of one launch: the plans of its matrices (those taken in spans, those taken step
 // by step; a plan that is done has no jobs), the tiles, and the K ranges.
@@ -1372,8 +1372,7 @@ List<Launch, kMostLaunches> launches_of(const OrthTable &T, const NewtonSchulz &
             const OrthPlan &p = l.plan[steps_direct(T.e[t].rows, T.e[t].cols)];
             if (p.jobs) longest = std::max(longest, chunks(p, T.e[t]));
         }
-        const uint64_t large = tiles(true, 0);
-        l.large = large >= (longest * large >= 2 * work(true) ? kEnoughUneven : kEnough);
+        l.large = tiles(true, 0) >= kEnough;
         const uint64_t wgs = tiles(l.large, 0);
         // K in ranges, of whole folds, where the longest workgroup would far outlast the chip's
         // share of the work (twice as long: 1024 x 2048 254 us whole, 265 in ranges)
@@ -1420,9 +1419,9 @@ hipError_t launch_products(const OrthTable &T, Matrices<MANY> &M, OrthHead *head
 
 // Whether all matrices are small. With larger ones beside them their products share the
 // larger ones' launches and cost nothing. By themselves, us in the launches of products and
-// here: 64 x 64 69 and 17, 64 x 147 75 and 27, 64 x 512 79 and 51, 128 x 128 70 and 53,
-// 256 of 64 x 64 164 and 18. (In a launch per step with chunks of 256 columns 64 x 2048 took
-// 64 for 91, but not to the same bits.)
+// here: 64 x 64 68 and 18, 64 x 147 74 and 28, 64 x 512 80 and 54, 128 x 128 69 and 54,
+// 256 of 64 x 64 164 and 20. (In a step the 64 x 512 form keeps 272 bytes a lane in scratch
+// memory: three of 64 x 512 97 us, one of 512 x 64 118.)
 bool all_fused(const OrthTable &T)
 {
     for (int t = 0; t < T.n; ++t)
