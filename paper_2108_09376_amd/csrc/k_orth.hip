@@ -457,16 +457,17 @@ __global__ __launch_bounds__(kThreads) void k_orth_start(Matrices<MANY> M, OrthS
 //    that its L2 serves their common rows and columns. us so and with neighbours on different
 //    XCDs: ResNet-50's step 988 and 1036, 512 x 4608 157 and 171, 12 of 193 x 301 102 and 122,
 //    2048 x 2048 681 and 676. The runs are equal in tiles, not in work: in ResNet-50's launches
-//    one XCD gets 1.4 to 2.3 times the mean's chunks.
+//    one XCD gets 1.5 to 2.0 times the mean's chunks.
 //
 // What bounds them is the latency of a workgroup's waves, not a unit. A symmetric product of
-// 2048 x 2048 (272 tiles on 256 CUs, 41 to 55 us) keeps the matrix cores busy for 26000 cycles
-// of each SIMD, LDS for 14000 of each CU, and the waves alive for 58000: one wave per SIMD waits
-// out its chunks' way; the product with X, two waves per SIMD, 49000 of 88000. In all 2048 x 2048,
-// 680 us, is 255 TFLOP/s of the textbook's products, three fp16 products each. ResNet-50's step,
+// 2048 x 2048 (272 tiles on 256 CUs, 41 to 51 us) keeps the matrix cores busy for 26000 cycles
+// of each SIMD and LDS for 14000 of each CU, while a wave lives 58000: one wave per SIMD waits
+// out its chunks' way; the product with X, two waves per SIMD, 49000 of 87000. In all 2048 x 2048,
+// 670 us, is 255 TFLOP/s of the textbook's products, three fp16 products each. ResNet-50's step,
 // 980 us: 100 for the two passes over momentum and gradients, which memory bounds, the rest the
-// products, 24 to 125 us each, with XCDs that end early. Few tiles: 5 to 11 us for each of 15 or
-// 17 products, a launch, the way to LDS and the tile's way out.
+// products, 25 to 126 us each, with XCDs that end early. Few tiles: 5 to 11 us for each of 15 or
+// 17 products; a wave lives 17000 cycles, 400 to 2000 of its SIMD's in matrix instructions, the
+// rest a launch, the way to LDS and the tile's way out.
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
