@@ -480,7 +480,8 @@ def torch_stream(stream, device):
     import torch
     if isinstance(stream, torch.cuda.Stream):
         return stream
-    return torch.cuda.ExternalStream(_stream(stream), device=device)
+    handle = _stream(stream)                             # 0, the default stream's, would mean a new one
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
 
 
 def _work(nbytes, like, stream):

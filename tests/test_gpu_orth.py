@@ -435,6 +435,26 @@ def test_workspace_belongs_to_the_stream(bc, monkeypatch, by_handle):
     assert torch.equal(out, want)
 
 
+def test_handle_of_the_default_stream(bc, monkeypatch):
+    """A handle of 0 names the default stream, also for the workspace that is made for it."""
+    device = torch.device("cuda", torch.cuda.current_device())
+    assert bc.torch_stream(0, device) == torch.cuda.default_stream(device)
+    side, on = torch.cuda.Stream(), []
+    assert bc.torch_stream(side, device) is side
+    assert bc.torch_stream(side.cuda_stream, device).cuda_stream == side.cuda_stream
+    g = gradient(11, 300, 400).cuda()
+    out = torch.empty_like(g)
+    real = torch.empty
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: on.append(torch.cuda.current_stream().cuda_stream) or real(*a, **k))
+    with torch.cuda.stream(side):
+        bc.bc_orthogonalize(g, out, stream=torch.cuda.default_stream().cuda_stream)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert on == [0]
+    check(out, *bounds(g, "f32"), "f32")
+
+
 def test_offsets_past_32_bits(bc):
     """A matrix whose X passes 2^32 bytes, with one element per row: its singular values are
     those elements, and each becomes what the iteration makes of it alone."""
