@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define BC_ABI_VERSION 11
+#define BC_ABI_VERSION 12
 
 typedef enum {
     BC_OK = 0,
@@ -691,6 +691,123 @@ bc_status bc_muon_step_many_work(const bc_matrix *params, int32_t n, int32_t ste
  */
 bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *muon,
                             int32_t dtype, void *d_work, int64_t work_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------
+ * Learning from a teacher and from a policy's own decisions. Score maps are channels-last,
+ * [n][h][w][c] in any dtype at any element alignment, of which the first `classes` channels
+ * are a pixel's class scores (the rest is never looked at); a batch of rows is a map with
+ * h = 1. Each loss comes with the gradient of its scores. Arithmetic is fp32 or wider, each
+ * result rounded once; sums over pixels are taken in a fixed order, so equal calls give equal
+ * bits. A NaN score stays within its pixel (and its image's sums). Rules for all:
+ *  - a pixel of weight 0 takes no part: loss 0, gradient 0, whatever else it holds;
+ *  - a score of -inf is a class that is masked out: its probability is 0;
+ *  - d_work: the caller's workspace of at least the bytes of the call's _work function,
+ *    aligned to 16 bytes; calls that may overlap in time need one each. Nothing is kept in
+ *    it (NULL is taken where 0 bytes are needed).
+ * ------------------------------------------------------------------------------ */
+
+/* Bytes of the workspace of bc_top_scores. Host only. Errors: as bc_top_scores. */
+bc_status bc_top_scores_work(bc_tensor scores, int32_t classes, int32_t k, int64_t *bytes);
+
+/*
+ * A teacher's record: the k largest class scores of each pixel, for the active blocks
+ * (every other block keeps its record: feature transfer, as of any layer's output).
+ *   d_top    [n][h][w][k] in scores.dtype, descending; of equal scores the lower class first
+ *            (-0 equals 0). The order of NaN scores is not specified.
+ *   d_index  int32 [n][h][w][k]: their classes, distinct.
+ *   d_rest   float32 [n][h][w] or NULL: log of the sum of exp(score / temperature) over all
+ *            other classes (-inf if there are none, or all are masked out).
+ *   k        1 .. min(classes, 64);  temperature > 0.
+ * The blocks are scores.h / grid_h x scores.w / grid_w pixels; index and capacity as
+ * bc_sparse_conv2d (d_idx = d_count = NULL: every block).
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE (classes, k, temperature), BC_ERR_DTYPE, BC_ERR_LAYOUT
+ * (NCHW), BC_ERR_NOT_DIVISIBLE, BC_ERR_CAPACITY (index; workspace), BC_ERR_ALIAS,
+ * BC_ERR_UNSUPPORTED (d_work not aligned), BC_ERR_HIP.
+ */
+bc_status bc_top_scores(const void *d_scores, bc_tensor scores, int32_t classes, int32_t k,
+                        float temperature, void *d_top, int32_t *d_index, float *d_rest,
+                        bc_grid g, const int32_t *d_idx, const int32_t *d_count, int32_t capacity,
+                        void *d_work, int64_t work_bytes, void *stream);
+
+/* Bytes of the workspace of bc_distill_loss. Host only. Errors: as bc_distill_loss. */
+bc_status bc_distill_loss_work(bc_tensor scores, int32_t classes, int32_t k, int64_t *bytes);
+
+/*
+ * Divergence of a student's scores from a teacher's record, and its gradient. A pixel's
+ * outcomes are the k classes of its record and, as one outcome more, all other classes:
+ *   p = softmax of (d_top / temperature, d_rest); the last is 0 where d_rest is NULL, so that
+ *       the record's own classes share the whole of it;
+ *   q = the student's probabilities of the same outcomes, softmax(scores / temperature);
+ *   L[n] = scale sum over pixels of weight sum over outcomes of p log(p / q),
+ *   d_grad = dL / dscores: weight scale / temperature times (q_j - p_j) for a class of the
+ *       record, times (q_rest - p_rest) z_j / z_rest for any other, z = exp(scores /
+ *       temperature); channels past `classes` get 0.
+ *   d_top     [n][h][w][k] in top_dtype (any), d_index int32: as bc_top_scores gives them, in any
+ *             order. An entry outside 0 .. classes - 1 is left out; a class that occurs twice
+ *             counts with both its scores.
+ *   d_weight  float32 [n][h][w] or NULL (1).  scale finite, temperature > 0, k 1 .. 64.
+ *   d_grad    like d_scores (may be d_scores itself), or NULL;  d_loss float32 [n] or NULL.
+ *             One of them is required.
+ * A pixel whose class scores, or whose record's, are all -inf takes no part. A masked
+ * class that the teacher gives a probability makes the loss +inf, not the gradient.
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_LAYOUT, BC_ERR_CAPACITY,
+ * BC_ERR_ALIAS, BC_ERR_UNSUPPORTED (d_work not aligned), BC_ERR_HIP.
+ */
+bc_status bc_distill_loss(const void *d_scores, bc_tensor scores, int32_t classes,
+                          const void *d_top, int32_t top_dtype, const int32_t *d_index, int32_t k,
+                          const float *d_rest, float temperature, const float *d_weight,
+                          float scale, void *d_grad, float *d_loss, void *d_work,
+                          int64_t work_bytes, void *stream);
+
+/* Bytes of the workspace of bc_action_log_probs. Host only. Errors: as there. */
+bc_status bc_action_log_probs_work(bc_tensor scores, int32_t classes, int64_t *bytes);
+
+/*
+ * Log probabilities of a policy's decisions, one per pixel.
+ *   classes >= 2: the decision is a class, pi = softmax(scores); d_action int32 [n][h][w].
+ *   classes == 1: execute or not (Section 3.5), pi(1) = sigmoid(score); d_action uint8
+ *            [n][h][w], nonzero = executed: the execution grid itself.
+ *   d_logp   float32 [n][h][w]: log pi(action); -inf for a masked class, 0 for an action
+ *            outside 0 .. classes - 1 (no decision).
+ *   d_entropy float32 [n][h][w] or NULL: -sum of pi log pi (0 if every class is masked).
+ * Errors: BC_ERR_NULL, BC_ERR_SHAPE, BC_ERR_DTYPE, BC_ERR_LAYOUT, BC_ERR_CAPACITY,
+ * BC_ERR_ALIAS, BC_ERR_UNSUPPORTED (d_work not aligned), BC_ERR_HIP.
+ */
+bc_status bc_action_log_probs(const void *d_scores, bc_tensor scores, int32_t classes,
+                              const void *d_action, float *d_logp, float *d_entropy,
+                              void *d_work, int64_t work_bytes, void *stream);
+
+/* Clipped policy loss: the ratio's range 1 - low .. 1 + high (0 <= low <= 1, high >= 0) and
+ * the weight of the divergence to the reference (>= 0). */
+typedef struct { float low, high, beta; } bc_policy_clip;
+
+/* Bytes of the workspace of bc_clipped_policy_loss. Host only. Errors: as there. */
+bc_status bc_clipped_policy_loss_work(bc_tensor scores, int32_t classes, int64_t *bytes);
+
+/*
+ * Policy loss for several updates on the decisions of one frame (bc_policy_logit_grad's loss
+ * is sound for the first update only), and its gradient. With l = log pi(action) as in
+ * bc_action_log_probs, r = exp(l - old) and A the advantage:
+ *   K = exp(ref - l) - (ref - l) - 1   (an estimate of the divergence from the reference;
+ *       0 without d_ref_logp),
+ *   L[n] = scale sum over pixels of weight (-min(r A, clip(r, 1 - low, 1 + high) A) + beta K),
+ *   d_grad = dL / dscores. A clipped decision (the minimum is its second term alone) has
+ *       no part in the first term's gradient.
+ *   d_advantage, d_old_logp   float32 [n][h][w] (bc_block_rewards' d_reward,
+ *                bc_action_log_probs' d_logp before the first update).
+ *   d_ref_logp   float32 [n][h][w] or NULL;  d_weight float32 [n][h][w] or NULL (1).
+ *   d_grad       like d_scores (may be d_scores itself), or NULL; channels past `classes`: 0.
+ *   d_loss       float32 [n] or NULL: L;  d_kl float32 [n] or NULL: scale sum of weight K.
+ *                d_grad or d_loss is required, d_ref_logp for d_kl.
+ * A pixel whose action is outside 0 .. classes - 1 or masked out takes no part.
+ * Errors: as bc_action_log_probs.
+ */
+bc_status bc_clipped_policy_loss(const void *d_scores, bc_tensor scores, int32_t classes,
+                                 const void *d_action, const float *d_advantage,
+                                 const float *d_old_logp, const float *d_ref_logp,
+                                 const float *d_weight, const bc_policy_clip *clip, float scale,
+                                 void *d_grad, float *d_loss, float *d_kl, void *d_work,
+                                 int64_t work_bytes, void *stream);
 
 #ifdef __cplusplus
 }

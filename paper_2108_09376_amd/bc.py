@@ -60,6 +60,10 @@ class bc_muon(ctypes.Structure):
                 ("ns", bc_newton_schulz)]
 
 
+class bc_policy_clip(ctypes.Structure):
+    _fields_ = [("low", ctypes.c_float), ("high", ctypes.c_float), ("beta", ctypes.c_float)]
+
+
 class bc_conv(ctypes.Structure):
     _fields_ = [("kh", ctypes.c_int32), ("kw", ctypes.c_int32), ("stride", ctypes.c_int32),
                 ("pad", ctypes.c_int32), ("relu", ctypes.c_int32)]
@@ -132,6 +136,17 @@ _sigs = {
     "bc_muon_step_many_work": ([ctypes.POINTER(bc_matrix), _i32, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
     "bc_muon_step_many": ([ctypes.POINTER(bc_matrix), _i32, ctypes.POINTER(bc_muon), _i32, _vp,
                            ctypes.c_int64, _vp], _i32),
+    "bc_top_scores_work": ([bc_tensor, _i32, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_top_scores": ([_vp, bc_tensor, _i32, _i32, _f32, _vp, _vp, _vp, bc_grid, _vp, _vp, _i32, _vp,
+                       ctypes.c_int64, _vp], _i32),
+    "bc_distill_loss_work": ([bc_tensor, _i32, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_distill_loss": ([_vp, bc_tensor, _i32, _vp, _i32, _vp, _i32, _vp, _f32, _vp, _f32, _vp, _vp, _vp,
+                         ctypes.c_int64, _vp], _i32),
+    "bc_action_log_probs_work": ([bc_tensor, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_action_log_probs": ([_vp, bc_tensor, _i32, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp], _i32),
+    "bc_clipped_policy_loss_work": ([bc_tensor, _i32, ctypes.POINTER(ctypes.c_int64)], _i32),
+    "bc_clipped_policy_loss": ([_vp, bc_tensor, _i32, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(bc_policy_clip),
+                                _f32, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp], _i32),
     "bc_block_rewards": ([_vp, _vp, _vp, _i32, bc_grid, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _vp], _i32),
 }
 for _name, (_args, _res) in _sigs.items():
@@ -143,7 +158,7 @@ EXPORTED = tuple(_sigs)
 
 # The ABI these bindings marshal for (BC_ABI_VERSION of include/bc.h); a library built
 # from other sources is refused rather than called with mismatched arguments.
-ABI_VERSION = 11
+ABI_VERSION = 12
 if _lib.bc_abi_version() != ABI_VERSION:
     raise ImportError(f"{LIB_PATH} has ABI {_lib.bc_abi_version()}, the bindings expect "
                       f"{ABI_VERSION}: rebuild with `python -m paper_2108_09376_amd.build`")
@@ -634,6 +649,170 @@ def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=N
                 _newton_schulz(steps, tuple(coef), eps))
     st = _lib.bc_muon_step_many(arr, len(params), ctypes.byref(h), dt, _ptr(work), _nbytes(work), _stream(stream))
     _check(st, "bc_muon_step_many")
+
+
+def _score_map(t, stream):
+    """Shape and descriptor of a score map [n, h, w, c] on the current device (and the stream's)."""
+    import torch
+    d = _desc(t, BC_NHWC)
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("the score map is not on the current device")
+    if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
+        raise ValueError("the stream is of another device than the score map")
+    return t.shape, d
+
+
+def _per_pixel(t, like, dtype, name, last=None):
+    """A contiguous tensor of one value (or `last`) per pixel of the map `like`, on its device
+    (or None)."""
+    if t is None:
+        return
+    n, h, w, _ = like.shape
+    s = t.shape
+    if not (t.dtype is dtype and t.is_contiguous() and t.device == like.device
+            and s == ((n, h, w) if last is None else (n, h, w, last))):
+        raise ValueError(f"{name} must be contiguous {dtype}, one {'value' if last is None else 'record'} per pixel, "
+                         "on the map's device")
+
+
+def _per_image(t, like, name):
+    import torch
+    if t is not None and not (t.dtype is torch.float32 and t.is_contiguous() and t.shape == like.shape[:1]
+                              and t.device == like.device):
+        raise ValueError(f"{name} must be contiguous float32, one value per image, on the map's device")
+
+
+def _score_work(work, nbytes, like, stream):
+    """Pointer and size of a caller's workspace, or of one made for the call (None, 0: none needed)."""
+    if work is None:
+        need = nbytes()
+        if not need:
+            return None, None, 0
+        work = _work(need, like, stream)
+    if work.device != like.device:
+        raise ValueError("the workspace is not on the map's device")
+    return work, work.data_ptr(), _nbytes(work)
+
+
+def bc_top_scores_work(scores, classes, k) -> int:
+    """Bytes of bc_top_scores' workspace for maps like scores (may be 0)."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_top_scores_work(_desc(scores, BC_NHWC), int(classes), int(k), ctypes.byref(n)),
+           "bc_top_scores_work")
+    return n.value
+
+
+def bc_top_scores(scores, classes, temperature, top, index, rest, grid, idx, count, work=None, stream=None):
+    """The k largest of the first `classes` channels of scores [n, h, w, c] per pixel of the
+    active blocks: top [n, h, w, k] (scores' dtype, descending, the lower class first among
+    equals), index int32 [n, h, w, k], and rest float32 [n, h, w] (or None), log-sum-exp of
+    the others divided by the temperature. work as for bc_layer_norm_grad."""
+    import torch
+    _, d = _score_map(scores, stream)
+    k = top.shape[-1]
+    _per_pixel(top, scores, scores.dtype, "top", k)
+    _per_pixel(index, scores, torch.int32, "index", k)
+    _per_pixel(rest, scores, torch.float32, "rest")
+    for t in (idx, count):
+        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous() and t.device == scores.device):
+            raise ValueError("the index must be contiguous int32 on the map's device")
+    cap = 0 if idx is None else int(idx.numel())
+    work, wp, nbytes = _score_work(work, lambda: bc_top_scores_work(scores, classes, k), scores, stream)
+    st = _lib.bc_top_scores(_ptr(scores), d, int(classes), int(k), float(temperature), _ptr(top), _ptr(index),
+                            _ptr(rest), _grid(grid), _ptr(idx), _ptr(count), cap, wp, nbytes, _stream(stream))
+    _check(st, "bc_top_scores")
+
+
+def bc_distill_loss_work(scores, classes, k) -> int:
+    """Bytes of bc_distill_loss's workspace for maps like scores."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_distill_loss_work(_desc(scores, BC_NHWC), int(classes), int(k), ctypes.byref(n)),
+           "bc_distill_loss_work")
+    return n.value
+
+
+def bc_distill_loss(scores, classes, top, index, rest, temperature, weight, scale, grad, loss, work=None, stream=None):
+    """loss [n] float32 = scale * sum of weight * divergence of the scores from the record (top
+    in any dtype, index int32, rest float32 or None), and grad [n, h, w, c], its gradient (either
+    may be None; grad may be scores). weight float32 [n, h, w] or None. work as for
+    bc_layer_norm_grad."""
+    import torch
+    shape, d = _score_map(scores, stream)
+    k = top.shape[-1]
+    _per_pixel(top, scores, top.dtype, "top", k)
+    _per_pixel(index, scores, torch.int32, "index", k)
+    _per_pixel(rest, scores, torch.float32, "rest")
+    _per_pixel(weight, scores, torch.float32, "weight")
+    _per_pixel(grad, scores, scores.dtype, "grad", shape[3])
+    _per_image(loss, scores, "loss")
+    work, wp, nbytes = _score_work(work, lambda: bc_distill_loss_work(scores, classes, k), scores, stream)
+    st = _lib.bc_distill_loss(_ptr(scores), d, int(classes), _ptr(top), _dtype_code(top), _ptr(index), int(k),
+                              _ptr(rest), float(temperature), _ptr(weight), float(scale), _ptr(grad), _ptr(loss),
+                              wp, nbytes, _stream(stream))
+    _check(st, "bc_distill_loss")
+
+
+def bc_action_log_probs_work(scores, classes) -> int:
+    """Bytes of bc_action_log_probs's workspace for maps like scores (may be 0)."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_action_log_probs_work(_desc(scores, BC_NHWC), int(classes), ctypes.byref(n)),
+           "bc_action_log_probs_work")
+    return n.value
+
+
+def _action(action, scores, classes):
+    import torch
+    _per_pixel(action, scores, torch.uint8 if classes == 1 else torch.int32, "action")
+
+
+def bc_action_log_probs(scores, classes, action, logp, entropy=None, work=None, stream=None):
+    """logp [n, h, w] float32 = log pi(action) (and entropy [n, h, w], if given) of scores
+    [n, h, w, c]: classes of a softmax (action int32), or with classes = 1 execute-or-not
+    decisions of a sigmoid (action uint8, the grid). work as for bc_layer_norm_grad."""
+    import torch
+    _, d = _score_map(scores, stream)
+    _action(action, scores, classes)
+    _per_pixel(logp, scores, torch.float32, "logp")
+    _per_pixel(entropy, scores, torch.float32, "entropy")
+    work, wp, nbytes = _score_work(work, lambda: bc_action_log_probs_work(scores, classes), scores, stream)
+    st = _lib.bc_action_log_probs(_ptr(scores), d, int(classes), _ptr(action), _ptr(logp), _ptr(entropy), wp, nbytes,
+                                  _stream(stream))
+    _check(st, "bc_action_log_probs")
+
+
+def bc_clipped_policy_loss_work(scores, classes) -> int:
+    """Bytes of bc_clipped_policy_loss's workspace for maps like scores."""
+    n = ctypes.c_int64()
+    _check(_lib.bc_clipped_policy_loss_work(_desc(scores, BC_NHWC), int(classes), ctypes.byref(n)),
+           "bc_clipped_policy_loss_work")
+    return n.value
+
+
+@functools.lru_cache(maxsize=64)
+def _policy_clip(clip) -> bc_policy_clip:
+    return bc_policy_clip(*[float(v) for v in clip])
+
+
+def bc_clipped_policy_loss(scores, classes, action, advantage, old_logp, ref_logp, weight, clip, scale, grad, loss,
+                           kl=None, work=None, stream=None):
+    """loss [n] = scale * sum of weight * (-min(r A, clip(r) A) + beta K), r = exp(log pi(action) -
+    old_logp), clip = (low, high, beta), and grad, its gradient by scores (may be scores itself; grad
+    or loss may be None). advantage, old_logp, ref_logp (or None), weight (or None) float32
+    [n, h, w]; kl [n] (or None) the divergence to the reference; scores, classes, action as for
+    bc_action_log_probs. work as for bc_layer_norm_grad."""
+    import torch
+    shape, d = _score_map(scores, stream)
+    _action(action, scores, classes)
+    for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")):
+        _per_pixel(t, scores, torch.float32, name)
+    _per_pixel(grad, scores, scores.dtype, "grad", shape[3])
+    _per_image(loss, scores, "loss")
+    _per_image(kl, scores, "kl")
+    work, wp, nbytes = _score_work(work, lambda: bc_clipped_policy_loss_work(scores, classes), scores, stream)
+    st = _lib.bc_clipped_policy_loss(_ptr(scores), d, int(classes), _ptr(action), _ptr(advantage), _ptr(old_logp),
+                                     _ptr(ref_logp), _ptr(weight), ctypes.byref(_policy_clip(tuple(clip))),
+                                     float(scale), _ptr(grad), _ptr(loss), _ptr(kl), wp, nbytes, _stream(stream))
+    _check(st, "bc_clipped_policy_loss")
 
 
 def _np_ptr(a):

@@ -1340,4 +1340,263 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
     return ok();
 }
 
+// ---------------------------------------------------------------- score maps
+
+static bc_status score_geom(const bc_tensor &t, int32_t classes, bool whole, bc::ScoreGeom &g)
+{
+    bc_status st = check_tensor(t, "scores");
+    if (st) return st;
+    if (t.layout != BC_NHWC) return fail(BC_ERR_LAYOUT, "score maps are channels-last");
+    if (classes < 1 || classes > t.c) return fail(BC_ERR_SHAPE, "%d classes of %d channels", classes, t.c);
+    g = bc::ScoreGeom{};
+    g.images = (uint32_t)t.n;
+    g.hw = (uint32_t)((size_t)t.h * t.w);             // at most 4e9 elements
+    g.c = t.c;
+    g.classes = classes;
+    g.len = whole ? t.c : classes;
+    return BC_OK;
+}
+
+static bc_status check_score_work(const void *d_work, int64_t work_bytes, size_t need)
+{
+    return need ? check_work(d_work, work_bytes, need) : BC_OK;
+}
+
+static bc_status check_temperature(float t)
+{
+    if (!(t > 0.f) || !std::isfinite(t) || !std::isfinite(1.f / t))
+        return fail(BC_ERR_SHAPE, "the temperature must be positive, and it and its inverse finite");
+    return BC_OK;
+}
+
+// Outputs against inputs and each other; an output may be `same` itself where it is outs[0].
+static bc_status check_outputs(const Extent *outs, int n_outs, const Extent *ins, int n_ins, const void *same)
+{
+    for (int i = 0; i < n_outs; ++i) {
+        for (int j = 0; j < n_ins; ++j)
+            if (!(i == 0 && ins[j].p == same && outs[i].p == same) && overlap(outs[i].p, outs[i].b, ins[j].p, ins[j].b))
+                return fail(BC_ERR_ALIAS, "an output overlaps an input");
+        for (int j = i + 1; j < n_outs; ++j)
+            if (overlap(outs[i].p, outs[i].b, outs[j].p, outs[j].b))
+                return fail(BC_ERR_ALIAS, "outputs overlap each other");
+    }
+    return BC_OK;
+}
+
+static bc_status check_record(int32_t k, int32_t most)
+{
+    if (k < 1 || k > most) return fail(BC_ERR_SHAPE, "records of %d entries (1 .. %d)", k, most);
+    return BC_OK;
+}
+
+static bc_status top_plan(const bc_tensor &t, int32_t classes, int32_t k, bc::ScoreGeom &g, bc::ScorePlan &p)
+{
+    bc_status st = score_geom(t, classes, false, g);
+    if (st) return st;
+    if ((st = check_record(k, std::min(classes, 64)))) return st;
+    p = bc::top_plan(g, t.dtype, k);
+    return BC_OK;
+}
+
+static bc_status distill_plan(const bc_tensor &t, int32_t classes, int32_t k, bc::ScoreGeom &g, bc::ScorePlan &p)
+{
+    bc_status st = score_geom(t, classes, true, g);
+    if (st) return st;
+    if ((st = check_record(k, 64))) return st;
+    p = bc::score_plan(g, t.dtype, k, true);
+    return BC_OK;
+}
+
+static bc_status action_plan(const bc_tensor &t, int32_t classes, bool loss, bc::ScoreGeom &g, bc::ScorePlan &p)
+{
+    bc_status st = score_geom(t, classes, loss, g);
+    if (st) return st;
+    p = bc::score_plan(g, t.dtype, 1, loss);
+    return BC_OK;
+}
+
+bc_status bc_top_scores_work(bc_tensor scores, int32_t classes, int32_t k, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    bc::ScoreGeom g;
+    bc::ScorePlan p;
+    bc_status st = top_plan(scores, classes, k, g, p);
+    if (st) return st;
+    *bytes = (int64_t)p.bytes;
+    return ok();
+}
+
+bc_status bc_top_scores(const void *d_scores, bc_tensor scores, int32_t classes, int32_t k,
+                        float temperature, void *d_top, int32_t *d_index, float *d_rest,
+                        bc_grid g, const int32_t *d_idx, const int32_t *d_count, int32_t capacity,
+                        void *d_work, int64_t work_bytes, void *stream)
+{
+    if (!d_scores || !d_top || !d_index) return fail(BC_ERR_NULL, "d_scores, d_top and d_index are required");
+    bc::ScoreGeom G;
+    bc::ScorePlan p;
+    bc_status st = top_plan(scores, classes, k, G, p);
+    if (st) return st;
+    if ((st = check_temperature(temperature))) return st;
+    LayerGeom L;
+    if ((st = block_geom(scores, g, L))) return st;
+    if ((st = check_index(d_idx, d_count, capacity, L.total_blocks))) return st;
+    if ((st = check_score_work(d_work, work_bytes, p.bytes))) return st;
+    const size_t px = (size_t)G.images * G.hw;
+    const Extent ins[3] = {{d_scores, tensor_bytes(scores)}, {d_idx, (size_t)capacity * 4}, {d_count, 4}};
+    const Extent outs[4] = {{d_top, px * k * esize_of(scores.dtype)}, {d_index, px * k * 4}, {d_rest, px * 4},
+                            {d_work, p.bytes}};
+    if ((st = check_outputs(outs, 4, ins, d_idx ? 3 : 1, nullptr))) return st;
+    bc::TopArgs a = {};
+    a.x = d_scores;
+    a.top = d_top;
+    a.index = d_index;
+    a.rest = d_rest;
+    a.k = k;
+    a.inv_t = 1.f / temperature;
+    a.gw = L.gw; a.bh = L.bh; a.bw = L.bw;
+    a.by_block = bc::Divisor((uint32_t)L.bh * (uint32_t)L.bw);
+    a.by_gw = bc::Divisor(L.gw);
+    a.by_bw = bc::Divisor(L.bw);
+    a.idx = d_idx;
+    a.count = d_count;
+    hipError_t e = bc::launch_top(a, G, p, d_work, scores.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "top scores launch");
+    return ok();
+}
+
+bc_status bc_distill_loss_work(bc_tensor scores, int32_t classes, int32_t k, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    bc::ScoreGeom g;
+    bc::ScorePlan p;
+    bc_status st = distill_plan(scores, classes, k, g, p);
+    if (st) return st;
+    *bytes = (int64_t)p.bytes;
+    return ok();
+}
+
+bc_status bc_distill_loss(const void *d_scores, bc_tensor scores, int32_t classes,
+                          const void *d_top, int32_t top_dtype, const int32_t *d_index, int32_t k,
+                          const float *d_rest, float temperature, const float *d_weight,
+                          float scale, void *d_grad, float *d_loss, void *d_work,
+                          int64_t work_bytes, void *stream)
+{
+    if (!d_scores || !d_top || !d_index) return fail(BC_ERR_NULL, "d_scores, d_top and d_index are required");
+    if (!d_grad && !d_loss) return fail(BC_ERR_NULL, "d_grad or d_loss is required");
+    bc::ScoreGeom G;
+    bc::ScorePlan p;
+    bc_status st = distill_plan(scores, classes, k, G, p);
+    if (st) return st;
+    if (!valid_dtype(top_dtype)) return fail(BC_ERR_DTYPE, "d_top: unknown dtype %d", top_dtype);
+    if ((st = check_temperature(temperature))) return st;
+    if (!std::isfinite(scale)) return fail(BC_ERR_SHAPE, "scale must be finite");
+    if ((st = check_score_work(d_work, work_bytes, p.bytes))) return st;
+    const size_t px = (size_t)G.images * G.hw, sb = tensor_bytes(scores);
+    const Extent ins[5] = {{d_scores, sb}, {d_top, px * k * esize_of(top_dtype)}, {d_index, px * k * 4},
+                           {d_rest, px * 4}, {d_weight, px * 4}};
+    const Extent outs[3] = {{d_grad, sb}, {d_loss, (size_t)G.images * 4}, {d_work, p.bytes}};
+    if ((st = check_outputs(outs, 3, ins, 5, d_scores))) return st;
+    bc::DistillArgs a = {};
+    a.x = d_scores;
+    a.top = d_top;
+    a.index = d_index;
+    a.rest = d_rest;
+    a.weight = d_weight;
+    a.grad = d_grad;
+    a.top_fmt = top_dtype;
+    a.k = k;
+    a.inv_t = 1.f / temperature;
+    a.scale = scale;
+    hipError_t e = bc::launch_distill(a, G, p, d_work, d_loss, scores.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "distillation launch");
+    return ok();
+}
+
+static bc_status action_work(const bc_tensor &scores, int32_t classes, bool loss, int64_t *bytes)
+{
+    if (!bytes) return fail(BC_ERR_NULL, "bytes is required");
+    bc::ScoreGeom g;
+    bc::ScorePlan p;
+    bc_status st = action_plan(scores, classes, loss, g, p);
+    if (st) return st;
+    *bytes = (int64_t)p.bytes;
+    return ok();
+}
+
+bc_status bc_action_log_probs_work(bc_tensor scores, int32_t classes, int64_t *bytes)
+{
+    return action_work(scores, classes, false, bytes);
+}
+
+bc_status bc_action_log_probs(const void *d_scores, bc_tensor scores, int32_t classes,
+                              const void *d_action, float *d_logp, float *d_entropy,
+                              void *d_work, int64_t work_bytes, void *stream)
+{
+    if (!d_scores || !d_action || !d_logp) return fail(BC_ERR_NULL, "d_scores, d_action and d_logp are required");
+    bc::ScoreGeom G;
+    bc::ScorePlan p;
+    bc_status st = action_plan(scores, classes, false, G, p);
+    if (st) return st;
+    if ((st = check_score_work(d_work, work_bytes, p.bytes))) return st;
+    const size_t px = (size_t)G.images * G.hw;
+    const Extent ins[2] = {{d_scores, tensor_bytes(scores)}, {d_action, px * (classes == 1 ? 1 : 4)}};
+    const Extent outs[3] = {{d_logp, px * 4}, {d_entropy, px * 4}, {d_work, p.bytes}};
+    if ((st = check_outputs(outs, 3, ins, 2, nullptr))) return st;
+    bc::LogpArgs a = {};
+    a.x = d_scores;
+    a.action = d_action;
+    a.logp = d_logp;
+    a.entropy = d_entropy;
+    hipError_t e = bc::launch_logp(a, G, p, d_work, scores.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "action log probabilities launch");
+    return ok();
+}
+
+bc_status bc_clipped_policy_loss_work(bc_tensor scores, int32_t classes, int64_t *bytes)
+{
+    return action_work(scores, classes, true, bytes);
+}
+
+bc_status bc_clipped_policy_loss(const void *d_scores, bc_tensor scores, int32_t classes,
+                                 const void *d_action, const float *d_advantage,
+                                 const float *d_old_logp, const float *d_ref_logp,
+                                 const float *d_weight, const bc_policy_clip *clip, float scale,
+                                 void *d_grad, float *d_loss, float *d_kl, void *d_work,
+                                 int64_t work_bytes, void *stream)
+{
+    if (!d_scores || !d_action || !d_advantage || !d_old_logp || !clip)
+        return fail(BC_ERR_NULL, "d_scores, d_action, d_advantage, d_old_logp and clip are required");
+    if (!d_grad && !d_loss) return fail(BC_ERR_NULL, "d_grad or d_loss is required");
+    if (d_kl && !d_ref_logp) return fail(BC_ERR_NULL, "d_kl needs d_ref_logp");
+    bc::ScoreGeom G;
+    bc::ScorePlan p;
+    bc_status st = action_plan(scores, classes, true, G, p);
+    if (st) return st;
+    if (!(clip->low >= 0.f && clip->low <= 1.f) || !(clip->high >= 0.f) || !std::isfinite(clip->high))
+        return fail(BC_ERR_SHAPE, "the clipped range must be 1 - low .. 1 + high with low in 0 .. 1 and high >= 0, finite");
+    if (!(clip->beta >= 0.f) || !std::isfinite(clip->beta) || !std::isfinite(scale))
+        return fail(BC_ERR_SHAPE, "beta must be finite and not negative, scale finite");
+    if ((st = check_score_work(d_work, work_bytes, p.bytes))) return st;
+    const size_t px = (size_t)G.images * G.hw, sb = tensor_bytes(scores), nb = (size_t)G.images * 4;
+    const Extent ins[6] = {{d_scores, sb}, {d_action, px * (classes == 1 ? 1 : 4)}, {d_advantage, px * 4},
+                           {d_old_logp, px * 4}, {d_ref_logp, px * 4}, {d_weight, px * 4}};
+    const Extent outs[4] = {{d_grad, sb}, {d_loss, nb}, {d_kl, nb}, {d_work, p.bytes}};
+    if ((st = check_outputs(outs, 4, ins, 6, d_scores))) return st;
+    bc::ClipArgs a = {};
+    a.x = d_scores;
+    a.action = d_action;
+    a.advantage = d_advantage;
+    a.old_logp = d_old_logp;
+    a.ref_logp = d_ref_logp;
+    a.weight = d_weight;
+    a.grad = d_grad;
+    a.low = clip->low;
+    a.high = clip->high;
+    a.beta = clip->beta;
+    a.scale = scale;
+    hipError_t e = bc::launch_clip(a, G, p, d_work, d_loss, d_kl, scores.dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "policy loss launch");
+    return ok();
+}
+
 }  // extern "C"

@@ -232,4 +232,66 @@ bool orth_supported(const NewtonSchulz &ns, const char **why);
 hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_fmt, int out_fmt, const NewtonSchulz &ns,
                        hipStream_t s);
 
+// Score maps (k_scores.hip, k_top.hip): `classes` scores in rows of c elements, of which `len` are
+// read or written (c, or only the classes); per workgroups share an image's rows, or each row
+// is cut into `chunks` of `chunk` elements.
+struct ScoreGeom {
+    uint32_t images, hw;
+    int c, classes, len;
+    uint32_t per;
+    int chunks, chunk;
+};
+struct ScorePlan {
+    int form;
+    bool split;
+    size_t stats, pick, part, bytes;           // parts of the workspace, and its size
+};
+struct DistillArgs {
+    const void *x, *top;
+    const int32_t *index;
+    const float *rest, *weight;
+    void *grad;
+    float4 *stats;
+    float *pick;
+    double2 *part;
+    int top_fmt, k;
+    float inv_t, scale;
+};
+struct ClipArgs {
+    const void *x, *action;
+    const float *advantage, *old_logp, *ref_logp, *weight;
+    void *grad;
+    float4 *stats;
+    float *pick;
+    double2 *part;
+    float low, high, beta, scale;
+};
+struct LogpArgs {
+    const void *x, *action;
+    float *logp, *entropy;
+    float4 *stats;
+    float *pick;
+};
+// A teacher's record (k_top.hip), of every pixel or of the active blocks' (as NormGeom).
+struct TopArgs {
+    const void *x;
+    void *top;
+    int32_t *index;
+    float *rest;
+    int k;
+    float inv_t;
+    unsigned long long *keys;                  // of chunks: [row][chunk][k]
+    float4 *stats;
+    int gw, bh, bw;
+    Divisor by_block, by_gw, by_bw;
+    const int32_t *idx, *count;
+};
+// sets g.per, g.chunks and g.chunk; picks: scores per row that chunks hand on; sums: a loss is summed
+ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums);
+ScorePlan top_plan(ScoreGeom &g, int fmt, int k);
+hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, int fmt, hipStream_t s);
+hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, float *kl, int fmt, hipStream_t s);
+hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, int fmt, hipStream_t s);
+hipError_t launch_top(TopArgs a, ScoreGeom g, const ScorePlan &p, void *work, int fmt, hipStream_t s);
+
 }  // namespace bc

@@ -42,23 +42,6 @@ __device__ __forceinline__ uint32_t row_count(const NormGeom &g)
     return g.idx ? (uint32_t)*g.count * (uint32_t)(g.bh * g.bw) : g.rows;
 }
 
-__device__ __forceinline__ uint32_t div(uint32_t n, const Divisor &d)
-{
-    const uint32_t t = __umulhi(n, d.mul);
-    return (t + ((n - t) >> d.first)) >> d.then;
-}
-
-// Pixel of row r: itself, or the pixel of an active block. Block rows of all images follow
-// one another (id / gw), and so do their pixel rows.
-__device__ __forceinline__ uint32_t row_pixel(const NormGeom &g, uint32_t r)
-{
-    if (!g.idx) return r;
-    const uint32_t k = div(r, g.by_block), p = r - k * (uint32_t)(g.bh * g.bw);
-    const uint32_t id = g.idx[k], row = div(id, g.by_gw), gx = id - row * g.gw;
-    const uint32_t py = div(p, g.by_bw), px = p - py * g.bw;
-    return (row * g.bh + py) * (g.gw * g.bw) + gx * g.bw + px;
-}
-
 // Sums of N values over the L lanes of a row: part of a wave, or two or four waves (through
 // `lds`, their slots, free for reuse after the next sum's barrier; the whole workgroup calls).
 template <int L, int N>

@@ -120,6 +120,27 @@ __device__ __forceinline__ float lane_sum(float v)
     return v;
 }
 
+// n / d by d's Divisor.
+template <typename D>
+__device__ __forceinline__ uint32_t div(uint32_t n, const D &d)
+{
+    const uint32_t t = __umulhi(n, d.mul);
+    return (t + ((n - t) >> d.first)) >> d.then;
+}
+
+// Pixel of row r: itself, or the pixel of an active block (geometry g: idx, gw, bh, bw and the
+// divisors by_block, by_gw, by_bw). Block rows of all images follow one another (id / gw), and
+// so do their pixel rows.
+template <typename G>
+__device__ __forceinline__ uint32_t row_pixel(const G &g, uint32_t r)
+{
+    if (!g.idx) return r;
+    const uint32_t k = div(r, g.by_block), p = r - k * (uint32_t)(g.bh * g.bw);
+    const uint32_t id = g.idx[k], row = div(id, g.by_gw), gx = id - row * g.gw;
+    const uint32_t py = div(p, g.by_bw), px = p - py * g.bw;
+    return (row * g.bh + py) * (g.gw * g.bw) + gx * g.bw + px;
+}
+
 // f(integral_constant of the format) for a bc_dtype.
 template <typename F>
 auto with_format(int fmt, F &&f)
