@@ -233,18 +233,23 @@ hipError_t launch_orth(const OrthTable &T, const OrthStep &h, bool step, int in_
                        hipStream_t s);
 
 // Score maps (k_scores.hip, k_top.hip): `classes` scores in rows of c elements, of which `len` are
-// read or written (c, or only the classes); per workgroups share an image's rows, or each row
+// read or written (c, or only the classes). `per` workgroups take an image's rows, or each row
 // is cut into `chunks` of `chunk` elements.
 struct ScoreGeom {
     uint32_t images, hw;
     int c, classes, len;
     uint32_t per;
     int chunks, chunk;
+    Divisor by_per, by_chunks, by_out;         // by_out: vectors (or elements) of a row that is written
 };
 struct ScorePlan {
     int form;
     bool split;
     size_t stats, pick, part, bytes;           // parts of the workspace, and its size
+};
+struct LossOut {
+    double2 *part;                             // each workgroup's sums, where an image has several
+    float *loss, *kl;                          // the images', or nullptr
 };
 struct DistillArgs {
     const void *x, *top;
@@ -253,7 +258,7 @@ struct DistillArgs {
     void *grad;
     float4 *stats;
     float *pick;
-    double2 *part;
+    LossOut out;
     int top_fmt, k;
     float inv_t, scale;
 };
@@ -263,7 +268,7 @@ struct ClipArgs {
     void *grad;
     float4 *stats;
     float *pick;
-    double2 *part;
+    LossOut out;
     float low, high, beta, scale;
 };
 struct LogpArgs {
@@ -283,10 +288,10 @@ struct TopArgs {
     unsigned long long *keys;                  // of chunks: [row][chunk][k]
     float4 *stats;
     int gw, bh, bw;
-    Divisor by_block, by_gw, by_bw;
+    Divisor by_block, by_gw, by_bw, by_k;
     const int32_t *idx, *count;
 };
-// sets g.per, g.chunks and g.chunk; picks: scores per row that chunks hand on; sums: a loss is summed
+// sets g's per, chunks and divisors; picks: scores per row that chunks hand on; sums: a loss is summed
 ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums);
 ScorePlan top_plan(ScoreGeom &g, int fmt, int k);
 hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, int fmt, hipStream_t s);

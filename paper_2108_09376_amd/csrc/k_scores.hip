@@ -25,23 +25,72 @@ namespace {
 
 constexpr int kMaxTop = 64;
 
-// The sums of a workgroup's groups (first thread of each) in the order of the groups.
-template <int L>
-__device__ __forceinline__ void write_part(double loss, double kl, double2 *out)
+// Sum over the workgroup of T threads, in the first thread.
+template <int T>
+__device__ __forceinline__ double2 team_sum(double x, double y)
 {
-    constexpr int G = kThreadsOf<L> / (L <= 64 ? L : kThreadsOf<L>);
-    __shared__ double2 sums[G];
-    if (threadIdx.x % L == 0) sums[threadIdx.x / L] = make_double2(loss, kl);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double2 s = sums[0];
-        for (int i = 1; i < G; ++i) {
-            s.x += sums[i].x;
-            s.y += sums[i].y;
-        }
-        *out = s;
+    __shared__ double2 waves[T / 64];
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        x += __shfl_xor(x, d);
+        y += __shfl_xor(y, d);
     }
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = make_double2(x, y);
     __syncthreads();
+    double2 s = waves[0];
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int i = 1; i < T / 64; ++i) {
+            s.x += waves[i].x;
+            s.y += waves[i].y;
+        }
+    return s;
+}
+
+__device__ __forceinline__ bool wanted(const LossOut &o) { return o.loss || o.kl; }
+
+// A workgroup's loss to its place, or to the image's where it has one to itself.
+__device__ __forceinline__ void write_sums(const LossOut &o, const ScoreGeom &g, uint32_t item, double loss, double kl)
+{
+    if (threadIdx.x != 0) return;
+    if (g.per == 1) {
+        if (o.loss) o.loss[item] = (float)loss;
+        if (o.kl) o.kl[item] = (float)kl;
+    } else {
+        o.part[item] = make_double2(loss, kl);
+    }
+}
+
+// Where a workgroup's work lies: its rows from `row` on (a group's own is row + group, if p < hw), and the
+// chunk of it.
+struct Place {
+    uint32_t item, image, p;
+    size_t row;
+    int chunk;
+};
+
+template <int G, int PASS>
+__device__ __forceinline__ Place place_of(const ScoreGeom &g)
+{
+    Place w;
+    uint32_t item = item_of();
+    w.chunk = 0;
+    if constexpr (PASS != kWhole) {
+        const uint32_t r = div(item, g.by_chunks);
+        w.chunk = (int)(item - r * (uint32_t)g.chunks);
+        item = r;
+    }
+    w.item = item;
+    w.image = div(item, g.by_per);
+    w.p = (item - w.image * g.per) * G;
+    w.row = (size_t)w.image * g.hw + w.p;
+    return w;
+}
+
+template <int PASS>
+__device__ __forceinline__ bool past_end(const ScoreGeom &g)
+{
+    return item_of() >= g.images * g.per * (PASS == kWhole ? 1u : (uint32_t)g.chunks);
 }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -64,6 +113,15 @@ __device__ __forceinline__ float exp_above_line(float x)
 
 // ---------------------------------------------------------------- divergence from a record
 
+// An entry's part p log(p / q) - p + q of the divergence, d = log(p / q): both distributions sum to 1, so
+// that the added terms do not count, but the first order of the errors in d cancels. A class's
+// second entry has no q of its own.
+__device__ __forceinline__ float divergence(float p, float q, float d, bool lead)
+{
+    if (!(p > 0.f)) return (lead ? q : 0.f) + p;                 // 0, or a NaN
+    return p * (lead ? exp_above_line(-d) : d - 1.f);
+}
+
 // The entries of a group's record, as its lanes share them.
 struct Record {
     int index[kMaxTop];                        // within the chunk; -1: not this entry's to write
@@ -75,12 +133,14 @@ template <int FMT, int L, int NV, int PASS>
 __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
-    constexpr int T = kThreadsOf<L>, G = L <= 64 ? T / L : 1;
+    constexpr int T = kThreadsOf<L>, G = kGroupsOf<L>;
     constexpr int EL = L < 64 ? L : 64, SLOTS = kMaxTop / EL;    // lanes that hold entries, entries of each
     __shared__ int head[T];                    // a thread's first entry + 1 (0: none)
     __shared__ Record records[G];
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
     __shared__ float pub[2];
+    if (past_end<PASS>(g)) return;
+    const Place w = place_of<G, PASS>(g);
     const int group = L <= 64 ? threadIdx.x / L : 0, lane = threadIdx.x % L;
     Record &rec = records[group];
     const bool holder = L <= 64 || threadIdx.x < 64;             // of entries
@@ -89,61 +149,49 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
         if constexpr (L > 64) __syncthreads();
         else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     };
-    head[threadIdx.x] = 0;
-    __syncthreads();
-
-    const size_t items = PASS == kWhole ? (size_t)g.images * g.per : (size_t)g.images * g.hw * g.chunks;
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        double loss = 0.0;
-        const size_t first = PASS == kWhole ? item / g.per * g.hw : item / g.chunks;
-        const int chunk = PASS == kWhole ? 0 : (int)(item % g.chunks);
-        uint32_t p = PASS == kWhole ? (uint32_t)(item % g.per) * G + group : 0;
-        // groups of one wave end at rows of their own; a workgroup has one group
-        for (; p < (PASS == kWhole ? g.hw : 1u); p += g.per * G) {
-            const Chunk c = chunk_of<PASS>(g, first + p, chunk);
-            const float wt = a.weight ? a.weight[c.row] : 1.f;
-            if (wt == 0.f) {
-                if (PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
-                continue;
-            }
-            if (L > 64) __syncthreads();                         // the last row's entries are done with
-            Row row;
-            row.load(a.x, c.base, c.len, c.live);
-            // entries: class, teacher's score, student's score
-            int idx[SLOTS];
-            float tt[SLOTS], zk[SLOTS];
+    const bool inside = w.p + group < g.hw;
+    const Chunk c = chunk_of<PASS>(g, inside ? w.row + group : w.row, w.chunk);
+    const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f;
+    double loss = 0.0;
+    if (wt == 0.f) {
+        if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
+    } else {
+        Row row;
+        row.load(a.x, c.base, c.len, c.live);
+        head[threadIdx.x] = 0;
+        meet();
+        // entries: class, teacher's score, student's score
+        int idx[SLOTS];
+        float tt[SLOTS], zk[SLOTS];
 #pragma unroll
-            for (int s = 0; s < SLOTS; ++s) {
-                const int e = s * EL + lane;
-                idx[s] = -1;
-                tt[s] = zk[s] = -kInf;
-                if (!holder || e >= a.k) continue;
-                const int i = a.index[c.row * a.k + e];
-                const bool valid = (unsigned)i < (unsigned)g.classes;
-                if (valid) {
-                    idx[s] = i;
-                    tt[s] = load_elem(a.top, a.top_fmt, c.row * a.k + e) * a.inv_t;
-                    if constexpr (PASS == kSecond) zk[s] = a.pick[c.row * a.k + e];
-                    else zk[s] = load_elem(a.x, FMT, c.row * (size_t)g.c + i);
-                }
-                const int local = valid && i >= c.off && i < c.off + c.len ? i - c.off : -1;
-                rec.index[e] = local;
-                if (local >= 0) rec.next[e] = atomicExch(&head[group * L + Row::owner(local, c.len)], e + 1);
-                if constexpr (PASS == kFirst)
-                    if (local >= 0) a.pick[c.row * a.k + e] = zk[s];
+        for (int s = 0; s < SLOTS; ++s) {
+            const int e = s * EL + lane;
+            idx[s] = -1;
+            tt[s] = zk[s] = -kInf;
+            if (!holder || e >= a.k) continue;
+            const int i = a.index[c.row * a.k + e];
+            const bool valid = (unsigned)i < (unsigned)g.classes;
+            if (valid) {
+                idx[s] = i;
+                tt[s] = load_elem(a.top, a.top_fmt, c.row * a.k + e) * a.inv_t;
+                if constexpr (PASS == kSecond) zk[s] = a.pick[c.row * a.k + e];
+                else zk[s] = load_elem(a.x, FMT, c.row * (size_t)g.c + i);
             }
-            meet();
-            Stats st = {};
-            if constexpr (PASS != kSecond) {
-                for (int h = head[threadIdx.x]; h; h = rec.next[h - 1]) row.mask(rec.index[h - 1], c.len);
-                st = team_stats<L, false>(row.template stats<false>(k2), waves, k2);
-            }
-            if constexpr (PASS == kFirst) {
-                if (threadIdx.x == 0) a.stats[item] = make_float4(st.m, st.s, 0.f, 0.f);
-                meet();
-                head[threadIdx.x] = 0;
-                continue;
-            }
+            const int local = valid && i >= c.off && i < c.off + c.len ? i - c.off : -1;
+            rec.index[e] = local;
+            if (local >= 0) rec.next[e] = atomicExch(&head[group * L + Row::owner(local, c.len)], e + 1);
+            if constexpr (PASS == kFirst)
+                if (local >= 0) a.pick[c.row * a.k + e] = zk[s];
+        }
+        meet();
+        Stats st = {};
+        if constexpr (PASS != kSecond) {
+            for (int h = head[threadIdx.x]; h; h = rec.next[h - 1]) row.mask(rec.index[h - 1], c.len);
+            st = team_stats<L, false>(row.template stats<false>(k2), waves, k2);
+        }
+        if constexpr (PASS == kFirst) {
+            if (threadIdx.x == 0) a.stats[c.row * g.chunks + w.chunk] = make_float4(st.m, st.s, 0.f, 0.f);
+        } else {
             float F = 0.f, m_r = 0.f;
             if (holder) {
                 if constexpr (PASS == kSecond) st = row_stats<false>(a.stats + c.row * g.chunks, g.chunks, k2);
@@ -205,10 +253,9 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
                 for (int s = 0; s < SLOTS; ++s) {
                     if (s * EL >= a.k) continue;
                     const float q = ek[s] * inv, pp = pk[s] * tinv;
-                    // log(p / q), and p log(p / q) - p + q: both distributions sum to 1
                     const float d = (tt[s] - Mt) - (zk[s] - M) * a.inv_t + logs;
                     if (idx[s] >= 0) {
-                        each += lead[s] ? (pp > 0.f ? pp * exp_above_line(-d) : q + pp) : (pp > 0.f ? pp * (d - 1.f) : pp);
+                        each += divergence(pp, q, d, lead[s]);
                         diff += pp - (lead[s] ? q : 0.f);
                     }
                 }
@@ -217,7 +264,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
                 const float dr = (rest - Mt) - ((st.m - M) * a.inv_t + __logf(st.s)) + logs;
                 each += p_r > 0.f ? (st.s == 0.f ? kInf : p_r * exp_above_line(-dr)) : q_r + p_r;
                 if (!(q_r > 0.5f)) diff = q_r - p_r;
-                if (part) loss += (double)(scale * each);
+                if (part && lane == 0) loss = (double)(scale * each);
                 const float by = scale * a.inv_t;
                 F = part && st.s != 0.f ? by * diff / st.s : 0.f;
                 m_r = st.m == -kInf ? 0.f : st.m;
@@ -258,11 +305,108 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
                         store_raw<FMT, 1>(a.grad, c.base + rec.index[h - 1], pack<FMT, 1>(y));
                     }
             }
-            head[threadIdx.x] = 0;
         }
-        if (PASS == kWhole && a.part) write_part<L>(loss, 0.0, a.part + item);
-        if (PASS == kSecond && a.part && chunk == 0 && threadIdx.x == 0) a.part[item / g.chunks] = make_double2(loss, 0.0);
     }
+    if (PASS == kFirst || !wanted(a.out) || w.chunk != 0) return;
+    if constexpr (L > 64) {
+        write_sums(a.out, g, w.item, loss, 0.0);
+    } else {
+        const double2 sum = team_sum<T>(lane == 0 ? loss : 0.0, 0.0);
+        write_sums(a.out, g, w.item, sum.x, 0.0);
+    }
+}
+
+// A pixel of few classes to a thread: its scores in registers and, to be picked by index, in
+// LDS, from where the workgroup's gradients leave in whole vectors.
+template <int FMT, int N>
+__global__ __launch_bounds__(256) void k_distill_pixel(DistillArgs a, ScoreGeom g)
+{
+    __shared__ float lds[256][N + 1];
+    if (past_end<kWhole>(g)) return;
+    const Place w = place_of<256, kWhole>(g);
+    const uint32_t rows = min(256u, g.hw - w.p);
+    const bool inside = threadIdx.x < rows;
+    const size_t r = w.row + (inside ? threadIdx.x : 0);
+    float *mine = lds[threadIdx.x];
+    const float wt = !inside ? 0.f : a.weight ? a.weight[r] : 1.f;
+    const float k2 = kLog2e * a.inv_t;
+    double loss = 0.0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine[j] = 0.f;
+    if (wt != 0.f) {
+        PixelScores<FMT, N> px;
+        px.load(a.x, r * (size_t)g.c, g.c, g.classes);
+#pragma unroll
+        for (int j = 0; j < N; ++j) mine[j] = px.z[j];
+        const size_t e0 = r * (size_t)a.k;
+        uint32_t record = 0;
+        const float rest = a.rest ? a.rest[r] : -kInf;
+        float Mt = rest;
+        for (int e = 0; e < a.k; ++e) {
+            const int i = a.index[e0 + e];
+            if ((unsigned)i >= (unsigned)g.classes) continue;
+            record |= 1u << i;
+            Mt = fmaxf(Mt, load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t);
+        }
+        float m_r = -kInf, M = -kInf;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            M = fmaxf(M, px.z[j]);
+            m_r = fmaxf(m_r, record >> j & 1 ? -kInf : px.z[j]);
+        }
+        M = M == -kInf ? 0.f : M;
+        Mt = Mt == -kInf ? 0.f : Mt;
+        m_r = m_r == -kInf ? 0.f : m_r;
+        float top = 0.f, s = 0.f, tp = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool in = record >> j & 1;
+            px.z[j] = exp2_of(px.z[j], in ? M : m_r, k2);
+            top += in ? px.z[j] : 0.f;
+            s += in ? 0.f : px.z[j];
+        }
+        for (int e = 0; e < a.k; ++e)
+            if ((unsigned)a.index[e0 + e] < (unsigned)g.classes) tp += exp_of(load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt);
+        const float er = s == 0.f ? 0.f : s * exp2_of(m_r, M, k2), total = top + er;
+        const float tr = a.rest ? exp_of(rest - Mt) : 0.f, ttotal = tp + tr;
+        const bool part = total != 0.f && ttotal != 0.f;        // a NaN takes part
+        const float inv = 1.f / total, tinv = 1.f / ttotal, logs = __logf(total) - __logf(ttotal);
+        const float q_r = er * inv, p_r = tr * tinv, scale = wt * a.scale;
+        float each = 0.f, diff = 0.f;
+        uint32_t seen = 0;
+        for (int e = 0; e < a.k; ++e) {
+            const int i = a.index[e0 + e];
+            if ((unsigned)i >= (unsigned)g.classes) continue;
+            const float t = load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt, x = mine[i] - M;
+            const bool lead = !(seen >> i & 1);
+            seen |= 1u << i;
+            const float p = exp_of(t) * tinv, q = __builtin_amdgcn_exp2f(x * k2) * inv, d = t - x * a.inv_t + logs;
+            each += divergence(p, q, d, lead);
+            diff += p - (lead ? q : 0.f);
+        }
+        const float dr = (rest - Mt) - ((m_r - M) * a.inv_t + __logf(s)) + logs;
+        each += p_r > 0.f ? (s == 0.f ? kInf : p_r * exp_above_line(-dr)) : q_r + p_r;
+        if (!(q_r > 0.5f)) diff = q_r - p_r;
+        if (part) loss = (double)(scale * each);
+        const float by = scale * a.inv_t, F = part && s != 0.f ? by * diff / s : 0.f, in_record = part ? by * inv : 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float f = record >> j & 1 ? in_record : F;
+            mine[j] = f == 0.f ? 0.f : px.z[j] * f;
+        }
+        if (part)
+            for (int e = 0; e < a.k; ++e) {
+                const int i = a.index[e0 + e];
+                if ((unsigned)i < (unsigned)g.classes)
+                    mine[i] -= by * tinv * exp_of(load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt);
+            }
+    }
+    __syncthreads();
+    if (a.grad)
+        store_pixels<FMT>(a.grad, w.row, rows, g.c, g.classes, g.by_out, [&](uint32_t p, int j) { return lds[p][j]; });
+    if (!wanted(a.out)) return;
+    const double2 sum = team_sum<256>(loss, 0.0);
+    write_sums(a.out, g, w.item, sum.x, 0.0);
 }
 
 // ---------------------------------------------------------------- policy
@@ -310,45 +454,38 @@ template <int FMT, int L, int NV, int PASS>
 __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
-    constexpr int T = kThreadsOf<L>, G = L <= 64 ? T / L : 1;
+    constexpr int T = kThreadsOf<L>, G = kGroupsOf<L>;
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
     __shared__ float pub[3];
+    if (past_end<PASS>(g)) return;
+    const Place w = place_of<G, PASS>(g);
     const int group = L <= 64 ? threadIdx.x / L : 0;
-    const int32_t *action = (const int32_t *)a.action;
-    const size_t items = PASS == kWhole ? (size_t)g.images * g.per : (size_t)g.images * g.hw * g.chunks;
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        double loss = 0.0, kl = 0.0;
-        const size_t first = PASS == kWhole ? item / g.per * g.hw : item / g.chunks;
-        const int chunk = PASS == kWhole ? 0 : (int)(item % g.chunks);
-        uint32_t p = PASS == kWhole ? (uint32_t)(item % g.per) * G + group : 0;
-        for (; p < (PASS == kWhole ? g.hw : 1u); p += g.per * G) {
-            const Chunk c = chunk_of<PASS>(g, first + p, chunk);
-            const float wt = a.weight ? a.weight[c.row] : 1.f;
-            const int act = action[c.row];
-            if (wt == 0.f || (unsigned)act >= (unsigned)g.classes) {
-                if (PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
-                continue;
+    const bool inside = w.p + group < g.hw;
+    const Chunk c = chunk_of<PASS>(g, inside ? w.row + group : w.row, w.chunk);
+    const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f;
+    const int act = ((const int32_t *)a.action)[c.row];
+    double loss = 0.0, kl = 0.0;
+    if (wt == 0.f || (unsigned)act >= (unsigned)g.classes) {
+        if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
+    } else {
+        Row row;
+        row.load(a.x, c.base, c.len, c.live);
+        const int at = act - c.off;                              // the action's place in the chunk
+        const bool here = at >= 0 && at < c.len, mine = here && Row::owner(at, c.len) == Row::lane();
+        float za = -kInf;
+        if constexpr (PASS == kSecond) za = a.pick[c.row];
+        else if (here) za = load_elem(a.x, FMT, c.base + at);
+        Stats st = {};
+        if constexpr (PASS != kSecond) {
+            if (mine) row.mask(at, c.len);
+            st = team_stats<L, false>(row.template stats<false>(kLog2e), waves, kLog2e);
+        }
+        if constexpr (PASS == kFirst) {
+            if (threadIdx.x == 0) {
+                a.stats[c.row * g.chunks + w.chunk] = make_float4(st.m, st.s, 0.f, 0.f);
+                if (here) a.pick[c.row] = za;
             }
-            Row row;
-            row.load(a.x, c.base, c.len, c.live);
-            float za = -kInf;
-            if constexpr (PASS == kSecond) za = a.pick[c.row];
-            else if (PASS == kWhole || (act >= c.off && act < c.off + c.len)) za = load_elem(a.x, FMT, c.row * (size_t)g.c + act);
-            const int at = act - c.off;                          // the action's place in the chunk
-            const bool mine = at >= 0 && at < c.len && Row::owner(at, c.len) == Row::lane();
-            Stats st = {};
-            if constexpr (PASS != kSecond) {
-                if (mine) row.mask(at, c.len);
-                st = team_stats<L, false>(row.template stats<false>(kLog2e), waves, kLog2e);
-            }
-            if constexpr (PASS == kFirst) {
-                if (threadIdx.x == 0) {
-                    a.stats[item] = make_float4(st.m, st.s, 0.f, 0.f);
-                    if (at >= 0 && at < c.len) a.pick[c.row] = za;
-                }
-                __syncthreads();
-                continue;
-            }
+        } else {
             float F = 0.f, own = 0.f, m = 0.f;
             if (L <= 64 || threadIdx.x < 64) {
                 if constexpr (PASS == kSecond) st = row_stats<false>(a.stats + c.row * g.chunks, g.chunks, kLog2e);
@@ -356,8 +493,10 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
                     const Chosen ch = chosen(za, st);
                     const Decision d = decide(a, c.row, ch.l);
                     const double by = (double)wt * (double)a.scale;
-                    loss += by * d.loss;
-                    kl += by * d.kl;
+                    if (Row::lane() == 0) {
+                        loss = by * d.loss;
+                        kl = by * d.kl;
+                    }
                     own = (float)(by * d.slope * ch.other);
                     F = st.s == 0.f ? 0.f : (float)(-by * d.slope * ch.other / (double)st.s);
                     m = st.m == -kInf ? 0.f : st.m;
@@ -384,9 +523,89 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
                 }
             }
         }
-        if (PASS == kWhole && a.part) write_part<L>(loss, kl, a.part + item);
-        if (PASS == kSecond && a.part && chunk == 0 && threadIdx.x == 0) a.part[item / g.chunks] = make_double2(loss, kl);
     }
+    if (PASS == kFirst || !wanted(a.out) || w.chunk != 0) return;
+    if constexpr (L > 64) {
+        write_sums(a.out, g, w.item, loss, kl);
+    } else {
+        const double2 sum = team_sum<T>(loss, kl);
+        write_sums(a.out, g, w.item, sum.x, sum.y);
+    }
+}
+
+// A pixel of few classes to a thread; with one class, decisions to execute its block or not:
+// pi(1) = sigmoid(z).
+struct Binary {
+    double l, other;                           // log pi(action), 1 - pi(action)
+};
+
+__device__ __forceinline__ Binary binary(float z, bool executed)
+{
+    const double x = executed ? (double)z : -(double)z, t = exp(-fabs(x));
+    return {(x < 0.0 ? x : 0.0) - log1p(t), (x < 0.0 ? 1.0 : t) / (1.0 + t)};
+}
+
+template <int FMT, int N>
+__global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
+{
+    __shared__ float lds[256][N + 1];
+    if (past_end<kWhole>(g)) return;
+    const Place w = place_of<256, kWhole>(g);
+    const uint32_t rows = min(256u, g.hw - w.p);
+    const bool inside = threadIdx.x < rows;
+    const size_t r = w.row + (inside ? threadIdx.x : 0);
+    float *mine = lds[threadIdx.x];
+    const float wt = !inside ? 0.f : a.weight ? a.weight[r] : 1.f;
+    const double by = (double)wt * (double)a.scale;
+    double loss = 0.0, kl = 0.0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine[j] = 0.f;
+    if constexpr (N == 1) {
+        const bool executed = ((const uint8_t *)a.action)[r] != 0;
+        const Binary b = binary(load_elem(a.x, FMT, r * (size_t)g.c), executed);
+        if (wt != 0.f && b.l != -(double)kInf) {
+            const Decision d = decide(a, r, b.l);
+            loss = by * d.loss;
+            kl = by * d.kl;
+            mine[0] = (float)(by * d.slope * (executed ? b.other : -b.other));
+        }
+    } else {
+        const int act = ((const int32_t *)a.action)[r];
+        if (wt != 0.f && (unsigned)act < (unsigned)g.classes) {
+            PixelScores<FMT, N> px;
+            px.load(a.x, r * (size_t)g.c, g.c, g.classes);
+            float za = -kInf, m = -kInf, s = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                za = j == act ? px.z[j] : za;
+                px.z[j] = j == act ? -kInf : px.z[j];
+                m = fmaxf(m, px.z[j]);
+            }
+            const float ref = m == -kInf ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                px.z[j] = exp2_of(px.z[j], ref, kLog2e);
+                s += px.z[j];
+            }
+            if (za != -kInf) {
+                const Chosen ch = chosen(za, {m, s, 0.f});
+                const Decision d = decide(a, r, ch.l);
+                loss = by * d.loss;
+                kl = by * d.kl;
+                const float F = s == 0.f ? 0.f : (float)(-by * d.slope * ch.other / (double)s);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mine[j] = F == 0.f ? 0.f : px.z[j] * F;
+                mine[act] = (float)(by * d.slope * ch.other);
+            }
+        }
+    }
+    __syncthreads();
+    if (a.grad)
+        store_pixels<FMT>(a.grad, w.row, rows, g.c, g.classes, g.by_out,
+                          [&](uint32_t p, int j) { return j < N ? lds[p][j] : 0.f; });
+    if (!wanted(a.out)) return;
+    const double2 sum = team_sum<256>(loss, kl);
+    write_sums(a.out, g, w.item, sum.x, sum.y);
 }
 
 // st: of all classes but a valid action.
@@ -399,68 +618,49 @@ __device__ __forceinline__ void finish_logp(const LogpArgs &a, size_t row, bool 
     a.entropy[row] = st.s == 0.f || h < 0.0 ? 0.f : (float)h;
 }
 
-template <int FMT, int L, int NV, int PASS>
+template <int FMT, int L, int NV, int PASS, bool SX>
 __global__ __launch_bounds__((kThreadsOf<L>)) void k_logp(LogpArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
-    constexpr int T = kThreadsOf<L>, G = L <= 64 ? T / L : 1;
+    constexpr int G = kGroupsOf<L>;
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
+    if (past_end<PASS>(g)) return;
+    const Place w = place_of<G, PASS>(g);
     const int group = L <= 64 ? threadIdx.x / L : 0;
-    const int32_t *action = (const int32_t *)a.action;
-    const size_t rows = (size_t)g.images * g.hw, items = PASS == kWhole ? (rows + G - 1) / G : rows * g.chunks;
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const size_t r = PASS == kWhole ? item * G + group : item / g.chunks;
-        if (r >= rows) continue;
-        const int chunk = PASS == kWhole ? 0 : (int)(item % g.chunks);
-        const Chunk c = chunk_of<PASS>(g, r, chunk);
-        const int act = action[r], at = act - c.off;
-        const bool valid = (unsigned)act < (unsigned)g.classes, here = valid && at >= 0 && at < c.len;
-        Row row;
-        row.load(a.x, c.base, c.len, c.live);
-        const float za = here ? load_elem(a.x, FMT, c.row * (size_t)g.c + act) : -kInf;
-        if (here && Row::owner(at, c.len) == Row::lane()) row.mask(at, c.len);
-        Stats st = a.entropy ? team_stats<L, true>(row.template stats<true>(kLog2e), waves, kLog2e)
-                             : team_stats<L, false>(row.template stats<false>(kLog2e), waves, kLog2e);
-        if (Row::lane() == 0) {
-            if constexpr (PASS == kFirst) {
-                a.stats[item] = make_float4(st.m, st.s, st.sx, 0.f);
-                if (here) a.pick[r] = za;
-            } else {
-                finish_logp(a, r, valid, za, st);
-            }
-        }
-        if constexpr (L > 64) __syncthreads();
+    if (w.p + group >= g.hw) return;
+    const Chunk c = chunk_of<PASS>(g, w.row + group, w.chunk);
+    Row row;
+    row.load(a.x, c.base, c.len, c.live);
+    const int act = ((const int32_t *)a.action)[c.row], at = act - c.off;
+    const bool valid = (unsigned)act < (unsigned)g.classes, here = valid && at >= 0 && at < c.len;
+    const float za = here ? load_elem(a.x, FMT, c.base + at) : -kInf;
+    if (here && Row::owner(at, c.len) == Row::lane()) row.mask(at, c.len);
+    const Stats st = team_stats<L, SX>(row.template stats<SX>(kLog2e), waves, kLog2e);
+    if (Row::lane() != 0) return;
+    if constexpr (PASS == kFirst) {
+        a.stats[c.row * g.chunks + w.chunk] = make_float4(st.m, st.s, st.sx, 0.f);
+        if (here) a.pick[c.row] = za;
+    } else {
+        finish_logp(a, c.row, valid, za, st);
     }
 }
 
 // The chunks of each row joined, one row per thread.
 __global__ __launch_bounds__(64) void k_logp_join(LogpArgs a, ScoreGeom g)
 {
-    const size_t rows = (size_t)g.images * g.hw;
-    for (size_t r = (size_t)blockIdx.x * 64 + threadIdx.x; r < rows; r += (size_t)gridDim.x * 64) {
-        const Stats st = row_stats<true>(a.stats + r * g.chunks, g.chunks, kLog2e);
-        const bool valid = (unsigned)((const int32_t *)a.action)[r] < (unsigned)g.classes;
-        finish_logp(a, r, valid, valid ? a.pick[r] : -kInf, st);
-    }
+    const size_t r = (size_t)item_of() * 64 + threadIdx.x;
+    if (r >= (size_t)g.images * g.hw) return;
+    const Stats st = row_stats<true>(a.stats + r * g.chunks, g.chunks, kLog2e);
+    const bool valid = (unsigned)((const int32_t *)a.action)[r] < (unsigned)g.classes;
+    finish_logp(a, r, valid, valid ? a.pick[r] : -kInf, st);
 }
 
-// Decisions to execute a block or not: pi(1) = sigmoid(z). A pixel belongs to one thread, which
-// writes its channels' gradient too (0 past the first).
-struct Binary {
-    double l, other;                           // log pi(action), 1 - pi(action)
-};
-
-__device__ __forceinline__ Binary binary(float z, bool executed)
+template <int FMT, int N>
+__global__ __launch_bounds__(256) void k_logp_pixel(LogpArgs a, ScoreGeom g)
 {
-    const double x = executed ? (double)z : -(double)z, t = exp(-fabs(x));
-    return {(x < 0.0 ? x : 0.0) - log1p(t), (x < 0.0 ? 1.0 : t) / (1.0 + t)};
-}
-
-template <int FMT>
-__global__ __launch_bounds__(256) void k_logp_binary(LogpArgs a, ScoreGeom g)
-{
-    const size_t rows = (size_t)g.images * g.hw;
-    for (size_t r = (size_t)blockIdx.x * 256 + threadIdx.x; r < rows; r += (size_t)gridDim.x * 256) {
+    const size_t r = (size_t)item_of() * 256 + threadIdx.x;
+    if (r >= (size_t)g.images * g.hw) return;
+    if constexpr (N == 1) {
         const float z = load_elem(a.x, FMT, r * (size_t)g.c);
         const Binary b = binary(z, ((const uint8_t *)a.action)[r] != 0);
         a.logp[r] = (float)b.l;
@@ -470,81 +670,54 @@ __global__ __launch_bounds__(256) void k_logp_binary(LogpArgs a, ScoreGeom g)
             const double far = up.other * fabs((double)z);
             a.entropy[r] = (float)(-up.l + (z - z == 0.f ? far : 0.0) + (z != z ? (double)z : 0.0));
         }
-    }
-}
-
-template <int FMT>
-__global__ __launch_bounds__(256) void k_clip_binary(ClipArgs a, ScoreGeom g)
-{
-    constexpr int VEC = kVec<FMT>;
-    const size_t items = (size_t)g.images * g.per;
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        double loss = 0.0, kl = 0.0;
-        const size_t first = item / g.per * g.hw;
-        for (uint32_t p = (uint32_t)(item % g.per) * 256 + threadIdx.x; p < g.hw; p += g.per * 256) {
-            const size_t r = first + p, base = r * (size_t)g.c;
-            const float wt = a.weight ? a.weight[r] : 1.f;
-            float y[1] = {0.f};
-            if (wt != 0.f) {
-                const bool executed = ((const uint8_t *)a.action)[r] != 0;
-                const float z = load_elem(a.x, FMT, base);
-                const Binary b = binary(z, executed);
-                if (b.l != -(double)kInf) {
-                    const Decision d = decide(a, r, b.l);
-                    const double by = (double)wt * (double)a.scale;
-                    loss += by * d.loss;
-                    kl += by * d.kl;
-                    y[0] = (float)(by * d.slope * (executed ? b.other : -b.other));
-                }
-            }
-            if (a.grad) {
-                store_raw<FMT, 1>(a.grad, base, pack<FMT, 1>(y));
-                const Raw<FMT, 1> zero = {};
-                const Raw<FMT, VEC> zeros = {};
-                int e = 1;
-                for (; e + VEC <= g.c; e += VEC) store_raw<FMT, VEC>(a.grad, base + e, zeros);
-                for (; e < g.c; ++e) store_raw<FMT, 1>(a.grad, base + e, zero);
-            }
+    } else {
+        PixelScores<FMT, N> px;
+        px.load(a.x, r * (size_t)g.c, g.c, g.classes);
+        const int act = ((const int32_t *)a.action)[r];
+        Stats st = {-kInf, 0.f, 0.f};
+        float za = -kInf;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            za = j == act ? px.z[j] : za;
+            px.z[j] = j == act ? -kInf : px.z[j];
+            st.m = fmaxf(st.m, px.z[j]);
         }
-        if (a.part) write_part<1>(loss, kl, a.part + item);
+        const float ref = st.m == -kInf ? 0.f : st.m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float x = px.z[j] - ref, e = __builtin_amdgcn_exp2f(x * kLog2e);
+            st.s += e;
+            st.sx += e * fmaxf(x, -1e30f);
+        }
+        finish_logp(a, r, (unsigned)act < (unsigned)g.classes, za, st);
     }
 }
 
 // ---------------------------------------------------------------- sums of the losses
 
-__global__ __launch_bounds__(256) void k_loss_sum(const double2 *part, uint32_t images, uint32_t per, float *loss,
-                                                  float *kl)
+__global__ __launch_bounds__(1024) void k_loss_sum(const double2 *part, uint32_t per, float *loss, float *kl)
 {
-    __shared__ double2 lds[256];
-    for (uint32_t i = blockIdx.x; i < images; i += gridDim.x) {
-        double2 s = make_double2(0.0, 0.0);
-        for (uint32_t p = threadIdx.x; p < per; p += 256) {
-            const double2 v = part[(size_t)i * per + p];
-            s.x += v.x;
-            s.y += v.y;
-        }
-        lds[threadIdx.x] = s;
-        __syncthreads();
-        for (int w = 128; w; w >>= 1) {
-            if ((int)threadIdx.x < w) {
-                lds[threadIdx.x].x += lds[threadIdx.x + w].x;
-                lds[threadIdx.x].y += lds[threadIdx.x + w].y;
-            }
-            __syncthreads();
-        }
-        if (threadIdx.x == 0) {
-            if (loss) loss[i] = (float)lds[0].x;
-            if (kl) kl[i] = (float)lds[0].y;
-        }
-        __syncthreads();
+    const uint32_t i = item_of();
+    double2 s = make_double2(0.0, 0.0);
+    for (uint32_t p = threadIdx.x; p < per; p += 1024) {
+        const double2 v = part[(size_t)i * per + p];
+        s.x += v.x;
+        s.y += v.y;
+    }
+    s = team_sum<1024>(s.x, s.y);
+    if (threadIdx.x == 0) {
+        if (loss) loss[i] = (float)s.x;
+        if (kl) kl[i] = (float)s.y;
     }
 }
 
 // ---------------------------------------------------------------- launches
 
-hipError_t launch_sum(const ScoreGeom &g, const double2 *part, uint32_t per, float *loss, float *kl, hipStream_t s)
+hipError_t launch_sum(const ScoreGeom &g, const LossOut &o, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_loss_sum, dim3(grid_of(g.images)), dim3(256), 0, s, part, g.images, per, loss, kl);
+    if (g.per == 1 || (!o.loss && !o.kl)) return hipSuccess;
+    const dim3 grid = grid_of(g.images);
+    hipLaunchKernelGGL(k_loss_sum, grid, dim3(1024), 0, s, o.part, g.per, o.loss, o.kl);
     return hipGetLastError();
 }
 
@@ -558,8 +731,8 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums)
     const size_t rows = (size_t)g.images * g.hw;
     ScorePlan p = {};
     const int nvec = g.len / vec;
-    p.form = 0;
-    while (p.form < kFormCount && kForms[p.form].lanes * kForms[p.form].nv < nvec) ++p.form;
+    p.form = g.classes <= kPixelClasses ? 0 : 1;
+    while (p.form && p.form < kFormCount && kForms[p.form].lanes * kForms[p.form].nv < nvec) ++p.form;
     g.chunks = 1;
     g.chunk = g.len;
     const int least = kForms[kChunkForm].lanes * kForms[kChunkForm].nv * vec;
@@ -569,8 +742,12 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums)
         g.chunks = (int)(((int64_t)g.len + least - 1) / least);
     }
     p.split = g.chunks > 1;
-    const int lanes = kForms[p.form].lanes, groups = g.classes == 1 ? 256 : lanes <= 64 ? 256 / lanes : 1;
-    g.per = p.split ? g.hw : std::min<uint32_t>((g.hw + groups - 1) / groups, lanes <= 64 ? 1024u : 8192u);
+    const int lanes = kForms[p.form].lanes;
+    const uint32_t groups = lanes <= 64 ? 256 / lanes : 1;
+    g.per = (g.hw - 1) / groups + 1;
+    g.by_per = Divisor(g.per);
+    g.by_chunks = Divisor((uint32_t)g.chunks);
+    g.by_out = Divisor((uint32_t)(g.c % vec ? g.c : g.c / vec));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -581,7 +758,7 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums)
         p.stats = take(rows * g.chunks * 16);
         p.pick = take(rows * (size_t)picks * 4);
     }
-    if (sums) p.part = take((size_t)g.images * g.per * 16);
+    if (sums && g.per > 1) p.part = take((size_t)g.images * g.per * 16);
     p.bytes = at;
     return p;
 }
@@ -591,26 +768,28 @@ hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *
     uint8_t *w = (uint8_t *)work;
     a.stats = (float4 *)(w + p.stats);
     a.pick = (float *)(w + p.pick);
-    a.part = loss ? (double2 *)(w + p.part) : nullptr;
-    const size_t rows = (size_t)g.images * g.hw;
+    if (loss) a.out = {(double2 *)(w + p.part), loss, nullptr};
+    const dim3 grid = grid_of((size_t)g.images * g.per * g.chunks);
     hipError_t e = with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if (p.split) {
             constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            const dim3 grid(grid_of(rows * g.chunks));
             hipLaunchKernelGGL((k_distill<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
             hipLaunchKernelGGL((k_distill<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
             return hipGetLastError();
         }
+        if (p.form == 0)
+            return with_pixel(g.classes, [&](auto n) {
+                hipLaunchKernelGGL((k_distill_pixel<FMT, decltype(n)::value>), grid, dim3(256), 0, s, a, g);
+                return hipGetLastError();
+            });
         return with_form(p.form, [&](auto l, auto n) {
             constexpr int L = decltype(l)::value, NV = decltype(n)::value;
-            hipLaunchKernelGGL((k_distill<FMT, L, NV, kWhole>), dim3(grid_of((size_t)g.images * g.per)),
-                               dim3(kThreadsOf<L>), 0, s, a, g);
+            hipLaunchKernelGGL((k_distill<FMT, L, NV, kWhole>), grid, dim3(kThreadsOf<L>), 0, s, a, g);
             return hipGetLastError();
         });
     });
-    if (e != hipSuccess || !loss) return e;
-    return launch_sum(g, a.part, g.per, loss, nullptr, s);
+    return e != hipSuccess ? e : launch_sum(g, a.out, s);
 }
 
 hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, float *kl, int fmt, hipStream_t s)
@@ -618,30 +797,32 @@ hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
     uint8_t *w = (uint8_t *)work;
     a.stats = (float4 *)(w + p.stats);
     a.pick = (float *)(w + p.pick);
-    a.part = loss || kl ? (double2 *)(w + p.part) : nullptr;
-    const size_t rows = (size_t)g.images * g.hw;
+    if (loss || kl) a.out = {(double2 *)(w + p.part), loss, kl};
+    const dim3 grid = grid_of((size_t)g.images * g.per * g.chunks);
     hipError_t e = with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
-        if (g.classes == 1) {
-            hipLaunchKernelGGL((k_clip_binary<FMT>), dim3(grid_of((size_t)g.images * g.per)), dim3(256), 0, s, a, g);
-            return hipGetLastError();
-        }
         if (p.split) {
             constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            const dim3 grid(grid_of(rows * g.chunks));
             hipLaunchKernelGGL((k_clip<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
             hipLaunchKernelGGL((k_clip<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
             return hipGetLastError();
         }
+        if (g.classes == 1) {
+            hipLaunchKernelGGL((k_clip_pixel<FMT, 1>), grid, dim3(256), 0, s, a, g);
+            return hipGetLastError();
+        }
+        if (p.form == 0)
+            return with_pixel(g.classes, [&](auto n) {
+                hipLaunchKernelGGL((k_clip_pixel<FMT, decltype(n)::value>), grid, dim3(256), 0, s, a, g);
+                return hipGetLastError();
+            });
         return with_form(p.form, [&](auto l, auto n) {
             constexpr int L = decltype(l)::value, NV = decltype(n)::value;
-            hipLaunchKernelGGL((k_clip<FMT, L, NV, kWhole>), dim3(grid_of((size_t)g.images * g.per)),
-                               dim3(kThreadsOf<L>), 0, s, a, g);
+            hipLaunchKernelGGL((k_clip<FMT, L, NV, kWhole>), grid, dim3(kThreadsOf<L>), 0, s, a, g);
             return hipGetLastError();
         });
     });
-    if (e != hipSuccess || !a.part) return e;
-    return launch_sum(g, a.part, g.per, loss, kl, s);
+    return e != hipSuccess ? e : launch_sum(g, a.out, s);
 }
 
 hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, int fmt, hipStream_t s)
@@ -650,25 +831,35 @@ hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
     a.stats = (float4 *)(w + p.stats);
     a.pick = (float *)(w + p.pick);
     const size_t rows = (size_t)g.images * g.hw;
-    return with_format(fmt, [&](auto f) {
+    const dim3 grid = grid_of((size_t)g.images * g.per * g.chunks), by_pixel = grid_of((rows + 255) / 256);
+    hipError_t e = with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if (g.classes == 1) {
-            hipLaunchKernelGGL((k_logp_binary<FMT>), dim3(grid_of((rows + 255) / 256)), dim3(256), 0, s, a, g);
+            hipLaunchKernelGGL((k_logp_pixel<FMT, 1>), by_pixel, dim3(256), 0, s, a, g);
             return hipGetLastError();
         }
-        if (p.split) {
-            constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            hipLaunchKernelGGL((k_logp<FMT, L, NV, kFirst>), dim3(grid_of(rows * g.chunks)), dim3(L), 0, s, a, g);
-            hipLaunchKernelGGL(k_logp_join, dim3(grid_of((rows + 63) / 64)), dim3(64), 0, s, a, g);
-            return hipGetLastError();
-        }
-        return with_form(p.form, [&](auto l, auto n) {
-            constexpr int L = decltype(l)::value, NV = decltype(n)::value, G = L <= 64 ? kThreadsOf<L> / L : 1;
-            hipLaunchKernelGGL((k_logp<FMT, L, NV, kWhole>), dim3(grid_of((rows + G - 1) / G)), dim3(kThreadsOf<L>), 0, s, a,
-                               g);
-            return hipGetLastError();
-        });
+        if (p.form == 0)
+            return with_pixel(g.classes, [&](auto n) {
+                hipLaunchKernelGGL((k_logp_pixel<FMT, decltype(n)::value>), by_pixel, dim3(256), 0, s, a, g);
+                return hipGetLastError();
+            });
+        auto rows_of = [&](auto sx) {
+            constexpr bool SX = decltype(sx)::value;
+            if (p.split) {
+                constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
+                hipLaunchKernelGGL((k_logp<FMT, L, NV, kFirst, SX>), grid, dim3(L), 0, s, a, g);
+                hipLaunchKernelGGL(k_logp_join, grid_of((rows + 63) / 64), dim3(64), 0, s, a, g);
+                return hipGetLastError();
+            }
+            return with_form(p.form, [&](auto l, auto n) {
+                constexpr int L = decltype(l)::value, NV = decltype(n)::value;
+                hipLaunchKernelGGL((k_logp<FMT, L, NV, kWhole, SX>), grid, dim3(kThreadsOf<L>), 0, s, a, g);
+                return hipGetLastError();
+            });
+        };
+        return a.entropy ? rows_of(std::true_type{}) : rows_of(std::false_type{});
     });
+    return e;
 }
 
 }  // namespace bc

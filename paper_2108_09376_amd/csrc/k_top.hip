@@ -50,69 +50,228 @@ __device__ __forceinline__ float rest_of(const TopArgs &a, const Stats &st)
     return st.s == 0.f ? -kInf : st.m * a.inv_t + __logf(st.s);
 }
 
+// Pixels of the map that a call runs on.
+__device__ __forceinline__ uint32_t pixel_count(const TopArgs &a, const ScoreGeom &g)
+{
+    return a.idx ? (uint32_t)*a.count * (uint32_t)(a.bh * a.bw) : g.images * g.hw;
+}
+
+// Rows of a few lanes: each entry is the largest key below the last.
+template <int FMT, int L>
+__global__ __launch_bounds__(256) void k_top_lanes(TopArgs a, ScoreGeom g)
+{
+    constexpr int G = kGroupsOf<L>, VEC = kVec<FMT>;
+    const uint32_t r = item_of() * G + threadIdx.x / L;
+    if (r >= pixel_count(a, g)) return;
+    const size_t px = row_pixel(a, r);
+    ScoreRow<FMT, L, 1> row;
+    row.load(a.x, px * (size_t)g.c, g.len, g.classes);
+    const int lane = row.lane(), nvec = g.len / VEC, tail = nvec * VEC + lane;
+    Key key[VEC + 1], last = ~(Key)0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) key[j] = lane < nvec && lane * VEC + j < g.classes ? key_of(get(row.v[0], j), lane * VEC + j) : 0;
+    key[VEC] = tail < g.classes ? key_of(get(row.t, 0), tail) : 0;
+    for (int i = 0; i < a.k; ++i) {
+        Key top = 0;
+#pragma unroll
+        for (int j = 0; j <= VEC; ++j) top = key[j] < last && key[j] > top ? key[j] : top;
+        last = lane_max_key<L>(top);
+        if (lane == 0) put<FMT>(a, px * a.k + i, last);
+    }
+    if (!a.rest) return;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        if (key[j] >= last) mask_elem<FMT, VEC>(row.v[0], j);
+    if (key[VEC] >= last) row.t = masked_raw<FMT, 1>();
+    const Stats st = row.template stats<false>(kLog2e * a.inv_t);
+    if (lane == 0) a.rest[px] = rest_of(a, st);
+}
+
+// Rows of a wave or a workgroup. Every wave finds the q-th largest of its lanes' maxima, q
+// enough that all waves together have k; the least of these is a score that at least k scores reach,
+// and few more than that do. Those that reach it are collected in LDS, and each one's place among
+// them is the number of larger keys. Where more reach it than LDS holds (long runs of equal
+// scores, parts of a row masked out), or fewer than k (NaN), the record is found by rounds.
+constexpr int kCandidates = 1024;
+
 template <int FMT, int L, int NV, int PASS>
-__global__ __launch_bounds__((kThreadsOf<L>)) void k_top(TopArgs a, ScoreGeom g)
+__global__ __launch_bounds__(L) void k_top(TopArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
-    constexpr int VEC = kVec<FMT>, T = kThreadsOf<L>, G = L <= 64 ? T / L : 1, W = L < 64 ? L : 64;
-    __shared__ Key best[L > 64 ? L / 64 : 1];
-    __shared__ Stats waves[L > 64 ? L / 64 : 1];
-    const int group = L <= 64 ? threadIdx.x / L : 0;
-    const float k2 = kLog2e * a.inv_t;
-    const size_t rows = a.idx ? (size_t)*a.count * (size_t)(a.bh * a.bw) : (size_t)g.images * g.hw;
-    const size_t items = PASS == kWhole ? (rows + G - 1) / G : rows * g.chunks;
-    for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const size_t r = PASS == kWhole ? item * G + group : item / g.chunks;
-        if (r >= rows) continue;
-        const int chunk = PASS == kWhole ? 0 : (int)(item % g.chunks);
-        const size_t px = row_pixel(a, (uint32_t)r);
-        const Chunk c = chunk_of<PASS>(g, px, chunk);
-        Row row;
-        row.load(a.x, c.base, c.len, c.live);
-        const int nvec = c.len / VEC, lane = Row::lane();
-        // f(score, class) of every element that this lane holds
-        auto each = [&](auto f) {
+    constexpr int VEC = kVec<FMT>, W = L / 64;
+    __shared__ __attribute__((aligned(16))) Key cand[kCandidates];
+    __shared__ Key record[64];
+    __shared__ Key best[W];
+    __shared__ float least[W];
+    __shared__ Stats waves[W];
+    __shared__ int head[L], next[64], count;
+    uint32_t r = item_of();
+    int chunk = 0;
+    if constexpr (PASS == kFirst) {
+        const uint32_t i = r;
+        r = div(i, g.by_chunks);
+        chunk = (int)(i - r * (uint32_t)g.chunks);
+    }
+    if (r >= pixel_count(a, g)) return;
+    const size_t px = row_pixel(a, r);
+    const Chunk c = chunk_of<PASS>(g, px, chunk);
+    Row row;
+    row.load(a.x, c.base, c.len, c.live);
+    const int lane = Row::lane(), nvec = c.len / VEC, k = min(a.k, c.live);
+    head[lane] = 0;
+    if (lane == 0) count = 0;
+
+    float m = get(row.t, 0);
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+        if (v < row.used)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int e = (v * L + lane) * VEC + j;
-                    if (e < c.live && v * L + lane < nvec) f(get(row.v[v], j), c.off + e);
-                }
-            const int e = nvec * VEC + lane;
-            if (e < c.live) f(get(row.t, 0), c.off + e);
+            for (int j = 0; j < VEC; ++j) m = fmaxf(m, get(row.v[v], j));
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    row.keep();
+    // waves whose lanes all hold a vector
+    const int full = min(W, nvec / 64);
+    float bar = -kInf;
+    if (full) {
+        float x = m;
+        const int q = (k + full - 1) / full;
+        for (int i = 0; i < q; ++i) {
+            bar = lane_max<64>(x);
+            const unsigned long long at = __ballot(x == bar);
+            if (at && (int)(threadIdx.x & 63) == __ffsll(at) - 1) x = -kInf;
+        }
+    }
+    if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = bar;
+    __syncthreads();
+    bar = least[0];
+    for (int w = 1; w < full; ++w) bar = fminf(bar, least[w]);
+    if (m >= bar) {
+        auto add = [&](float z, int e) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kCandidates) cand[at] = key_of(z, c.off + e);
         };
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = (v * L + lane) * VEC;
+            uint32_t hit = 0;
+            if (v < row.used && v * L + lane < nvec)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) hit |= get(row.v[v], j) >= bar && at + j < c.live ? 1u << j : 0u;
+            if (hit)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (hit >> j & 1) add(get(row.v[v], j), at + j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const int e = nvec * VEC + lane;
+        if (e < c.live && get(row.t, 0) >= bar) add(get(row.t, 0), e);
+    }
+    __syncthreads();
+    const int n = count;
+    if (n >= k && n <= kCandidates) {
+        for (int i = lane; i < n; i += L) {
+            const Key mine = cand[i];
+            int place = 0;
+            for (int o = 0; o < n; ++o) place += cand[o] > mine;
+            if (place < k) {
+                record[place] = mine;
+                const int e = class_of(mine) - c.off;
+                next[place] = atomicExch(&head[Row::owner(e, c.len)], place + 1);
+            }
+        }
+        __syncthreads();
+    } else {
+        // each entry the largest key below the last, over the row in memory: it is seldom needed,
+        // and would take the registers from the other way
         Key last = ~(Key)0;
-        for (int i = 0; i < a.k; ++i) {
-            Key k = 0;
-            each([&](float z, int cls) {
-                const Key o = key_of(z, cls);
-                k = o < last && o > k ? o : k;
-            });
-            k = lane_max_key<W>(k);
-            if constexpr (L > 64) {
-                __syncthreads();
-                if ((threadIdx.x & 63) == 0) best[threadIdx.x >> 6] = k;
-                __syncthreads();
-                for (int w = 0; w < L / 64; ++w) k = best[w] > k ? best[w] : k;
+        for (int i = 0; i < k; ++i) {
+            Key top = 0;
+            for (int e = lane; e < c.live; e += L) {
+                const Key o = key_of(load_elem(a.x, FMT, c.base + e), c.off + e);
+                top = o < last && o > top ? o : top;
             }
-            last = k;
+            top = lane_max_key<64>(top);
+            __syncthreads();
+            if ((lane & 63) == 0) best[lane >> 6] = top;
+            __syncthreads();
+            last = best[0];
+            for (int w = 1; w < W; ++w) last = best[w] > last ? best[w] : last;
             if (lane == 0) {
-                if constexpr (PASS == kFirst) a.keys[item * a.k + i] = k;
-                else put<FMT>(a, px * a.k + i, k);
+                record[i] = last;
+                const int own = Row::owner(class_of(last) - c.off, c.len);
+                next[i] = head[own];
+                head[own] = i + 1;
             }
+        }
+        __syncthreads();
+    }
+    if constexpr (PASS == kFirst) {
+        if (lane < a.k) a.keys[((size_t)r * g.chunks + chunk) * a.k + lane] = lane < k ? record[lane] : 0;
+    } else {
+        if (lane < a.k) put<FMT>(a, px * a.k + lane, record[lane]);
+    }
+    if (!a.rest) return;
+    for (int h = head[lane]; h; h = next[h - 1]) row.mask(class_of(record[h - 1]) - c.off, c.len);
+    const Stats st = team_stats<L, false>(row.template stats<false>(kLog2e * a.inv_t), waves, kLog2e * a.inv_t);
+    if (lane == 0) {
+        if constexpr (PASS == kFirst) a.stats[(size_t)r * g.chunks + chunk] = make_float4(st.m, st.s, 0.f, 0.f);
+        else a.rest[px] = rest_of(a, st);
+    }
+}
+
+// A pixel of few classes to a thread: k times the largest key that is left, the scores in registers.
+// The records leave through LDS, entry after entry.
+template <int FMT, int N>
+__global__ __launch_bounds__(256) void k_top_pixel(TopArgs a, ScoreGeom g)
+{
+    __shared__ float lds[256][N + 1];
+    __shared__ uint32_t pixel[256];
+    __shared__ uint8_t cls[256][N + 1];
+    const uint32_t total = pixel_count(a, g), first = item_of() * 256;
+    if (first >= total) return;
+    const uint32_t rows = min(256u, total - first);
+    if (threadIdx.x < rows) {
+        const uint32_t at = row_pixel(a, first + threadIdx.x);
+        pixel[threadIdx.x] = at;
+        PixelScores<FMT, N> px;
+        px.load(a.x, at * (size_t)g.c, g.c, g.classes);
+        int key[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            lds[threadIdx.x][j] = px.z[j];
+            key[j] = (int)((uint32_t)(key_of(px.z[j], 0) >> 32) ^ 0x80000000u);
+        }
+        uint32_t left = g.classes == 32 ? ~0u : (1u << g.classes) - 1u;
+        for (int i = 0; i < a.k; ++i) {
+            int top = (int)0x80000000u, at = 0;                  // below every key
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if ((left >> j & 1) && key[j] > top) {
+                    top = key[j];
+                    at = j;
+                }
+            cls[threadIdx.x][i] = (uint8_t)at;
+            left &= ~(1u << at);
         }
         if (a.rest) {
-            each([&](float z, int cls) {
-                if (key_of(z, cls) >= last) row.mask(cls - c.off, c.len);
-            });
-            const Stats st = team_stats<L, false>(row.template stats<false>(k2), waves, k2);
-            if (lane == 0) {
-                if constexpr (PASS == kFirst) a.stats[item] = make_float4(st.m, st.s, 0.f, 0.f);
-                else a.rest[px] = rest_of(a, st);
-            }
+            float m = -kInf, s = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, left >> j & 1 ? px.z[j] : -kInf);
+            const float ref = m == -kInf ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                s += left >> j & 1 ? exp2_of(px.z[j], ref, kLog2e * a.inv_t) : 0.f;
+            a.rest[at] = rest_of(a, {m, s, 0.f});
         }
-        if constexpr (L > 64) __syncthreads();
+    }
+    __syncthreads();
+    for (uint32_t f = threadIdx.x; f < rows * (uint32_t)a.k; f += 256) {
+        const uint32_t p = div(f, a.by_k), e = f - p * (uint32_t)a.k;
+        const size_t at = pixel[p] * (size_t)a.k + e;
+        const float y[1] = {lds[p][cls[p][e]]};
+        store_raw<FMT, 1>(a.top, at, pack<FMT, 1>(y));
+        a.index[at] = cls[p][e];
     }
 }
 
@@ -121,8 +280,9 @@ template <int FMT>
 __global__ __launch_bounds__(64) void k_top_join(TopArgs a, ScoreGeom g)
 {
     const float k2 = kLog2e * a.inv_t;
-    const size_t rows = a.idx ? (size_t)*a.count * (size_t)(a.bh * a.bw) : (size_t)g.images * g.hw;
-    for (size_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    {
+        const size_t r = item_of();
+        if (r >= pixel_count(a, g)) return;
         const size_t px = row_pixel(a, (uint32_t)r);
         const Key *keys = a.keys + r * g.chunks * a.k;
         const int n = g.chunks * a.k;
@@ -136,7 +296,7 @@ __global__ __launch_bounds__(64) void k_top_join(TopArgs a, ScoreGeom g)
             last = lane_max_key<64>(k);
             if (threadIdx.x == 0) put<FMT>(a, px * a.k + i, last);
         }
-        if (!a.rest) continue;
+        if (!a.rest) return;
         // the others: outside every chunk's record, and inside one but not of this record
         Stats st = {-kInf, 0.f, 0.f};
         for (int i = threadIdx.x; i < g.chunks; i += 64) {
@@ -171,18 +331,27 @@ hipError_t launch_top(TopArgs a, ScoreGeom g, const ScorePlan &p, void *work, in
     uint8_t *w = (uint8_t *)work;
     a.stats = (float4 *)(w + p.stats);
     a.keys = (unsigned long long *)(w + p.pick);
+    a.by_k = Divisor((uint32_t)a.k);
     const size_t rows = (size_t)g.images * g.hw;
     return with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if (p.split) {
             constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            hipLaunchKernelGGL((k_top<FMT, L, NV, kFirst>), dim3(grid_of(rows * g.chunks)), dim3(L), 0, s, a, g);
-            hipLaunchKernelGGL((k_top_join<FMT>), dim3(grid_of(rows)), dim3(64), 0, s, a, g);
+            hipLaunchKernelGGL((k_top<FMT, L, NV, kFirst>), grid_of(rows * g.chunks), dim3(L), 0, s, a, g);
+            hipLaunchKernelGGL((k_top_join<FMT>), grid_of(rows), dim3(64), 0, s, a, g);
             return hipGetLastError();
         }
+        if (p.form == 0)
+            return with_pixel(g.classes, [&](auto n) {
+                hipLaunchKernelGGL((k_top_pixel<FMT, decltype(n)::value>), grid_of((rows + 255) / 256), dim3(256), 0, s, a, g);
+                return hipGetLastError();
+            });
         return with_form(p.form, [&](auto l, auto n) {
-            constexpr int L = decltype(l)::value, NV = decltype(n)::value, G = L <= 64 ? kThreadsOf<L> / L : 1;
-            hipLaunchKernelGGL((k_top<FMT, L, NV, kWhole>), dim3(grid_of((rows + G - 1) / G)), dim3(kThreadsOf<L>), 0, s, a, g);
+            constexpr int L = decltype(l)::value, NV = decltype(n)::value, G = kGroupsOf<L>;
+            if constexpr (L < 64)
+                hipLaunchKernelGGL((k_top_lanes<FMT, L>), grid_of((rows + G - 1) / G), dim3(256), 0, s, a, g);
+            else
+                hipLaunchKernelGGL((k_top<FMT, L, NV, kWhole>), grid_of(rows), dim3(L), 0, s, a, g);
             return hipGetLastError();
         });
     });

@@ -88,6 +88,7 @@ struct ScoreRow {
     static constexpr int VEC = kVec<FMT>;
     Raw<FMT, VEC> v[NV];
     Raw<FMT, 1> t;
+    int used;                                  // vectors of a lane that some lane has a score in
 
     static __device__ __forceinline__ int lane() { return threadIdx.x % L; }
     // the lane that holds element e
@@ -100,11 +101,15 @@ struct ScoreRow {
     __device__ __forceinline__ void load(const void *x, size_t base, int len, int live)
     {
         const int nvec = len / VEC, here = min(nvec, (live + VEC - 1) / VEC);
+        if (here == NV * L) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int i = k * L + lane();
-            v[k] = masked_raw<FMT, VEC>();
-            if (i < here) v[k] = load_raw<FMT, VEC>(x, base + (size_t)i * VEC);
+            for (int k = 0; k < NV; ++k) v[k] = load_raw<FMT, VEC>(x, base + (size_t)(k * L + lane()) * VEC);
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                v[k] = masked_raw<FMT, VEC>();
+                if (k * L + lane() < here) v[k] = load_raw<FMT, VEC>(x, base + (size_t)(k * L + lane()) * VEC);
+            }
         }
         const int e = nvec * VEC + lane();
         t = masked_raw<FMT, 1>();
@@ -118,6 +123,19 @@ struct ScoreRow {
                     for (int j = 0; j < VEC; ++j)
                         if (at + j >= live) mask_elem<FMT, VEC>(v[k], j);
             }
+        used = (here + L - 1) / L;
+    }
+
+    // Between two passes over a row it stays as stored: the words are made opaque, or the compiler
+    // would keep the converted values too, at twice the registers.
+    __device__ __forceinline__ void keep()
+    {
+        if constexpr (FMT != kF32 && NV >= 2) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(v[k].w[i]));
+        }
     }
 
     // Element e of a row that this lane holds to -inf.
@@ -128,25 +146,33 @@ struct ScoreRow {
             t = masked_raw<FMT, 1>();
             return;
         }
+        // selects, not branches: the compiler would turn those into an array in memory
+        const int word = FMT == kF32 ? e % VEC : e % VEC >> 1;
+        const uint32_t keep = FMT == kF32 ? 0u : e & 1 ? 0xFFFFu : 0xFFFF0000u;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (k == at)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (j == e % VEC) mask_elem<FMT, VEC>(v[k], j);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = v[k].w[i];
+                v[k].w[i] = k == at && i == word ? (w & keep) | (kMaskedWord<FMT> & ~keep) : w;
+            }
     }
 
     // Statistics over the lanes of a wave that hold the row (all of them if L >= 64).
     template <bool SX>
-    __device__ __forceinline__ Stats stats(float k2) const
+    __device__ __forceinline__ Stats stats(float k2)
     {
         constexpr int W = L < 64 ? L : 64;
         float m = get(t, 0);
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            if (k < used)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) m = fmaxf(m, get(v[k], j));
+                for (int j = 0; j < VEC; ++j) m = fmaxf(m, get(v[k], j));
+            __builtin_amdgcn_sched_barrier(0);
+        }
         m = lane_max<W>(m);
+        keep();
         const float ref = m == -kInf ? 0.f : m;
         float s = 0.f, sx = 0.f;
         auto add = [&](float z) {
@@ -156,9 +182,13 @@ struct ScoreRow {
         };
         add(get(t, 0));
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            if (k < used)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) add(get(v[k], j));
+                for (int j = 0; j < VEC; ++j) add(get(v[k], j));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        keep();
         s = lane_sum<W>(s);
         if constexpr (SX) sx = lane_sum<W>(sx);
         return {m, s, sx};
@@ -180,6 +210,7 @@ struct ScoreRow {
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) y[j] = at + j < live ? y[j] : 0.f;
             store_raw<FMT, VEC>(out, base + at, pack<FMT, VEC>(y));
+            __builtin_amdgcn_sched_barrier(0);
         }
         const int e = nvec * VEC + lane();
         if (e < len) {
@@ -211,14 +242,17 @@ __device__ __forceinline__ float load_elem(const void *p, int fmt, size_t i)
     return get(load_raw<kF16, 1>(p, i), 0);
 }
 
-// Forms of a row: lanes (threads of a workgroup from 128 on) and vectors of each.
+// Forms of a row: a thread to itself (up to kPixelClasses scores); or lanes (threads of a
+// workgroup from 128 on) and vectors of each.
+constexpr int kPixelClasses = 32;
 struct Form {
     int lanes, nv;
 };
-constexpr Form kForms[] = {{8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
-constexpr int kFormCount = 8, kChunkForm = 4;
+constexpr Form kForms[] = {{1, 0}, {8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
+constexpr int kFormCount = 9, kChunkForm = 5;
 
 template <int L> constexpr int kThreadsOf = L <= 64 ? 256 : L;
+template <int L> constexpr int kGroupsOf = L <= 64 ? 256 / L : 1;  // rows of a workgroup
 
 // Which part of the work a launch does: whole rows; a chunk's statistics; a chunk's gradient.
 enum Pass { kWhole, kFirst, kSecond };
@@ -271,23 +305,88 @@ __device__ __forceinline__ Stats row_stats(const float4 *part, int chunks, float
     return st;
 }
 
-// f(lanes, vectors) of a form, as integral constants.
+// A launch of any number of workgroups below 2^32, and a workgroup's own number.
+inline dim3 grid_of(size_t items)
+{
+    const unsigned x = (unsigned)std::min<size_t>(std::max<size_t>(items, 1), 1u << 16);
+    return dim3(x, (unsigned)((items + x - 1) / x));
+}
+
+__device__ __forceinline__ uint32_t item_of() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
+// f(lanes, vectors) of a form of rows that lanes share, as integral constants.
 template <typename F>
 hipError_t with_form(int form, F &&f)
 {
     using std::integral_constant;
     switch (form) {
-    case 0: return f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    case 1: return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    case 2: return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    case 3: return f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-    case 4: return f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
-    case 5: return f(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-    case 6: return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    case 1: return f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    case 2: return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    case 3: return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    case 4: return f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+    case 5: return f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+    case 6: return f(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+    case 7: return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
     default: return f(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
     }
 }
 
-inline unsigned grid_of(size_t items) { return (unsigned)std::min<size_t>(std::max<size_t>(items, 1), 1u << 20); }
+// f(classes of a pixel in registers, as an integral constant).
+template <typename F>
+hipError_t with_pixel(int classes, F &&f)
+{
+    if (classes <= 8) return f(std::integral_constant<int, 8>{});
+    if (classes <= 16) return f(std::integral_constant<int, 16>{});
+    if (classes <= 24) return f(std::integral_constant<int, 24>{});
+    return f(std::integral_constant<int, 32>{});
+}
+
+// The scores of a thread's own pixel, -inf past its classes.
+template <int FMT, int N>
+struct PixelScores {
+    static constexpr int VEC = kVec<FMT>;
+    float z[N];
+
+    __device__ __forceinline__ void load(const void *x, size_t base, int c, int classes)
+    {
+#pragma unroll
+        for (int at = 0; at < N; at += VEC) {
+            if (at >= classes) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) z[at + j] = -kInf;
+            } else if (at + VEC <= c) {
+                const Raw<FMT, VEC> r = load_raw<FMT, VEC>(x, base + at);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) z[at + j] = at + j < classes ? get(r, j) : -kInf;
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    z[at + j] = at + j < classes ? get(load_raw<FMT, 1>(x, base + at + j), 0) : -kInf;
+            }
+        }
+    }
+};
+
+// Rows [first, first + rows) of `out`, c elements each, by a workgroup of 256 threads:
+// value(row, j) for j < classes, 0 past them. by_out: by the vectors of a row, or its elements if it is not
+// whole vectors.
+template <int FMT, typename F>
+__device__ __forceinline__ void store_pixels(void *out, size_t first, uint32_t rows, int c, int classes, const Divisor &by_out,
+                                             F value)
+{
+    auto go = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const uint32_t per = (uint32_t)c / W;
+        for (uint32_t f = threadIdx.x; f < rows * per; f += 256) {
+            const uint32_t r = div(f, by_out), at = (f - r * per) * W;
+            float y[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) y[j] = (int)at + j < classes ? value(r, (int)at + j) : 0.f;
+            store_raw<FMT, W>(out, (first + r) * (size_t)c + at, pack<FMT, W>(y));
+        }
+    };
+    if (c % kVec<FMT> == 0) go(std::integral_constant<int, kVec<FMT>>{});
+    else go(std::integral_constant<int, 1>{});
+}
 
 }  // namespace bc

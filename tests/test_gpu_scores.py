@@ -540,7 +540,8 @@ def test_refusals_of_the_binding(B):
         B.bc_distill_loss(buf[:x.numel()].view(x.shape), 30, st["top"], st["index"], None, 1.0, None, 1.0,
                           buf[8:].view(x.shape), None)
     assert e.value.status == B.BC_ERR_ALIAS
+    st = new_state(1, 400, 40, torch.float32)
     with pytest.raises(B.BCError) as e:
-        B.bc_distill_loss(x, 30, st["top"], st["index"], None, 1.0, None, 1.0, st["g1"], st["l1"],
+        B.bc_distill_loss(st["x"], 40, st["top"], st["index"], None, 1.0, None, 1.0, st["g1"], st["l1"],
                           work=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.status == B.BC_ERR_CAPACITY

@@ -55,16 +55,18 @@ def test_maps_and_classes(B):
         for classes in (0, -1, 31):
             assert call(B, classes=classes) == B.BC_ERR_SHAPE
     for call in (distill, clip):
-        assert call(B, work=None) == B.BC_ERR_NULL
-        assert call(B, work=WORK + 8) == B.BC_ERR_UNSUPPORTED
-        assert call(B, nbytes=8) == B.BC_ERR_CAPACITY and call(B, nbytes=-1) == B.BC_ERR_CAPACITY
+        # an image of more pixels than a workgroup takes needs a workspace
+        wide = dict(m=(2, 30, 40, 60, 0, 1))
+        assert call(B, **wide, work=None) == B.BC_ERR_NULL
+        assert call(B, **wide, work=WORK + 8) == B.BC_ERR_UNSUPPORTED
+        assert call(B, **wide, nbytes=8) == B.BC_ERR_CAPACITY and call(B, **wide, nbytes=-1) == B.BC_ERR_CAPACITY
         assert call(B, grad=None, loss=None) == B.BC_ERR_NULL
         assert call(B, scale=NAN) == B.BC_ERR_SHAPE and call(B, scale=INF) == B.BC_ERR_SHAPE
         assert call(B, loss=GRAD + 4) == B.BC_ERR_ALIAS
         assert call(B, grad=X + 4) == B.BC_ERR_ALIAS
         assert call(B, weight=GRAD) == B.BC_ERR_ALIAS
-        assert call(B, loss=X) == B.BC_ERR_ALIAS and call(B, work=X) == B.BC_ERR_ALIAS
-        assert call(B, loss=WORK) == B.BC_ERR_ALIAS
+        assert call(B, loss=X) == B.BC_ERR_ALIAS and call(B, **wide, work=X) == B.BC_ERR_ALIAS
+        assert call(B, **wide, loss=WORK) == B.BC_ERR_ALIAS
     for call in (top, logp):                                       # long rows are split: these need one too
         long = (1, 100000, 1, 1, 0, 1)
         more = dict(grid=(1, 1)) if call is top else {}
@@ -130,7 +132,9 @@ def test_workspaces(B):
         assert f(t, 19, 4, None) == B.BC_ERR_NULL and f(t, 65, 4, ctypes.byref(n)) == B.BC_ERR_SHAPE
         assert f(t, 19, 65, ctypes.byref(n)) == B.BC_ERR_SHAPE
     x = torch.empty((2, 3, 4, 24))
-    assert B.bc_distill_loss_work(x, 20, 3) > 0 and B.bc_clipped_policy_loss_work(x, 20) > 0
+    assert B.bc_distill_loss_work(x, 20, 3) == 0 == B.bc_clipped_policy_loss_work(x, 20)
+    y = torch.empty((2, 1, 400, 40))
+    assert B.bc_distill_loss_work(y, 40, 3) > 0 and B.bc_clipped_policy_loss_work(y, 40) > 0
     with pytest.raises(ValueError):
         B.bc_distill_loss_work(x.transpose(1, 2), 20, 3)
     with pytest.raises(ValueError):                                # not on a GPU: never handed on
