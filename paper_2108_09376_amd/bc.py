@@ -652,44 +652,42 @@ def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=N
 
 
 def _score_map(t, stream):
-    """Shape and descriptor of a score map [n, h, w, c] on the current device (and the stream's)."""
-    import torch
+    """(n, h, w, c), device and descriptor of a score map on the current device (and the stream's)."""
     d = _desc(t, BC_NHWC)
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    dev = t.get_device()                                 # -1: not on a GPU
+    if _raw_stream is None and dev >= 0:
+        _stream(None)                                    # sets _device_index
+    if dev < 0 or dev != _device_index():
         raise ValueError("the score map is not on the current device")
-    if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
+    if stream is not None and getattr(stream, "device_index", dev) != dev:
         raise ValueError("the stream is of another device than the score map")
-    return t.shape, d
+    return t.shape, dev, d
 
 
-def _per_pixel(t, like, dtype, name, last=None):
-    """A contiguous tensor of one value (or `last`) per pixel of the map `like`, on its device
-    (or None)."""
-    if t is None:
-        return
-    n, h, w, _ = like.shape
-    s = t.shape
-    if not (t.dtype is dtype and t.is_contiguous() and t.device == like.device
-            and s == ((n, h, w) if last is None else (n, h, w, last))):
-        raise ValueError(f"{name} must be contiguous {dtype}, one {'value' if last is None else 'record'} per pixel, "
-                         "on the map's device")
+def _value(t, shape, dtype, dev, name):
+    """A contiguous tensor of that shape and type on the map's device (or None)."""
+    if t is not None and not (t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous {dtype}, {tuple(shape)}, on the map's device")
 
 
-def _per_image(t, like, name):
+_F32 = _I32 = _U8 = None
+
+
+def _types():
+    """torch's types, known once a tensor has come."""
+    global _F32, _I32, _U8
     import torch
-    if t is not None and not (t.dtype is torch.float32 and t.is_contiguous() and t.shape == like.shape[:1]
-                              and t.device == like.device):
-        raise ValueError(f"{name} must be contiguous float32, one value per image, on the map's device")
+    _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
 def _score_work(work, nbytes, like, stream):
-    """Pointer and size of a caller's workspace, or of one made for the call (None, 0: none needed)."""
+    """A caller's workspace, or one made for the call, with pointer and size (None, 0: none needed)."""
     if work is None:
         need = nbytes()
         if not need:
             return None, None, 0
         work = _work(need, like, stream)
-    if work.device != like.device:
+    if work.get_device() != like.get_device():
         raise ValueError("the workspace is not on the map's device")
     return work, work.data_ptr(), _nbytes(work)
 
@@ -707,15 +705,14 @@ def bc_top_scores(scores, classes, temperature, top, index, rest, grid, idx, cou
     active blocks: top [n, h, w, k] (scores' dtype, descending, the lower class first among
     equals), index int32 [n, h, w, k], and rest float32 [n, h, w] (or None), log-sum-exp of
     the others divided by the temperature. work as for bc_layer_norm_grad."""
-    import torch
-    _, d = _score_map(scores, stream)
-    k = top.shape[-1]
-    _per_pixel(top, scores, scores.dtype, "top", k)
-    _per_pixel(index, scores, torch.int32, "index", k)
-    _per_pixel(rest, scores, torch.float32, "rest")
+    shape, dev, d = _score_map(scores, stream)
+    _F32 is None and _types()
+    pixels, k = shape[:3], top.shape[-1]
+    _value(top, pixels + (k,), scores.dtype, dev, "top")
+    _value(index, pixels + (k,), _I32, dev, "index")
+    _value(rest, pixels, _F32, dev, "rest")
     for t in (idx, count):
-        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous() and t.device == scores.device):
-            raise ValueError("the index must be contiguous int32 on the map's device")
+        t is not None and _value(t, t.shape, _I32, dev, "the index")
     cap = 0 if idx is None else int(idx.numel())
     work, wp, nbytes = _score_work(work, lambda: bc_top_scores_work(scores, classes, k), scores, stream)
     st = _lib.bc_top_scores(_ptr(scores), d, int(classes), int(k), float(temperature), _ptr(top), _ptr(index),
@@ -736,15 +733,15 @@ def bc_distill_loss(scores, classes, top, index, rest, temperature, weight, scal
     in any dtype, index int32, rest float32 or None), and grad [n, h, w, c], its gradient (either
     may be None; grad may be scores). weight float32 [n, h, w] or None. work as for
     bc_layer_norm_grad."""
-    import torch
-    shape, d = _score_map(scores, stream)
-    k = top.shape[-1]
-    _per_pixel(top, scores, top.dtype, "top", k)
-    _per_pixel(index, scores, torch.int32, "index", k)
-    _per_pixel(rest, scores, torch.float32, "rest")
-    _per_pixel(weight, scores, torch.float32, "weight")
-    _per_pixel(grad, scores, scores.dtype, "grad", shape[3])
-    _per_image(loss, scores, "loss")
+    shape, dev, d = _score_map(scores, stream)
+    _F32 is None and _types()
+    pixels, k = shape[:3], top.shape[-1]
+    _value(top, pixels + (k,), top.dtype, dev, "top")
+    _value(index, pixels + (k,), _I32, dev, "index")
+    _value(rest, pixels, _F32, dev, "rest")
+    _value(weight, pixels, _F32, dev, "weight")
+    _value(grad, shape, scores.dtype, dev, "grad")
+    _value(loss, shape[:1], _F32, dev, "loss")
     work, wp, nbytes = _score_work(work, lambda: bc_distill_loss_work(scores, classes, k), scores, stream)
     st = _lib.bc_distill_loss(_ptr(scores), d, int(classes), _ptr(top), _dtype_code(top), _ptr(index), int(k),
                               _ptr(rest), float(temperature), _ptr(weight), float(scale), _ptr(grad), _ptr(loss),
@@ -760,20 +757,16 @@ def bc_action_log_probs_work(scores, classes) -> int:
     return n.value
 
 
-def _action(action, scores, classes):
-    import torch
-    _per_pixel(action, scores, torch.uint8 if classes == 1 else torch.int32, "action")
-
-
 def bc_action_log_probs(scores, classes, action, logp, entropy=None, work=None, stream=None):
     """logp [n, h, w] float32 = log pi(action) (and entropy [n, h, w], if given) of scores
     [n, h, w, c]: classes of a softmax (action int32), or with classes = 1 execute-or-not
     decisions of a sigmoid (action uint8, the grid). work as for bc_layer_norm_grad."""
-    import torch
-    _, d = _score_map(scores, stream)
-    _action(action, scores, classes)
-    _per_pixel(logp, scores, torch.float32, "logp")
-    _per_pixel(entropy, scores, torch.float32, "entropy")
+    shape, dev, d = _score_map(scores, stream)
+    _F32 is None and _types()
+    pixels = shape[:3]
+    _value(action, pixels, _U8 if classes == 1 else _I32, dev, "action")
+    _value(logp, pixels, _F32, dev, "logp")
+    _value(entropy, pixels, _F32, dev, "entropy")
     work, wp, nbytes = _score_work(work, lambda: bc_action_log_probs_work(scores, classes), scores, stream)
     st = _lib.bc_action_log_probs(_ptr(scores), d, int(classes), _ptr(action), _ptr(logp), _ptr(entropy), wp, nbytes,
                                   _stream(stream))
@@ -800,14 +793,17 @@ def bc_clipped_policy_loss(scores, classes, action, advantage, old_logp, ref_log
     or loss may be None). advantage, old_logp, ref_logp (or None), weight (or None) float32
     [n, h, w]; kl [n] (or None) the divergence to the reference; scores, classes, action as for
     bc_action_log_probs. work as for bc_layer_norm_grad."""
-    import torch
-    shape, d = _score_map(scores, stream)
-    _action(action, scores, classes)
-    for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")):
-        _per_pixel(t, scores, torch.float32, name)
-    _per_pixel(grad, scores, scores.dtype, "grad", shape[3])
-    _per_image(loss, scores, "loss")
-    _per_image(kl, scores, "kl")
+    shape, dev, d = _score_map(scores, stream)
+    _F32 is None and _types()
+    pixels, images = shape[:3], shape[:1]
+    _value(action, pixels, _U8 if classes == 1 else _I32, dev, "action")
+    _value(advantage, pixels, _F32, dev, "advantage")
+    _value(old_logp, pixels, _F32, dev, "old_logp")
+    _value(ref_logp, pixels, _F32, dev, "ref_logp")
+    _value(weight, pixels, _F32, dev, "weight")
+    _value(grad, shape, scores.dtype, dev, "grad")
+    _value(loss, images, _F32, dev, "loss")
+    _value(kl, images, _F32, dev, "kl")
     work, wp, nbytes = _score_work(work, lambda: bc_clipped_policy_loss_work(scores, classes), scores, stream)
     st = _lib.bc_clipped_policy_loss(_ptr(scores), d, int(classes), _ptr(action), _ptr(advantage), _ptr(old_logp),
                                      _ptr(ref_logp), _ptr(weight), ctypes.byref(_policy_clip(tuple(clip))),

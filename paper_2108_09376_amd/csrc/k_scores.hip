@@ -25,25 +25,46 @@ namespace {
 
 constexpr int kMaxTop = 64;
 
-// Sum over the workgroup of T threads, in the first thread.
-template <int T>
+// Sums over a wave, from exchanges in the register file, and over the workgroup of T threads, in
+// its first thread.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v)
+{
+    const long long b = __double_as_longlong(v);
+    const int lo = __builtin_amdgcn_mov_dpp((int)b, CTRL, 0xF, 0xF, false);
+    const int hi = __builtin_amdgcn_mov_dpp((int)(b >> 32), CTRL, 0xF, 0xF, false);
+    return __longlong_as_double((long long)hi << 32 | (uint32_t)lo);
+}
+
+__device__ __forceinline__ double row_sum(double v)              // over 16 lanes
+{
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    return v + dpp<0x140>(v);
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v = row_sum(v);
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+template <int T, bool TWO>
 __device__ __forceinline__ double2 team_sum(double x, double y)
 {
     __shared__ double2 waves[T / 64];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        x += __shfl_xor(x, d);
-        y += __shfl_xor(y, d);
-    }
+    x = wave_sum(x);
+    if constexpr (TWO) y = wave_sum(y);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = make_double2(x, y);
     __syncthreads();
-    double2 s = waves[0];
-    if (threadIdx.x == 0)
-#pragma unroll
-        for (int i = 1; i < T / 64; ++i) {
-            s.x += waves[i].x;
-            s.y += waves[i].y;
-        }
+    double2 s = make_double2(0.0, 0.0);
+    if (threadIdx.x < 64) {                                      // at most 16 waves
+        if (threadIdx.x < T / 64) s = waves[threadIdx.x];
+        s.x = row_sum(s.x);
+        if constexpr (TWO) s.y = row_sum(s.y);
+    }
     return s;
 }
 
@@ -130,9 +151,9 @@ struct Record {
 };
 
 template <int FMT, int L, int NV, int PASS>
-__global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, ScoreGeom g)
+__global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_distill(DistillArgs a, ScoreGeom g)
 {
-    using Row = ScoreRow<FMT, L, NV>;
+    using Row = RowOf<FMT, L, NV>;
     constexpr int T = kThreadsOf<L>, G = kGroupsOf<L>;
     constexpr int EL = L < 64 ? L : 64, SLOTS = kMaxTop / EL;    // lanes that hold entries, entries of each
     __shared__ int head[T];                    // a thread's first entry + 1 (0: none)
@@ -157,7 +178,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
         if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
     } else {
         Row row;
-        row.load(a.x, c.base, c.len, c.live);
+        if constexpr (NV) row.load(a.x, c.base, c.len, c.live);
         head[threadIdx.x] = 0;
         meet();
         // entries: class, teacher's score, student's score
@@ -186,8 +207,11 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
         meet();
         Stats st = {};
         if constexpr (PASS != kSecond) {
-            for (int h = head[threadIdx.x]; h; h = rec.next[h - 1]) row.mask(rec.index[h - 1], c.len);
-            st = team_stats<L, false>(row.template stats<false>(k2), waves, k2);
+            const int entry = head[threadIdx.x];
+            st = row.template stats<false>(a.x, c.base, c.len, c.live, k2, [&](auto mask) {
+                for (int h = entry; h; h = rec.next[h - 1]) mask(rec.index[h - 1]);
+            });
+            st = team_stats<L, false>(st, waves, k2);
         }
         if constexpr (PASS == kFirst) {
             if (threadIdx.x == 0) a.stats[c.row * g.chunks + w.chunk] = make_float4(st.m, st.s, 0.f, 0.f);
@@ -244,7 +268,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
                 const float er = st.m == -kInf ? st.s : st.s * exp2_of(st.m, M, k2);
                 const float total = top + er, tr = a.rest ? exp_of(rest - Mt) : 0.f, ttotal = tp + tr;
                 const bool part = total != 0.f && ttotal != 0.f;    // a NaN takes part
-                const float inv = 1.f / total, tinv = 1.f / ttotal;
+                const float inv = __builtin_amdgcn_rcpf(total), tinv = __builtin_amdgcn_rcpf(ttotal);
                 const float logs = __logf(total) - __logf(ttotal);
                 const float q_r = er * inv, p_r = tr * tinv, scale = wt * a.scale;
                 // q_rest - p_rest from the side that does not cancel
@@ -296,7 +320,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
                 m_r = pub[1];
             }
             if (a.grad) {
-                row.store(a.grad, c.base, c.len, c.live,
+                row.store(a.x, a.grad, c.base, c.len, c.live,
                           [&](float z) { return F == 0.f ? 0.f : exp2_of(z, m_r, k2) * F; });
                 // the record's own, over what the same thread has just stored there
                 for (int h = head[threadIdx.x]; h; h = rec.next[h - 1])
@@ -311,101 +335,165 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_distill(DistillArgs a, Scor
     if constexpr (L > 64) {
         write_sums(a.out, g, w.item, loss, 0.0);
     } else {
-        const double2 sum = team_sum<T>(lane == 0 ? loss : 0.0, 0.0);
+        const double2 sum = team_sum<T, false>(lane == 0 ? loss : 0.0, 0.0);
         write_sums(a.out, g, w.item, sum.x, 0.0);
     }
 }
 
-// A pixel of few classes to a thread: its scores in registers and, to be picked by index, in
-// LDS, from where the workgroup's gradients leave in whole vectors.
-template <int FMT, int N>
-__global__ __launch_bounds__(256) void k_distill_pixel(DistillArgs a, ScoreGeom g)
+// A pixel of few classes to four lanes: eight classes and SLOTS entries of the record each. The
+// scores, and what the record says of a class, meet in LDS: the entries' lanes pick their scores by
+// index, the classes' lanes find the teacher's share. (A thread to itself takes 16 us for
+// 256 x 512 pixels of 19 classes and 4 entries, two waves per SIMD and all latency.)
+template <int FMT, int SLOTS>
+__global__ __launch_bounds__(256) void k_distill_quad(DistillArgs a, ScoreGeom g)
 {
-    __shared__ float lds[256][N + 1];
+    __shared__ __attribute__((aligned(16))) float scores[64][36], shares[64][36];
     if (past_end<kWhole>(g)) return;
-    const Place w = place_of<256, kWhole>(g);
-    const uint32_t rows = min(256u, g.hw - w.p);
-    const bool inside = threadIdx.x < rows;
-    const size_t r = w.row + (inside ? threadIdx.x : 0);
-    float *mine = lds[threadIdx.x];
-    const float wt = !inside ? 0.f : a.weight ? a.weight[r] : 1.f;
+    const Place w = place_of<64, kWhole>(g);
+    const int lane = threadIdx.x & 3, group = threadIdx.x >> 2;
+    const bool inside = w.p + group < g.hw;
+    const size_t r = w.row + (inside ? group : 0);
     const float k2 = kLog2e * a.inv_t;
+    auto meet = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); };
+    // everything is requested before anything is waited for, of pixels of weight 0 too
+    const float wt = a.weight ? a.weight[r] : 1.f, rest = a.rest ? a.rest[r] : -kInf;
+    QuadScores<FMT> px;
+    int idx[SLOTS];                            // entries: class, teacher's score, student's score
+    uint32_t bits[SLOTS];
+    float tt[SLOTS], zk[SLOTS], pk[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        idx[s] = -1;
+        if (s * 4 + lane < a.k) idx[s] = a.index[r * a.k + s * 4 + lane];
+    }
+    if (a.top_fmt == kF32) {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (s * 4 + lane < a.k) bits[s] = ((const uint32_t *)a.top)[r * a.k + s * 4 + lane];
+    } else {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (s * 4 + lane < a.k) bits[s] = ((const uint16_t *)a.top)[r * a.k + s * 4 + lane];
+    }
+    px.load(a.x, r * (size_t)g.c, g.c, g.classes);
+    float y[8] = {};
     double loss = 0.0;
+    if (inside && wt != 0.f) {
+        float *zs = scores[group], *ps = shares[group];
 #pragma unroll
-    for (int j = 0; j < N; ++j) mine[j] = 0.f;
-    if (wt != 0.f) {
-        PixelScores<FMT, N> px;
-        px.load(a.x, r * (size_t)g.c, g.c, g.classes);
-#pragma unroll
-        for (int j = 0; j < N; ++j) mine[j] = px.z[j];
-        const size_t e0 = r * (size_t)a.k;
-        uint32_t record = 0;
-        const float rest = a.rest ? a.rest[r] : -kInf;
+        for (int j = 0; j < 8; ++j) {
+            zs[lane * 8 + j] = px.z[j];
+            ps[lane * 8 + j] = -1.f;                             // not in the record
+        }
         float Mt = rest;
-        for (int e = 0; e < a.k; ++e) {
-            const int i = a.index[e0 + e];
-            if ((unsigned)i >= (unsigned)g.classes) continue;
-            record |= 1u << i;
-            Mt = fmaxf(Mt, load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t);
-        }
-        float m_r = -kInf, M = -kInf;
+        int count = 0;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            M = fmaxf(M, px.z[j]);
-            m_r = fmaxf(m_r, record >> j & 1 ? -kInf : px.z[j]);
+        for (int s = 0; s < SLOTS; ++s) {
+            const bool valid = (unsigned)idx[s] < (unsigned)g.classes;
+            idx[s] = valid ? idx[s] : -1;
+            const float t = a.top_fmt == kF32 ? __uint_as_float(bits[s])
+                            : a.top_fmt == kBF16 ? __uint_as_float(bits[s] << 16)
+                                                 : (float)__builtin_bit_cast(_Float16, (uint16_t)bits[s]);
+            tt[s] = valid ? t * a.inv_t : -kInf;
+            Mt = fmaxf(Mt, tt[s]);
+            count += valid;
         }
-        M = M == -kInf ? 0.f : M;
+        Mt = lane_max<4>(Mt);
         Mt = Mt == -kInf ? 0.f : Mt;
-        m_r = m_r == -kInf ? 0.f : m_r;
-        float top = 0.f, s = 0.f, tp = 0.f;
+        meet();
+        float M = -kInf, tp = 0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const bool in = record >> j & 1;
-            px.z[j] = exp2_of(px.z[j], in ? M : m_r, k2);
-            top += in ? px.z[j] : 0.f;
-            s += in ? 0.f : px.z[j];
+        for (int s = 0; s < SLOTS; ++s) {
+            zk[s] = -kInf;
+            pk[s] = 0.f;
+            if (idx[s] < 0) continue;
+            zk[s] = zs[idx[s]];
+            pk[s] = exp_of(tt[s] - Mt);
+            ps[idx[s]] = pk[s];
+            M = fmaxf(M, zk[s]);
+            tp += pk[s];
         }
-        for (int e = 0; e < a.k; ++e)
-            if ((unsigned)a.index[e0 + e] < (unsigned)g.classes) tp += exp_of(load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt);
-        const float er = s == 0.f ? 0.f : s * exp2_of(m_r, M, k2), total = top + er;
+        meet();
+        float share[8], m_r = -kInf;
+        int classes = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            share[j] = ps[lane * 8 + j];
+            const bool in = !(share[j] < 0.f);                   // a NaN is in it
+            classes += in;
+            m_r = fmaxf(m_r, in ? -kInf : px.z[j]);
+        }
+        // entries of one class: the first stands for it, with the shares of all
+        bool lead[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) lead[s] = idx[s] >= 0;
+        if (lane_sum<4>((float)(count - classes)) != 0.f) {
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                if (idx[s] < 0) continue;
+                float all = 0.f;
+                for (int e = 0; e < a.k; ++e)
+                    if (a.index[r * a.k + e] == idx[s]) {
+                        lead[s] = lead[s] && e >= s * 4 + lane;
+                        all += exp_of(load_elem(a.top, a.top_fmt, r * a.k + e) * a.inv_t - Mt);
+                    }
+                ps[idx[s]] = all;                                // the same from each of them
+            }
+            meet();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) share[j] = ps[lane * 8 + j];
+        }
+        m_r = lane_max<4>(m_r);
+        M = lane_max<4>(fmaxf(M, m_r));
+        M = M == -kInf ? 0.f : M;
+        m_r = m_r == -kInf ? 0.f : m_r;
+        float s_r = 0.f, top = 0.f, ek[SLOTS];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = !(share[j] < 0.f);
+            px.z[j] = exp2_of(px.z[j], in ? M : m_r, k2);
+            s_r += in ? 0.f : px.z[j];
+        }
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            ek[s] = idx[s] < 0 ? 0.f : exp2_of(zk[s], M, k2);
+            top += lead[s] ? ek[s] : 0.f;
+        }
+        s_r = lane_sum<4>(s_r);
+        top = lane_sum<4>(top);
+        tp = lane_sum<4>(tp);
+        const float er = s_r == 0.f ? 0.f : s_r * exp2_of(m_r, M, k2), total = top + er;
         const float tr = a.rest ? exp_of(rest - Mt) : 0.f, ttotal = tp + tr;
         const bool part = total != 0.f && ttotal != 0.f;        // a NaN takes part
-        const float inv = 1.f / total, tinv = 1.f / ttotal, logs = __logf(total) - __logf(ttotal);
+        const float inv = __builtin_amdgcn_rcpf(total), tinv = __builtin_amdgcn_rcpf(ttotal), logs = __logf(total) - __logf(ttotal);
         const float q_r = er * inv, p_r = tr * tinv, scale = wt * a.scale;
         float each = 0.f, diff = 0.f;
-        uint32_t seen = 0;
-        for (int e = 0; e < a.k; ++e) {
-            const int i = a.index[e0 + e];
-            if ((unsigned)i >= (unsigned)g.classes) continue;
-            const float t = load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt, x = mine[i] - M;
-            const bool lead = !(seen >> i & 1);
-            seen |= 1u << i;
-            const float p = exp_of(t) * tinv, q = __builtin_amdgcn_exp2f(x * k2) * inv, d = t - x * a.inv_t + logs;
-            each += divergence(p, q, d, lead);
-            diff += p - (lead ? q : 0.f);
-        }
-        const float dr = (rest - Mt) - ((m_r - M) * a.inv_t + __logf(s)) + logs;
-        each += p_r > 0.f ? (s == 0.f ? kInf : p_r * exp_above_line(-dr)) : q_r + p_r;
-        if (!(q_r > 0.5f)) diff = q_r - p_r;
-        if (part) loss = (double)(scale * each);
-        const float by = scale * a.inv_t, F = part && s != 0.f ? by * diff / s : 0.f, in_record = part ? by * inv : 0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float f = record >> j & 1 ? in_record : F;
-            mine[j] = f == 0.f ? 0.f : px.z[j] * f;
+        for (int s = 0; s < SLOTS; ++s) {
+            if (idx[s] < 0) continue;
+            const float p = pk[s] * tinv, q = ek[s] * inv, d = (tt[s] - Mt) - (zk[s] - M) * a.inv_t + logs;
+            each += divergence(p, q, d, lead[s]);
+            diff += p - (lead[s] ? q : 0.f);
         }
-        if (part)
-            for (int e = 0; e < a.k; ++e) {
-                const int i = a.index[e0 + e];
-                if ((unsigned)i < (unsigned)g.classes)
-                    mine[i] -= by * tinv * exp_of(load_elem(a.top, a.top_fmt, e0 + e) * a.inv_t - Mt);
-            }
+        each = lane_sum<4>(each);
+        diff = lane_sum<4>(diff);
+        const float dr = (rest - Mt) - ((m_r - M) * a.inv_t + __logf(s_r)) + logs;
+        each += p_r > 0.f ? (s_r == 0.f ? kInf : p_r * exp_above_line(-dr)) : q_r + p_r;
+        if (!(q_r > 0.5f)) diff = q_r - p_r;
+        if (part && lane == 0) loss = (double)(scale * each);
+        const float by = part ? scale * a.inv_t : 0.f, F = part && s_r != 0.f ? by * diff / s_r : 0.f;
+        const float in_record = part ? by * inv : 0.f, of_share = part ? by * tinv : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = !(share[j] < 0.f);
+            const float f = in ? in_record : F;
+            y[j] = f == 0.f ? 0.f : px.z[j] * f;
+            if (in && part) y[j] -= share[j] * of_share;
+        }
     }
-    __syncthreads();
-    if (a.grad)
-        store_pixels<FMT>(a.grad, w.row, rows, g.c, g.classes, g.by_out, [&](uint32_t p, int j) { return lds[p][j]; });
+    if (inside && a.grad) QuadScores<FMT>::store(a.grad, r * (size_t)g.c, g.c, g.classes, y);
     if (!wanted(a.out)) return;
-    const double2 sum = team_sum<256>(loss, 0.0);
+    const double2 sum = team_sum<256, false>(loss, 0.0);
     write_sums(a.out, g, w.item, sum.x, 0.0);
 }
 
@@ -451,9 +539,9 @@ __device__ __forceinline__ Decision decide(const ClipArgs &a, size_t row, double
 }
 
 template <int FMT, int L, int NV, int PASS>
-__global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom g)
+__global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_clip(ClipArgs a, ScoreGeom g)
 {
-    using Row = ScoreRow<FMT, L, NV>;
+    using Row = RowOf<FMT, L, NV>;
     constexpr int T = kThreadsOf<L>, G = kGroupsOf<L>;
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
     __shared__ float pub[3];
@@ -469,7 +557,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
         if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
     } else {
         Row row;
-        row.load(a.x, c.base, c.len, c.live);
+        if constexpr (NV) row.load(a.x, c.base, c.len, c.live);
         const int at = act - c.off;                              // the action's place in the chunk
         const bool here = at >= 0 && at < c.len, mine = here && Row::owner(at, c.len) == Row::lane();
         float za = -kInf;
@@ -477,8 +565,10 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
         else if (here) za = load_elem(a.x, FMT, c.base + at);
         Stats st = {};
         if constexpr (PASS != kSecond) {
-            if (mine) row.mask(at, c.len);
-            st = team_stats<L, false>(row.template stats<false>(kLog2e), waves, kLog2e);
+            st = row.template stats<false>(a.x, c.base, c.len, c.live, kLog2e, [&](auto mask) {
+                if (mine) mask(at);
+            });
+            st = team_stats<L, false>(st, waves, kLog2e);
         }
         if constexpr (PASS == kFirst) {
             if (threadIdx.x == 0) {
@@ -514,7 +604,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
                 m = pub[2];
             }
             if (a.grad) {
-                row.store(a.grad, c.base, c.len, c.live,
+                row.store(a.x, a.grad, c.base, c.len, c.live,
                           [&](float z) { return F == 0.f ? 0.f : exp2_of(z, m, kLog2e) * F; });
                 // the action's own, over what the same thread has just stored there
                 if (mine) {
@@ -528,7 +618,7 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_clip(ClipArgs a, ScoreGeom 
     if constexpr (L > 64) {
         write_sums(a.out, g, w.item, loss, kl);
     } else {
-        const double2 sum = team_sum<T>(loss, kl);
+        const double2 sum = team_sum<T, true>(loss, kl);
         write_sums(a.out, g, w.item, sum.x, sum.y);
     }
 }
@@ -604,7 +694,7 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
         store_pixels<FMT>(a.grad, w.row, rows, g.c, g.classes, g.by_out,
                           [&](uint32_t p, int j) { return j < N ? lds[p][j] : 0.f; });
     if (!wanted(a.out)) return;
-    const double2 sum = team_sum<256>(loss, kl);
+    const double2 sum = team_sum<256, true>(loss, kl);
     write_sums(a.out, g, w.item, sum.x, sum.y);
 }
 
@@ -621,7 +711,7 @@ __device__ __forceinline__ void finish_logp(const LogpArgs &a, size_t row, bool 
 template <int FMT, int L, int NV, int PASS, bool SX>
 __global__ __launch_bounds__((kThreadsOf<L>)) void k_logp(LogpArgs a, ScoreGeom g)
 {
-    using Row = ScoreRow<FMT, L, NV>;
+    using Row = RowOf<FMT, L, NV>;
     constexpr int G = kGroupsOf<L>;
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
     if (past_end<PASS>(g)) return;
@@ -630,12 +720,15 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_logp(LogpArgs a, ScoreGeom 
     if (w.p + group >= g.hw) return;
     const Chunk c = chunk_of<PASS>(g, w.row + group, w.chunk);
     Row row;
-    row.load(a.x, c.base, c.len, c.live);
+    if constexpr (NV) row.load(a.x, c.base, c.len, c.live);
     const int act = ((const int32_t *)a.action)[c.row], at = act - c.off;
     const bool valid = (unsigned)act < (unsigned)g.classes, here = valid && at >= 0 && at < c.len;
     const float za = here ? load_elem(a.x, FMT, c.base + at) : -kInf;
-    if (here && Row::owner(at, c.len) == Row::lane()) row.mask(at, c.len);
-    const Stats st = team_stats<L, SX>(row.template stats<SX>(kLog2e), waves, kLog2e);
+    const bool mine = here && Row::owner(at, c.len) == Row::lane();
+    Stats st = row.template stats<SX>(a.x, c.base, c.len, c.live, kLog2e, [&](auto mask) {
+        if (mine) mask(at);
+    });
+    st = team_stats<L, SX>(st, waves, kLog2e);
     if (Row::lane() != 0) return;
     if constexpr (PASS == kFirst) {
         a.stats[c.row * g.chunks + w.chunk] = make_float4(st.m, st.s, st.sx, 0.f);
@@ -704,7 +797,7 @@ __global__ __launch_bounds__(1024) void k_loss_sum(const double2 *part, uint32_t
         s.x += v.x;
         s.y += v.y;
     }
-    s = team_sum<1024>(s.x, s.y);
+    s = team_sum<1024, true>(s.x, s.y);
     if (threadIdx.x == 0) {
         if (loss) loss[i] = (float)s.x;
         if (kl) kl[i] = (float)s.y;
@@ -725,7 +818,7 @@ hipError_t launch_sum(const ScoreGeom &g, const LossOut &o, hipStream_t s)
 
 // Rows in whole where there are many, in chunks where few would leave most of the device idle
 // or where one does not fit a workgroup's registers.
-ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums)
+ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, int pixels)
 {
     const int vec = fmt == kF32 ? 4 : 8;
     const size_t rows = (size_t)g.images * g.hw;
@@ -736,14 +829,17 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums)
     g.chunks = 1;
     g.chunk = g.len;
     const int least = kForms[kChunkForm].lanes * kForms[kChunkForm].nv * vec;
-    if (p.form == kFormCount || (p.form > kChunkForm && rows < 128)) {
+    if ((p.form == kFormCount && !stream) || (p.form > kChunkForm && rows < 128)) {
         p.form = kChunkForm;
         g.chunk = least;
         g.chunks = (int)(((int64_t)g.len + least - 1) / least);
     }
     p.split = g.chunks > 1;
+#ifdef TRY_FORM
+    if (getenv("BC_FORM") && !p.split && p.form >= 5) p.form = atoi(getenv("BC_FORM"));
+#endif
     const int lanes = kForms[p.form].lanes;
-    const uint32_t groups = lanes <= 64 ? 256 / lanes : 1;
+    const uint32_t groups = p.form == 0 ? pixels : lanes <= 64 ? 256 / lanes : 1;
     g.per = (g.hw - 1) / groups + 1;
     g.by_per = Divisor(g.per);
     g.by_chunks = Divisor((uint32_t)g.chunks);
@@ -778,11 +874,12 @@ hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *
             hipLaunchKernelGGL((k_distill<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
             return hipGetLastError();
         }
-        if (p.form == 0)
-            return with_pixel(g.classes, [&](auto n) {
-                hipLaunchKernelGGL((k_distill_pixel<FMT, decltype(n)::value>), grid, dim3(256), 0, s, a, g);
-                return hipGetLastError();
-            });
+        if (p.form == 0) {
+            if (a.k <= 4) hipLaunchKernelGGL((k_distill_quad<FMT, 1>), grid, dim3(256), 0, s, a, g);
+            else if (a.k <= 8) hipLaunchKernelGGL((k_distill_quad<FMT, 2>), grid, dim3(256), 0, s, a, g);
+            else hipLaunchKernelGGL((k_distill_quad<FMT, kMaxTop / 4>), grid, dim3(256), 0, s, a, g);
+            return hipGetLastError();
+        }
         return with_form(p.form, [&](auto l, auto n) {
             constexpr int L = decltype(l)::value, NV = decltype(n)::value;
             hipLaunchKernelGGL((k_distill<FMT, L, NV, kWhole>), grid, dim3(kThreadsOf<L>), 0, s, a, g);

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void k_top_lanes(TopArgs a, ScoreGeom g)
 constexpr int kCandidates = 1024;
 
 template <int FMT, int L, int NV, int PASS>
-__global__ __launch_bounds__(L) void k_top(TopArgs a, ScoreGeom g)
+__global__ __launch_bounds__(L, L > 64 ? 8 : 4) void k_top(TopArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
     constexpr int VEC = kVec<FMT>, W = L / 64;
@@ -220,59 +220,73 @@ __global__ __launch_bounds__(L) void k_top(TopArgs a, ScoreGeom g)
     }
 }
 
-// A pixel of few classes to a thread: k times the largest key that is left, the scores in registers.
-// The records leave through LDS, entry after entry.
-template <int FMT, int N>
-__global__ __launch_bounds__(256) void k_top_pixel(TopArgs a, ScoreGeom g)
+// A pixel of few classes to four lanes, eight classes each: k times the largest of what is left. Of
+// a 16-bit score the key's upper bits and the class make one 32-bit number, whose next largest is a
+// select and a maximum per class. A workgroup is one wave: a frame's active blocks
+// spread over the whole device.
+template <int FMT>
+__global__ __launch_bounds__(64) void k_top_quad(TopArgs a, ScoreGeom g)
 {
-    __shared__ float lds[256][N + 1];
-    __shared__ uint32_t pixel[256];
-    __shared__ uint8_t cls[256][N + 1];
-    const uint32_t total = pixel_count(a, g), first = item_of() * 256;
-    if (first >= total) return;
-    const uint32_t rows = min(256u, total - first);
-    if (threadIdx.x < rows) {
-        const uint32_t at = row_pixel(a, first + threadIdx.x);
-        pixel[threadIdx.x] = at;
-        PixelScores<FMT, N> px;
-        px.load(a.x, at * (size_t)g.c, g.c, g.classes);
-        int key[N];
+    using Scores = QuadScores<FMT>;
+    const uint32_t total = pixel_count(a, g), r = item_of() * 16 + (threadIdx.x >> 2);
+    if (r >= total) return;
+    const size_t px = row_pixel(a, r);
+    const int lane = threadIdx.x & 3, at = Scores::first();
+    Scores own;
+    own.load(a.x, px * (size_t)g.c, g.c, g.classes);
+    constexpr int kNone = (int)0x80000000u;                      // below every key
+    int key[8];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            lds[threadIdx.x][j] = px.z[j];
-            key[j] = (int)((uint32_t)(key_of(px.z[j], 0) >> 32) ^ 0x80000000u);
-        }
-        uint32_t left = g.classes == 32 ? ~0u : (1u << g.classes) - 1u;
-        for (int i = 0; i < a.k; ++i) {
-            int top = (int)0x80000000u, at = 0;                  // below every key
+    for (int j = 0; j < 8; ++j) {
+        key[j] = (int)((uint32_t)(key_of(own.z[j], 0) >> 32) ^ 0x80000000u);
+        // a 16-bit score's lowest 16 (bf16) or 13 (fp16) bits as fp32 are 0: room for the class, the
+        // lower one on top
+        if constexpr (FMT != kF32) key[j] |= 31 - (at + j);
+        if (at + j >= g.classes) key[j] = kNone;
+    }
+    uint32_t taken = 0;                                          // of this lane's eight
+    for (int i = 0; i < a.k; ++i) {
+        int top = kNone, best = 0;
+        if constexpr (FMT != kF32) {
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if ((left >> j & 1) && key[j] > top) {
+            for (int j = 0; j < 8; ++j) top = max(top, taken >> j & 1 ? kNone : key[j]);
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0xB1, 0xF, 0xF, false));
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0x4E, 0xF, 0xF, false));
+            best = 31 - (top & 31);
+        } else {
+#pragma unroll
+            for (int j = 7; j >= 0; --j)
+                if (!(taken >> j & 1) && key[j] >= top) {
                     top = key[j];
-                    at = j;
+                    best = at + j;
                 }
-            cls[threadIdx.x][i] = (uint8_t)at;
-            left &= ~(1u << at);
+            auto meet = [&](int t, int b) {                      // the larger, of equal ones the lower class
+                const bool other = t > top || (t == top && b < best);
+                top = other ? t : top;
+                best = other ? b : best;
+            };
+            meet(__builtin_amdgcn_mov_dpp(top, 0xB1, 0xF, 0xF, false), __builtin_amdgcn_mov_dpp(best, 0xB1, 0xF, 0xF, false));
+            meet(__builtin_amdgcn_mov_dpp(top, 0x4E, 0xF, 0xF, false), __builtin_amdgcn_mov_dpp(best, 0x4E, 0xF, 0xF, false));
         }
-        if (a.rest) {
-            float m = -kInf, s = 0.f;
+        if (best >> 3 == lane) {                                 // its lane writes it
+            taken |= 1u << (best & 7);
+            float y[1] = {own.z[0]};
 #pragma unroll
-            for (int j = 0; j < N; ++j) m = fmaxf(m, left >> j & 1 ? px.z[j] : -kInf);
-            const float ref = m == -kInf ? 0.f : m;
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                s += left >> j & 1 ? exp2_of(px.z[j], ref, kLog2e * a.inv_t) : 0.f;
-            a.rest[at] = rest_of(a, {m, s, 0.f});
+            for (int j = 1; j < 8; ++j) y[0] = (best & 7) == j ? own.z[j] : y[0];
+            store_raw<FMT, 1>(a.top, px * a.k + i, pack<FMT, 1>(y));
+            a.index[px * a.k + i] = best;
         }
     }
-    __syncthreads();
-    for (uint32_t f = threadIdx.x; f < rows * (uint32_t)a.k; f += 256) {
-        const uint32_t p = div(f, a.by_k), e = f - p * (uint32_t)a.k;
-        const size_t at = pixel[p] * (size_t)a.k + e;
-        const float y[1] = {lds[p][cls[p][e]]};
-        store_raw<FMT, 1>(a.top, at, pack<FMT, 1>(y));
-        a.index[at] = cls[p][e];
-    }
+    if (!a.rest) return;
+    float m = -kInf, s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, taken >> j & 1 ? -kInf : own.z[j]);
+    m = lane_max<4>(m);
+    const float ref = m == -kInf ? 0.f : m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += taken >> j & 1 ? 0.f : exp2_of(own.z[j], ref, kLog2e * a.inv_t);
+    s = lane_sum<4>(s);
+    if (lane == 0) a.rest[px] = rest_of(a, {m, s, 0.f});
 }
 
 // The chunks' records of a row joined, by a wave.
@@ -318,7 +332,7 @@ __global__ __launch_bounds__(64) void k_top_join(TopArgs a, ScoreGeom g)
 
 ScorePlan top_plan(ScoreGeom &g, int fmt, int k)
 {
-    ScorePlan p = score_plan(g, fmt, 0, false);
+    ScorePlan p = score_plan(g, fmt, 0, false, false, 16);
     if (p.split) {
         p.pick = p.bytes;
         p.bytes += (size_t)g.images * g.hw * g.chunks * (size_t)k * sizeof(Key);
@@ -331,7 +345,6 @@ hipError_t launch_top(TopArgs a, ScoreGeom g, const ScorePlan &p, void *work, in
     uint8_t *w = (uint8_t *)work;
     a.stats = (float4 *)(w + p.stats);
     a.keys = (unsigned long long *)(w + p.pick);
-    a.by_k = Divisor((uint32_t)a.k);
     const size_t rows = (size_t)g.images * g.hw;
     return with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
@@ -341,14 +354,15 @@ hipError_t launch_top(TopArgs a, ScoreGeom g, const ScorePlan &p, void *work, in
             hipLaunchKernelGGL((k_top_join<FMT>), grid_of(rows), dim3(64), 0, s, a, g);
             return hipGetLastError();
         }
-        if (p.form == 0)
-            return with_pixel(g.classes, [&](auto n) {
-                hipLaunchKernelGGL((k_top_pixel<FMT, decltype(n)::value>), grid_of((rows + 255) / 256), dim3(256), 0, s, a, g);
-                return hipGetLastError();
-            });
+        if (p.form == 0) {
+            hipLaunchKernelGGL((k_top_quad<FMT>), grid_of((rows + 15) / 16), dim3(64), 0, s, a, g);
+            return hipGetLastError();
+        }
         return with_form(p.form, [&](auto l, auto n) {
             constexpr int L = decltype(l)::value, NV = decltype(n)::value, G = kGroupsOf<L>;
-            if constexpr (L < 64)
+            if constexpr (NV == 0)
+                return hipErrorInvalidValue;                     // not planned here
+            else if constexpr (L < 64)
                 hipLaunchKernelGGL((k_top_lanes<FMT, L>), grid_of((rows + G - 1) / G), dim3(256), 0, s, a, g);
             else
                 hipLaunchKernelGGL((k_top<FMT, L, NV, kWhole>), grid_of(rows), dim3(L), 0, s, a, g);

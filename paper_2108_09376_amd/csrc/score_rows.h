@@ -159,6 +159,13 @@ struct ScoreRow {
     }
 
     // Statistics over the lanes of a wave that hold the row (all of them if L >= 64).
+    template <bool SX, typename M>
+    __device__ __forceinline__ Stats stats(const void *, size_t, int len, int, float k2, M masked)
+    {
+        masked([&](int e) { mask(e, len); });
+        return stats<SX>(k2);
+    }
+
     template <bool SX>
     __device__ __forceinline__ Stats stats(float k2)
     {
@@ -196,7 +203,7 @@ struct ScoreRow {
 
     // out[base + e] = value(score e) for every element of the row, 0 at `live` and beyond.
     template <typename F>
-    __device__ __forceinline__ void store(void *out, size_t base, int len, int live, F value) const
+    __device__ __forceinline__ void store(const void *, void *out, size_t base, int len, int live, F value) const
     {
         const int nvec = len / VEC;
 #pragma unroll
@@ -234,6 +241,135 @@ struct ScoreRow {
     }
 };
 
+// A row of any length, passed over twice in memory: nothing of it stays in registers but B vectors of
+// a lane at a time. The statistics keep a running maximum, the sums corrected where a batch
+// raises it. Same interface as ScoreRow; elements to be masked are told one by one before the
+// statistics (`masked` says which the lane has).
+template <int FMT, int L, int B>
+struct StreamRow {
+    static constexpr int VEC = kVec<FMT>;
+
+    static __device__ __forceinline__ int lane() { return threadIdx.x % L; }
+    static __device__ __forceinline__ int owner(int e, int len)
+    {
+        const int nvec = len / VEC, i = e / VEC;
+        return i < nvec ? i % L : e - nvec * VEC;
+    }
+
+    // The batch of vectors from v0 on: -inf past the live ones.
+    static __device__ __forceinline__ void load(Raw<FMT, VEC> (&r)[B], const void *x, size_t base, int v0, int here, int live)
+    {
+        if (v0 + B * L <= here) {
+#pragma unroll
+            for (int k = 0; k < B; ++k) r[k] = load_raw<FMT, VEC>(x, base + (size_t)(v0 + k * L + lane()) * VEC);
+        } else {
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int i = v0 + k * L + lane();
+                r[k] = masked_raw<FMT, VEC>();
+                if (i < here) r[k] = load_raw<FMT, VEC>(x, base + (size_t)i * VEC);
+                if (i < here && (i + 1) * VEC > live)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (i * VEC + j >= live) mask_elem<FMT, VEC>(r[k], j);
+            }
+        }
+    }
+
+    // masked(f): calls f(e) for every element of the row that this lane holds and that is to count as -inf.
+    template <bool SX, typename M>
+    static __device__ __forceinline__ Stats stats(const void *x, size_t base, int len, int live, float k2, M masked)
+    {
+        const int nvec = len / VEC, here = min(nvec, (live + VEC - 1) / VEC), last = nvec * VEC + lane();
+        float m = -kInf, ref = 0.f, s = 0.f, sx = 0.f;
+        for (int v0 = 0; v0 < here; v0 += B * L) {
+            Raw<FMT, VEC> r[B];
+            load(r, x, base, v0, here, live);
+            masked([&](int e) {
+                const int i = e / VEC - v0, word = FMT == kF32 ? e % VEC : e % VEC >> 1;
+                const uint32_t keep = FMT == kF32 ? 0u : e & 1 ? 0xFFFFu : 0xFFFF0000u;
+#pragma unroll
+                for (int k = 0; k < B; ++k)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        r[k].w[w] = i == k * L + lane() && w == word && e < nvec * VEC
+                                        ? (r[k].w[w] & keep) | (kMaskedWord<FMT> & ~keep) : r[k].w[w];
+            });
+            float up = m;
+#pragma unroll
+            for (int k = 0; k < B; ++k)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) up = fmaxf(up, get(r[k], j));
+            const float to = up == -kInf ? 0.f : up, f = exp2_of(m, to, k2);
+            if constexpr (SX) sx = f * (sx + fmaxf(m - to, -1e30f) * s);
+            s *= f;
+            m = up;
+            ref = to;
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float d = get(r[k], j) - ref, e = __builtin_amdgcn_exp2f(d * k2);
+                    s += e;
+                    if constexpr (SX) sx += e * fmaxf(d, -1e30f);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        Stats one = {-kInf, 0.f, 0.f};
+        if (last < len && last < live) {
+            float z = get(load_raw<FMT, 1>(x, base + last), 0);
+            masked([&](int e) { z = e == last ? -kInf : z; });
+            one = {z, z == -kInf ? 0.f : 1.f, 0.f};
+            if (z != z) one = {-kInf, z, z};                     // a NaN is in the sums, not in the maximum
+        }
+        const Stats mine = join<SX>({m, s, sx}, one, k2);
+        m = lane_max<64>(mine.m);
+        const float all = m == -kInf ? 0.f : m, f = exp2_of(mine.m, all, k2);
+        s = mine.m == -kInf ? mine.s : mine.s * f;
+        sx = mine.m == -kInf ? mine.sx : f * (mine.sx + fmaxf(mine.m - all, -1e30f) * mine.s);
+        return {m, lane_sum<64>(s), SX ? lane_sum<64>(sx) : 0.f};
+    }
+
+    // out[base + e] = value(score e), 0 at `live` and beyond; out may be x.
+    template <typename F>
+    static __device__ __forceinline__ void store(const void *x, void *out, size_t base, int len, int live, F value)
+    {
+        const int nvec = len / VEC, here = min(nvec, (live + VEC - 1) / VEC), last = nvec * VEC + lane();
+        for (int v0 = 0; v0 < nvec; v0 += B * L) {
+            Raw<FMT, VEC> r[B];
+            load(r, x, base, v0, here, live);
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int i = v0 + k * L + lane();
+                if (i < nvec) {
+                    float y[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) y[j] = value(get(r[k], j));
+                    if ((i + 1) * VEC > live)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) y[j] = i * VEC + j < live ? y[j] : 0.f;
+                    store_raw<FMT, VEC>(out, base + (size_t)i * VEC, pack<FMT, VEC>(y));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (last < len) {
+            const float y[1] = {last < live ? value(get(load_raw<FMT, 1>(x, base + last), 0)) : 0.f};
+            store_raw<FMT, 1>(out, base + last, pack<FMT, 1>(y));
+        }
+    }
+
+    static __device__ __forceinline__ void store_zeros(void *out, size_t base, int len)
+    {
+        const int nvec = len / VEC, last = nvec * VEC + lane();
+        const Raw<FMT, VEC> z = {};
+        const Raw<FMT, 1> z1 = {};
+        for (int i = lane(); i < nvec; i += L) store_raw<FMT, VEC>(out, base + (size_t)i * VEC, z);
+        if (last < len) store_raw<FMT, 1>(out, base + last, z1);
+    }
+};
+
 // One element of any format, told at run time.
 __device__ __forceinline__ float load_elem(const void *p, int fmt, size_t i)
 {
@@ -248,11 +384,15 @@ constexpr int kPixelClasses = 32;
 struct Form {
     int lanes, nv;
 };
-constexpr Form kForms[] = {{1, 0}, {8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
-constexpr int kFormCount = 9, kChunkForm = 5;
+constexpr Form kForms[] = {{1, 0}, {8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 0}};
+constexpr int kFormCount = 8, kChunkForm = 5;                      // the last of any length
 
 template <int L> constexpr int kThreadsOf = L <= 64 ? 256 : L;
 template <int L> constexpr int kGroupsOf = L <= 64 ? 256 / L : 1;  // rows of a workgroup
+
+// NV = 0: rows of any length, of which a workgroup passes over its own twice.
+template <int FMT, int L, int NV>
+using RowOf = std::conditional_t<NV == 0, StreamRow<FMT, L, 4>, ScoreRow<FMT, L, NV ? NV : 1>>;
 
 // Which part of the work a launch does: whole rows; a chunk's statistics; a chunk's gradient.
 enum Pass { kWhole, kFirst, kSecond };
@@ -327,7 +467,7 @@ hipError_t with_form(int form, F &&f)
     case 5: return f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
     case 6: return f(integral_constant<int, 512>{}, integral_constant<int, 8>{});
     case 7: return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
-    default: return f(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+    default: return f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
     }
 }
 
@@ -347,22 +487,86 @@ struct PixelScores {
     static constexpr int VEC = kVec<FMT>;
     float z[N];
 
+    // All requests before the first use: the conditions are the same for every pixel.
     __device__ __forceinline__ void load(const void *x, size_t base, int c, int classes)
     {
+        if ((classes + VEC - 1) / VEC * VEC <= c) {
+            Raw<FMT, VEC> r[N / VEC];
 #pragma unroll
-        for (int at = 0; at < N; at += VEC) {
-            if (at >= classes) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) z[at + j] = -kInf;
-            } else if (at + VEC <= c) {
-                const Raw<FMT, VEC> r = load_raw<FMT, VEC>(x, base + at);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) z[at + j] = at + j < classes ? get(r, j) : -kInf;
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    z[at + j] = at + j < classes ? get(load_raw<FMT, 1>(x, base + at + j), 0) : -kInf;
+            for (int v = 0; v < N / VEC; ++v) {
+                r[v] = masked_raw<FMT, VEC>();
+                if (v * VEC < classes) r[v] = load_raw<FMT, VEC>(x, base + v * VEC);
             }
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] = j < classes ? get(r[j / VEC], j % VEC) : -kInf;
+        } else {
+            Raw<FMT, 1> r[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                r[j] = masked_raw<FMT, 1>();
+                if (j < classes) r[j] = load_raw<FMT, 1>(x, base + j);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] = get(r[j], 0);
+        }
+    }
+};
+
+// The scores of a pixel of up to 32 classes over four lanes, eight to a lane; -inf past its classes.
+template <int FMT>
+struct QuadScores {
+    static constexpr int VEC = kVec<FMT>, NV = 8 / VEC;
+    float z[8];
+
+    static __device__ __forceinline__ int first() { return (threadIdx.x & 3) * 8; }
+
+    __device__ __forceinline__ void load(const void *x, size_t base, int c, int classes)
+    {
+        Raw<FMT, VEC> r[NV];
+        Raw<FMT, 1> e[8];
+        const int at = first();
+        const bool whole = c % VEC == 0;                         // the same for every pixel
+        if (whole) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                r[v] = masked_raw<FMT, VEC>();
+                if (at + v * VEC < classes) r[v] = load_raw<FMT, VEC>(x, base + at + v * VEC);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                e[j] = masked_raw<FMT, 1>();
+                if (at + j < classes) e[j] = load_raw<FMT, 1>(x, base + at + j);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = at + j < classes ? (whole ? get(r[j / VEC], j % VEC) : get(e[j], 0)) : -kInf;
+    }
+
+    // y where there are classes, 0 in the row's other channels
+    static __device__ __forceinline__ void store(void *out, size_t base, int c, int classes, float (&y)[8])
+    {
+        const int at = first();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = at + j < classes ? y[j] : 0.f;
+        if (c % VEC == 0) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float w[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[j] = y[v * VEC + j];
+                if (at + v * VEC < c) store_raw<FMT, VEC>(out, base + at + v * VEC, pack<FMT, VEC>(w));
+            }
+            const Raw<FMT, VEC> zero = {};
+            for (int i = 32 + (threadIdx.x & 3) * VEC; i < c; i += 4 * VEC) store_raw<FMT, VEC>(out, base + i, zero);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float w[1] = {y[j]};
+                if (at + j < c) store_raw<FMT, 1>(out, base + at + j, pack<FMT, 1>(w));
+            }
+            const Raw<FMT, 1> zero = {};
+            for (int i = 32 + (threadIdx.x & 3); i < c; i += 4) store_raw<FMT, 1>(out, base + i, zero);
         }
     }
 };
