@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_di
     };
     const bool inside = w.p + group < g.hw;
     const Chunk c = chunk_of<PASS>(g, inside ? w.row + group : w.row, w.chunk);
-    const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f;
+    const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f, rest = a.rest ? a.rest[c.row] : -kInf;
     double loss = 0.0;
     if (wt == 0.f) {
         if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
@@ -222,8 +222,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_di
                 // a class's first entry stands for it; entries of one class that no chunk shares are
                 // found by their index
                 bool lead[SLOTS];
-                float M = st.m, Mt = a.rest ? a.rest[c.row] : -kInf;
-                const float rest = Mt;
+                float M = st.m, Mt = rest;
 #pragma unroll
                 for (int s = 0; s < SLOTS; ++s) {
                     lead[s] = idx[s] >= 0;
@@ -522,15 +521,25 @@ struct Decision {
     double loss, kl, slope;
 };
 
-__device__ __forceinline__ Decision decide(const ClipArgs &a, size_t row, double l)
+// What a decision is judged by: requested before the row's scores are waited for.
+struct Given {
+    float advantage, old_logp, ref_logp;
+};
+
+__device__ __forceinline__ Given given(const ClipArgs &a, size_t row)
 {
-    const double adv = a.advantage[row], r = exp(l - (double)a.old_logp[row]);
+    return {a.advantage[row], a.old_logp[row], a.ref_logp ? a.ref_logp[row] : 0.f};
+}
+
+__device__ __forceinline__ Decision decide(const ClipArgs &a, const Given &v, double l)
+{
+    const double adv = v.advantage, r = exp(l - (double)v.old_logp);
     const double lo = 1.0 - (double)a.low, hi = 1.0 + (double)a.high;
     const double kept = r * adv, held = (r < lo ? lo : r > hi ? hi : r) * adv;
     const bool open = !(kept > held);                            // a NaN stays one
     Decision d = {-(open ? kept : held), 0.0, open ? -kept : 0.0};
     if (a.ref_logp) {
-        const double x = (double)a.ref_logp[row] - l, up = expm1(x);
+        const double x = (double)v.ref_logp - l, up = expm1(x);
         d.kl = up - x;
         d.loss += (double)a.beta * d.kl;
         d.slope -= (double)a.beta * up;
@@ -552,6 +561,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
     const Chunk c = chunk_of<PASS>(g, inside ? w.row + group : w.row, w.chunk);
     const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f;
     const int act = ((const int32_t *)a.action)[c.row];
+    const Given v = given(a, c.row);
     double loss = 0.0, kl = 0.0;
     if (wt == 0.f || (unsigned)act >= (unsigned)g.classes) {
         if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
@@ -581,7 +591,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
                 if constexpr (PASS == kSecond) st = row_stats<false>(a.stats + c.row * g.chunks, g.chunks, kLog2e);
                 if (za != -kInf) {                               // a masked class was not chosen here
                     const Chosen ch = chosen(za, st);
-                    const Decision d = decide(a, c.row, ch.l);
+                    const Decision d = decide(a, v, ch.l);
                     const double by = (double)wt * (double)a.scale;
                     if (Row::lane() == 0) {
                         loss = by * d.loss;
@@ -647,6 +657,7 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
     float *mine = lds[threadIdx.x];
     const float wt = !inside ? 0.f : a.weight ? a.weight[r] : 1.f;
     const double by = (double)wt * (double)a.scale;
+    const Given v = given(a, r);
     double loss = 0.0, kl = 0.0;
 #pragma unroll
     for (int j = 0; j < N; ++j) mine[j] = 0.f;
@@ -654,7 +665,7 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
         const bool executed = ((const uint8_t *)a.action)[r] != 0;
         const Binary b = binary(load_elem(a.x, FMT, r * (size_t)g.c), executed);
         if (wt != 0.f && b.l != -(double)kInf) {
-            const Decision d = decide(a, r, b.l);
+            const Decision d = decide(a, v, b.l);
             loss = by * d.loss;
             kl = by * d.kl;
             mine[0] = (float)(by * d.slope * (executed ? b.other : -b.other));
@@ -679,7 +690,7 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
             }
             if (za != -kInf) {
                 const Chosen ch = chosen(za, {m, s, 0.f});
-                const Decision d = decide(a, r, ch.l);
+                const Decision d = decide(a, v, ch.l);
                 loss = by * d.loss;
                 kl = by * d.kl;
                 const float F = s == 0.f ? 0.f : (float)(-by * d.slope * ch.other / (double)s);
@@ -738,14 +749,15 @@ __global__ __launch_bounds__((kThreadsOf<L>)) void k_logp(LogpArgs a, ScoreGeom 
     }
 }
 
-// The chunks of each row joined, one row per thread.
+// The chunks of a row joined, by a wave.
 __global__ __launch_bounds__(64) void k_logp_join(LogpArgs a, ScoreGeom g)
 {
-    const size_t r = (size_t)item_of() * 64 + threadIdx.x;
+    const size_t r = item_of();
     if (r >= (size_t)g.images * g.hw) return;
-    const Stats st = row_stats<true>(a.stats + r * g.chunks, g.chunks, kLog2e);
     const bool valid = (unsigned)((const int32_t *)a.action)[r] < (unsigned)g.classes;
-    finish_logp(a, r, valid, valid ? a.pick[r] : -kInf, st);
+    const float za = valid ? a.pick[r] : -kInf;
+    const Stats st = row_stats<true>(a.stats + r * g.chunks, g.chunks, kLog2e);
+    if (threadIdx.x == 0) finish_logp(a, r, valid, za, st);
 }
 
 template <int FMT, int N>
@@ -945,7 +957,7 @@ hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
             if (p.split) {
                 constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
                 hipLaunchKernelGGL((k_logp<FMT, L, NV, kFirst, SX>), grid, dim3(L), 0, s, a, g);
-                hipLaunchKernelGGL(k_logp_join, grid_of((rows + 63) / 64), dim3(64), 0, s, a, g);
+                hipLaunchKernelGGL(k_logp_join, grid_of(rows), dim3(64), 0, s, a, g);
                 return hipGetLastError();
             }
             return with_form(p.form, [&](auto l, auto n) {

@@ -87,24 +87,101 @@ __global__ __launch_bounds__(256) void k_top_lanes(TopArgs a, ScoreGeom g)
     if (lane == 0) a.rest[px] = rest_of(a, st);
 }
 
-// Rows of a wave or a workgroup. Every wave finds the q-th largest of its lanes' maxima, q
-// enough that all waves together have k; the least of these is a score that at least k scores reach,
-// and few more than that do. Those that reach it are collected in LDS, and each one's place among
-// them is the number of larger keys. Where more reach it than LDS holds (long runs of equal
-// scores, parts of a row masked out), or fewer than k (NaN), the record is found by rounds.
-constexpr int kCandidates = 1024;
+// Rows of a wave or a workgroup. Every thread knows the largest score of its part; the first wave
+// halves the range of these until it has a bar that at least k of them reach, and not many
+// more, while the others sum their exponentials. Threads whose maximum reaches it (holders) lay their
+// part of the row in LDS, where their wave looks through it, an element to a lane; the scores that
+// reach the bar are collected, and each one's place among them is the number of larger keys. The rest
+// is the other threads' sums and the holders' elements outside the record.
+// What all waves of a long row do is what counts: 16 waves to a row of 65536, 8 to a SIMD, so that an
+// instruction of theirs takes 32 cycles, and one of the first wave alone next to none.
+// Rows of which LDS does not hold what reaches the bar (long runs of equal scores, parts masked
+// out), or of which fewer than k do (NaN), are left to top_slow.
+constexpr int kCandidates = 512;
+// Holders of a wave: k of 64 spread over the waves, with 84 holders, come in less than once in 10^5 rows.
+template <int L> constexpr int kHolders = L == 64 ? 64 : L == 256 ? 44 : L == 512 ? 28 : 20;
+
+template <int W>
+struct TopShared {
+    Key cand[kCandidates], record[64];
+    int counts[2][W], count;
+    Stats waves[W];
+};
+
+// A row, or a chunk of it, over the row in memory: the k-th score and the last class to have it are
+// found by halving, counting each time.
+template <int FMT, int L>
+__device__ __noinline__ void top_slow(const void *x, Chunk c, int k, float k2, TopShared<L / 64> *sh, Stats *st)
+{
+    constexpr int VEC = kVec<FMT>, W = L / 64;
+    const int lane = threadIdx.x % L, nvec = c.live / VEC;
+    int turn = 0;
+    // f(score, class) of all elements; a NaN counts as -inf
+    auto see = [&](auto f) {
+        for (int i = lane; i < nvec; i += L) {
+            const Raw<FMT, VEC> r = load_raw<FMT, VEC>(x, c.base + (size_t)i * VEC);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f(get(r, j), c.off + i * VEC + j);
+        }
+        if (nvec * VEC + lane < c.live) f(get(load_raw<FMT, 1>(x, c.base + nvec * VEC + lane), 0), c.off + nvec * VEC + lane);
+    };
+    auto number = [&](auto f) {
+        int own = 0;
+        see([&](float z, int cls) { own += f(fmaxf(z, -kInf), cls); });
+        const int wave = (int)lane_sum<64>((float)own);
+        turn ^= 1;
+        if ((lane & 63) == 0) sh->counts[turn][lane >> 6] = wave;
+        __syncthreads();
+        int all = 0;
+        for (int w = 0; w < W; ++w) all += sh->counts[turn][w];
+        return all;
+    };
+    auto of = [](uint32_t key) { return score_of((Key)(key ^ 0x80000000u) << 32); };
+    // keys of 16-bit scores end in zeros
+    constexpr int kZeros = FMT == kF32 ? 0 : FMT == kBF16 ? 16 : 13;
+    int low = -(0x7F800000 >> kZeros), high = (0x7F800000 >> kZeros) + 1;
+    while ((uint32_t)high - (uint32_t)low > 1u) {
+        const int mid = (int)((uint32_t)low + (((uint32_t)high - (uint32_t)low) >> 1));
+        const float b = of((uint32_t)mid << kZeros);
+        if (number([&](float z, int) { return z >= b; }) >= k) low = mid;
+        else high = mid;
+    }
+    const float kth = of((uint32_t)low << kZeros);
+    const int need = k - number([&](float z, int) { return z > kth; });
+    int first = c.off, last = c.off + c.live - 1;                // the class of the k-th is in [first, last]
+    while (first < last) {
+        const int mid = first + ((last - first) >> 1);
+        if (number([&](float z, int cls) { return z == kth && cls <= mid; }) >= need) last = mid;
+        else first = mid + 1;
+    }
+    auto in = [&](float z, int cls) {
+        const float y = fmaxf(z, -kInf);
+        return y > kth || (y == kth && cls <= first);
+    };
+    if (lane == 0) sh->count = 0;
+    __syncthreads();
+    float m = -kInf, s = 0.f;
+    see([&](float z, int cls) {
+        if (in(z, cls)) sh->cand[atomicAdd(&sh->count, 1) & (kCandidates - 1)] = key_of(z, cls);
+        else m = fmaxf(m, z);
+    });
+    const float ref = m == -kInf ? 0.f : m;
+    see([&](float z, int cls) { s += in(z, cls) ? 0.f : exp2_of(z, ref, k2); });
+    *st = wave_join<false>({m, s, 0.f}, k2);
+    __syncthreads();
+}
 
 template <int FMT, int L, int NV, int PASS>
-__global__ __launch_bounds__(L, L > 64 ? 8 : 4) void k_top(TopArgs a, ScoreGeom g)
+__global__ __launch_bounds__(L, L > 256 ? 8 : L == 256 ? 5 : 3) void k_top(TopArgs a, ScoreGeom g)
 {
     using Row = ScoreRow<FMT, L, NV>;
-    constexpr int VEC = kVec<FMT>, W = L / 64;
-    __shared__ __attribute__((aligned(16))) Key cand[kCandidates];
-    __shared__ Key record[64];
-    __shared__ Key best[W];
-    __shared__ float least[W];
-    __shared__ Stats waves[W];
-    __shared__ int head[L], next[64], count;
+    constexpr int VEC = kVec<FMT>, W = L / 64, H = kHolders<L>;
+    constexpr int kPart = NV * 4 + 1;                            // words of a thread's part: its vectors, the last element
+    __shared__ TopShared<W> sh;
+    __shared__ float maxima[L];
+    __shared__ uint32_t part[W][H][kPart];
+    __shared__ int who[W][H];
+    __shared__ float bar_of;
     uint32_t r = item_of();
     int chunk = 0;
     if constexpr (PASS == kFirst) {
@@ -115,105 +192,137 @@ __global__ __launch_bounds__(L, L > 64 ? 8 : 4) void k_top(TopArgs a, ScoreGeom 
     if (r >= pixel_count(a, g)) return;
     const size_t px = row_pixel(a, r);
     const Chunk c = chunk_of<PASS>(g, px, chunk);
+    const int lane = Row::lane(), wave = lane >> 6, nvec = c.len / VEC, k = min(a.k, c.live);
+    const float k2 = kLog2e * a.inv_t;
+    float own_sum = 0.f;
     Row row;
     row.load(a.x, c.base, c.len, c.live);
-    const int lane = Row::lane(), nvec = c.len / VEC, k = min(a.k, c.live);
-    head[lane] = 0;
-    if (lane == 0) count = 0;
-
-    float m = get(row.t, 0);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        if (v < row.used)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) m = fmaxf(m, get(row.v[v], j));
-        __builtin_amdgcn_sched_barrier(0);
-    }
+    if (lane == 0) sh.count = 0;
+    const float m = row.largest();
     row.keep();
-    // waves whose lanes all hold a vector
-    const int full = min(W, nvec / 64);
-    float bar = -kInf;
-    if (full) {
-        float x = m;
-        const int q = (k + full - 1) / full;
-        for (int i = 0; i < q; ++i) {
-            bar = lane_max<64>(x);
-            const unsigned long long at = __ballot(x == bar);
-            if (at && (int)(threadIdx.x & 63) == __ffsll(at) - 1) x = -kInf;
-        }
-    }
-    if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = bar;
+    maxima[lane] = m;
     __syncthreads();
-    bar = least[0];
-    for (int w = 1; w < full; ++w) bar = fminf(bar, least[w]);
-    if (m >= bar) {
-        auto add = [&](float z, int e) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kCandidates) cand[at] = key_of(z, c.off + e);
+    if (wave == 0) {
+        float own[W], low = kInf, high = -kInf;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            own[w] = maxima[w * 64 + lane];
+            high = fmaxf(high, own[w]);
+            low = fminf(low, own[w] == -kInf ? kInf : own[w]);
+        }
+        high = lane_max<64>(high);
+        low = -lane_max<64>(-low);
+        auto reach = [&](float b) {                              // how many maxima do
+            int n = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) n += __popcll(__ballot(own[w] >= b));
+            return n;
         };
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int at = (v * L + lane) * VEC;
-            uint32_t hit = 0;
-            if (v < row.used && v * L + lane < nvec)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) hit |= get(row.v[v], j) >= bar && at + j < c.live ? 1u << j : 0u;
-            if (hit)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (hit >> j & 1) add(get(row.v[v], j), at + j);
-            __builtin_amdgcn_sched_barrier(0);
+        float bar = -kInf;
+        if (low < kInf && reach(low) >= k) {
+            bar = low;
+            // `bar` is reached by k at least, `high` by fewer: until as many as are wanted reach the bar
+            for (int i = 0; i < 24; ++i) {
+                const float mid = 0.5f * bar + 0.5f * high;
+                if (!(mid > bar)) break;
+                const int n = reach(mid);
+                if (n < k) high = mid;
+                else bar = mid;
+                if (n >= k && n <= k + k / 4 + 4) break;
+            }
         }
-        const int e = nvec * VEC + lane;
-        if (e < c.live && get(row.t, 0) >= bar) add(get(row.t, 0), e);
+        if (lane == 0) bar_of = bar;
+    }
+    if (a.rest) own_sum = row.own_sum(m, k2);
+    row.keep();
+    __syncthreads();
+    const float bar = bar_of;
+    const bool holder = m >= bar;
+    const unsigned long long of_wave = __ballot(holder);
+    const int holders = __popcll(of_wave), rank = __popcll(of_wave & ((1ull << (lane & 63)) - 1ull));
+    if (holder && rank < H) {
+        who[wave][rank] = lane;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[wave][rank][v * 4 + i] = row.v[v].w[i];
+        part[wave][rank][NV * 4] = row.t.w[0];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    // f(score, class) of the elements of the wave's holders, in their order, two holders at a time
+    const int staged = min(holders, H), per_holder = NV * VEC + (c.len > nvec * VEC);
+    auto held = [&](auto f) {
+        for (int h = 0; h < staged; h += 2) {
+            const int h2 = min(h + 1, staged - 1), own = who[wave][h], own2 = who[wave][h2];
+            for (int e = lane & 63; e < per_holder; e += 64) {
+                const bool tail = e == NV * VEC;
+                Raw<FMT, 1> z, z2;
+                if constexpr (FMT == kF32) {
+                    z.w[0] = part[wave][h][e];
+                    z2.w[0] = part[wave][h2][e];
+                } else {
+                    z.w[0] = tail ? part[wave][h][NV * 4] : ((const uint16_t *)part[wave][h])[e];
+                    z2.w[0] = tail ? part[wave][h2][NV * 4] : ((const uint16_t *)part[wave][h2])[e];
+                }
+                const int i = (e / VEC) * L, j = e % VEC;
+                if (tail || i + own < nvec) f(get(z, 0), tail ? nvec * VEC + own : (i + own) * VEC + j);
+                if (h2 > h && (tail || i + own2 < nvec)) f(get(z2, 0), tail ? nvec * VEC + own2 : (i + own2) * VEC + j);
+            }
+        }
+    };
+    if (holders > H) {
+        if ((lane & 63) == 0) atomicAdd(&sh.count, kCandidates + 1);
+    } else {
+        held([&](float z, int e) {
+            if (z >= bar && e < c.live) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < kCandidates) sh.cand[at] = key_of(z, c.off + e);
+            }
+        });
     }
     __syncthreads();
-    const int n = count;
-    if (n >= k && n <= kCandidates) {
-        for (int i = lane; i < n; i += L) {
-            const Key mine = cand[i];
-            int place = 0;
-            for (int o = 0; o < n; ++o) place += cand[o] > mine;
-            if (place < k) {
-                record[place] = mine;
-                const int e = class_of(mine) - c.off;
-                next[place] = atomicExch(&head[Row::owner(e, c.len)], place + 1);
-            }
-        }
-        __syncthreads();
-    } else {
-        // each entry the largest key below the last, over the row in memory: it is seldom needed,
-        // and would take the registers from the other way
-        Key last = ~(Key)0;
-        for (int i = 0; i < k; ++i) {
-            Key top = 0;
-            for (int e = lane; e < c.live; e += L) {
-                const Key o = key_of(load_elem(a.x, FMT, c.base + e), c.off + e);
-                top = o < last && o > top ? o : top;
-            }
-            top = lane_max_key<64>(top);
-            __syncthreads();
-            if ((lane & 63) == 0) best[lane >> 6] = top;
-            __syncthreads();
-            last = best[0];
-            for (int w = 1; w < W; ++w) last = best[w] > last ? best[w] : last;
-            if (lane == 0) {
-                record[i] = last;
-                const int own = Row::owner(class_of(last) - c.off, c.len);
-                next[i] = head[own];
-                head[own] = i + 1;
-            }
-        }
-        __syncthreads();
+    const bool plain = sh.count >= k && sh.count <= kCandidates;
+    Stats st = {m, own_sum, 0.f};
+    if (!plain) {
+        __syncthreads();                                         // before the count is taken back
+        top_slow<FMT, L>(a.x, c, k, k2, &sh, &st);
     }
-    if constexpr (PASS == kFirst) {
-        if (lane < a.k) a.keys[((size_t)r * g.chunks + chunk) * a.k + lane] = lane < k ? record[lane] : 0;
-    } else {
-        if (lane < a.k) put<FMT>(a, px * a.k + lane, record[lane]);
+    const int found = min(sh.count, kCandidates), padded = (found + 7) & ~7;
+    if (lane < padded - found) sh.cand[found + lane] = 0;
+    __syncthreads();
+    for (int i = lane; i < found; i += L) {
+        const Key mine = sh.cand[i];
+        int place = 0;
+        for (int o = 0; o < padded; o += 8)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) place += sh.cand[o + j] > mine;
+        if (place < k) {
+            sh.record[place] = mine;
+            if constexpr (PASS == kWhole) put<FMT>(a, px * a.k + place, mine);
+        }
     }
+    __syncthreads();
+    if constexpr (PASS == kFirst)
+        if (lane < a.k) a.keys[((size_t)r * g.chunks + chunk) * a.k + lane] = lane < k ? sh.record[lane] : 0;
     if (!a.rest) return;
-    for (int h = head[lane]; h; h = next[h - 1]) row.mask(class_of(record[h - 1]) - c.off, c.len);
-    const Stats st = team_stats<L, false>(row.template stats<false>(kLog2e * a.inv_t), waves, kLog2e * a.inv_t);
+    if (plain) {
+        if (holder) st = {-kInf, 0.f, 0.f};
+        const Key last = sh.record[k - 1];
+        auto rest = [&](float z, int e) { return key_of(z, c.off + e) < last || z != z; };   // a NaN did not reach the bar
+        // against the other threads' maximum, unless the record's last score is far above it
+        const float clean = lane_max<64>(st.m);
+        if (clean > -kInf && (score_of(last) - clean) * k2 < 60.f) {
+            float s = 0.f;
+            held([&](float z, int e) { s += e < c.live && rest(z, e) ? exp2_of(z, clean, k2) : 0.f; });
+            st = join<false>(st, {clean, s, 0.f}, k2);
+        } else {
+            held([&](float z, int e) {
+                if (e < c.live && rest(z, e) && z != -kInf) st = join<false>(st, {z, 1.f, 0.f}, k2);
+            });
+        }
+        st = wave_join<false>(st, k2);
+    }
+    st = team_stats<L, false>(st, sh.waves, k2);
     if (lane == 0) {
         if constexpr (PASS == kFirst) a.stats[(size_t)r * g.chunks + chunk] = make_float4(st.m, st.s, 0.f, 0.f);
         else a.rest[px] = rest_of(a, st);

@@ -80,6 +80,53 @@ __device__ __forceinline__ Stats join(const Stats &a, const Stats &b, float k2)
     return r;
 }
 
+// The largest of the elements seen. 16-bit ones are compared two at once as integers: among signed
+// ones a number that is not negative is right; where all are negative, the smallest unsigned one is
+// the largest number.
+template <int FMT>
+struct Largest {
+    typedef short S2 __attribute__((ext_vector_type(2)));
+    typedef unsigned short U2 __attribute__((ext_vector_type(2)));
+    float f = -kInf;
+    S2 up = {(short)0x8000, (short)0x8000};
+    U2 low = {0xFFFF, 0xFFFF};
+
+    __device__ __forceinline__ void see(const Raw<FMT, kVec<FMT>> &r)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (FMT == kF32) {
+                f = fmaxf(f, __uint_as_float(r.w[i]));
+            } else {
+                up = __builtin_elementwise_max(up, __builtin_bit_cast(S2, r.w[i]));
+                low = __builtin_elementwise_min(low, __builtin_bit_cast(U2, r.w[i]));
+            }
+        }
+    }
+
+    // together with one more (a NaN may or may not be passed on)
+    __device__ __forceinline__ float with(float other) const
+    {
+        if constexpr (FMT == kF32) return fmaxf(f, other);
+        const short u = up.x > up.y ? up.x : up.y;
+        const unsigned short l = low.x < low.y ? low.x : low.y;
+        Raw<FMT, 1> r;
+        r.w[0] = u >= 0 ? (uint16_t)u : l;
+        return fmaxf(l == 0xFFFF && u < 0 ? -kInf : get(r, 0), other);
+    }
+};
+
+// The statistics of a wave's lanes joined.
+template <bool SX>
+__device__ __forceinline__ Stats wave_join(const Stats &a, float k2)
+{
+    const float m = lane_max<64>(a.m), all = m == -kInf ? 0.f : m, f = exp2_of(a.m, all, k2);
+    const bool none = a.m == -kInf;                              // its sums are 0, or a NaN
+    Stats r = {m, lane_sum<64>(none ? a.s : a.s * f), 0.f};
+    if constexpr (SX) r.sx = lane_sum<64>(none ? a.sx : f * (a.sx + fmaxf(a.m - all, -1e30f) * a.s));
+    return r;
+}
+
 // A row, or a chunk of it, held by L lanes of a wave (or by a workgroup of L threads) in NV
 // vectors of 16 bytes each and one element of the row's last len % VEC. Vector i of the row
 // is v[i / L] of lane i % L. Elements at `live` and beyond are -inf and are not read.
@@ -158,6 +205,33 @@ struct ScoreRow {
             }
     }
 
+    // The largest score that this lane holds.
+    __device__ __forceinline__ float largest() const
+    {
+        Largest<FMT> l;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (k < used) l.see(v[k]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return l.with(get(t, 0));
+    }
+
+    // This lane's sum of exp2((z - m) k2) against the largest score m that it holds.
+    __device__ __forceinline__ float own_sum(float m, float k2) const
+    {
+        const float ref = m == -kInf ? 0.f : m;
+        float s = exp2_of(get(t, 0), ref, k2);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (k < used)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) s += exp2_of(get(v[k], j), ref, k2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return s;
+    }
+
     // Statistics over the lanes of a wave that hold the row (all of them if L >= 64).
     template <bool SX, typename M>
     __device__ __forceinline__ Stats stats(const void *, size_t, int len, int, float k2, M masked)
@@ -170,15 +244,7 @@ struct ScoreRow {
     __device__ __forceinline__ Stats stats(float k2)
     {
         constexpr int W = L < 64 ? L : 64;
-        float m = get(t, 0);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (k < used)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) m = fmaxf(m, get(v[k], j));
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        m = lane_max<W>(m);
+        const float m = lane_max<W>(largest());
         keep();
         const float ref = m == -kInf ? 0.f : m;
         float s = 0.f, sx = 0.f;
@@ -295,11 +361,10 @@ struct StreamRow {
                         r[k].w[w] = i == k * L + lane() && w == word && e < nvec * VEC
                                         ? (r[k].w[w] & keep) | (kMaskedWord<FMT> & ~keep) : r[k].w[w];
             });
-            float up = m;
+            Largest<FMT> l;
 #pragma unroll
-            for (int k = 0; k < B; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) up = fmaxf(up, get(r[k], j));
+            for (int k = 0; k < B; ++k) l.see(r[k]);
+            const float up = l.with(m);
             const float to = up == -kInf ? 0.f : up, f = exp2_of(m, to, k2);
             if constexpr (SX) sx = f * (sx + fmaxf(m - to, -1e30f) * s);
             s *= f;
@@ -324,11 +389,7 @@ struct StreamRow {
             if (z != z) one = {-kInf, z, z};                     // a NaN is in the sums, not in the maximum
         }
         const Stats mine = join<SX>({m, s, sx}, one, k2);
-        m = lane_max<64>(mine.m);
-        const float all = m == -kInf ? 0.f : m, f = exp2_of(mine.m, all, k2);
-        s = mine.m == -kInf ? mine.s : mine.s * f;
-        sx = mine.m == -kInf ? mine.sx : f * (mine.sx + fmaxf(mine.m - all, -1e30f) * mine.s);
-        return {m, lane_sum<64>(s), SX ? lane_sum<64>(sx) : 0.f};
+        return wave_join<SX>(mine, k2);
     }
 
     // out[base + e] = value(score e), 0 at `live` and beyond; out may be x.
@@ -416,7 +477,7 @@ __device__ __forceinline__ Chunk chunk_of(const ScoreGeom &g, size_t row, int ch
     return c;
 }
 
-// Statistics of a row over its workgroup (L > 64; through lds, read by the first wave only,
+// Statistics of a row over its workgroup (L > 64; through lds, known to the first wave only,
 // after a barrier that every thread passes), or over its lanes.
 template <int L, bool SX>
 __device__ __forceinline__ Stats team_stats(Stats st, Stats *lds, float k2)
@@ -425,24 +486,24 @@ __device__ __forceinline__ Stats team_stats(Stats st, Stats *lds, float k2)
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = st;
         __syncthreads();
         if (threadIdx.x < 64) {
-            st = lds[0];
-#pragma unroll
-            for (int i = 1; i < L / 64; ++i) st = join<SX>(st, lds[i], k2);
+            st = {-kInf, 0.f, 0.f};
+            if (threadIdx.x < L / 64) st = lds[threadIdx.x];
+            st = wave_join<SX>(st, k2);
         }
     }
     return st;
 }
 
-// A chunk's statistics of all chunks of a row, by the first wave.
+// Statistics of a row from those of its chunks, by a whole wave.
 template <bool SX>
 __device__ __forceinline__ Stats row_stats(const float4 *part, int chunks, float k2)
 {
     Stats st = {-kInf, 0.f, 0.f};
-    for (int i = 0; i < chunks; ++i) {
+    for (int i = threadIdx.x & 63; i < chunks; i += 64) {
         const float4 p = part[i];
         st = join<SX>(st, {p.x, p.y, p.z}, k2);
     }
-    return st;
+    return wave_join<SX>(st, k2);
 }
 
 // A launch of any number of workgroups below 2^32, and a workgroup's own number.

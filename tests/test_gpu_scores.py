@@ -132,6 +132,39 @@ def test_top_scores_of_many_long_rows(B, dtype, classes, k):
         assert torch.equal(got, got[:, :, :8].repeat(1, 1, 17, *[1] * (got.dim() - 3)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_top_scores_of_awkward_rows(B, dtype):
+    """Rows that few scores stand out of, or that lie badly over the lanes: runs of equal scores at and
+    across the record's end, all masked but a few, largest scores side by side, in one lane's
+    vectors, in the last elements; NaN, for which classes are distinct and in range."""
+    r = np.random.default_rng(4)
+    for classes, k in ((520, 64), (1100, 9), (4099, 64), (8200, 64), (17000, 33), (33003, 64), (50001, 64)):
+        rows = r.normal(0, 2, (1, 1, 12, classes))
+        rows[0, 0, 1] = -3.0
+        rows[0, 0, 2, ::2] = 9.0                                   # half of it equal and largest
+        rows[0, 0, 3] = -np.inf
+        rows[0, 0, 3, classes - 3:] = 1.0
+        rows[0, 0, 4] = -np.inf
+        rows[0, 0, 4, 5] = -7.0
+        rows[0, 0, 5, 100:100 + k] += 20.0                         # side by side
+        rows[0, 0, 6, -k:] += 20.0                                 # at the end
+        rows[0, 0, 7, 7::2048] += 20.0                             # in few lanes
+        rows[0, 0, 8] = np.round(rows[0, 0, 8])                    # few values
+        rows[0, 0, 9] = -np.abs(rows[0, 0, 9]) - 1e-3              # all negative
+        rows[0, 0, 10] = r.integers(0, 2, classes) * -0.0          # zeros of both signs
+        rows[0, 0, 10][r.random(classes) < 0.5] = 0.0
+        rows[0, 0, 11, 3:] = 0.0
+        print(dtype, classes, k, flush=True)
+        x, *got = run_top(B, rows, dtype, classes, k, 1.0, off=1)
+        check_top(x, got, classes, k, 1.0)
+        for share in (0.01, 0.9, 1.0):
+            z = rows[:, :, :2].copy()
+            z[r.random(z.shape) < share] = np.nan
+            x, top, index, rest = run_top(B, z, dtype, classes, k, 1.0)
+            for row in host(index).reshape(2, k):
+                assert len(set(row.tolist())) == k and row.min() >= 0 and row.max() < classes
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("c,classes,k", [(64, 19, 4), (24, 24, 3), (30000, 30000, 20)])
 def test_top_scores_on_active_blocks(B, dtype, c, classes, k):
