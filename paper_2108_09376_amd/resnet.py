@@ -264,6 +264,20 @@ class PolicyNet:
         bc.bc_policy_probabilities(self.buffers[-1], self.prob, stream)
         return self.prob
 
+    def log_probs(self, mask, entropy=None, stream=None):
+        """log pi(a_b) of the decisions `mask` (uint8 [1, gh, gw]) at the last forward pass, float32
+        [1, gh, gw] (a new tensor): the old or the reference policy's, for backward. Their
+        entropies go to `entropy` if given."""
+        out = self._like_prob(stream)
+        bc.bc_action_log_probs(self.buffers[-1], 1, mask, out, entropy, stream=stream)
+        return out
+
+    def _like_prob(self, stream):
+        if stream is None:
+            return torch.empty_like(self.prob)
+        with torch.cuda.stream(bc.torch_stream(stream, self.device)):      # memory of the call's stream
+            return torch.empty_like(self.prob)
+
     # ------------------------------------------------------------------ online update
     def _init_training(self):
         """fp32 master weights ([cout][k][k][cin], the layout the convolutions read), the
@@ -281,6 +295,8 @@ class PolicyNet:
             self.db.append(torch.zeros_like(b))
         self.gbufs = [[torch.empty((1, oh, ow, c), dtype=dt, device=dev) for _ in range(2)]
                       for (oh, ow, c) in self.shapes]
+        self.loss, self.kl = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
+        self.loss_work = torch.empty(bc.bc_clipped_policy_loss_work(self.buffers[-1], 1), dtype=torch.uint8, device=dev)
         self.v_g = [torch.zeros_like(g) for g in self.gains]
         self.dg = [torch.zeros_like(g) for g in self.gains]
         if self.norm:
@@ -291,17 +307,25 @@ class PolicyNet:
     def _matrices(self):
         return [(self.master[i], self.v_w[i], self.dw[i], self.weights[i]) for i in self.normed]
 
-    def backward(self, reward, mask, prob, stream=None):
+    def backward(self, reward, mask, prob, stream=None, old_logp=None, ref_logp=None, clip=(0.2, 0.2, 0.0)):
         """Adds the gradients of L = -sum_b R_b log pi(a_b) at the last forward pass to
         self.dw / self.db (and the norms' gains' to self.dg). reward, prob float32
-        [1, gh, gw]; mask uint8 (the executed grid a_b)."""
+        [1, gh, gw]; mask uint8 (the executed grid a_b). With old_logp (log_probs before the first
+        update on these decisions) L is the clipped policy loss of bc_clipped_policy_loss, of
+        clip = (low, high, beta) and, if given, the reference's ref_logp: sound for several
+        updates on one frame's decisions, which REINFORCE is not. prob is not read then; the loss
+        and the divergence to the reference are left in self.loss and self.kl (float32 [1])."""
         if not hasattr(self, "master"):
             self._init_training()
             if stream is not None:                    # the state was filled on torch's current stream
                 bc.torch_stream(stream, self.device).wait_stream(torch.cuda.current_stream(self.device))
         last = len(self.layers) - 1
         cur = {last: self.gbufs[last][0]}
-        bc.bc_policy_logit_grad(reward, mask, prob, cur[last], stream)
+        if old_logp is None:
+            bc.bc_policy_logit_grad(reward, mask, prob, cur[last], stream)
+        else:
+            bc.bc_clipped_policy_loss(self.buffers[last], 1, mask, reward, old_logp, ref_logp, None, clip, 1.0, cur[last],
+                                      self.loss, None if ref_logp is None else self.kl, work=self.loss_work, stream=stream)
         for li in range(last, -1, -1):
             l = self.layers[li]
             gp = cur.pop(li)                          # complete: every consumer came later
@@ -345,10 +369,10 @@ class PolicyNet:
             bc.bc_muon_step_many(self._matrices(), matrix_lr, momentum, weight_decay, work=self.work, stream=stream)
         bc.bc_rmsprop_step_many(params, lr, alpha, eps, weight_decay, stream)
 
-    def train_step(self, reward, mask, prob, stream=None, **hyper):
+    def train_step(self, reward, mask, prob, stream=None, old_logp=None, ref_logp=None, clip=(0.2, 0.2, 0.0), **hyper):
         """The online update of Section 4: backward pass at the last forward pass, then one
-        step of update(**hyper)."""
-        self.backward(reward, mask, prob, stream)
+        step of update(**hyper). old_logp, ref_logp and clip as for backward."""
+        self.backward(reward, mask, prob, stream, old_logp, ref_logp, clip)
         self.update(stream=stream, **hyper)
 
 
@@ -538,3 +562,44 @@ class SparseSwiftNet(SparseResNet):
     @property
     def logits(self):
         return self.buffers[-1]
+
+    # ------------------------------------------------------------------ learning from a teacher
+    def new_record(self, k: int):
+        """Tensors for a record of the k largest class scores of every pixel of the output: (top,
+        index, rest), see bc_top_scores."""
+        shape = self.logits.shape[:3]
+        return (torch.zeros((*shape, k), dtype=self.dtype, device=self.device),
+                torch.zeros((*shape, k), dtype=torch.int32, device=self.device),
+                torch.zeros(shape, dtype=torch.float32, device=self.device))
+
+    def record(self, rec, temperature: float = 1.0, index=None, stream=None):
+        """This network's scores into `rec` (new_record): of every block, or with the device (idx,
+        count) pair `index` of the executed blocks, the others keeping theirs."""
+        idx, cnt = index if index is not None else (None, None)
+        bc.bc_top_scores(self.logits, self.classes, temperature, *rec, self.grid, idx, cnt, stream=stream)
+
+    def _init_head(self):
+        """fp32 weights of the last layer, the updates' state, gradients and the workspace."""
+        m = self.weights[-1].float().contiguous()
+        z = torch.zeros_like
+        self.head = dict(w=m, v_w=z(m), dw=z(m), v_b=z(self.biases[-1]), db=z(self.biases[-1]), grad=torch.empty_like(self.logits),
+                         loss=torch.zeros(1, dtype=torch.float32, device=self.device))
+        need = bc.bc_distill_loss_work(self.logits, self.classes, 64)    # of the longest record
+        self.head["work"] = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def distill_step(self, rec, temperature: float = 1.0, weight=None, lr=1e-4, alpha=0.99, eps=1e-8, weight_decay=0.0,
+                     stream=None):
+        """One RMSprop step of the last layer (dec.logits) towards a teacher's record at the last
+        frame: the mean divergence over the pixels (bc_distill_loss; times `weight`, float32
+        [1, h/4, w/4], if given), whose value is left in self.head["loss"]."""
+        if not hasattr(self, "head"):
+            self._init_head()
+            if stream is not None:                    # the state was filled on torch's current stream
+                bc.torch_stream(stream, self.device).wait_stream(torch.cuda.current_stream(self.device))
+        hd, l = self.head, self.layers[-1]
+        n, h, w, _ = self.logits.shape
+        bc.bc_distill_loss(self.logits, self.classes, *rec, temperature, weight, 1.0 / (n * h * w), hd["grad"], hd["loss"],
+                           work=hd["work"], stream=stream)
+        bc.bc_conv2d_weight_grad((l.k, l.k, l.stride, l.pad, 0), self.buffers[l.src], hd["grad"], hd["dw"], hd["db"], stream)
+        bc.bc_rmsprop_step_many([(hd["w"], hd["v_w"], hd["dw"], self.weights[-1]), (self.biases[-1], hd["v_b"], hd["db"], None)],
+                                lr, alpha, eps, weight_decay, stream)
