@@ -652,7 +652,8 @@ def bc_muon_step_many(params, lr, momentum, weight_decay, nesterov=True, steps=N
 
 
 def _score_map(t, stream):
-    """(n, h, w, c), device and descriptor of a score map on the current device (and the stream's)."""
+    """Number of images and pixels, device and descriptor of a score map on the current device (and
+    the stream's)."""
     d = _desc(t, BC_NHWC)
     dev = t.get_device()                                 # -1: not on a GPU
     if _raw_stream is None and dev >= 0:
@@ -661,13 +662,15 @@ def _score_map(t, stream):
         raise ValueError("the score map is not on the current device")
     if stream is not None and getattr(stream, "device_index", dev) != dev:
         raise ValueError("the stream is of another device than the score map")
-    return t.shape, dev, d
+    n, h, w, _ = t.shape
+    return n, n * h * w, dev, d
 
 
-def _value(t, shape, dtype, dev, name):
-    """A contiguous tensor of that shape and type on the map's device (or None)."""
-    if t is not None and not (t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous {dtype}, {tuple(shape)}, on the map's device")
+def _value(t, count, dtype, dev, name):
+    """A contiguous tensor of so many values of that type on the map's device (or None). (Comparing
+    shapes takes as long as all of these.)"""
+    if t is not None and not (t.numel() == count and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be {count} contiguous values of {dtype} on the map's device")
 
 
 _F32 = _I32 = _U8 = None
@@ -705,14 +708,14 @@ def bc_top_scores(scores, classes, temperature, top, index, rest, grid, idx, cou
     active blocks: top [n, h, w, k] (scores' dtype, descending, the lower class first among
     equals), index int32 [n, h, w, k], and rest float32 [n, h, w] (or None), log-sum-exp of
     the others divided by the temperature. work as for bc_layer_norm_grad."""
-    shape, dev, d = _score_map(scores, stream)
+    images, pixels, dev, d = _score_map(scores, stream)
     _F32 is None and _types()
-    pixels, k = shape[:3], top.shape[-1]
-    _value(top, pixels + (k,), scores.dtype, dev, "top")
-    _value(index, pixels + (k,), _I32, dev, "index")
+    k = top.shape[-1]
+    _value(top, pixels * k, scores.dtype, dev, "top")
+    _value(index, pixels * k, _I32, dev, "index")
     _value(rest, pixels, _F32, dev, "rest")
     for t in (idx, count):
-        t is not None and _value(t, t.shape, _I32, dev, "the index")
+        t is not None and _value(t, t.numel(), _I32, dev, "the index")
     cap = 0 if idx is None else int(idx.numel())
     work, wp, nbytes = _score_work(work, lambda: bc_top_scores_work(scores, classes, k), scores, stream)
     st = _lib.bc_top_scores(_ptr(scores), d, int(classes), int(k), float(temperature), _ptr(top), _ptr(index),
@@ -733,15 +736,15 @@ def bc_distill_loss(scores, classes, top, index, rest, temperature, weight, scal
     in any dtype, index int32, rest float32 or None), and grad [n, h, w, c], its gradient (either
     may be None; grad may be scores). weight float32 [n, h, w] or None. work as for
     bc_layer_norm_grad."""
-    shape, dev, d = _score_map(scores, stream)
+    images, pixels, dev, d = _score_map(scores, stream)
     _F32 is None and _types()
-    pixels, k = shape[:3], top.shape[-1]
-    _value(top, pixels + (k,), top.dtype, dev, "top")
-    _value(index, pixels + (k,), _I32, dev, "index")
+    k = top.shape[-1]
+    _value(top, pixels * k, top.dtype, dev, "top")
+    _value(index, pixels * k, _I32, dev, "index")
     _value(rest, pixels, _F32, dev, "rest")
     _value(weight, pixels, _F32, dev, "weight")
-    _value(grad, shape, scores.dtype, dev, "grad")
-    _value(loss, shape[:1], _F32, dev, "loss")
+    _value(grad, scores.numel(), scores.dtype, dev, "grad")
+    _value(loss, images, _F32, dev, "loss")
     work, wp, nbytes = _score_work(work, lambda: bc_distill_loss_work(scores, classes, k), scores, stream)
     st = _lib.bc_distill_loss(_ptr(scores), d, int(classes), _ptr(top), _dtype_code(top), _ptr(index), int(k),
                               _ptr(rest), float(temperature), _ptr(weight), float(scale), _ptr(grad), _ptr(loss),
@@ -761,9 +764,8 @@ def bc_action_log_probs(scores, classes, action, logp, entropy=None, work=None, 
     """logp [n, h, w] float32 = log pi(action) (and entropy [n, h, w], if given) of scores
     [n, h, w, c]: classes of a softmax (action int32), or with classes = 1 execute-or-not
     decisions of a sigmoid (action uint8, the grid). work as for bc_layer_norm_grad."""
-    shape, dev, d = _score_map(scores, stream)
+    images, pixels, dev, d = _score_map(scores, stream)
     _F32 is None and _types()
-    pixels = shape[:3]
     _value(action, pixels, _U8 if classes == 1 else _I32, dev, "action")
     _value(logp, pixels, _F32, dev, "logp")
     _value(entropy, pixels, _F32, dev, "entropy")
@@ -793,15 +795,14 @@ def bc_clipped_policy_loss(scores, classes, action, advantage, old_logp, ref_log
     or loss may be None). advantage, old_logp, ref_logp (or None), weight (or None) float32
     [n, h, w]; kl [n] (or None) the divergence to the reference; scores, classes, action as for
     bc_action_log_probs. work as for bc_layer_norm_grad."""
-    shape, dev, d = _score_map(scores, stream)
+    images, pixels, dev, d = _score_map(scores, stream)
     _F32 is None and _types()
-    pixels, images = shape[:3], shape[:1]
     _value(action, pixels, _U8 if classes == 1 else _I32, dev, "action")
     _value(advantage, pixels, _F32, dev, "advantage")
     _value(old_logp, pixels, _F32, dev, "old_logp")
     _value(ref_logp, pixels, _F32, dev, "ref_logp")
     _value(weight, pixels, _F32, dev, "weight")
-    _value(grad, shape, scores.dtype, dev, "grad")
+    _value(grad, scores.numel(), scores.dtype, dev, "grad")
     _value(loss, images, _F32, dev, "loss")
     _value(kl, images, _F32, dev, "kl")
     work, wp, nbytes = _score_work(work, lambda: bc_clipped_policy_loss_work(scores, classes), scores, stream)

@@ -68,7 +68,7 @@ __device__ __forceinline__ double2 team_sum(double x, double y)
     return s;
 }
 
-__device__ __forceinline__ bool wanted(const LossOut &o) { return o.loss || o.kl; }
+__host__ __device__ __forceinline__ bool wanted(const LossOut &o) { return o.loss || o.kl; }
 
 // A workgroup's loss to its place, or to the image's where it has one to itself.
 __device__ __forceinline__ void write_sums(const LossOut &o, const ScoreGeom &g, uint32_t item, double loss, double kl)
@@ -501,19 +501,19 @@ __global__ __launch_bounds__(256) void k_distill_quad(DistillArgs a, ScoreGeom g
 // Log probability of an action with score za above -inf, and 1 - its probability, from the
 // statistics of the other classes.
 struct Chosen {
-    double l, other;
+    double l, other, pi;
 };
 
 __device__ __forceinline__ Chosen chosen(float za, const Stats &st)
 {
-    if (st.s == 0.f) return {0.0, 0.0};
+    if (st.s == 0.f) return {0.0, 0.0, 1.0};
     const double d = (double)st.m - (double)za;
     if (d > 0.0) {                                               // exp(-d) below s: past exp's range too
         const double t = exp(-d), s = (double)st.s + t;
-        return {-d - log(s), (double)st.s / s};
+        return {-d - log(s), (double)st.s / s, t / s};
     }
     const double x = (double)st.s * exp(d);
-    return {-log1p(x), x / (1.0 + x)};
+    return {-log1p(x), x / (1.0 + x), 1.0 / (1.0 + x)};
 }
 
 // The clipped loss of one decision with log probability l, and its derivative by l.
@@ -521,30 +521,62 @@ struct Decision {
     double loss, kl, slope;
 };
 
-// What a decision is judged by: requested before the row's scores are waited for.
+// What a decision is judged by: requested, and its exponentials taken, before the row's scores are
+// waited for. r = exp(l - old) = pi exp(-old), exp(ref - l) = exp(ref) / pi.
 struct Given {
-    float advantage, old_logp, ref_logp;
+    double advantage, old_logp, ref_logp, inv_old, ref;
+    bool far;                                  // past exp's range: taken from l itself
 };
 
 __device__ __forceinline__ Given given(const ClipArgs &a, size_t row)
 {
-    return {a.advantage[row], a.old_logp[row], a.ref_logp ? a.ref_logp[row] : 0.f};
+    const double adv = a.advantage[row], old = a.old_logp[row], ref = a.ref_logp ? a.ref_logp[row] : 0.f;
+    Given v = {adv, old, ref, exp(-old), 0.0, !(fabs(old) < 600.0 && fabs(ref) < 600.0)};
+    if (a.ref_logp) v.ref = exp(ref);
+    return v;
 }
 
-__device__ __forceinline__ Decision decide(const ClipArgs &a, const Given &v, double l)
+__device__ __forceinline__ Decision decide(const ClipArgs &a, const Given &v, const Chosen &c)
 {
-    const double adv = v.advantage, r = exp(l - (double)v.old_logp);
+    const bool direct = v.far || !(c.l > -600.0);
+    const double r = direct ? exp(c.l - v.old_logp) : v.inv_old * c.pi;
     const double lo = 1.0 - (double)a.low, hi = 1.0 + (double)a.high;
-    const double kept = r * adv, held = (r < lo ? lo : r > hi ? hi : r) * adv;
+    const double kept = r * v.advantage, held = (r < lo ? lo : r > hi ? hi : r) * v.advantage;
     const bool open = !(kept > held);                            // a NaN stays one
     Decision d = {-(open ? kept : held), 0.0, open ? -kept : 0.0};
     if (a.ref_logp) {
-        const double x = (double)v.ref_logp - l, up = expm1(x);
-        d.kl = up - x;
+        const double x = v.ref_logp - c.l, up = direct ? expm1(x) : v.ref / c.pi - 1.0;
+        // next to 0 the difference is a rounding's: x^2 / 2 + x^3 / 6 there
+        d.kl = fabs(x) < 1e-4 ? x * x * (0.5 + x * (1.0 / 6.0)) : up - x;
         d.loss += (double)a.beta * d.kl;
-        d.slope -= (double)a.beta * up;
+        d.slope -= (double)a.beta * (fabs(x) < 1e-4 ? x + d.kl : up);
     }
     return d;
+}
+
+// The losses of rows in chunks, an image to a workgroup, from what the first pass has left: runs beside the
+// second pass, as more workgroups of its launch.
+template <int L>
+__device__ __forceinline__ void clip_sums(const ClipArgs &a, const ScoreGeom &g, uint32_t image)
+{
+    double loss = 0.0, kl = 0.0;
+    for (uint32_t p = threadIdx.x >> 6; p < g.hw; p += L / 64) {
+        const size_t r = (size_t)image * g.hw + p;
+        const float wt = a.weight ? a.weight[r] : 1.f;
+        if (wt == 0.f || (unsigned)((const int32_t *)a.action)[r] >= (unsigned)g.classes) continue;
+        const float za = a.pick[r];
+        const Given v = given(a, r);
+        const Stats st = row_stats<false>(a.stats + r * g.chunks, g.chunks, kLog2e);
+        if ((threadIdx.x & 63) != 0 || za == -kInf) continue;
+        const Decision d = decide(a, v, chosen(za, st));
+        const double by = (double)wt * (double)a.scale;
+        loss += by * d.loss;
+        kl += by * d.kl;
+    }
+    const double2 sum = team_sum<L, true>(loss, kl);
+    if (threadIdx.x != 0) return;
+    if (a.out.loss) a.out.loss[image] = (float)sum.x;
+    if (a.out.kl) a.out.kl[image] = (float)sum.y;
 }
 
 template <int FMT, int L, int NV, int PASS>
@@ -554,20 +586,27 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
     constexpr int T = kThreadsOf<L>, G = kGroupsOf<L>;
     __shared__ Stats waves[L > 64 ? L / 64 : 1];
     __shared__ float pub[3];
-    if (past_end<PASS>(g)) return;
+    if (past_end<PASS>(g)) {
+        const uint32_t image = item_of() - g.images * g.per * (uint32_t)g.chunks;
+        if (PASS == kSecond && image < g.images) clip_sums<T>(a, g, image);
+        return;
+    }
     const Place w = place_of<G, PASS>(g);
     const int group = L <= 64 ? threadIdx.x / L : 0;
     const bool inside = w.p + group < g.hw;
     const Chunk c = chunk_of<PASS>(g, inside ? w.row + group : w.row, w.chunk);
     const float wt = !inside ? 0.f : a.weight ? a.weight[c.row] : 1.f;
+    Row row;
+    // a row that counts is requested before its action is known
+    if constexpr (NV)
+        if (wt != 0.f) row.load(a.x, c.base, c.len, c.live);
     const int act = ((const int32_t *)a.action)[c.row];
-    const Given v = given(a, c.row);
     double loss = 0.0, kl = 0.0;
+    Given v = {};
+    if (PASS != kFirst && (L <= 64 || threadIdx.x < 64)) v = given(a, c.row);
     if (wt == 0.f || (unsigned)act >= (unsigned)g.classes) {
         if (inside && PASS != kFirst && a.grad) Row::store_zeros(a.grad, c.base, c.len);
     } else {
-        Row row;
-        if constexpr (NV) row.load(a.x, c.base, c.len, c.live);
         const int at = act - c.off;                              // the action's place in the chunk
         const bool here = at >= 0 && at < c.len, mine = here && Row::owner(at, c.len) == Row::lane();
         float za = -kInf;
@@ -591,7 +630,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
                 if constexpr (PASS == kSecond) st = row_stats<false>(a.stats + c.row * g.chunks, g.chunks, kLog2e);
                 if (za != -kInf) {                               // a masked class was not chosen here
                     const Chosen ch = chosen(za, st);
-                    const Decision d = decide(a, v, ch.l);
+                    const Decision d = decide(a, v, ch);
                     const double by = (double)wt * (double)a.scale;
                     if (Row::lane() == 0) {
                         loss = by * d.loss;
@@ -624,7 +663,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
             }
         }
     }
-    if (PASS == kFirst || !wanted(a.out) || w.chunk != 0) return;
+    if (PASS != kWhole || !wanted(a.out)) return;
     if constexpr (L > 64) {
         write_sums(a.out, g, w.item, loss, kl);
     } else {
@@ -635,14 +674,10 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
 
 // A pixel of few classes to a thread; with one class, decisions to execute its block or not:
 // pi(1) = sigmoid(z).
-struct Binary {
-    double l, other;                           // log pi(action), 1 - pi(action)
-};
-
-__device__ __forceinline__ Binary binary(float z, bool executed)
+__device__ __forceinline__ Chosen binary(float z, bool executed)
 {
-    const double x = executed ? (double)z : -(double)z, t = exp(-fabs(x));
-    return {(x < 0.0 ? x : 0.0) - log1p(t), (x < 0.0 ? 1.0 : t) / (1.0 + t)};
+    const double x = executed ? (double)z : -(double)z, t = exp(-fabs(x)), inv = 1.0 / (1.0 + t);
+    return {(x < 0.0 ? x : 0.0) - log1p(t), (x < 0.0 ? 1.0 : t) * inv, (x < 0.0 ? t : 1.0) * inv};
 }
 
 template <int FMT, int N>
@@ -663,9 +698,9 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
     for (int j = 0; j < N; ++j) mine[j] = 0.f;
     if constexpr (N == 1) {
         const bool executed = ((const uint8_t *)a.action)[r] != 0;
-        const Binary b = binary(load_elem(a.x, FMT, r * (size_t)g.c), executed);
+        const Chosen b = binary(load_elem(a.x, FMT, r * (size_t)g.c), executed);
         if (wt != 0.f && b.l != -(double)kInf) {
-            const Decision d = decide(a, v, b.l);
+            const Decision d = decide(a, v, b);
             loss = by * d.loss;
             kl = by * d.kl;
             mine[0] = (float)(by * d.slope * (executed ? b.other : -b.other));
@@ -690,7 +725,7 @@ __global__ __launch_bounds__(256) void k_clip_pixel(ClipArgs a, ScoreGeom g)
             }
             if (za != -kInf) {
                 const Chosen ch = chosen(za, {m, s, 0.f});
-                const Decision d = decide(a, v, ch.l);
+                const Decision d = decide(a, v, ch);
                 loss = by * d.loss;
                 kl = by * d.kl;
                 const float F = s == 0.f ? 0.f : (float)(-by * d.slope * ch.other / (double)s);
@@ -767,11 +802,11 @@ __global__ __launch_bounds__(256) void k_logp_pixel(LogpArgs a, ScoreGeom g)
     if (r >= (size_t)g.images * g.hw) return;
     if constexpr (N == 1) {
         const float z = load_elem(a.x, FMT, r * (size_t)g.c);
-        const Binary b = binary(z, ((const uint8_t *)a.action)[r] != 0);
+        const Chosen b = binary(z, ((const uint8_t *)a.action)[r] != 0);
         a.logp[r] = (float)b.l;
         if (a.entropy) {
             // both outcomes: the likelier one's log plus what the other's adds
-            const Binary up = binary(fabsf(z), true);
+            const Chosen up = binary(fabsf(z), true);
             const double far = up.other * fabs((double)z);
             a.entropy[r] = (float)(-up.l + (z - z == 0.f ? far : 0.0) + (z != z ? (double)z : 0.0));
         }
@@ -840,17 +875,21 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, i
     while (p.form && p.form < kFormCount && kForms[p.form].lanes * kForms[p.form].nv < nvec) ++p.form;
     g.chunks = 1;
     g.chunk = g.len;
-    const int least = kForms[kChunkForm].lanes * kForms[kChunkForm].nv * vec;
     if ((p.form == kFormCount && !stream) || (p.form > kChunkForm && rows < 128)) {
+        // chunks of 8 vectors per thread, or, where these are few (and joined from their sums), of 2
         p.form = kChunkForm;
-        g.chunk = least;
-        g.chunks = (int)(((int64_t)g.len + least - 1) / least);
+        auto cut = [&](int nv) {
+            g.chunk = kForms[kChunkForm].lanes * nv * vec;
+            g.chunks = (int)(((int64_t)g.len + g.chunk - 1) / g.chunk);
+        };
+        cut(kForms[kChunkForm].nv);
+        if (stream && rows * g.chunks < 256) {
+            p.form = kSmallChunk;
+            cut(2);
+        }
     }
     p.split = g.chunks > 1;
-#ifdef TRY_FORM
-    if (getenv("BC_FORM") && !p.split && p.form >= 5) p.form = atoi(getenv("BC_FORM"));
-#endif
-    const int lanes = kForms[p.form].lanes;
+    const int lanes = p.split ? kForms[kChunkForm].lanes : kForms[p.form].lanes;
     const uint32_t groups = p.form == 0 ? pixels : lanes <= 64 ? 256 / lanes : 1;
     g.per = (g.hw - 1) / groups + 1;
     g.by_per = Divisor(g.per);
@@ -881,10 +920,12 @@ hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *
     hipError_t e = with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if (p.split) {
-            constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            hipLaunchKernelGGL((k_distill<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
-            hipLaunchKernelGGL((k_distill<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
-            return hipGetLastError();
+            return with_chunk(p.form, [&](auto l, auto n) {
+                constexpr int L = decltype(l)::value, NV = decltype(n)::value;
+                hipLaunchKernelGGL((k_distill<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
+                hipLaunchKernelGGL((k_distill<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
+                return hipGetLastError();
+            });
         }
         if (p.form == 0) {
             if (a.k <= 4) hipLaunchKernelGGL((k_distill_quad<FMT, 1>), grid, dim3(256), 0, s, a, g);
@@ -911,10 +952,13 @@ hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
     hipError_t e = with_format(fmt, [&](auto f) {
         constexpr int FMT = decltype(f)::value;
         if (p.split) {
-            constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-            hipLaunchKernelGGL((k_clip<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
-            hipLaunchKernelGGL((k_clip<FMT, L, NV, kSecond>), grid, dim3(L), 0, s, a, g);
-            return hipGetLastError();
+            return with_chunk(p.form, [&](auto l, auto n) {
+                constexpr int L = decltype(l)::value, NV = decltype(n)::value;
+                hipLaunchKernelGGL((k_clip<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
+                const dim3 sums = grid_of((size_t)g.images * g.per * g.chunks + (wanted(a.out) ? g.images : 0));
+                hipLaunchKernelGGL((k_clip<FMT, L, NV, kSecond>), sums, dim3(L), 0, s, a, g);
+                return hipGetLastError();
+            });
         }
         if (g.classes == 1) {
             hipLaunchKernelGGL((k_clip_pixel<FMT, 1>), grid, dim3(256), 0, s, a, g);
@@ -931,7 +975,7 @@ hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
             return hipGetLastError();
         });
     });
-    return e != hipSuccess ? e : launch_sum(g, a.out, s);
+    return e != hipSuccess || p.split ? e : launch_sum(g, a.out, s);
 }
 
 hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, int fmt, hipStream_t s)
@@ -955,10 +999,12 @@ hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
         auto rows_of = [&](auto sx) {
             constexpr bool SX = decltype(sx)::value;
             if (p.split) {
-                constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
-                hipLaunchKernelGGL((k_logp<FMT, L, NV, kFirst, SX>), grid, dim3(L), 0, s, a, g);
-                hipLaunchKernelGGL(k_logp_join, grid_of(rows), dim3(64), 0, s, a, g);
-                return hipGetLastError();
+                return with_chunk(p.form, [&](auto l, auto n) {
+                    constexpr int L = decltype(l)::value, NV = decltype(n)::value;
+                    hipLaunchKernelGGL((k_logp<FMT, L, NV, kFirst, SX>), grid, dim3(L), 0, s, a, g);
+                    hipLaunchKernelGGL(k_logp_join, grid_of(rows), dim3(64), 0, s, a, g);
+                    return hipGetLastError();
+                });
             }
             return with_form(p.form, [&](auto l, auto n) {
                 constexpr int L = decltype(l)::value, NV = decltype(n)::value;

@@ -446,7 +446,7 @@ struct Form {
     int lanes, nv;
 };
 constexpr Form kForms[] = {{1, 0}, {8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 0}};
-constexpr int kFormCount = 8, kChunkForm = 5;                      // the last of any length
+constexpr int kFormCount = 8, kChunkForm = 5, kSmallChunk = -1;                      // the last of any length
 
 template <int L> constexpr int kThreadsOf = L <= 64 ? 256 : L;
 template <int L> constexpr int kGroupsOf = L <= 64 ? 256 / L : 1;  // rows of a workgroup
@@ -530,6 +530,15 @@ hipError_t with_form(int form, F &&f)
     case 7: return f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
     default: return f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
     }
+}
+
+// f(lanes, vectors) of a chunk.
+template <typename F>
+hipError_t with_chunk(int form, F &&f)
+{
+    constexpr std::integral_constant<int, kForms[kChunkForm].lanes> lanes{};
+    if (form == kSmallChunk) return f(lanes, std::integral_constant<int, 2>{});
+    return f(lanes, std::integral_constant<int, kForms[kChunkForm].nv>{});
 }
 
 // f(classes of a pixel in registers, as an integral constant).

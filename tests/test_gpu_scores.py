@@ -552,7 +552,7 @@ def test_refusals_of_the_binding(B):
     bad(B.bc_action_log_probs, x, 30, st["act"].long(), st["old"])
     bad(B.bc_action_log_probs, x, 1, st["act"], st["old"])
     bad(B.bc_action_log_probs, x, 30, st["act"][:1], st["old"])
-    bad(B.bc_action_log_probs, x.transpose(1, 2), 30, st["act"], st["old"])
+    bad(B.bc_action_log_probs, x.transpose(0, 2), 30, st["act"], st["old"])
     bad(B.bc_action_log_probs, x, 30, st["act"], st["old"].cpu())
     bad(B.bc_distill_loss, x, 30, st["top"], st["index"].long(), None, 1.0, None, 1.0, st["g1"], st["l1"])
     bad(B.bc_distill_loss, x, 30, st["top"], st["index"], None, 1.0, None, 1.0, st["g1"].half(), st["l1"])
