@@ -698,7 +698,8 @@ bc_status bc_muon_step_many(const bc_matrix *params, int32_t n, const bc_muon *m
  * are a pixel's class scores (the rest is never looked at); a batch of rows is a map with
  * h = 1. Each loss comes with the gradient of its scores. Arithmetic is fp32 or wider, each
  * result rounded once; sums over pixels are taken in a fixed order, so equal calls give equal
- * bits. A NaN score stays within its pixel (and its image's sums). Rules for all:
+ * bits. A NaN score stays within its pixel (and its image's sums). At most 2^30 channels
+ * (BC_ERR_UNSUPPORTED). Rules for all:
  *  - a pixel of weight 0 takes no part: loss 0, gradient 0, whatever else it holds;
  *  - a score of -inf is a class that is masked out: its probability is 0;
  *  - d_work: the caller's workspace of at least the bytes of the call's _work function,
@@ -713,7 +714,8 @@ bc_status bc_top_scores_work(bc_tensor scores, int32_t classes, int32_t k, int64
  * A teacher's record: the k largest class scores of each pixel, for the active blocks
  * (every other block keeps its record: feature transfer, as of any layer's output).
  *   d_top    [n][h][w][k] in scores.dtype, descending; of equal scores the lower class first
- *            (-0 equals 0). The order of NaN scores is not specified.
+ *            (-0 equals 0, and may be given as 0). Which record a pixel with a NaN score gets is
+ *            not specified, but that its classes are distinct and in range.
  *   d_index  int32 [n][h][w][k]: their classes, distinct.
  *   d_rest   float32 [n][h][w] or NULL: log of the sum of exp(score / temperature) over all
  *            other classes (-inf if there are none, or all are masked out).
@@ -722,7 +724,7 @@ bc_status bc_top_scores_work(bc_tensor scores, int32_t classes, int32_t k, int64
  * bc_sparse_conv2d (d_idx = d_count = NULL: every block).
  * Errors: BC_ERR_NULL, BC_ERR_SHAPE (classes, k, temperature), BC_ERR_DTYPE, BC_ERR_LAYOUT
  * (NCHW), BC_ERR_NOT_DIVISIBLE, BC_ERR_CAPACITY (index; workspace), BC_ERR_ALIAS,
- * BC_ERR_UNSUPPORTED (d_work not aligned), BC_ERR_HIP.
+ * BC_ERR_UNSUPPORTED (d_work not aligned; channels), BC_ERR_HIP.
  */
 bc_status bc_top_scores(const void *d_scores, bc_tensor scores, int32_t classes, int32_t k,
                         float temperature, void *d_top, int32_t *d_index, float *d_rest,

@@ -1348,6 +1348,7 @@ static bc_status score_geom(const bc_tensor &t, int32_t classes, bool whole, bc:
     if (st) return st;
     if (t.layout != BC_NHWC) return fail(BC_ERR_LAYOUT, "score maps are channels-last");
     if (classes < 1 || classes > t.c) return fail(BC_ERR_SHAPE, "%d classes of %d channels", classes, t.c);
+    if (t.c > (1 << 30)) return fail(BC_ERR_UNSUPPORTED, "more than 2^30 channels");
     g = bc::ScoreGeom{};
     g.images = (uint32_t)t.n;
     g.hw = (uint32_t)((size_t)t.h * t.w);             // at most 4e9 elements
@@ -1364,17 +1365,17 @@ static bc_status check_score_work(const void *d_work, int64_t work_bytes, size_t
 
 static bc_status check_temperature(float t)
 {
-    if (!(t > 0.f) || !std::isfinite(t) || !std::isfinite(1.f / t))
+    if (!(t > 0.f) || !std::isfinite(t) || !std::isfinite(2.f / t))   // log2(e) / t
         return fail(BC_ERR_SHAPE, "the temperature must be positive, and it and its inverse finite");
     return BC_OK;
 }
 
-// Outputs against inputs and each other; an output may be `same` itself where it is outs[0].
-static bc_status check_outputs(const Extent *outs, int n_outs, const Extent *ins, int n_ins, const void *same)
+// Outputs against inputs and each other; outs[0] may be ins[0] itself with `in_place`.
+static bc_status check_outputs(const Extent *outs, int n_outs, const Extent *ins, int n_ins, bool in_place)
 {
     for (int i = 0; i < n_outs; ++i) {
         for (int j = 0; j < n_ins; ++j)
-            if (!(i == 0 && ins[j].p == same && outs[i].p == same) && overlap(outs[i].p, outs[i].b, ins[j].p, ins[j].b))
+            if (!(in_place && i == 0 && j == 0 && outs[0].p == ins[0].p) && overlap(outs[i].p, outs[i].b, ins[j].p, ins[j].b))
                 return fail(BC_ERR_ALIAS, "an output overlaps an input");
         for (int j = i + 1; j < n_outs; ++j)
             if (overlap(outs[i].p, outs[i].b, outs[j].p, outs[j].b))
@@ -1445,7 +1446,7 @@ bc_status bc_top_scores(const void *d_scores, bc_tensor scores, int32_t classes,
     const Extent ins[3] = {{d_scores, tensor_bytes(scores)}, {d_idx, (size_t)capacity * 4}, {d_count, 4}};
     const Extent outs[4] = {{d_top, px * k * esize_of(scores.dtype)}, {d_index, px * k * 4}, {d_rest, px * 4},
                             {d_work, p.bytes}};
-    if ((st = check_outputs(outs, 4, ins, d_idx ? 3 : 1, nullptr))) return st;
+    if ((st = check_outputs(outs, 4, ins, d_idx ? 3 : 1, false))) return st;
     bc::TopArgs a = {};
     a.x = d_scores;
     a.top = d_top;
@@ -1495,7 +1496,7 @@ bc_status bc_distill_loss(const void *d_scores, bc_tensor scores, int32_t classe
     const Extent ins[5] = {{d_scores, sb}, {d_top, px * k * esize_of(top_dtype)}, {d_index, px * k * 4},
                            {d_rest, px * 4}, {d_weight, px * 4}};
     const Extent outs[3] = {{d_grad, sb}, {d_loss, (size_t)G.images * 4}, {d_work, p.bytes}};
-    if ((st = check_outputs(outs, 3, ins, 5, d_scores))) return st;
+    if ((st = check_outputs(outs, 3, ins, 5, true))) return st;
     bc::DistillArgs a = {};
     a.x = d_scores;
     a.top = d_top;
@@ -1541,7 +1542,7 @@ bc_status bc_action_log_probs(const void *d_scores, bc_tensor scores, int32_t cl
     const size_t px = (size_t)G.images * G.hw;
     const Extent ins[2] = {{d_scores, tensor_bytes(scores)}, {d_action, px * (classes == 1 ? 1 : 4)}};
     const Extent outs[3] = {{d_logp, px * 4}, {d_entropy, px * 4}, {d_work, p.bytes}};
-    if ((st = check_outputs(outs, 3, ins, 2, nullptr))) return st;
+    if ((st = check_outputs(outs, 3, ins, 2, false))) return st;
     bc::LogpArgs a = {};
     a.x = d_scores;
     a.action = d_action;
@@ -1581,7 +1582,7 @@ bc_status bc_clipped_policy_loss(const void *d_scores, bc_tensor scores, int32_t
     const Extent ins[6] = {{d_scores, sb}, {d_action, px * (classes == 1 ? 1 : 4)}, {d_advantage, px * 4},
                            {d_old_logp, px * 4}, {d_ref_logp, px * 4}, {d_weight, px * 4}};
     const Extent outs[4] = {{d_grad, sb}, {d_loss, nb}, {d_kl, nb}, {d_work, p.bytes}};
-    if ((st = check_outputs(outs, 4, ins, 6, d_scores))) return st;
+    if ((st = check_outputs(outs, 4, ins, 6, true))) return st;
     bc::ClipArgs a = {};
     a.x = d_scores;
     a.action = d_action;

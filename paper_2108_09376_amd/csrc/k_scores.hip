@@ -506,7 +506,10 @@ struct Chosen {
 
 __device__ __forceinline__ Chosen chosen(float za, const Stats &st)
 {
-    if (st.s == 0.f) return {0.0, 0.0, 1.0};
+    if (st.s == 0.f) {                                           // the only class; a NaN stays one
+        const double none = (double)za - (double)za;
+        return {none, none, 1.0 + none};
+    }
     const double d = (double)st.m - (double)za;
     if (d > 0.0) {                                               // exp(-d) below s: past exp's range too
         const double t = exp(-d), s = (double)st.s + t;

@@ -465,6 +465,59 @@ def test_nan_stays_in_its_pixel(B):
                 assert torch.isnan(q[~keep.cuda()]).all(), i
 
 
+def test_a_class_alone(B):
+    """Every class but one masked: its probability is 1, its gradient 0; a NaN there stays one."""
+    for c in (5, 40, 600, 9000, 70000):
+        for rows in (1, 200):
+            x = torch.full((1, 1, rows, c), float("-inf"), device="cuda")
+            x[..., c // 2] = 3.0
+            x[0, 0, -1, c // 2] = float("nan") if rows > 1 else 3.0
+            act = torch.full((1, 1, rows), c // 2, dtype=torch.int32, device="cuda")
+            one = torch.ones((1, 1, rows), device="cuda")
+            lp, ent, grad, loss = torch.empty_like(one), torch.empty_like(one), torch.empty_like(x), torch.empty(1, device="cuda")
+            B.bc_action_log_probs(x, c, act, lp, ent)
+            B.bc_clipped_policy_loss(x, c, act, one, one * 0, None, None, (0.2, 0.2, 0.0), 1.0, grad, loss)
+            torch.cuda.synchronize()
+            n = rows - (rows > 1)
+            assert not lp[0, 0, :n].any() and not ent[0, 0, :n].any() and not grad[0, 0, :n].any(), c
+            if rows > 1:
+                assert torch.isnan(lp[0, 0, -1]) and torch.isnan(grad[0, 0, -1, c // 2]) and torch.isnan(loss).all()
+            else:
+                assert float(loss) == -1.0
+
+
+def test_offsets_past_32_bits(B):
+    """2.2e9 scores: the last rows of a large map have what they have in a small one."""
+    rows, c, k = 17000, 131072, 5
+    x = torch.empty((1, 1, rows, c), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    tail = (2 * torch.randn((1, 1, 8, c), generator=g, device="cuda")).bfloat16()
+    x[:, :, :-8] = tail[:, :, :1]
+    x[:, :, -8:] = tail
+    act = torch.randint(0, c, (1, 1, rows), generator=g, device="cuda", dtype=torch.int32)
+    one = torch.ones((1, 1, rows), device="cuda")
+    outs = []
+    for v, a, o in ((x, act, one), (x[:, :, -200:].clone(), act[:, :, -200:].contiguous(), one[:, :, -200:].contiguous())):
+        n = v.shape[2]
+        top, index = torch.empty((1, 1, n, k), dtype=v.dtype, device="cuda"), torch.empty((1, 1, n, k), dtype=torch.int32, device="cuda")
+        rest, lp, loss = torch.empty_like(o), torch.empty_like(o), torch.empty(1, device="cuda")
+        B.bc_top_scores(v, c, 1.0, top, index, rest, (1, 1), None, None)
+        B.bc_action_log_probs(v, c, a, lp)
+        y = v.clone() if n == 200 else None
+        w = o * 1e4
+        B.bc_clipped_policy_loss(v, c, a, o, lp - 0.1, None, w, (0.2, 0.2, 0.0), 1.0, y if n == 200 else v, loss)
+        first = (y if n == 200 else v)[:, :, -8:].clone()
+        if n != 200:
+            v[:, :, :-8] = tail[:, :, :1]
+            v[:, :, -8:] = tail
+        grad = torch.empty_like(v) if n == 200 else v
+        B.bc_distill_loss(v, c, top, index, None, 1.0, w, 1.0, grad, loss)
+        outs.append([t[:, :, -8:].clone() for t in (top, index, rest, lp)] + [first, grad[:, :, -8:].clone()])
+        torch.cuda.synchronize()
+    for p, q in zip(*outs):
+        assert torch.equal(p, q)
+
+
 # ------------------------------------------------------------------ streams, graphs, devices
 
 def all_calls(B, st, work, stream=None):

@@ -52,6 +52,7 @@ def test_maps_and_classes(B):
         assert call(B, m=(2, 30, 4, 6, 3, 1)) == B.BC_ERR_DTYPE
         assert call(B, m=(0, 30, 4, 6, 0, 1)) == B.BC_ERR_SHAPE
         assert call(B, m=(2, 2 ** 31 - 1, 4, 6, 0, 1)) == B.BC_ERR_SHAPE   # past 4e9 elements
+        assert call(B, m=(1, (1 << 30) + 1, 1, 1, 0, 1)) == B.BC_ERR_UNSUPPORTED
         for classes in (0, -1, 31):
             assert call(B, classes=classes) == B.BC_ERR_SHAPE
     for call in (distill, clip):
@@ -63,6 +64,7 @@ def test_maps_and_classes(B):
         assert call(B, grad=None, loss=None) == B.BC_ERR_NULL
         assert call(B, scale=NAN) == B.BC_ERR_SHAPE and call(B, scale=INF) == B.BC_ERR_SHAPE
         assert call(B, loss=GRAD + 4) == B.BC_ERR_ALIAS
+        assert call(B, grad=X, weight=X) == B.BC_ERR_ALIAS         # in place over its weights
         assert call(B, grad=X + 4) == B.BC_ERR_ALIAS
         assert call(B, weight=GRAD) == B.BC_ERR_ALIAS
         assert call(B, loss=X) == B.BC_ERR_ALIAS and call(B, **wide, work=X) == B.BC_ERR_ALIAS
@@ -81,7 +83,7 @@ def test_records(B):
         assert top(B, m=(2, 300, 4, 6, 0, 1), classes=300, k=k) == B.BC_ERR_SHAPE
         assert distill(B, k=k) == B.BC_ERR_SHAPE
     assert top(B, k=31) == B.BC_ERR_SHAPE                          # more than the classes
-    for t in (0.0, -1.0, NAN, INF, 1e-45):
+    for t in (0.0, -1.0, NAN, INF, 1e-45, 3e-39, 5e-39):
         assert top(B, t=t) == B.BC_ERR_SHAPE and distill(B, t=t) == B.BC_ERR_SHAPE
     for key in ("out", "index"):
         assert top(B, **{key: None}) == B.BC_ERR_NULL
