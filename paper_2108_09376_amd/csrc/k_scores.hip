@@ -58,7 +58,7 @@ __device__ __forceinline__ double2 team_sum(double x, double y)
     x = wave_sum(x);
     if constexpr (TWO) y = wave_sum(y);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = make_double2(x, y);
-    __syncthreads();
+    lds_barrier();
     double2 s = make_double2(0.0, 0.0);
     if (threadIdx.x < 64) {                                      // at most 16 waves
         if (threadIdx.x < T / 64) s = waves[threadIdx.x];
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_di
     const bool holder = L <= 64 || threadIdx.x < 64;             // of entries
     const float k2 = kLog2e * a.inv_t;
     auto meet = [] {
-        if constexpr (L > 64) __syncthreads();
+        if constexpr (L > 64) lds_barrier();
         else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     };
     const bool inside = w.p + group < g.hw;

@@ -159,6 +159,7 @@ __device__ __noinline__ void top_slow(const void *x, Chunk c, int k, float k2, T
         return y > kth || (y == kth && cls <= first);
     };
     if (lane == 0) sh->count = 0;
+    for (int i = lane; i < kCandidates; i += L) sh->cand[i] = 0;
     __syncthreads();
     float m = -kInf, s = 0.f;
     see([&](float z, int cls) {
@@ -198,6 +199,7 @@ __global__ __launch_bounds__(L, L > 256 ? 8 : L == 256 ? 5 : 3) void k_top(TopAr
     Row row;
     row.load(a.x, c.base, c.len, c.live);
     if (lane == 0) sh.count = 0;
+    for (int i = lane; i < kCandidates; i += L) sh.cand[i] = 0;
     const float m = row.largest();
     row.keep();
     maxima[lane] = m;
@@ -287,23 +289,21 @@ __global__ __launch_bounds__(L, L > 256 ? 8 : L == 256 ? 5 : 3) void k_top(TopAr
         __syncthreads();                                         // before the count is taken back
         top_slow<FMT, L>(a.x, c, k, k2, &sh, &st);
     }
-    const int found = min(sh.count, kCandidates), padded = (found + 7) & ~7;
-    if (lane < padded - found) sh.cand[found + lane] = 0;
-    __syncthreads();
+    const int found = min(sh.count, kCandidates);
     for (int i = lane; i < found; i += L) {
         const Key mine = sh.cand[i];
         int place = 0;
-        for (int o = 0; o < padded; o += 8)
+        for (int o = 0; o < found; o += 8)                       // 0 behind the last
 #pragma unroll
             for (int j = 0; j < 8; ++j) place += sh.cand[o + j] > mine;
-        if (place < k) {
-            sh.record[place] = mine;
-            if constexpr (PASS == kWhole) put<FMT>(a, px * a.k + place, mine);
-        }
+        if (place < k) sh.record[place] = mine;
     }
     __syncthreads();
-    if constexpr (PASS == kFirst)
-        if (lane < a.k) a.keys[((size_t)r * g.chunks + chunk) * a.k + lane] = lane < k ? sh.record[lane] : 0;
+    const int entry = lane - (L - 64);                           // the last wave writes the record
+    if (entry >= 0 && entry < a.k) {
+        if constexpr (PASS == kFirst) a.keys[((size_t)r * g.chunks + chunk) * a.k + entry] = entry < k ? sh.record[entry] : 0;
+        else put<FMT>(a, px * a.k + entry, sh.record[entry]);
+    }
     if (!a.rest) return;
     if (plain) {
         if (holder) st = {-kInf, 0.f, 0.f};

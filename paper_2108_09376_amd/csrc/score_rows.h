@@ -56,6 +56,15 @@ __device__ __forceinline__ float lane_max(float v)
     return v;
 }
 
+// A barrier for what passes through LDS alone: stores to memory need not be done by then, as
+// __syncthreads would have it.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // What a wave knows of a row, or of its part: the maximum, the sum of exp2((z - max) k2),
 // and the sum of those times (z - max) where an entropy is wanted. Nothing above -inf: the
 // maximum is -inf and the sums are 0.
@@ -484,7 +493,7 @@ __device__ __forceinline__ Stats team_stats(Stats st, Stats *lds, float k2)
 {
     if constexpr (L > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = st;
-        __syncthreads();
+        lds_barrier();
         if (threadIdx.x < 64) {
             st = {-kInf, 0.f, 0.f};
             if (threadIdx.x < L / 64) st = lds[threadIdx.x];
