@@ -1404,7 +1404,7 @@ static bc_status distill_plan(const bc_tensor &t, int32_t classes, int32_t k, bc
     bc_status st = score_geom(t, classes, true, g);
     if (st) return st;
     if ((st = check_record(k, 64))) return st;
-    p = bc::score_plan(g, t.dtype, k, true, true, 64);
+    p = bc::score_plan(g, t.dtype, k, true, true, 64, 257);
     return BC_OK;
 }
 
@@ -1412,7 +1412,7 @@ static bc_status action_plan(const bc_tensor &t, int32_t classes, bool loss, bc:
 {
     bc_status st = score_geom(t, classes, loss, g);
     if (st) return st;
-    p = bc::score_plan(g, t.dtype, 1, loss, true, 256);
+    p = bc::score_plan(g, t.dtype, 1, loss, true, 256, 128);
     return BC_OK;
 }
 

@@ -293,8 +293,8 @@ struct TopArgs {
 };
 // sets g's per, chunks and divisors; picks: scores per row that chunks hand on; sums: a loss is
 // summed; stream: a workgroup may pass over a row that does not fit its registers; pixels: of a
-// workgroup, where pixels have few classes
-ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, int pixels);
+// workgroup, where pixels have few classes; few: long rows below so many are cut
+ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, int pixels, int few);
 ScorePlan top_plan(ScoreGeom &g, int fmt, int k);
 hipError_t launch_distill(DistillArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, int fmt, hipStream_t s);
 hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, float *loss, float *kl, int fmt, hipStream_t s);

@@ -557,8 +557,11 @@ __device__ __forceinline__ Decision decide(const ClipArgs &a, const Given &v, co
     return d;
 }
 
-// The losses of rows in chunks, an image to a workgroup, from what the first pass has left: runs beside the
-// second pass, as more workgroups of its launch.
+// The losses of images of few rows, in chunks, an image to a workgroup, from what the first pass has left:
+// runs beside the second pass, as more workgroups of its launch. (Of 16 rows and more the rows one after
+// another take longer than a launch of their own: 13 us for 16 of 32768, and 35 for 64.)
+constexpr uint32_t kBeside = 4;
+
 template <int L>
 __device__ __forceinline__ void clip_sums(const ClipArgs &a, const ScoreGeom &g, uint32_t image)
 {
@@ -591,7 +594,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
     __shared__ float pub[3];
     if (past_end<PASS>(g)) {
         const uint32_t image = item_of() - g.images * g.per * (uint32_t)g.chunks;
-        if (PASS == kSecond && image < g.images) clip_sums<T>(a, g, image);
+        if (PASS == kSecond && g.hw <= kBeside && image < g.images) clip_sums<T>(a, g, image);
         return;
     }
     const Place w = place_of<G, PASS>(g);
@@ -666,7 +669,7 @@ __global__ __launch_bounds__(kThreadsOf<L>, NV <= 8 && L > 64 ? 8 : 4) void k_cl
             }
         }
     }
-    if (PASS != kWhole || !wanted(a.out)) return;
+    if (PASS == kFirst || !wanted(a.out) || w.chunk != 0 || (PASS == kSecond && g.hw <= kBeside)) return;
     if constexpr (L > 64) {
         write_sums(a.out, g, w.item, loss, kl);
     } else {
@@ -866,9 +869,19 @@ hipError_t launch_sum(const ScoreGeom &g, const LossOut &o, hipStream_t s)
 
 }  // namespace
 
-// Rows in whole where there are many, in chunks where few would leave most of the device idle
-// or where one does not fit a workgroup's registers.
-ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, int pixels)
+// Rows in whole where there are many, in chunks where few would leave most of the device idle: with
+// chunks of 8 vectors per thread, or of 2 while even those of 8 are few. Divergence and gradient,
+// bf16, us whole / in chunks of 8 / of 2:
+//   classes    16 rows              128                  256                  512
+//    32768     15.0 / 16.2 / 10.9   16.6 / 17.5 / 13.9   18.9 / 21.3 / 18.7   25.3 / 29.8 / 31.8
+//   131072     37.3 / 13.6 / 11.2   40.9 / 26.8 / 29.8   47.9 / 43.4 / 48.4   71.0 / 74.1 / 81.6
+// so that it is cut below 257 rows; the policy's calls below 128 (131072 classes, 128 rows: 26.5 / 23.0 /
+// 23.9; 256: 35.6 / 38.9 / 40.2).
+// Rows past a workgroup's registers (16384 vectors in 1024 threads leave room for one workgroup on a compute
+// unit) are passed over twice in memory: 4096 rows of 131072 505 us, from registers 546.
+// Pixels of up to 32 classes take four lanes (divergence of 256 x 512 pixels of 19: 13.0 us, eight lanes
+// through lists 28) or, for the policy's calls, a thread (15.1, eight lanes 26).
+ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, int pixels, int few)
 {
     const int vec = fmt == kF32 ? 4 : 8;
     const size_t rows = (size_t)g.images * g.hw;
@@ -878,15 +891,14 @@ ScorePlan score_plan(ScoreGeom &g, int fmt, int picks, bool sums, bool stream, i
     while (p.form && p.form < kFormCount && kForms[p.form].lanes * kForms[p.form].nv < nvec) ++p.form;
     g.chunks = 1;
     g.chunk = g.len;
-    if ((p.form == kFormCount && !stream) || (p.form > kChunkForm && rows < 128)) {
-        // chunks of 8 vectors per thread, or, where these are few (and joined from their sums), of 2
+    if ((p.form == kFormCount && !stream) || (p.form > kChunkForm && rows < (size_t)few)) {
         p.form = kChunkForm;
         auto cut = [&](int nv) {
             g.chunk = kForms[kChunkForm].lanes * nv * vec;
             g.chunks = (int)(((int64_t)g.len + g.chunk - 1) / g.chunk);
         };
         cut(kForms[kChunkForm].nv);
-        if (stream && rows * g.chunks < 256) {
+        if (stream && rows * g.chunks <= 512) {
             p.form = kSmallChunk;
             cut(2);
         }
@@ -958,7 +970,8 @@ hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
             return with_chunk(p.form, [&](auto l, auto n) {
                 constexpr int L = decltype(l)::value, NV = decltype(n)::value;
                 hipLaunchKernelGGL((k_clip<FMT, L, NV, kFirst>), grid, dim3(L), 0, s, a, g);
-                const dim3 sums = grid_of((size_t)g.images * g.per * g.chunks + (wanted(a.out) ? g.images : 0));
+                const bool beside = wanted(a.out) && g.hw <= kBeside;
+                const dim3 sums = grid_of((size_t)g.images * g.per * g.chunks + (beside ? g.images : 0));
                 hipLaunchKernelGGL((k_clip<FMT, L, NV, kSecond>), sums, dim3(L), 0, s, a, g);
                 return hipGetLastError();
             });
@@ -978,7 +991,7 @@ hipError_t launch_clip(ClipArgs a, ScoreGeom g, const ScorePlan &p, void *work, 
             return hipGetLastError();
         });
     });
-    return e != hipSuccess || p.split ? e : launch_sum(g, a.out, s);
+    return e != hipSuccess || (p.split && g.hw <= kBeside) ? e : launch_sum(g, a.out, s);
 }
 
 hipError_t launch_logp(LogpArgs a, ScoreGeom g, const ScorePlan &p, void *work, int fmt, hipStream_t s)

@@ -398,50 +398,82 @@ __global__ __launch_bounds__(64) void k_top_quad(TopArgs a, ScoreGeom g)
     if (lane == 0) a.rest[px] = rest_of(a, {m, s, 0.f});
 }
 
-// The chunks' records of a row joined, by a wave.
+// The chunks' records of a row joined. A key's place is its own in its chunk's record and, of every
+// other one, the number of larger keys, found by halving (64 of 131072 classes of 16 rows: 27 us in
+// all; of 65536 it took 62 with rounds here). Records that do not fit LDS are joined by rounds, each entry the largest
+// key below the last.
+constexpr int kJoined = 2048;
+
 template <int FMT>
-__global__ __launch_bounds__(64) void k_top_join(TopArgs a, ScoreGeom g)
+__global__ __launch_bounds__(256) void k_top_join(TopArgs a, ScoreGeom g)
 {
+    __shared__ Key lds[kJoined];
+    __shared__ Stats waves[4];
     const float k2 = kLog2e * a.inv_t;
-    {
-        const size_t r = item_of();
-        if (r >= pixel_count(a, g)) return;
-        const size_t px = row_pixel(a, (uint32_t)r);
-        const Key *keys = a.keys + r * g.chunks * a.k;
-        const int n = g.chunks * a.k;
+    const uint32_t r = item_of();
+    if (r >= pixel_count(a, g)) return;
+    const size_t px = row_pixel(a, r);
+    const Key *keys = a.keys + (size_t)r * g.chunks * a.k;
+    const int n = g.chunks * a.k;
+    Stats st = {-kInf, 0.f, 0.f};                                // the others: outside every chunk's record,
+    auto other = [&](Key o) {                                    // and inside one but not of this record
+        const float z = score_of(o);
+        if (o && z != -kInf) st = join<false>(st, {z, 1.f, 0.f}, k2);
+    };
+    if (n <= kJoined) {
+        for (int e = threadIdx.x; e < n; e += 256) lds[e] = keys[e];
+        __syncthreads();
+        for (int e = threadIdx.x; e < n; e += 256) {
+            const Key mine = lds[e];
+            const int own = e / a.k;
+            int place = e - own * a.k;
+            for (int c = 0; c < g.chunks && place < a.k; ++c) {
+                if (c == own) continue;
+                int low = 0, high = a.k;
+                while (low < high) {
+                    const int mid = (low + high) >> 1;
+                    if (lds[c * a.k + mid] > mine) low = mid + 1;
+                    else high = mid;
+                }
+                place += low;
+            }
+            if (mine && place < a.k) put<FMT>(a, px * a.k + place, mine);
+            else other(mine);
+        }
+    } else {
         Key last = ~(Key)0;
-        for (int i = 0; i < a.k; ++i) {
-            Key k = 0;
-            for (int e = threadIdx.x; e < n; e += 64) {
-                const Key o = keys[e];
-                k = o < last && o > k ? o : k;
+        if (threadIdx.x < 64)
+            for (int i = 0; i < a.k; ++i) {
+                Key k = 0;
+                for (int e = threadIdx.x; e < n; e += 64) {
+                    const Key o = keys[e];
+                    k = o < last && o > k ? o : k;
+                }
+                last = lane_max_key<64>(k);
+                if (threadIdx.x == 0) put<FMT>(a, px * a.k + i, last);
             }
-            last = lane_max_key<64>(k);
-            if (threadIdx.x == 0) put<FMT>(a, px * a.k + i, last);
-        }
-        if (!a.rest) return;
-        // the others: outside every chunk's record, and inside one but not of this record
-        Stats st = {-kInf, 0.f, 0.f};
-        for (int i = threadIdx.x; i < g.chunks; i += 64) {
-            const float4 p = a.stats[r * g.chunks + i];
-            st = join<false>(st, {p.x, p.y, 0.f}, k2);
-        }
-        for (int e = threadIdx.x; e < n; e += 64)
-            if (keys[e] < last && keys[e]) {
-                const float z = score_of(keys[e]);
-                if (z != -kInf) st = join<false>(st, {z, 1.f, 0.f}, k2);
-            }
-        const float m = lane_max<64>(st.m);
-        const float s = lane_sum<64>(st.m == -kInf ? st.s : st.s * exp2_of(st.m, m, k2));
-        if (threadIdx.x == 0) a.rest[px] = rest_of(a, {m, s, 0.f});
+        if (threadIdx.x == 0) lds[0] = last;
+        __syncthreads();
+        last = lds[0];
+        for (int e = threadIdx.x; e < n; e += 256)
+            if (keys[e] < last) other(keys[e]);
     }
+    if (!a.rest) return;
+    for (int i = threadIdx.x; i < g.chunks; i += 256) {
+        const float4 p = a.stats[(size_t)r * g.chunks + i];
+        st = join<false>(st, {p.x, p.y, 0.f}, k2);
+    }
+    st = team_stats<256, false>(wave_join<false>(st, k2), waves, k2);
+    if (threadIdx.x == 0) a.rest[px] = rest_of(a, st);
 }
 
 }  // namespace
 
+// Rows stay whole as long as they fit a workgroup's registers, few or not: 16 rows of 32768 classes, 64
+// entries, take 13 us whole; in chunks the second launch alone takes longer.
 ScorePlan top_plan(ScoreGeom &g, int fmt, int k)
 {
-    ScorePlan p = score_plan(g, fmt, 0, false, false, 16);
+    ScorePlan p = score_plan(g, fmt, 0, false, false, 16, 0);
     if (p.split) {
         p.pick = p.bytes;
         p.bytes += (size_t)g.images * g.hw * g.chunks * (size_t)k * sizeof(Key);
@@ -460,7 +492,7 @@ hipError_t launch_top(TopArgs a, ScoreGeom g, const ScorePlan &p, void *work, in
         if (p.split) {
             constexpr int L = kForms[kChunkForm].lanes, NV = kForms[kChunkForm].nv;
             hipLaunchKernelGGL((k_top<FMT, L, NV, kFirst>), grid_of(rows * g.chunks), dim3(L), 0, s, a, g);
-            hipLaunchKernelGGL((k_top_join<FMT>), grid_of(rows), dim3(64), 0, s, a, g);
+            hipLaunchKernelGGL((k_top_join<FMT>), grid_of(rows), dim3(256), 0, s, a, g);
             return hipGetLastError();
         }
         if (p.form == 0) {

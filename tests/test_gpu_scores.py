@@ -138,7 +138,8 @@ def test_top_scores_of_awkward_rows(B, dtype):
     across the record's end, all masked but a few, largest scores side by side, in one lane's
     vectors, in the last elements; NaN, for which classes are distinct and in range."""
     r = np.random.default_rng(4)
-    for classes, k in ((520, 64), (1100, 9), (4099, 64), (8200, 64), (17000, 33), (33003, 64), (50001, 64)):
+    for classes, k in ((520, 64), (1100, 9), (4099, 64), (8200, 64), (17000, 33), (33003, 64), (50001, 64), (90001, 64),
+                       (700001, 64)):                            # the last two in chunks, joined in LDS and by rounds
         rows = r.normal(0, 2, (1, 1, 12, classes))
         rows[0, 0, 1] = -3.0
         rows[0, 0, 2, ::2] = 9.0                                   # half of it equal and largest
