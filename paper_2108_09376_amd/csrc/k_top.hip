@@ -109,9 +109,10 @@ struct TopShared {
 };
 
 // A row, or a chunk of it, over the row in memory: the k-th score and the last class to have it are
-// found by halving, counting each time.
+// found by halving, counting each time. Inlined though seldom run: around a call the kernel keeps its
+// registers in scratch memory on every path (2048 rows of 65536 bf16 classes 91.9 us, inlined 73.5).
 template <int FMT, int L>
-__device__ __noinline__ void top_slow(const void *x, Chunk c, int k, float k2, TopShared<L / 64> *sh, Stats *st)
+__device__ __forceinline__ void top_slow(const void *x, Chunk c, int k, float k2, TopShared<L / 64> *sh, Stats *st)
 {
     constexpr int VEC = kVec<FMT>, W = L / 64;
     const int lane = threadIdx.x % L, nvec = c.live / VEC;
