@@ -11,10 +11,21 @@
 // record alone (a difference of sums would lose it where the record holds nearly everything), and a
 // class of the record gets w (q_j - p_j).
 //
-// All are bound by memory: a row is read once, kept in registers, and its gradient written
-// from there. A row belongs to 8 to 64 lanes of a wave, or to a workgroup of up to 1024
-// threads. Few rows, and rows too long for a workgroup's registers, are split into chunks:
+// Long calls are bound by memory, so a row is read from it once and its gradient written from
+// registers: a row belongs to 8 to 64 lanes of a wave, or to a workgroup of up to 1024 threads. A
+// row past a workgroup's registers (above 32768 fp32 or 65536 16-bit classes) is passed over
+// twice, the second time mostly from the last-level cache. Few long rows are split into chunks:
 // one launch leaves each chunk's maximum and sum, a second joins them and writes the gradient.
+// Pixels of up to 32 classes take a thread or four lanes, so that nothing is exchanged over more.
+// Small calls are bound by the call itself (6 us of the host, a launch 1.5 to 4) and by the chain of
+// a row: load, maximum, sum, loss in fp64.
+// Measured, kernels alone (a large copy reaches 4.9 TB/s, reads and writes together):
+//   divergence 4096 rows of 131072 bf16      502 us, 4.3 TB/s (1.06 GB read, 1.06 written, by the counters)
+//              256 x 512 pixels of 19 of 64  11.9 us; its memory alone takes 6.8, the rest is instructions
+//   log probabilities and entropy, 8192 rows of 32768 fp16   91 us, 5.9 TB/s read, half of
+//              it from the last-level cache, which the call before filled
+//   policy loss 8 x 1024 rows of 32768 bf16  150 to 158 us: 537 MB written at 3.5 TB/s, 267 read, most
+//              of them from that cache; rows of weight 0 are written as 0 and not read
 //
 // A row's loss goes to its workgroup's sum, and the workgroups' sums are added by a launch of their
 // own, each in its order and in fp64: no atomics, equal bits in every run.

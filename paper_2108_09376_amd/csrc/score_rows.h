@@ -449,13 +449,13 @@ __device__ __forceinline__ float load_elem(const void *p, int fmt, size_t i)
 }
 
 // Forms of a row: a thread to itself (up to kPixelClasses scores); or lanes (threads of a
-// workgroup from 128 on) and vectors of each.
+// workgroup from 128 on) and vectors of each, 0 for a row of any length, which is not held.
 constexpr int kPixelClasses = 32;
 struct Form {
     int lanes, nv;
 };
 constexpr Form kForms[] = {{1, 0}, {8, 1}, {32, 1}, {64, 2}, {64, 8}, {256, 8}, {512, 8}, {1024, 8}, {1024, 0}};
-constexpr int kFormCount = 8, kChunkForm = 5, kSmallChunk = -1;                      // the last of any length
+constexpr int kFormCount = 8, kChunkForm = 5, kSmallChunk = -1;
 
 template <int L> constexpr int kThreadsOf = L <= 64 ? 256 : L;
 template <int L> constexpr int kGroupsOf = L <= 64 ? 256 / L : 1;  // rows of a workgroup
